@@ -312,6 +312,106 @@ int dppf_consensus_static(float *x, int M, int64_t d, int64_t ld, float alpha, f
 int dppf_static_device_status(void *cuda_stream);
 
 /*
+ * ---- A worker's local step on a language model: first layer, loss, optimiser -------------------
+ *
+ * The operators that a worker needs between two rounds when the replica is a language model.  They
+ * work on ordinary tensors (any address that is aligned to the element type, any row stride; 16-byte
+ * aligned rows run faster) of fp32 or bf16, in fp32 arithmetic with one rounding at the end; sums run
+ * in a fixed order.  Streams, return values and "arguments are checked before any CUDA call" are as
+ * above.  Type arguments are DPPF_FLOAT32 or DPPF_BFLOAT16; ids and targets are signed 32- or 64-bit
+ * integers (id_bits, target_bits: 32 or 64), contiguous.
+ */
+#define DPPF_FLOAT32 0
+#define DPPF_BFLOAT16 1
+#define DPPF_MAX_WIDTH 65536          /* columns of an embedding table */
+#define DPPF_MAX_VOCABULARY 262144    /* columns of the logits */
+#define DPPF_MAX_POLICY_TOKENS 16777216
+
+/*
+ * Embedding lookup with a scale: out[t, 0..H) = scale * table[ids[t], 0..H), one rounding to out's
+ * type; zeros where ids[t] is outside [0, V) (padding).  table[V, ld_table], out[T, ld_out].
+ * T == 0 does nothing.
+ */
+int dppf_embedding(const void *table, int table_type, int64_t V, int H, int64_t ld_table, const void *ids, int id_bits,
+                   int64_t T, float scale, void *out, int out_type, int64_t ld_out, void *cuda_stream);
+
+/*
+ * Its gradient: grad_table[v] = scale * (sum over t with ids[t] == v of grad_out[t]), or, with
+ * accumulate != 0, that sum added to what grad_table holds.  Without accumulate every row of
+ * grad_table is written (zeros for ids that do not occur); with it only the rows of ids that occur
+ * are touched.  Ids outside [0, V) contribute nothing.  The tokens are sorted by id (stably), each sum
+ * runs in token order in fp32 and is rounded once; results are the same from run to run for given sizes.
+ * Columns H..ld-1 are not touched.  ws: dppf_embedding_workspace_bytes(T, H) bytes, 128-byte aligned, no
+ * initialisation (may be null when T == 0).  The helper returns 0 for invalid T or H.
+ */
+size_t dppf_embedding_workspace_bytes(int64_t T, int H);
+int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, const void *ids, int id_bits, int64_t T,
+                        float scale, void *grad_table, int table_type, int64_t V, int H, int64_t ld_table,
+                        int accumulate, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Clipped policy loss with a KL term, from logits[T, ld] (V columns of `type`), with its gradient.
+ * For token t with z = logits[t] / temperature and y = targets[t]:
+ *   lp = z_y - log sum_v exp z_v;   q = exp(lp - old_logp[t]);   A = advantage[t]
+ *   L  = -min(q A, clip(q, 1 - clip_low, 1 + clip_high) A) + kl_coef k,   k = exp(ref - lp) - (ref - lp) - 1
+ *   sums_out[0] = sum_t weight[t] L_t;  [1] = sum_t weight[t] k_t;  [2] = sum_t weight[t] [t is clipped]
+ *   logp_out[t] = lp
+ *   grad_logits[t, v] = weight[t] (dL/dlp) / temperature ([v == y] - exp(z_v - log sum exp z))
+ * A token is clipped (and its ratio passes no gradient) if A > 0 and q > 1 + clip_high, or A < 0 and
+ * q < 1 - clip_low.  A == 0 leaves the KL term alone.  weight carries the mask and the normalisation
+ * (e.g. mask / number of tokens); a row with weight 0, or with a target outside [0, V), is not read:
+ * its logp is 0, its gradient row 0 and it adds nothing, whatever the row holds.
+ * ref_logp NULL: no KL term (kl_coef must be 0, sums_out[1] is 0).  grad_logits NULL: forward only.
+ * grad_logits may be logits itself (same ld): the logits are replaced by their gradient; other overlaps
+ * are refused.  Logits of -inf have probability 0; a row that holds NaN or +inf, or nothing but -inf,
+ * gives NaN.  old_logp, ref_logp, advantage, weight, logp_out: device fp32[T]; sums_out: device fp32[3].
+ * clip_low in [0, 1], clip_high >= 0, temperature > 0; 1 <= V <= DPPF_MAX_VOCABULARY.
+ * ws: dppf_policy_workspace_bytes(T) bytes, 128-byte aligned, its first 256 bytes ZERO before the first
+ * call (every call leaves them ready for the next; T may change).  dppf_device_status(ws, stream):
+ * DPPF_ERR_TIMEOUT if a bounded wait on an asynchronous copy gave up (the rows concerned are NaN).
+ */
+size_t dppf_policy_workspace_bytes(int64_t T);
+int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld, const void *targets, int target_bits,
+                     const float *old_logp, const float *ref_logp, const float *advantage, const float *weight,
+                     float clip_low, float clip_high, float kl_coef, float temperature, float *sums_out,
+                     float *logp_out, void *grad_logits, int64_t ld_grad, void *ws, size_t ws_bytes,
+                     void *cuda_stream);
+
+/*
+ * One AdamW step over many tensors at once (the recurrence of dppf_adamw_step, element by element), in one
+ * launch per 500 tensors.  tensors_host: HOST array; it is copied during the call.
+ *   param, grad       numel elements of param_type / grad_type (one type each for all tensors); grad is
+ *                     read only and multiplied by *grad_scale first (device fp32[1], e.g. a clipping
+ *                     coefficient; NULL = 1).  If *grad_scale is not finite NOTHING is changed.
+ *   decay             factor on weight_decay for this tensor (0: none, as for norms and biases)
+ * state_bits 32: exp_avg, exp_avg_sq are fp32[numel], zero before step 1; scales are ignored.  With fp32
+ *   parameters and gradients and no grad_scale the result equals dppf_adamw_step bit for bit.
+ * state_bits 8: in blocks of 256 elements from the tensor's start, exp_avg[i] e4m3 codes with one fp32 scale
+ *   per block (exp_avg_scale[ceil(numel / 256)]): m = code * scale; exp_avg_sq[i] codes of the ROOT of the
+ *   second moment: sqrt(v) = code * scale (exp_avg_sq_scale).  All zero before step 1.  New scale =
+ *   (largest magnitude of the block) / 448; m is rounded to nearest, sqrt(v) up or down in
+ *   proportion by a hash of (element, seed) -- pass another seed each step, e.g. the step -- and never to
+ *   zero unless it is zero.  The parameters are updated from the moments before they are rounded.
+ *   A gradient that is not finite makes its whole block of 256 states NaN (with 32 bits: one element).
+ * bf16 parameters are rounded to nearest after the step (updates below half their spacing are lost; keep
+ * fp32 parameters where that matters).  The arrays of one tensor must not overlap each other, and no two
+ * tensors may overlap.  Tensors with numel 0 are skipped.
+ */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *exp_avg;
+    void *exp_avg_sq;
+    float *exp_avg_scale;
+    float *exp_avg_sq_scale;
+    int64_t numel;
+    float decay;
+} dppf_tensor;
+int dppf_adamw_tensors(const dppf_tensor *tensors_host, int n_tensors, int param_type, int grad_type, int state_bits,
+                       float lr, float beta1, float beta2, float eps, float weight_decay, int step,
+                       const float *grad_scale, uint32_t seed, void *cuda_stream);
+
+/*
  * Host-side scalars of a DPPF run (no device work, no CUDA call).
  *
  * dppf_lambda_schedule: push strength at iteration t of T (appendix, "How to schedule the

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -24,9 +25,19 @@ EXPORTS = ("dppf_workspace_bytes", "dppf_consensus", "dppf_consensus_ex", "dppf_
            "dppf_distance_partials", "dppf_update_from_sums", "dppf_worker_update", "dppf_adamw_step_and_consensus_ex",
            "dppf_consensus_rounds", "dppf_consensus_rounds_ex", "dppf_debug_set_poll_limits",
            "dppf_adamw_step", "dppf_adamw_step_and_consensus",
+           "dppf_embedding", "dppf_embedding_grad", "dppf_embedding_workspace_bytes",
+           "dppf_policy_loss", "dppf_policy_workspace_bytes", "dppf_adamw_tensors",
            "dppf_lambda_schedule", "dppf_lr_cosine", "dppf_qsr_period", "dppf_round_metrics")
 
+FLOAT32, BFLOAT16 = 0, 1
+STATE_BLOCK = 256            # elements that share a scale in the 8-bit optimiser states
+
 _lib = None
+
+
+class _Tensor(ctypes.Structure):      # dppf_tensor
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")] + \
+               [("numel", ctypes.c_int64), ("decay", ctypes.c_float)]
 
 
 class DppfError(RuntimeError):
@@ -102,6 +113,18 @@ def load(rebuild_if_stale: bool = False) -> ctypes.CDLL:
     lib.dppf_debug_set_poll_limits.restype = i32
     lib.dppf_consensus_static.argtypes = [vp, i32, i64, i64, f32, f32, vp, vp]
     lib.dppf_consensus_static.restype = i32
+    lib.dppf_embedding.argtypes = [vp, i32, i64, i32, i64, vp, i32, i64, f32, vp, i32, i64, vp]
+    lib.dppf_embedding.restype = i32
+    lib.dppf_embedding_workspace_bytes.argtypes = [i64, i32]
+    lib.dppf_embedding_workspace_bytes.restype = sz
+    lib.dppf_embedding_grad.argtypes = [vp, i32, i64, vp, i32, i64, f32, vp, i32, i64, i32, i64, i32, vp, sz, vp]
+    lib.dppf_embedding_grad.restype = i32
+    lib.dppf_policy_workspace_bytes.argtypes = [i64]
+    lib.dppf_policy_workspace_bytes.restype = sz
+    lib.dppf_policy_loss.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, i64, vp, sz, vp]
+    lib.dppf_policy_loss.restype = i32
+    lib.dppf_adamw_tensors.argtypes = [ctypes.POINTER(_Tensor), i32, i32, i32, i32, f32, f32, f32, f32, f32, i32, vp, ctypes.c_uint32, vp]
+    lib.dppf_adamw_tensors.restype = i32
     lib.dppf_status_string.argtypes = [i32]
     lib.dppf_status_string.restype = ctypes.c_char_p
     lib.dppf_launch_count.argtypes = [i32, i64, i32, i32]
@@ -361,3 +384,195 @@ def adamw_launch_count(M: int, path=PATH_AUTO) -> int:
 def dppf_static_device_status() -> int:
     """Status word of the built-in scratch that dppf_consensus_static uses on the current device."""
     return int(load().dppf_static_device_status(_stream()))
+
+
+# ---------------------------------------------------------------- a worker's local step on a language model
+# The functions below launch on the current stream of the device that holds their tensors.
+
+_TYPES = {torch.float32: FLOAT32, torch.bfloat16: BFLOAT16}
+_ID_BITS = {torch.int32: 32, torch.int64: 64}
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{what} must be fp32 or bf16, not {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _matrix(t: torch.Tensor, what: str):
+    """(rows, columns, row stride) of a 2-D CUDA tensor with unit column stride."""
+    if t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what} must be a 2-D CUDA tensor with unit column stride")
+    rows, cols = t.shape
+    return rows, cols, (t.stride(0) if rows > 1 else cols)
+
+
+def _vector(t: torch.Tensor, n: int, what: str, device, dtypes=(torch.float32,)) -> torch.Tensor:
+    if t.dtype not in dtypes or t.device != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous tensor of {n} entries of type {' or '.join(str(d) for d in dtypes)} on {device}")
+    return t
+
+
+def _call(device, fn, where, *args):
+    """fn(*args, stream) with `device` current; raises on a status other than OK."""
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    _check(rc, where)
+
+
+def dppf_embedding(table, ids, scale=1.0, out=None, out_dtype=None):
+    """Rows ``ids`` of ``table[V, H]`` times ``scale`` -> ``out[*ids.shape, H]`` (zeros where an id is
+    outside [0, V)).  ``out_dtype`` (default: the table's) is used when ``out`` is not given."""
+    V, H, ld = _matrix(table, "table")
+    ids = _vector(ids, ids.numel(), "ids", table.device, tuple(_ID_BITS))
+    if out is None:
+        out = torch.empty((*ids.shape, H), dtype=out_dtype or table.dtype, device=table.device)
+    elif out.device != table.device or out.numel() != ids.numel() * H or out.shape[-1:] != (H,):
+        raise ValueError("out must hold one row of H columns per id, on the table's device")
+    flat = out if out.dim() == 2 else out.view(-1, H)
+    _, _, ld_out = _matrix(flat, "out")
+    _call(table.device, load().dppf_embedding, "dppf_embedding", table.data_ptr(), _type(table, "table"), V, H, ld, ids.data_ptr(), _ID_BITS[ids.dtype],
+          ids.numel(), scale, flat.data_ptr(), _type(flat, "out"), ld_out)
+    return out
+
+
+def embedding_workspace_bytes(T: int, H: int) -> int:
+    return int(load().dppf_embedding_workspace_bytes(int(T), int(H)))
+
+
+def alloc_embedding_workspace(T: int, H: int, device="cuda") -> torch.Tensor:
+    n = embedding_workspace_bytes(T, H)
+    if n == 0:
+        raise ValueError("invalid T or H")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def dppf_embedding_grad(grad_out, ids, grad_table, scale=1.0, accumulate=False, ws=None):
+    """Gradient of :func:`dppf_embedding` with respect to the table, written to (or, with ``accumulate``,
+    added to) ``grad_table[V, H]``; ``grad_out[*ids.shape, H]``.  Returns the workspace used (None for no tokens)."""
+    V, H, ld = _matrix(grad_table, "grad_table")
+    dev = grad_table.device
+    ids = _vector(ids, ids.numel(), "ids", dev, tuple(_ID_BITS))
+    T = ids.numel()
+    if grad_out.device != dev or grad_out.numel() != T * H or grad_out.shape[-1:] != (H,):
+        raise ValueError("grad_out must hold one row of H columns per id, on the table's device")
+    flat = grad_out if grad_out.dim() == 2 else grad_out.view(-1, H)
+    _, _, ld_out = _matrix(flat, "grad_out")
+    if ws is None and T:
+        ws = alloc_embedding_workspace(T, H, dev)
+    _call(dev, load().dppf_embedding_grad, "dppf_embedding_grad", flat.data_ptr(), _type(flat, "grad_out"), ld_out, ids.data_ptr(), _ID_BITS[ids.dtype], T, scale,
+          grad_table.data_ptr(), _type(grad_table, "grad_table"), V, H, ld, int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    return ws
+
+
+class PolicyLoss(NamedTuple):
+    loss: torch.Tensor          # 0-d: sum of weight * loss
+    kl: torch.Tensor            # 0-d: sum of weight * KL estimate
+    clipped: torch.Tensor       # 0-d: sum of weight over clipped tokens
+    logp: torch.Tensor          # [T]
+    ws: torch.Tensor
+
+
+def alloc_policy_workspace(T: int, device="cuda") -> torch.Tensor:
+    """Workspace of :func:`dppf_policy_loss` for up to T tokens, zeroed as its first call needs it."""
+    n = int(load().dppf_policy_workspace_bytes(int(T)))
+    if n == 0:
+        raise ValueError("invalid T")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def dppf_policy_loss(logits, targets, old_logp, advantage, weight, ref_logp=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0,
+                     temperature=1.0, grad_logits=None, ws=None) -> PolicyLoss:
+    """Clipped policy loss with a KL term from ``logits[T, V]``; with ``grad_logits`` (may be ``logits``) also its
+    gradient.  ``weight`` carries mask and normalisation; rows with weight 0 are not read."""
+    T, V, ld = _matrix(logits, "logits")
+    dev, code = logits.device, _type(logits, "logits")
+    targets = _vector(targets, T, "targets", dev, tuple(_ID_BITS))
+    for t, what in ((old_logp, "old_logp"), (advantage, "advantage"), (weight, "weight"), (ref_logp, "ref_logp")):
+        if t is not None:
+            _vector(t, T, what, dev)
+    ld_grad = 0
+    if grad_logits is not None:
+        rows, cols, ld_grad = _matrix(grad_logits, "grad_logits")
+        if grad_logits.dtype != logits.dtype or grad_logits.device != dev or (rows, cols) != (T, V):
+            raise ValueError("grad_logits must have the type, shape and device of logits")
+    ws = alloc_policy_workspace(T, dev) if ws is None else ws
+    out = torch.empty(3 + T, dtype=torch.float32, device=dev)
+    sums, logp = out[:3], out[3:]
+    _call(dev, load().dppf_policy_loss, "dppf_policy_loss", logits.data_ptr(), code, T, V, ld, targets.data_ptr(), _ID_BITS[targets.dtype], old_logp.data_ptr(),
+          _ptr(ref_logp), advantage.data_ptr(), weight.data_ptr(), clip_low, clip_high, kl_coef, temperature, sums.data_ptr(), logp.data_ptr(), _ptr(grad_logits),
+          ld_grad, ws.data_ptr(), ws.numel() * ws.element_size())
+    loss, kl, clipped = sums.unbind()
+    return PolicyLoss(loss, kl, clipped, logp, ws)
+
+
+class AdamWTensors:
+    """The tensors of :func:`dppf_adamw_tensors`: parameters, gradients and optimiser state, held for as long as
+    the object lives.  ``state_bits`` 32: fp32 moments; 8: e4m3 codes with one fp32 scale per 256 elements (of the
+    first moment, and of the root of the second).  State that is not given starts at zero.  ``decay``: factor on the
+    weight decay per tensor (default 1)."""
+
+    def __init__(self, params, grads, state_bits=32, exp_avgs=None, exp_avg_sqs=None, exp_avg_scales=None, exp_avg_sq_scales=None, decay=None):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        self.params, self.state_bits = list(params), state_bits
+        if not self.params:
+            raise ValueError("no tensors")
+        self.device, n = self.params[0].device, len(self.params)
+        self.param_type = _type(self.params[0], "params")
+        dtype = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        sizes = [p.numel() for p in self.params]
+        blocks = [-(-k // STATE_BLOCK) for k in sizes]
+
+        def state(given, counts, kind, what):
+            if given is None:
+                return [torch.zeros(c, dtype=kind, device=self.device) for c in counts]
+            given = list(given)
+            if len(given) != n:
+                raise ValueError(f"{what} must have one entry per tensor")
+            return [_vector(t, c, what, self.device, (kind,)) for t, c in zip(given, counts)]
+
+        for p in self.params:
+            _vector(p, p.numel(), "params", self.device, (self.params[0].dtype,))
+        if not self.params[0].is_cuda:
+            raise ValueError("params must be CUDA tensors")
+        self.exp_avgs = state(exp_avgs, sizes, dtype, "exp_avgs")
+        self.exp_avg_sqs = state(exp_avg_sqs, sizes, dtype, "exp_avg_sqs")
+        self.exp_avg_scales = self.exp_avg_sq_scales = None
+        if state_bits == 8:
+            self.exp_avg_scales = state(exp_avg_scales, blocks, torch.float32, "exp_avg_scales")
+            self.exp_avg_sq_scales = state(exp_avg_sq_scales, blocks, torch.float32, "exp_avg_sq_scales")
+        self.decay = [1.0] * n if decay is None else [float(d) for d in decay]
+        if len(self.decay) != n:
+            raise ValueError("decay must have one entry per tensor")
+        self._table = (_Tensor * n)()
+        for k, e in enumerate(self._table):
+            e.param, e.numel, e.decay = self.params[k].data_ptr(), sizes[k], self.decay[k]
+            e.exp_avg, e.exp_avg_sq = self.exp_avgs[k].data_ptr(), self.exp_avg_sqs[k].data_ptr()
+            if state_bits == 8:
+                e.exp_avg_scale, e.exp_avg_sq_scale = self.exp_avg_scales[k].data_ptr(), self.exp_avg_sq_scales[k].data_ptr()
+        self.bind_grads(grads)
+
+    def bind_grads(self, grads) -> None:
+        """Use these gradient tensors from now on (all fp32 or all bf16)."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError("grads must have one entry per tensor")
+        self.grad_type = _type(grads[0], "grads")
+        for p, g in zip(self.params, grads):
+            _vector(g, p.numel(), "grads", self.device, (grads[0].dtype,))
+        self.grads = grads
+        for e, g in zip(self._table, grads):
+            e.grad = g.data_ptr()
+
+
+def dppf_adamw_tensors(tensors: AdamWTensors, lr, beta1, beta2, eps, weight_decay, step, grad_scale=None, seed=0) -> None:
+    """One AdamW step on all tensors.  ``grad_scale``: fp32 CUDA tensor of one entry that multiplies the gradients
+    (the step is skipped if it is not finite); ``seed``: for the rounding of 8-bit states, another one each step."""
+    if grad_scale is not None:
+        _vector(grad_scale, 1, "grad_scale", tensors.device)
+    _call(tensors.device, load().dppf_adamw_tensors, "dppf_adamw_tensors", tensors._table, len(tensors.params), tensors.param_type, tensors.grad_type, tensors.state_bits,
+          lr, beta1, beta2, eps, weight_decay, int(step), _ptr(grad_scale), int(seed) & 0xffffffff)

@@ -76,6 +76,12 @@ bool coop_supported(int dev) {
 // the testing hook dppf_debug_set_poll_limits changes them.
 std::atomic<int> g_spin_first{kSpinLimit}, g_spin_later{kSpinLimit};
 
+}  // namespace
+namespace dppf_internal {
+int first_pass_polls() { return g_spin_first.load(std::memory_order_relaxed); }
+}
+namespace {
+
 int max_blocks_for(int M) { return M <= kMaxTemplateM ? kMaxBlocksSmallM : kMaxBlocksLargeM; }
 
 size_t norms_stage_offset(int M) {

@@ -1,0 +1,116 @@
+// Shared pieces of the kernels around a worker's local step on a language model (embedding, policy
+// loss, AdamW over many tensors): element types, vectors of eight elements, cluster accesses.
+#pragma once
+#include "chunk_ring.cuh"
+#include <cuda_bf16.h>
+#include <cfloat>
+
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(bf16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ bf16 from_float<bf16>(float x) { return __float2bfloat16_rn(x); }
+
+// ---------------------------------------------------------------- N consecutive elements as fp32
+// N * sizeof(T) bytes in as few accesses as its alignment to min(16, N * sizeof(T)) bytes allows.
+// kOnce: the data is not used again (streaming loads and stores).
+
+__device__ __forceinline__ float bf16_low(unsigned u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_high(unsigned u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ unsigned bf16_pair(float lo, float hi) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<unsigned *>(&h);
+}
+
+template <int N> struct Words;                       // N 32-bit words
+template <> struct Words<1> { using type = unsigned; };
+template <> struct Words<2> { using type = uint2; };
+template <> struct Words<4> { using type = uint4; };
+
+template <typename T, int N>
+__device__ __forceinline__ void load_vec(const T *p, float (&f)[N]) {
+    if constexpr (N == 1) {
+        f[0] = to_float(__ldcs(p));
+    } else {
+        constexpr int kWords = N * (int)sizeof(T) / 4, kPer = kWords < 4 ? kWords : 4;
+        using W = typename Words<kPer>::type;
+        unsigned u[kWords];
+#pragma unroll
+        for (int i = 0; i < kWords / kPer; ++i) {
+            const W w = __ldcs(reinterpret_cast<const W *>(p) + i);
+            memcpy(&u[i * kPer], &w, sizeof(W));
+        }
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = __uint_as_float(u[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) { f[2 * i] = bf16_low(u[i]); f[2 * i + 1] = bf16_high(u[i]); }
+        }
+    }
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_vec(T *p, const float (&f)[N]) {
+    if constexpr (N == 1) {
+        __stcs(p, from_float<T>(f[0]));
+    } else {
+        constexpr int kWords = N * (int)sizeof(T) / 4, kPer = kWords < 4 ? kWords : 4;
+        using W = typename Words<kPer>::type;
+        unsigned u[kWords];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) u[i] = __float_as_uint(f[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) u[i] = bf16_pair(f[2 * i], f[2 * i + 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < kWords / kPer; ++i) {
+            W w;
+            memcpy(&w, &u[i * kPer], sizeof(W));
+            __stcs(reinterpret_cast<W *>(p) + i, w);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- clusters
+
+__device__ __forceinline__ unsigned cluster_rank() {
+    unsigned r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ unsigned cluster_size() {
+    unsigned r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// Shared-memory address of the same variable in another block of the cluster.
+__device__ __forceinline__ unsigned cluster_map(const void *p, unsigned rank) {
+    unsigned a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void cluster_store2(unsigned a, float x, float y) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(x), "f"(y) : "memory");
+}
+__device__ __forceinline__ unsigned cluster_load(unsigned a) {
+    unsigned v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {   // 2 ulp; results below 2^-126 are 0
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+}  // namespace

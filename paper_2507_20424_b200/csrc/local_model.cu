@@ -1,0 +1,460 @@
+// Operators of a worker's local step on a language model: host side and C ABI (include/dppf.h).
+//   local_common.cuh   element types, vectors of eight elements, cluster accesses
+//   embedding.cuh      lookup with a scale; the table's gradient by sorted tokens
+//   policy_loss.cuh    clipped policy loss with a KL term, forward and backward, from logits
+//   adamw_tensors.cuh  AdamW over many tensors, optimiser state in fp32 or in 8 bits
+#include "dppf.h"
+
+#include "adamw_tensors.cuh"
+#include "embedding.cuh"
+#include "policy_loss.cuh"
+
+namespace dppf_internal {
+int first_pass_polls();          // poll budget set by dppf_debug_set_poll_limits
+}
+
+namespace {
+
+constexpr int kMaxDevices = 64;
+
+int current_device() {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return -1;
+    return dev;
+}
+
+int multiprocessors(int dev) {
+    static std::atomic<int> known[kMaxDevices];
+    int n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return -1;
+        known[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
+template <typename K>
+bool allow_smem(K kernel, int dev, std::atomic<int> *done, int bytes) {
+    if (done[dev].load(std::memory_order_relaxed)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done[dev].store(1, std::memory_order_relaxed);
+    return true;
+}
+
+int launched() { return cudaGetLastError() == cudaSuccess ? DPPF_OK : DPPF_ERR_CUDA; }
+
+bool all_finite(std::initializer_list<float> vals) {
+    for (float f : vals)
+        if (!std::isfinite(f)) return false;
+    return true;
+}
+
+bool ranges_meet(const void *a, size_t abytes, const void *b, size_t bbytes) {
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+    return a && b && abytes && bbytes && pa < pb + bbytes && pb < pa + abytes;
+}
+
+bool known_type(int t) { return t == DPPF_FLOAT32 || t == DPPF_BFLOAT16; }
+size_t type_bytes(int t) { return t == DPPF_FLOAT32 ? 4 : 2; }
+bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Bytes from the first element of row 0 to the last one of row rows - 1.
+size_t matrix_bytes(int64_t rows, int64_t cols, int64_t ld, int type) {
+    return rows > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * type_bytes(type) : 0;
+}
+
+constexpr int64_t kMaxLd = (int64_t)1 << 40;
+
+// ---------------------------------------------------------------- embedding
+
+template <typename TW, typename TO>
+int launch_lookup(LookupArgs a, bool vec, cudaStream_t s) {
+    constexpr int kWide = 8;
+    a.groups = vec ? a.H / kWide : a.H;
+    // about eight groups a thread, at least one row a block
+    long long rows = (8LL * kLookupThreads) / a.groups;
+    if (rows < 1) rows = 1;
+    // short lookups: fewer rows a block, so that more blocks share the work
+    while (rows > 1 && (a.T + rows - 1) / rows < 592) rows = (rows + 1) / 2;
+    a.rows_per_block = (unsigned)rows;
+    const long long grid = (a.T + rows - 1) / rows;
+    if (grid > INT_MAX) return DPPF_ERR_INVALID_ARG;
+    if (vec) lookup_kernel<TW, TO, kWide><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
+    else lookup_kernel<TW, TO, 1><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
+    return launched();
+}
+
+// Rows of a matrix start on 16-byte boundaries.
+bool rows_on_16(const void *p, int64_t ld, int type) { return aligned_to(p, 16) && (size_t)ld * type_bytes(type) % 16 == 0; }
+
+// Places of the sorted tokens that a thread walks: long enough that few sums are split, short enough
+// that about 1,000 threads an SM are at work (8 to 128).
+int reduce_tile(int64_t T, int H) {
+    const double rows = (double)T * ((H + 7) / 8) / (148.0 * 1024.0);
+    int tile = 8;
+    while (tile < 128 && tile < rows) tile *= 2;
+    return tile;
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+struct EmbeddingLayout {
+    size_t key[2], pos[2], part, total;
+    int tile, tiles;
+};
+EmbeddingLayout embedding_layout(int64_t T, int H) {
+    EmbeddingLayout l;
+    l.tile = reduce_tile(T, H);
+    l.tiles = (int)((T + l.tile - 1) / l.tile);
+    size_t at = 0;
+    const size_t words = round256((size_t)T * 4);
+    for (int i = 0; i < 2; ++i) { l.key[i] = at; at += words; l.pos[i] = at; at += words; }
+    l.part = at;
+    at += round256((size_t)l.tiles * 2 * (size_t)H * 4);
+    l.total = at;
+    return l;
+}
+
+template <typename TG, typename TW, int N>
+void launch_reduce(const ReduceArgs &a, dim3 grid, cudaStream_t s) {
+    embedding_reduce_kernel<TG, TW, N><<<grid, kReduceThreads, 0, s>>>(a);
+    if (a.tiles > 1) embedding_join_kernel<TW, N><<<grid, kReduceThreads, 0, s>>>(a);
+}
+template <int N>
+void launch_reduce_types(const ReduceArgs &a, int tg, int tw, dim3 grid, cudaStream_t s) {
+    if (tg == DPPF_FLOAT32) {
+        if (tw == DPPF_FLOAT32) launch_reduce<float, float, N>(a, grid, s);
+        else launch_reduce<float, bf16, N>(a, grid, s);
+    } else {
+        if (tw == DPPF_FLOAT32) launch_reduce<bf16, float, N>(a, grid, s);
+        else launch_reduce<bf16, bf16, N>(a, grid, s);
+    }
+}
+
+std::atomic<int> g_sort_ready[kMaxDevices];
+
+// ---------------------------------------------------------------- policy loss
+
+constexpr size_t kPolicyHeaderBytes = 256;
+constexpr int kPolicySliceMax = 200 * 1024;        // shared memory of one block's slice at most
+constexpr int kPolicySliceGood = 72 * 1024;        // three blocks fit an SM: one loads while another writes
+
+std::atomic<int> g_policy_ready[2][kMaxDevices];
+
+template <typename T>
+int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
+    std::atomic<int> *ready = g_policy_ready[sizeof(T) == 4 ? 0 : 1];
+    if (!allow_smem(policy_kernel<T>, dev, ready, kPolicySliceMax)) return DPPF_ERR_CUDA;
+    const int sms = multiprocessors(dev);
+    if (sms < 0) return DPPF_ERR_CUDA;
+    // 16-byte vectors a row can span, whatever its alignment
+    const int vectors = (int)(((size_t)a.V * sizeof(T) + 15 + 15) / 16);
+    int C = 1;
+    auto slice_bytes = [&](int c) { return (vectors + c - 1) / c * 16; };
+    while (C < kPolicyMaxCluster && slice_bytes(C) > kPolicySliceGood) C *= 2;
+    // few rows: split them further while SMs are idle and a slice stays above 8 KB
+    while (C < kPolicyMaxCluster && (long long)a.T * C < 2LL * sms && slice_bytes(C) > 16 * 1024) C *= 2;
+    if (slice_bytes(C) > kPolicySliceMax) return DPPF_ERR_INVALID_ARG;
+    a.slice = (vectors + C - 1) / C;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.T * (unsigned)C);
+    cfg.blockDim = dim3(kPolicyThreads);
+    cfg.dynamicSmemBytes = (size_t)a.slice * 16;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)C;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, policy_kernel<T>, a) != cudaSuccess) { cudaGetLastError(); return DPPF_ERR_CUDA; }
+    return DPPF_OK;
+}
+
+// ---------------------------------------------------------------- AdamW over many tensors
+
+template <typename TP, typename TG, int kBits, int kEntries>
+int launch_tensors(const TensorTable<kEntries> &tab, int sms, cudaStream_t s) {
+    const int grid = tab.units < sms * 8 ? tab.units : sms * 8;
+    adamw_tensors_kernel<TP, TG, kBits, kEntries><<<grid, kTensorThreads, 0, s>>>(tab);
+    return launched();
+}
+template <int kEntries>
+int launch_tensors_types(const TensorTable<kEntries> &tab, int tp, int tg, int bits, int sms, cudaStream_t s) {
+#define DPPF_TENSORS(P, G) \
+    return bits == 8 ? launch_tensors<P, G, 8, kEntries>(tab, sms, s) : launch_tensors<P, G, 32, kEntries>(tab, sms, s)
+    if (tp == DPPF_FLOAT32 && tg == DPPF_FLOAT32) DPPF_TENSORS(float, float);
+    if (tp == DPPF_FLOAT32) DPPF_TENSORS(float, bf16);
+    if (tg == DPPF_FLOAT32) DPPF_TENSORS(bf16, float);
+    DPPF_TENSORS(bf16, bf16);
+#undef DPPF_TENSORS
+}
+
+struct TensorScalars {
+    const float *grad_scale;
+    AdamArgs args;
+    float b1, lr, wd;
+    unsigned seed_term;
+    int tp, tg, bits;
+};
+
+int64_t units_of(int64_t n) { return (n + kUnit - 1) / kUnit; }
+
+// Tensors [first, last) as one launch, or as many as the table and the unit count allow.
+template <int kEntries>
+int launch_table(const dppf_tensor *ts, int first, int last, const TensorScalars &p, int sms, cudaStream_t s) {
+    TensorTable<kEntries> tab;
+    tab.grad_scale = p.grad_scale;
+    tab.args = p.args;
+    tab.b1 = p.b1;
+    tab.seed_term = p.seed_term;
+    int k = first;
+    while (k < last) {
+        tab.n = 0;
+        int64_t units = 0;
+        for (; k < last && tab.n < kEntries; ++k) {
+            const dppf_tensor &t = ts[k];
+            if (t.numel == 0) continue;
+            if (units + units_of(t.numel) > INT_MAX / 2 && tab.n) break;
+            TensorEntry &e = tab.e[tab.n++];
+            e.param = t.param; e.grad = t.grad; e.m = t.exp_avg; e.v = t.exp_avg_sq;
+            e.m_scale = t.exp_avg_scale; e.v_scale = t.exp_avg_sq_scale;
+            e.n = t.numel;
+            e.decay = (float)(1.0 - (double)p.lr * (double)p.wd * (double)t.decay);
+            e.first_unit = (int)units;
+            units += units_of(t.numel);
+        }
+        if (tab.n == 0) break;
+        tab.units = (int)units;
+        const int rc = launch_tensors_types<kEntries>(tab, p.tp, p.tg, p.bits, sms, s);
+        if (rc != DPPF_OK) return rc;
+    }
+    return DPPF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dppf_embedding(const void *table, int table_type, int64_t V, int H, int64_t ld_table, const void *ids, int id_bits, int64_t T,
+                   float scale, void *out, int out_type, int64_t ld_out, void *cuda_stream) {
+    if (!known_type(table_type) || !known_type(out_type) || (id_bits != 32 && id_bits != 64)) return DPPF_ERR_INVALID_ARG;
+    if (V < 1 || V > INT_MAX - 1 || H < 1 || H > DPPF_MAX_WIDTH || T < 0 || T > INT_MAX || ld_table < H || ld_out < H || ld_table > kMaxLd || ld_out > kMaxLd ||
+        !std::isfinite(scale))
+        return DPPF_ERR_INVALID_ARG;
+    if (T == 0) return DPPF_OK;
+    if (!table || !ids || !out) return DPPF_ERR_INVALID_ARG;
+    if (!aligned_to(table, type_bytes(table_type)) || !aligned_to(out, type_bytes(out_type)) || !aligned_to(ids, id_bits / 8)) return DPPF_ERR_ALIGNMENT;
+    const size_t out_bytes = matrix_bytes(T, H, ld_out, out_type);
+    if (ranges_meet(out, out_bytes, table, matrix_bytes(V, H, ld_table, table_type)) || ranges_meet(out, out_bytes, ids, (size_t)T * (id_bits / 8)))
+        return DPPF_ERR_INVALID_ARG;
+    if (current_device() < 0) return DPPF_ERR_CUDA;
+    LookupArgs a;
+    a.table = table; a.ids = ids; a.out = out;
+    a.ld_table = ld_table; a.ld_out = ld_out; a.T = T; a.V = V; a.H = H; a.ids64 = id_bits == 64;
+    a.scale = scale;
+    const bool vec = H % 8 == 0 && rows_on_16(table, ld_table, table_type) && rows_on_16(out, ld_out, out_type);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    if (table_type == DPPF_FLOAT32) return out_type == DPPF_FLOAT32 ? launch_lookup<float, float>(a, vec, s) : launch_lookup<float, bf16>(a, vec, s);
+    return out_type == DPPF_FLOAT32 ? launch_lookup<bf16, float>(a, vec, s) : launch_lookup<bf16, bf16>(a, vec, s);
+}
+
+size_t dppf_embedding_workspace_bytes(int64_t T, int H) {
+    if (T < 1 || T > INT_MAX || H < 1 || H > DPPF_MAX_WIDTH) return 0;
+    return embedding_layout(T, H).total;
+}
+
+int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, const void *ids, int id_bits, int64_t T, float scale,
+                        void *grad_table, int table_type, int64_t V, int H, int64_t ld_table, int accumulate, void *ws,
+                        size_t ws_bytes, void *cuda_stream) {
+    if (!known_type(table_type) || !known_type(out_type) || (id_bits != 32 && id_bits != 64)) return DPPF_ERR_INVALID_ARG;
+    if (V < 1 || V > INT_MAX - 1 || H < 1 || H > DPPF_MAX_WIDTH || T < 0 || T > INT_MAX || ld_table < H || ld_out < H || ld_table > kMaxLd || ld_out > kMaxLd ||
+        !std::isfinite(scale))
+        return DPPF_ERR_INVALID_ARG;
+    if (!grad_table) return DPPF_ERR_INVALID_ARG;
+    if (!aligned_to(grad_table, type_bytes(table_type))) return DPPF_ERR_ALIGNMENT;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    if (T == 0) {
+        if (accumulate) return DPPF_OK;
+        return cudaMemset2DAsync(grad_table, (size_t)ld_table * type_bytes(table_type), 0, (size_t)H * type_bytes(table_type), (size_t)V, s) == cudaSuccess
+                   ? DPPF_OK : DPPF_ERR_CUDA;
+    }
+    if (!grad_out || !ids || !ws) return DPPF_ERR_INVALID_ARG;
+    if (!aligned_to(grad_out, type_bytes(out_type)) || !aligned_to(ids, id_bits / 8) || !aligned_to(ws, 128)) return DPPF_ERR_ALIGNMENT;
+    const EmbeddingLayout l = embedding_layout(T, H);
+    if (ws_bytes < l.total) return DPPF_ERR_WORKSPACE;
+    const size_t table_bytes = matrix_bytes(V, H, ld_table, table_type), out_bytes = matrix_bytes(T, H, ld_out, out_type), id_bytes = (size_t)T * (id_bits / 8);
+    if (ranges_meet(grad_table, table_bytes, grad_out, out_bytes) || ranges_meet(grad_table, table_bytes, ids, id_bytes) ||
+        ranges_meet(ws, l.total, grad_table, table_bytes) || ranges_meet(ws, l.total, grad_out, out_bytes) || ranges_meet(ws, l.total, ids, id_bytes))
+        return DPPF_ERR_INVALID_ARG;
+    const int dev = current_device();
+    if (dev < 0) return DPPF_ERR_CUDA;
+    const int sms = multiprocessors(dev);
+    if (sms < 0 || !allow_smem(embedding_sort_kernel, dev, g_sort_ready, kSortWarps * kBins * 4)) return DPPF_ERR_CUDA;
+
+    SortArgs a;
+    a.ids = ids; a.ids64 = id_bits == 64; a.V = V; a.T = (unsigned)T;
+    unsigned char *base = static_cast<unsigned char *>(ws);
+    for (int i = 0; i < 2; ++i) {
+        a.key[i] = reinterpret_cast<unsigned *>(base + l.key[i]);
+        a.pos[i] = reinterpret_cast<unsigned *>(base + l.pos[i]);
+    }
+    int bits = 1;
+    while (((int64_t)1 << bits) <= V) ++bits;                    // keys 0 .. V
+    a.passes = (bits + kDigitBits - 1) / kDigitBits;
+    a.bits = (bits + a.passes - 1) / a.passes;
+    const size_t es = type_bytes(table_type);
+    a.zero = accumulate ? nullptr : grad_table;
+    a.zero_ld = ld_table * (int64_t)es;
+    a.zero_width = (int64_t)H * (int64_t)es;
+    a.zero_vec = rows_on_16(grad_table, ld_table, table_type) && a.zero_width % 16 == 0;
+    int C = 1;
+    while (C < kSortMaxCluster && T > 2048LL * C) C *= 2;        // up to 64 tokens a warp before another block joins
+    long long fill = 0;                                          // blocks that write zeros
+    if (a.zero) {
+        fill = (V * a.zero_width + 65535) / 65536;
+        if (fill > 2LL * sms) fill = 2LL * sms;
+        fill = (fill + C - 1) / C * C;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(C + fill));
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = (size_t)kSortWarps * ((size_t)1 << a.bits) * 4;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)C;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, embedding_sort_kernel, a) != cudaSuccess) { cudaGetLastError(); return DPPF_ERR_CUDA; }
+
+    ReduceArgs r;
+    r.key = a.key[a.passes & 1]; r.pos = a.pos[a.passes & 1];
+    r.dout = grad_out; r.dtable = grad_table;
+    r.part = reinterpret_cast<float *>(base + l.part);
+    r.ld_dout = ld_out; r.ld_dtable = ld_table;
+    r.T = (unsigned)T; r.V = (unsigned)V; r.H = H;
+    r.tile = l.tile; r.tiles = l.tiles;
+    r.add = accumulate ? 1 : 0;
+    r.scale = scale;
+    const bool vec = H % 8 == 0 && rows_on_16(grad_table, ld_table, table_type) && rows_on_16(grad_out, ld_out, out_type);
+    r.groups = vec ? H / 8 : H;
+    r.row_threads = 1;
+    while (r.row_threads < kReduceThreads && r.row_threads < r.groups) r.row_threads *= 2;
+    const int per_block = kReduceThreads / r.row_threads;
+    const dim3 grid((unsigned)((r.tiles + per_block - 1) / per_block), (unsigned)((r.groups + r.row_threads - 1) / r.row_threads));
+    if (vec) launch_reduce_types<8>(r, out_type, table_type, grid, s);
+    else launch_reduce_types<1>(r, out_type, table_type, grid, s);
+    return launched();
+}
+
+size_t dppf_policy_workspace_bytes(int64_t T) {
+    if (T < 1 || T > DPPF_MAX_POLICY_TOKENS) return 0;
+    return kPolicyHeaderBytes + round256((size_t)T * 3 * sizeof(float));
+}
+
+int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld, const void *targets, int target_bits,
+                     const float *old_logp, const float *ref_logp, const float *advantage, const float *weight, float clip_low,
+                     float clip_high, float kl_coef, float temperature, float *sums_out, float *logp_out, void *grad_logits,
+                     int64_t ld_grad, void *ws, size_t ws_bytes, void *cuda_stream) {
+    if (!known_type(type) || (target_bits != 32 && target_bits != 64)) return DPPF_ERR_INVALID_ARG;
+    if (T < 1 || T > DPPF_MAX_POLICY_TOKENS || V < 1 || V > DPPF_MAX_VOCABULARY || ld < V || ld > kMaxLd) return DPPF_ERR_INVALID_ARG;
+    if (grad_logits && (ld_grad < V || ld_grad > kMaxLd)) return DPPF_ERR_INVALID_ARG;
+    if (!all_finite({clip_low, clip_high, kl_coef, temperature}) || clip_low < 0.f || clip_low > 1.f || clip_high < 0.f || !(temperature > 0.f) ||
+        !std::isfinite(1.4426950408889634 / temperature))
+        return DPPF_ERR_INVALID_ARG;
+    if (!logits || !targets || !old_logp || !advantage || !weight || !sums_out || !logp_out || !ws) return DPPF_ERR_INVALID_ARG;
+    if (kl_coef != 0.f && !ref_logp) return DPPF_ERR_INVALID_ARG;
+    if (!aligned_to(logits, type_bytes(type)) || !aligned_to(grad_logits, type_bytes(type)) || !aligned_to(targets, target_bits / 8) || !aligned_to(ws, 128) ||
+        !aligned_to(old_logp, 4) || !aligned_to(ref_logp, 4) || !aligned_to(advantage, 4) || !aligned_to(weight, 4) || !aligned_to(sums_out, 4) ||
+        !aligned_to(logp_out, 4))
+        return DPPF_ERR_ALIGNMENT;
+    const size_t need = dppf_policy_workspace_bytes(T);
+    if (ws_bytes < need) return DPPF_ERR_WORKSPACE;
+    const size_t in_bytes = matrix_bytes(T, V, ld, type), grad_bytes = grad_logits ? matrix_bytes(T, V, ld_grad, type) : 0, row = (size_t)T * 4;
+    const bool in_place = grad_logits == logits && ld_grad == ld;
+    if (!in_place && ranges_meet(grad_logits, grad_bytes, logits, in_bytes)) return DPPF_ERR_INVALID_ARG;
+    struct Range { const void *p; size_t n; };
+    const Range written[] = {{grad_logits, grad_bytes}, {logp_out, row}, {sums_out, 12}, {ws, need}};
+    const Range read[] = {{targets, (size_t)T * (target_bits / 8)}, {old_logp, row}, {ref_logp, row}, {advantage, row}, {weight, row}};
+    for (int i = 0; i < 4; ++i) {
+        for (const Range &r : read)
+            if (ranges_meet(written[i].p, written[i].n, r.p, r.n)) return DPPF_ERR_INVALID_ARG;
+        for (int k = 0; k < i; ++k)
+            if (ranges_meet(written[i].p, written[i].n, written[k].p, written[k].n)) return DPPF_ERR_INVALID_ARG;
+        if (i > 0 && ranges_meet(written[i].p, written[i].n, logits, in_bytes)) return DPPF_ERR_INVALID_ARG;
+    }
+    const int dev = current_device();
+    if (dev < 0) return DPPF_ERR_CUDA;
+    PolicyArgs a;
+    a.logits = logits; a.grad = grad_logits; a.ld = ld; a.ld_grad = ld_grad;
+    a.targets = targets; a.targets64 = target_bits == 64;
+    a.old_logp = old_logp; a.ref_logp = ref_logp; a.advantage = advantage; a.weight = weight;
+    a.logp = logp_out; a.sums = sums_out;
+    a.hdr = reinterpret_cast<PolicyHeader *>(ws);
+    a.terms = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + kPolicyHeaderBytes);
+    a.T = (int)T; a.V = V; a.slice = 0;
+    a.spin = dppf_internal::first_pass_polls();
+    a.clip_lo = (float)(1.0 - (double)clip_low);
+    a.clip_hi = (float)(1.0 + (double)clip_high);
+    a.kl_coef = kl_coef;
+    a.log2e_t = (float)(1.4426950408889634 / (double)temperature);
+    a.inv_t = (float)(1.0 / (double)temperature);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return type == DPPF_FLOAT32 ? launch_policy<float>(a, dev, s) : launch_policy<bf16>(a, dev, s);
+}
+
+int dppf_adamw_tensors(const dppf_tensor *tensors_host, int n_tensors, int param_type, int grad_type, int state_bits, float lr,
+                       float beta1, float beta2, float eps, float weight_decay, int step, const float *grad_scale, uint32_t seed,
+                       void *cuda_stream) {
+    if (n_tensors < 0 || (n_tensors && !tensors_host) || !known_type(param_type) || !known_type(grad_type) || (state_bits != 8 && state_bits != 32))
+        return DPPF_ERR_INVALID_ARG;
+    if (!all_finite({lr, beta1, beta2, eps, weight_decay}) || step < 1) return DPPF_ERR_INVALID_ARG;
+    if (!(beta1 >= 0.f && beta1 < 1.f && beta2 >= 0.f && beta2 < 1.f)) return DPPF_ERR_INVALID_ARG;
+    if (!aligned_to(grad_scale, 4)) return DPPF_ERR_ALIGNMENT;
+    int present = 0;
+    for (int k = 0; k < n_tensors; ++k) {
+        const dppf_tensor &t = tensors_host[k];
+        if (t.numel < 0 || t.numel > ((int64_t)1 << 40) || !std::isfinite(t.decay)) return DPPF_ERR_INVALID_ARG;
+        if (t.numel == 0) continue;
+        ++present;
+        const size_t n = (size_t)t.numel, scales = state_bits == 8 ? (n + kStateBlock - 1) / kStateBlock * 4 : 0;
+        if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq) return DPPF_ERR_INVALID_ARG;
+        if (state_bits == 8 && (!t.exp_avg_scale || !t.exp_avg_sq_scale)) return DPPF_ERR_INVALID_ARG;
+        if (!aligned_to(t.param, type_bytes(param_type)) || !aligned_to(t.grad, type_bytes(grad_type))) return DPPF_ERR_ALIGNMENT;
+        if (state_bits == 32 ? !aligned_to(t.exp_avg, 4) || !aligned_to(t.exp_avg_sq, 4) : !aligned_to(t.exp_avg_scale, 4) || !aligned_to(t.exp_avg_sq_scale, 4))
+            return DPPF_ERR_ALIGNMENT;
+        const size_t state = n * (size_t)(state_bits / 8);
+        const void *p[6] = {t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale};
+        const size_t b[6] = {n * type_bytes(param_type), n * type_bytes(grad_type), state, state, scales, scales};
+        for (int i = 0; i < 6; ++i)
+            for (int j = 0; j < i; ++j)
+                if (ranges_meet(p[i], b[i], p[j], b[j])) return DPPF_ERR_INVALID_ARG;
+    }
+    if (present == 0) return DPPF_OK;
+    const int dev = current_device();
+    const int sms = dev < 0 ? -1 : multiprocessors(dev);
+    if (sms < 0) return DPPF_ERR_CUDA;
+    TensorScalars p;
+    p.grad_scale = grad_scale;
+    const double bc1 = 1.0 - std::pow((double)beta1, (double)step), bc2 = 1.0 - std::pow((double)beta2, (double)step);
+    p.args.m1 = p.args.m2 = nullptr;
+    p.args.g = nullptr;
+    p.args.decay = 0.f;                                          // each tensor's own
+    p.args.one_minus_b1 = (float)(1.0 - (double)beta1);
+    p.args.b2 = beta2;
+    p.args.one_minus_b2 = (float)(1.0 - (double)beta2);
+    p.args.step_size = (float)((double)lr / bc1);
+    p.args.inv_sqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
+    p.args.eps = eps;
+    p.b1 = beta1; p.lr = lr; p.wd = weight_decay;
+    p.seed_term = seed * 0x9e3779b9u;
+    p.tp = param_type; p.tg = grad_type; p.bits = state_bits;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    if (present <= kSmallTable) return launch_table<kSmallTable>(tensors_host, 0, n_tensors, p, sms, s);
+    return launch_table<kLargeTable>(tensors_host, 0, n_tensors, p, sms, s);
+}
+
+}  // extern "C"
