@@ -2,12 +2,14 @@
 #pragma once
 #include "adamw_element.cuh"
 #include "local_common.cuh"
+#include <cuda_fp16.h>
+#include <type_traits>
 
 namespace {
 
-// The recurrence is that of adamw1.  A work unit is 2048 consecutive elements of one tensor, eight
-// warps of 256; the table of tensors travels in the launch's parameters (nothing on the device can be
-// stale), and a block finds a unit's tensor by bisection.
+// The recurrence is that of adamw1.  A work unit is 256 consecutive elements of one tensor, held by a
+// warp, eight a lane; the table of tensors travels in the launch's parameters (nothing on the device can
+// be stale).  A warp finds its first unit's tensor by bisection and walks the table from there.
 //
 // States in 8 bits: blocks of 256 elements counted from the tensor's start, which is what a warp holds.
 //   m = code_m * scale_m,  sqrt(v) = code_r * scale_r,  codes e4m3, scale = (block's largest) / 448.
@@ -20,8 +22,8 @@ namespace {
 // operations (no fused multiply-adds), so that a few lines of plain code give the same codes.
 
 constexpr int kTensorThreads = 256;
-constexpr int kUnit = 2048;
-constexpr int kStateBlock = 256;
+constexpr int kTensorWarps = kTensorThreads / 32;
+constexpr int kStateBlock = 256;                       // elements of a work unit, and of a block of 8-bit states
 constexpr int kSmallTable = 60, kLargeTable = 500;     // table sizes: 4 KB and 32 KB of launch parameters
 
 struct TensorEntry {
@@ -44,6 +46,90 @@ struct TensorTable {
     int n, units;
 };
 
+// ---------------------------------------------------------------- eight elements of a lane, as stored
+// kVec: elements 8 lane .. 8 lane + 7 of the unit, in 16-byte accesses (8-byte for codes); otherwise elements
+// lane, lane + 32, ..., which any alignment allows.  Elements past the tensor's end read as zero.
+
+template <typename T> struct Raw { unsigned w[2 * sizeof(T)]; };
+
+template <bool kVec> __device__ __forceinline__ long long element_at(long long e0, int k) { return kVec ? e0 + k : e0 + 32 * k; }
+
+template <typename T, bool kVec>
+__device__ __forceinline__ Raw<T> load_raw(const void *base, long long e0, long long n) {
+    const T *p = static_cast<const T *>(base);
+    constexpr int kWords = 2 * (int)sizeof(T);
+    Raw<T> r;
+    if (kVec && e0 + 8 <= n) {
+        if constexpr (kWords == 2) {
+            const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p + e0));
+            r.w[0] = u.x; r.w[1] = u.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) {
+                const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p + e0) + i);
+                r.w[4 * i] = u.x; r.w[4 * i + 1] = u.y; r.w[4 * i + 2] = u.z; r.w[4 * i + 3] = u.w;
+            }
+        }
+        return r;
+    }
+    using U = typename std::conditional<sizeof(T) == 4, unsigned, typename std::conditional<sizeof(T) == 2, unsigned short, unsigned char>::type>::type;
+    constexpr int kPer = 4 / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+        r.w[i] = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const long long e = element_at<kVec>(e0, i * kPer + j);
+            if (e < n) r.w[i] |= (unsigned)__ldcs(reinterpret_cast<const U *>(p) + e) << (8 * (int)sizeof(T) * j);
+        }
+    }
+    return r;
+}
+
+template <typename T, bool kVec>
+__device__ __forceinline__ void store_raw(void *base, long long e0, long long n, const Raw<T> &r) {
+    T *p = static_cast<T *>(base);
+    constexpr int kWords = 2 * (int)sizeof(T);
+    if (kVec && e0 + 8 <= n) {
+        if constexpr (kWords == 2) {
+            __stcs(reinterpret_cast<uint2 *>(p + e0), make_uint2(r.w[0], r.w[1]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i)
+                __stcs(reinterpret_cast<uint4 *>(p + e0) + i, make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]));
+        }
+        return;
+    }
+    using U = typename std::conditional<sizeof(T) == 4, unsigned, typename std::conditional<sizeof(T) == 2, unsigned short, unsigned char>::type>::type;
+    constexpr int kPer = 4 / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i)
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const long long e = element_at<kVec>(e0, i * kPer + j);
+            if (e < n) __stcs(reinterpret_cast<U *>(p) + e, (U)(r.w[i] >> (8 * (int)sizeof(T) * j)));
+        }
+}
+
+__device__ __forceinline__ float2 pair_of(const Raw<float> &r, int i) { return make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1])); }
+__device__ __forceinline__ float2 pair_of(const Raw<bf16> &r, int i) { return make_float2(bf16_low(r.w[i]), bf16_high(r.w[i])); }
+__device__ __forceinline__ void set_pair(Raw<float> &r, int i, float2 f) { r.w[2 * i] = __float_as_uint(f.x); r.w[2 * i + 1] = __float_as_uint(f.y); }
+__device__ __forceinline__ void set_pair(Raw<bf16> &r, int i, float2 f) { r.w[i] = bf16_pair(f.x, f.y); }
+
+// ---------------------------------------------------------------- 8-bit states
+
+using code8 = unsigned char;
+
+__device__ __forceinline__ float2 e4m3_values(const Raw<code8> &r, int i) {       // codes 2 i, 2 i + 1
+    unsigned h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)(r.w[i >> 1] >> (16 * (i & 1)))));   // exact
+    return __half22float2(*reinterpret_cast<__half2 *>(&h));
+}
+__device__ __forceinline__ unsigned e4m3_nearest(float2 y) {
+    unsigned short c;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(y.y), "f"(y.x));
+    return c;
+}
 // Two elements of a pair share one 32-bit hash (the finalizer of MurmurHash3, by Austin Appleby).
 __device__ __forceinline__ unsigned pair_hash(unsigned pair, unsigned seed_term) {
     unsigned h = pair + seed_term;
@@ -51,182 +137,163 @@ __device__ __forceinline__ unsigned pair_hash(unsigned pair, unsigned seed_term)
     h ^= h >> 13; h *= 0xc2b2ae35u;
     return h ^ (h >> 16);
 }
-
-// e4m3 magnitudes: an fp32 number's bits from bit 20 on, once 2^-120 has matched the exponents' offsets.
-__device__ __forceinline__ float e4m3_value(unsigned code) { return __uint_as_float((code & 0x7fu) << 20) * 0x1p120f; }
-__device__ __forceinline__ unsigned e4m3_random(float y, unsigned bits20) {
-    const unsigned c = (__float_as_uint(__fmul_rn(y, 0x1p-120f)) + bits20) >> 20;
-    return min(c, 0x7eu);
+// e4m3 magnitudes are an fp32 number's bits from bit 20 on, once 2^-120 has matched the exponents'
+// offsets (z = y 2^-120; y is at most 448 and a few ulp).  16 random bits are added below bit 20; the code comes
+// back in the top byte.  What is not zero does not become zero.
+__device__ __forceinline__ unsigned e4m3_random_top(float y, float z, unsigned random_at_8) {
+    const unsigned t = (__float_as_uint(z) << 4) + random_at_8;
+    return y > 0.f ? max(t, 1u << 24) : t;
 }
-__device__ __forceinline__ unsigned e4m3_nearest2(float lo, float hi) {       // two codes
-    unsigned short c;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(hi), "f"(lo));
-    return c;
+__device__ __forceinline__ float max_abs(float a, float b) {                      // NaN if either is
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(fabsf(b)));
+    return d;
 }
 // Scale of a block from its largest magnitude (fp32 bits order as magnitudes do; NaN is above infinity).
-__device__ __forceinline__ void block_scale(unsigned top_bits, float &scale, float &over) {
-    scale = __fmul_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, top_bits)), 1.0f / 448.0f);
+__device__ __forceinline__ void block_scale(float top, float &scale, float &over) {
+    scale = __fmul_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu)), 1.0f / 448.0f);
     if (scale < 0x1p-126f) scale = 0.f;
     over = scale == 0.f ? 0.f : __fdiv_rn(1.f, scale);
 }
 
-// Eight elements of a lane: consecutive (kVec) or 32 apart (any alignment).
+template <typename TP, typename TG>
+struct Unit8 {
+    Raw<TP> p;
+    Raw<TG> g;
+    Raw<code8> m, r;
+    float ms, rs;
+};
+
 template <typename TP, typename TG, bool kVec>
-__device__ __forceinline__ void adamw8_elements(const TensorEntry &t, long long base, int lane, const AdamArgs &a, float b1,
-                                                float gs, unsigned seed_term) {
-    const long long blk = base / kStateBlock;
-    const float ms = __ldcg(t.m_scale + blk), rs = __ldcg(t.v_scale + blk);
-    TP *param = static_cast<TP *>(t.param);
-    const TG *grad = static_cast<const TG *>(t.grad);
-    unsigned char *mc = static_cast<unsigned char *>(t.m), *rc = static_cast<unsigned char *>(t.v);
-    float p[8], g[8], m[8], r[8];
-    unsigned cm[8], cr[8];
-    const long long e0 = base + (kVec ? lane * 8 : lane);
-    auto at = [&](int k) { return kVec ? e0 + k : e0 + 32 * k; };
-    const bool whole = kVec && e0 + 8 <= t.n;
-    if (whole) {
-        load_vec<TP, 8>(param + e0, p);
-        load_vec<TG, 8>(grad + e0, g);
-        const uint2 um = __ldcs(reinterpret_cast<const uint2 *>(mc + e0)), ur = __ldcs(reinterpret_cast<const uint2 *>(rc + e0));
+__device__ __forceinline__ void load_unit8(const TensorEntry &t, int blk, int lane, Unit8<TP, TG> &u) {
+    const long long e0 = (long long)blk * kStateBlock + (kVec ? lane * 8 : lane);
+    u.p = load_raw<TP, kVec>(t.param, e0, t.n);
+    u.g = load_raw<TG, kVec>(t.grad, e0, t.n);
+    u.m = load_raw<code8, kVec>(t.m, e0, t.n);
+    u.r = load_raw<code8, kVec>(t.v, e0, t.n);
+    u.ms = __ldcg(t.m_scale + blk);
+    u.rs = __ldcg(t.v_scale + blk);
+}
+
+template <typename TP, typename TG, bool kVec>
+__device__ __forceinline__ void step_unit8(const TensorEntry &t, int blk, int lane, Unit8<TP, TG> &u, const AdamArgs &a, float b1,
+                                           float gs, unsigned seed_term) {
+    const long long e0 = (long long)blk * kStateBlock + (kVec ? lane * 8 : lane);
+    float2 m[4], r[4];
+    float mtop = 0.f, rtop = 0.f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            cm[k] = ((k < 4 ? um.x : um.y) >> (8 * (k & 3))) & 0xffu;
-            cr[k] = ((k < 4 ? ur.x : ur.y) >> (8 * (k & 3))) & 0xffu;
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const bool in = at(k) < t.n;
-            p[k] = in ? to_float(param[at(k)]) : 0.f;
-            g[k] = in ? to_float(grad[at(k)]) : 0.f;
-            cm[k] = in ? mc[at(k)] : 0u;
-            cr[k] = in ? rc[at(k)] : 0u;
-        }
+    for (int i = 0; i < 4; ++i) {
+        const float2 g = mul2(pair_of(u.g, i), both(gs));
+        const float2 old = mul2(e4m3_values(u.m, i), both(u.ms)), root = mul2(e4m3_values(u.r, i), both(u.rs));
+        const float2 m0 = mul2(old, both(b1)), m1 = mul2(g, both(a.one_minus_b1));
+        const float2 v0 = mul2(mul2(root, root), both(a.b2)), v1 = mul2(mul2(g, g), both(a.one_minus_b2));
+        m[i] = make_float2(__fadd_rn(m0.x, m1.x), __fadd_rn(m0.y, m1.y));
+        r[i] = make_float2(__fsqrt_rn(__fadd_rn(v0.x, v1.x)), __fsqrt_rn(__fadd_rn(v0.y, v1.y)));
+        mtop = max_abs(max_abs(mtop, m[i].x), m[i].y);
+        rtop = max_abs(max_abs(rtop, r[i].x), r[i].y);
+        // the update itself, in 2 ulp: it is small against the parameter that it is added to
+        const float2 den = fma2(r[i], both(a.inv_sqrt_bc2), both(a.eps));
+        const float2 step = make_float2(__fdividef(m[i].x, den.x), __fdividef(m[i].y, den.y));
+        set_pair(u.p, i, fma2(both(-a.step_size), step, mul2(pair_of(u.p, i), both(t.decay))));
     }
-    unsigned mtop = 0, rtop = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const float mag = e4m3_value(cm[k]);
-        const float old = __fmul_rn((cm[k] & 0x80u) ? -mag : mag, ms);
-        const float root = __fmul_rn(e4m3_value(cr[k]), rs);
-        const float gk = __fmul_rn(g[k], gs);
-        m[k] = __fadd_rn(__fmul_rn(old, b1), __fmul_rn(gk, a.one_minus_b1));
-        const float v = __fadd_rn(__fmul_rn(__fmul_rn(root, root), a.b2), __fmul_rn(__fmul_rn(gk, gk), a.one_minus_b2));
-        r[k] = __fsqrt_rn(v);
-        mtop = max(mtop, __float_as_uint(m[k]) & 0x7fffffffu);
-        rtop = max(rtop, __float_as_uint(r[k]) & 0x7fffffffu);
-        p[k] = __fmul_rn(p[k], t.decay);
-        p[k] = __fmaf_rn(-a.step_size, __fdiv_rn(m[k], __fmaf_rn(r[k], a.inv_sqrt_bc2, a.eps)), p[k]);
-    }
+    store_raw<TP, kVec>(t.param, e0, t.n, u.p);
     float msc, mover, rsc, rover;
     block_scale(mtop, msc, mover);
     block_scale(rtop, rsc, rover);
+    unsigned top[8];
 #pragma unroll
-    for (int k = 0; k < 8; k += 2) {
-        const unsigned c = e4m3_nearest2(__fmul_rn(m[k], mover), __fmul_rn(m[k + 1], mover));
-        cm[k] = c & 0xffu;
-        cm[k + 1] = (c >> 8) & 0xffu;
+    for (int i = 0; i < 4; ++i) {
+        const unsigned c = e4m3_nearest(mul2(m[i], both(mover)));
+        if (i & 1) u.m.w[i >> 1] |= c << 16;
+        else u.m.w[i >> 1] = c;
+        const float2 y = mul2(r[i], both(rover)), z = mul2(y, both(0x1p-120f));
+        if (kVec) {
+            const unsigned h = pair_hash(((unsigned)e0 >> 1) + i, seed_term);
+            top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h, 0, 0x4104));          // low half at bit 8
+            top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h, 0, 0x4324));      // high half at bit 8
+        } else {
+            const unsigned first = (unsigned)element_at<kVec>(e0, 2 * i);          // both of the lane's parity
+            const unsigned h0 = pair_hash(first >> 1, seed_term), h1 = pair_hash((first >> 1) + 16, seed_term);
+            const unsigned pick = (first & 1) ? 0x4324 : 0x4104;
+            top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h0, 0, pick));
+            top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h1, 0, pick));
+        }
     }
-    unsigned h = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const unsigned idx = (unsigned)at(k);
-        if (!kVec || (k & 1) == 0) h = pair_hash(idx >> 1, seed_term);
-        const unsigned half = (idx & 1u) ? h >> 16 : h & 0xffffu;
-        cr[k] = e4m3_random(__fmul_rn(r[k], rover), half << 4);
-        if (r[k] > 0.f && rover > 0.f) cr[k] = max(cr[k], 1u);
-    }
-    if (whole) {
-        uint2 um, ur;
-        um.x = cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24;
-        um.y = cm[4] | cm[5] << 8 | cm[6] << 16 | cm[7] << 24;
-        ur.x = cr[0] | cr[1] << 8 | cr[2] << 16 | cr[3] << 24;
-        ur.y = cr[4] | cr[5] << 8 | cr[6] << 16 | cr[7] << 24;
-        store_vec<TP, 8>(param + e0, p);
-        __stcs(reinterpret_cast<uint2 *>(mc + e0), um);
-        __stcs(reinterpret_cast<uint2 *>(rc + e0), ur);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (at(k) < t.n) {
-                param[at(k)] = from_float<TP>(p[k]);
-                mc[at(k)] = (unsigned char)cm[k];
-                rc[at(k)] = (unsigned char)cr[k];
-            }
-    }
+    for (int i = 0; i < 2; ++i)
+        u.r.w[i] = __byte_perm(__byte_perm(top[4 * i], top[4 * i + 1], 0x0073), __byte_perm(top[4 * i + 2], top[4 * i + 3], 0x0073), 0x5410);
+    store_raw<code8, kVec>(t.m, e0, t.n, u.m);
+    store_raw<code8, kVec>(t.v, e0, t.n, u.r);
     if (lane == 0) {
         t.m_scale[blk] = msc;
         t.v_scale[blk] = rsc;
     }
 }
 
+// ---------------------------------------------------------------- fp32 states
+
 template <typename TP, typename TG, bool kVec>
-__device__ __forceinline__ void adamw32_elements(const TensorEntry &t, long long base, int lane, const AdamArgs &a, float gs) {
-    TP *param = static_cast<TP *>(t.param);
-    const TG *grad = static_cast<const TG *>(t.grad);
-    float *pm = static_cast<float *>(t.m), *pv = static_cast<float *>(t.v);
+__device__ __forceinline__ void step_unit32(const TensorEntry &t, int blk, int lane, const AdamArgs &a, float gs) {
+    const long long e0 = (long long)blk * kStateBlock + (kVec ? lane * 8 : lane);
     AdamArgs mine = a;
     mine.decay = t.decay;
-    float p[8], g[8], m[8], v[8];
-    const long long e0 = base + (kVec ? lane * 8 : lane);
-    auto at = [&](int k) { return kVec ? e0 + k : e0 + 32 * k; };
-    const bool whole = kVec && e0 + 8 <= t.n;
-    if (whole) {
-        load_vec<TP, 8>(param + e0, p);
-        load_vec<TG, 8>(grad + e0, g);
-        load_vec<float, 8>(pm + e0, m);
-        load_vec<float, 8>(pv + e0, v);
-    } else {
+    Raw<TP> p = load_raw<TP, kVec>(t.param, e0, t.n);
+    const Raw<TG> g = load_raw<TG, kVec>(t.grad, e0, t.n);
+    Raw<float> m = load_raw<float, kVec>(t.m, e0, t.n), v = load_raw<float, kVec>(t.v, e0, t.n);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (at(k) < t.n) {
-                p[k] = to_float(param[at(k)]);
-                g[k] = to_float(grad[at(k)]);
-                m[k] = pm[at(k)];
-                v[k] = pv[at(k)];
-            } else {
-                p[k] = g[k] = m[k] = v[k] = 0.f;
-            }
+    for (int i = 0; i < 4; ++i) {
+        float2 pp = pair_of(p, i), mm = pair_of(m, i), vv = pair_of(v, i);
+        const float2 gg = pair_of(g, i);
+        adamw1(pp.x, mm.x, vv.x, __fmul_rn(gg.x, gs), mine);
+        adamw1(pp.y, mm.y, vv.y, __fmul_rn(gg.y, gs), mine);
+        set_pair(p, i, pp);
+        set_pair(m, i, mm);
+        set_pair(v, i, vv);
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) adamw1(p[k], m[k], v[k], __fmul_rn(g[k], gs), mine);
-    if (whole) {
-        store_vec<TP, 8>(param + e0, p);
-        store_vec<float, 8>(pm + e0, m);
-        store_vec<float, 8>(pv + e0, v);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (at(k) < t.n) {
-                param[at(k)] = from_float<TP>(p[k]);
-                pm[at(k)] = m[k];
-                pv[at(k)] = v[k];
-            }
-    }
+    store_raw<TP, kVec>(t.param, e0, t.n, p);
+    store_raw<float, kVec>(t.m, e0, t.n, m);
+    store_raw<float, kVec>(t.v, e0, t.n, v);
+}
+
+// ---------------------------------------------------------------- the kernel
+
+template <int kBits>
+__device__ __forceinline__ bool takes_vectors(const TensorEntry &t) {
+    const uintptr_t wide = reinterpret_cast<uintptr_t>(t.param) | reinterpret_cast<uintptr_t>(t.grad);
+    const uintptr_t states = reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v);
+    return kBits == 32 ? ((wide | states) & 15u) == 0 : (wide & 15u) == 0 && (states & 7u) == 0;
 }
 
 template <typename TP, typename TG, int kBits, int kEntries>
-__global__ void __launch_bounds__(kTensorThreads) adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
+__global__ void __launch_bounds__(kTensorThreads, kBits == 8 ? 4 : 3)
+adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
     const float gs = tab.grad_scale ? __ldg(tab.grad_scale) : 1.f;
     if (!isfinite(gs)) return;                              // a step whose gradients overflowed is skipped whole
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int u = blockIdx.x; u < tab.units; u += gridDim.x) {
-        int lo = 0, hi = tab.n;                             // the last tensor with first_unit <= u
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (tab.e[mid].first_unit <= u) lo = mid; else hi = mid;
-        }
-        const TensorEntry &t = tab.e[lo];
-        const long long base = (long long)(u - t.first_unit) * kUnit + warp * kStateBlock;
-        if (base >= t.n) continue;
-        const uintptr_t wide = reinterpret_cast<uintptr_t>(t.param) | reinterpret_cast<uintptr_t>(t.grad);
-        const uintptr_t states = reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v);
+    const int lane = threadIdx.x & 31;
+    const int stride = gridDim.x * kTensorWarps;
+    int u = blockIdx.x * kTensorWarps + (threadIdx.x >> 5);
+    if (u >= tab.units) return;
+    int k = 0, hi = tab.n;                                  // the last tensor with first_unit <= u
+    while (hi - k > 1) {
+        const int mid = (k + hi) >> 1;
+        if (tab.e[mid].first_unit <= u) k = mid; else hi = mid;
+    }
+    for (; u < tab.units; u += stride) {
+        while (k + 1 < tab.n && tab.e[k + 1].first_unit <= u) ++k;
+        const TensorEntry &t = tab.e[k];
+        const int blk = u - t.first_unit;
         if constexpr (kBits == 32) {
-            if (((wide | states) & 15u) == 0) adamw32_elements<TP, TG, true>(t, base, lane, tab.args, gs);
-            else adamw32_elements<TP, TG, false>(t, base, lane, tab.args, gs);
+            if (takes_vectors<kBits>(t)) step_unit32<TP, TG, true>(t, blk, lane, tab.args, gs);
+            else step_unit32<TP, TG, false>(t, blk, lane, tab.args, gs);
         } else {
-            if ((wide & 15u) == 0 && (states & 7u) == 0) adamw8_elements<TP, TG, true>(t, base, lane, tab.args, tab.b1, gs, tab.seed_term);
-            else adamw8_elements<TP, TG, false>(t, base, lane, tab.args, tab.b1, gs, tab.seed_term);
+            Unit8<TP, TG> x;
+            if (takes_vectors<kBits>(t)) {
+                load_unit8<TP, TG, true>(t, blk, lane, x);
+                step_unit8<TP, TG, true>(t, blk, lane, x, tab.args, tab.b1, gs, tab.seed_term);
+            } else {
+                load_unit8<TP, TG, false>(t, blk, lane, x);
+                step_unit8<TP, TG, false>(t, blk, lane, x, tab.args, tab.b1, gs, tab.seed_term);
+            }
         }
     }
 }

@@ -78,6 +78,32 @@ __device__ __forceinline__ void store_vec(T *p, const float (&f)[N]) {
     }
 }
 
+// ---------------------------------------------------------------- two fp32 operations in one instruction
+// Each result is rounded by itself.  There is no packed sum here: one that follows a packed product was
+// seen to come out as a fused multiply-add, in spite of .rn, so separately rounded sums are scalar.
+
+__device__ __forceinline__ unsigned long long pack2(float2 a) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x), "f"(a.y));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(unsigned long long a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)));
+    return unpack2(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)), "l"(pack2(c)));
+    return unpack2(r);
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // ---------------------------------------------------------------- clusters
 
 __device__ __forceinline__ unsigned cluster_rank() {

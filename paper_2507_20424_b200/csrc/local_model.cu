@@ -176,7 +176,8 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
 
 template <typename TP, typename TG, int kBits, int kEntries>
 int launch_tensors(const TensorTable<kEntries> &tab, int sms, cudaStream_t s) {
-    const int grid = tab.units < sms * 8 ? tab.units : sms * 8;
+    const int blocks = (tab.units + kTensorWarps - 1) / kTensorWarps, most = sms * (kBits == 8 ? 4 : 3);
+    const int grid = blocks < most ? blocks : most;
     adamw_tensors_kernel<TP, TG, kBits, kEntries><<<grid, kTensorThreads, 0, s>>>(tab);
     return launched();
 }
@@ -199,7 +200,7 @@ struct TensorScalars {
     int tp, tg, bits;
 };
 
-int64_t units_of(int64_t n) { return (n + kUnit - 1) / kUnit; }
+int64_t units_of(int64_t n) { return (n + kStateBlock - 1) / kStateBlock; }
 
 // Tensors [first, last) as one launch, or as many as the table and the unit count allow.
 template <int kEntries>
