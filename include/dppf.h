@@ -379,7 +379,7 @@ int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld,
 
 /*
  * One AdamW step over many tensors at once (the recurrence of dppf_adamw_step, element by element), in one
- * launch per 500 tensors.  tensors_host: HOST array; it is copied during the call.
+ * launch per 440 tensors.  tensors_host: HOST array; it is copied during the call.
  *   param, grad       numel elements of param_type / grad_type (one type each for all tensors); grad is
  *                     read only and multiplied by *grad_scale first (device fp32[1], e.g. a clipping
  *                     coefficient; NULL = 1).  If *grad_scale is not finite NOTHING is changed.

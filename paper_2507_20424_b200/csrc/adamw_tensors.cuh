@@ -24,7 +24,15 @@ namespace {
 constexpr int kTensorThreads = 256;
 constexpr int kTensorWarps = kTensorThreads / 32;
 constexpr int kStateBlock = 256;                       // elements of a work unit, and of a block of 8-bit states
-constexpr int kSmallTable = 60, kLargeTable = 500;     // table sizes: 4 KB and 32 KB of launch parameters
+constexpr int kGroup = 4;                              // units that a warp takes at a time with 8-bit states, where there are enough
+constexpr int kSmallTable = 50, kLargeTable = 440;     // table sizes: under 4 KB and 32 KB of launch parameters
+
+// Resident blocks an SM.  Fewer loads in flight run faster once there are enough of them, since reads and writes
+// share the memory: fp32 states with fp32 parameters and gradients 2 blocks (86.6M elements: 371 us; 3: 425 us), with
+// bf16 ones 3 (295 us; 2: 364 us, 4: 336 us), with one of each 3.  8-bit states are bound by instructions and registers: 2 blocks of
+// 128 registers and groups of four units (300M bf16: 535 us; groups of 2, 80 registers: 587 us; single units: 675 to 780 us).
+template <typename TP, typename TG, int kBits>
+struct TensorShape { static constexpr int kBlocks = kBits == 8 || sizeof(TP) + sizeof(TG) == 8 ? 2 : 3; };
 
 struct TensorEntry {
     void *param;
@@ -34,6 +42,8 @@ struct TensorEntry {
     long long n;
     float decay;                 // 1 - lr * weight decay of this tensor
     int first_unit;
+    int lead;                    // 32 bits: elements that the first unit begins before the tensor (0 .. 63); 8 bits: 0; -1: only
+                                 // accesses of any alignment
 };
 
 template <int kEntries>
@@ -44,71 +54,146 @@ struct TensorTable {
     float b1;
     unsigned seed_term;
     int n, units;
+    int group;                   // units a warp takes at a time: 1, or (8-bit states) kGroup
 };
 
 // ---------------------------------------------------------------- eight elements of a lane, as stored
-// kVec: elements 8 lane .. 8 lane + 7 of the unit, in 16-byte accesses (8-byte for codes); otherwise elements
-// lane, lane + 32, ..., which any alignment allows.  Elements past the tensor's end read as zero.
+enum Access {
+    kAnyAlignment,   // elements lane, lane + 32, ... of the unit; those outside the tensor read as zero and are not written
+    kAligned,        // elements 8 lane .. 8 lane + 7 of a unit that lies inside its tensor, in 16-byte accesses (8-byte ones for codes)
+    kSkewed          // the same for a unit that does not start on a 16-byte boundary: read and written in the aligned 16-byte
+                     // pieces that cover it, and moved into place between neighbouring lanes.  Pieces reach over the unit's ends
+                     // into the same 16 bytes as one of its elements: what is read there is not used, and those two pieces are
+                     // written element by element.  Codes have to be 8-byte aligned all the same.
+};
 
 template <typename T> struct Raw { unsigned w[2 * sizeof(T)]; };
+template <typename T> struct Bits { using type = unsigned; };
+template <> struct Bits<bf16> { using type = unsigned short; };
+template <> struct Bits<unsigned char> { using type = unsigned char; };
 
-template <bool kVec> __device__ __forceinline__ long long element_at(long long e0, int k) { return kVec ? e0 + k : e0 + 32 * k; }
+// Bytes by which a tensor's units start after a 16-byte boundary: the same for all of them.
+__device__ __forceinline__ unsigned skew(const void *p) { return (unsigned)(reinterpret_cast<uintptr_t>(p) & 15u); }
 
-template <typename T, bool kVec>
-__device__ __forceinline__ Raw<T> load_raw(const void *base, long long e0, long long n) {
+// A lane's element k of eight, counted from the unit's first.
+template <int kAccess> __device__ __forceinline__ int lane_element(int lane, int k) { return kAccess == kAnyAlignment ? lane + 32 * k : 8 * lane + k; }
+
+// `first`: the unit's first element (may be negative with kAnyAlignment).
+template <typename T, int kAccess>
+__device__ __forceinline__ Raw<T> load_raw(const void *base, long long first, long long n, int lane) {
     const T *p = static_cast<const T *>(base);
-    constexpr int kWords = 2 * (int)sizeof(T);
+    constexpr int kWords = 2 * (int)sizeof(T), kPer = 4 / (int)sizeof(T);
     Raw<T> r;
-    if (kVec && e0 + 8 <= n) {
-        if constexpr (kWords == 2) {
-            const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p + e0));
-            r.w[0] = u.x; r.w[1] = u.y;
-        } else {
+    if constexpr (kAccess == kAnyAlignment) {
+        using U = typename Bits<T>::type;
 #pragma unroll
-            for (int i = 0; i < kWords / 4; ++i) {
-                const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p + e0) + i);
-                r.w[4 * i] = u.x; r.w[4 * i + 1] = u.y; r.w[4 * i + 2] = u.z; r.w[4 * i + 3] = u.w;
+        for (int i = 0; i < kWords; ++i) {
+            r.w[i] = 0;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const long long e = first + lane_element<kAccess>(lane, i * kPer + j);
+                if (e >= 0 && e < n) r.w[i] |= (unsigned)__ldcs(reinterpret_cast<const U *>(p) + e) << (8 * (int)sizeof(T) * j);
             }
         }
-        return r;
-    }
-    using U = typename std::conditional<sizeof(T) == 4, unsigned, typename std::conditional<sizeof(T) == 2, unsigned short, unsigned char>::type>::type;
-    constexpr int kPer = 4 / (int)sizeof(T);
+    } else if constexpr (kWords == 2) {
+        const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p + first + 8 * lane));
+        r.w[0] = u.x; r.w[1] = u.y;
+    } else {                                                  // kSkewed: the covering pieces, for settle()
+        const char *q = reinterpret_cast<const char *>(p + first + 8 * lane) - (kAccess == kSkewed ? skew(p) : 0u);
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-        r.w[i] = 0;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const long long e = element_at<kVec>(e0, i * kPer + j);
-            if (e < n) r.w[i] |= (unsigned)__ldcs(reinterpret_cast<const U *>(p) + e) << (8 * (int)sizeof(T) * j);
+        for (int i = 0; i < kWords / 4; ++i) {
+            const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(q) + i);
+            r.w[4 * i] = u.x; r.w[4 * i + 1] = u.y; r.w[4 * i + 2] = u.z; r.w[4 * i + 3] = u.w;
         }
     }
     return r;
 }
 
-template <typename T, bool kVec>
-__device__ __forceinline__ void store_raw(void *base, long long e0, long long n, const Raw<T> &r) {
-    T *p = static_cast<T *>(base);
-    constexpr int kWords = 2 * (int)sizeof(T);
-    if (kVec && e0 + 8 <= n) {
-        if constexpr (kWords == 2) {
-            __stcs(reinterpret_cast<uint2 *>(p + e0), make_uint2(r.w[0], r.w[1]));
-        } else {
+// x[j] <- the 32 bits that start `off` bytes after word j (off even, below 16)
+template <int kWords>
+__device__ __forceinline__ void move_down(unsigned (&x)[kWords + 4], unsigned off) {
+    if (off & 8u) {
 #pragma unroll
-            for (int i = 0; i < kWords / 4; ++i)
-                __stcs(reinterpret_cast<uint4 *>(p + e0) + i, make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]));
-        }
-        return;
+        for (int j = 0; j < kWords + 2; ++j) x[j] = x[j + 2];
     }
-    using U = typename std::conditional<sizeof(T) == 4, unsigned, typename std::conditional<sizeof(T) == 2, unsigned short, unsigned char>::type>::type;
-    constexpr int kPer = 4 / (int)sizeof(T);
+    if (off & 4u) {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i)
+        for (int j = 0; j < kWords + 1; ++j) x[j] = x[j + 1];
+    }
+    if (off & 2u) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const long long e = element_at<kVec>(e0, i * kPer + j);
-            if (e < n) __stcs(reinterpret_cast<U *>(p) + e, (U)(r.w[i] >> (8 * (int)sizeof(T) * j)));
+        for (int j = 0; j < kWords; ++j) x[j] = __byte_perm(x[j], x[j + 1], 0x5432);
+    }
+}
+
+// The pieces that cover a stretch of whole units end 16 bytes later if they are skewed: that last piece, in lane 0.
+template <typename T>
+__device__ __forceinline__ uint4 load_end(const void *base, long long end, int lane) {
+    const T *p = static_cast<const T *>(base);
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (lane == 0 && skew(p)) u = __ldcs(reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p + end) - skew(p)));
+    return u;
+}
+template <typename T>
+__device__ __forceinline__ uint4 first_piece(const Raw<T> &r) { return make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]); }
+// Moves a skewed unit's elements to their lanes; `next`: the 16 bytes that follow the unit's pieces (lane 0's counts).
+template <typename T>
+__device__ __forceinline__ void settle(const void *base, Raw<T> &r, uint4 next, int lane) {
+    constexpr int kWords = 2 * (int)sizeof(T);
+    if (skew(base)) {
+        unsigned x[kWords + 4];
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) x[i] = r.w[i];
+        x[kWords] = __shfl_sync(0xffffffffu, lane ? x[0] : next.x, lane + 1);
+        x[kWords + 1] = __shfl_sync(0xffffffffu, lane ? x[1] : next.y, lane + 1);
+        x[kWords + 2] = __shfl_sync(0xffffffffu, lane ? x[2] : next.z, lane + 1);
+        x[kWords + 3] = __shfl_sync(0xffffffffu, lane ? x[3] : next.w, lane + 1);
+        move_down<kWords>(x, skew(base));
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) r.w[i] = x[i];
+    }
+}
+
+template <typename T, int kAccess>
+__device__ __forceinline__ void store_raw(void *base, long long first, long long n, int lane, const Raw<T> &r) {
+    T *p = static_cast<T *>(base);
+    using U = typename Bits<T>::type;
+    constexpr int kWords = 2 * (int)sizeof(T), kPer = 4 / (int)sizeof(T), kShift = 8 * (int)sizeof(T);
+    if constexpr (kAccess == kAnyAlignment) {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const long long e = first + lane_element<kAccess>(lane, i * kPer + j);
+                if (e >= 0 && e < n) __stcs(reinterpret_cast<U *>(p) + e, (U)(r.w[i] >> (kShift * j)));
+            }
+    } else if constexpr (kWords == 2) {
+        __stcs(reinterpret_cast<uint2 *>(p + first + 8 * lane), make_uint2(r.w[0], r.w[1]));
+    } else {
+        const unsigned off = kAccess == kSkewed ? skew(p) : 0u;
+        uint4 *q = reinterpret_cast<uint4 *>(reinterpret_cast<char *>(p + first + 8 * lane) - off);
+        if (off == 0) {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) __stcs(q + i, make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]));
+        } else {
+            unsigned x[kWords + 4];                           // the lane before's last 16 bytes (lane 0: lane 31's), then this one's
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = __shfl_sync(0xffffffffu, r.w[kWords - 4 + j], lane + 31);
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) x[4 + j] = r.w[j];
+            move_down<kWords>(x, 16u - off);
+            if (lane) __stcs(q, make_uint4(x[0], x[1], x[2], x[3]));
+            if constexpr (kWords == 8) __stcs(q + 1, make_uint4(x[4], x[5], x[6], x[7]));
+            if (lane == 0) {                                  // first bytes: the unit's last piece; the others: its first
+                U *head = reinterpret_cast<U *>(q), *tail = reinterpret_cast<U *>(q + kStateBlock * sizeof(T) / 16);
+                const int split = (int)(off / sizeof(T));
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) (i * kPer + j < split ? tail : head)[i * kPer + j] = (U)(x[i] >> (kShift * j));
+            }
         }
+    }
 }
 
 __device__ __forceinline__ float2 pair_of(const Raw<float> &r, int i) { return make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1])); }
@@ -144,18 +229,27 @@ __device__ __forceinline__ unsigned e4m3_random_top(float y, float z, unsigned r
     const unsigned t = (__float_as_uint(z) << 4) + random_at_8;
     return y > 0.f ? max(t, 1u << 24) : t;
 }
+// Correctly rounded square roots of two numbers that are zero or at least 2^-100 (smaller ones: 1 ulp), without the
+// range branch of the library's: an approximate root s = v y, y ~ 1/sqrt(v), corrected by its exact residual,
+// s + (v - s s) y / 2 (Markstein, IBM J. Res. Dev. 34, 1990).  Infinity gives NaN.
+__device__ __forceinline__ float2 sqrt2(float2 v) {
+    float2 y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, 0x1p-126f)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, 0x1p-126f)));
+    const float2 s = mul2(v, y), half = mul2(y, both(0.5f));
+    const float2 rest = fma2(make_float2(-s.x, -s.y), s, v);
+    return fma2(rest, half, s);
+}
+__device__ __forceinline__ float reciprocal(float x) {                            // 1 ulp; infinity below 2^-126
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float max_abs(float a, float b) {                      // NaN if either is
     float d;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(fabsf(b)));
     return d;
 }
-// Scale of a block from its largest magnitude (fp32 bits order as magnitudes do; NaN is above infinity).
-__device__ __forceinline__ void block_scale(float top, float &scale, float &over) {
-    scale = __fmul_rn(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu)), 1.0f / 448.0f);
-    if (scale < 0x1p-126f) scale = 0.f;
-    over = scale == 0.f ? 0.f : __fdiv_rn(1.f, scale);
-}
-
 template <typename TP, typename TG>
 struct Unit8 {
     Raw<TP> p;
@@ -164,82 +258,105 @@ struct Unit8 {
     float ms, rs;
 };
 
-template <typename TP, typename TG, bool kVec>
-__device__ __forceinline__ void load_unit8(const TensorEntry &t, int blk, int lane, Unit8<TP, TG> &u) {
-    const long long e0 = (long long)blk * kStateBlock + (kVec ? lane * 8 : lane);
-    u.p = load_raw<TP, kVec>(t.param, e0, t.n);
-    u.g = load_raw<TG, kVec>(t.grad, e0, t.n);
-    u.m = load_raw<code8, kVec>(t.m, e0, t.n);
-    u.r = load_raw<code8, kVec>(t.v, e0, t.n);
-    u.ms = __ldcg(t.m_scale + blk);
-    u.rs = __ldcg(t.v_scale + blk);
-}
-
-template <typename TP, typename TG, bool kVec>
-__device__ __forceinline__ void step_unit8(const TensorEntry &t, int blk, int lane, Unit8<TP, TG> &u, const AdamArgs &a, float b1,
-                                           float gs, unsigned seed_term) {
-    const long long e0 = (long long)blk * kStateBlock + (kVec ? lane * 8 : lane);
-    float2 m[4], r[4];
-    float mtop = 0.f, rtop = 0.f;
+// kUnits consecutive units of one tensor, so that constants, addresses and the division behind a unit's two scales
+// are shared: lane i works out the i-th scale of the 2 kUnits.
+template <typename TP, typename TG, int kAccess, int kUnits>
+__device__ __forceinline__ void step_units8(const TensorEntry &t, int blk, int lane, const AdamArgs &a, float b1, float gs, unsigned seed_term) {
+    const long long first = (long long)blk * kStateBlock;
+    Unit8<TP, TG> us[kUnits];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 g = mul2(pair_of(u.g, i), both(gs));
-        const float2 old = mul2(e4m3_values(u.m, i), both(u.ms)), root = mul2(e4m3_values(u.r, i), both(u.rs));
-        const float2 m0 = mul2(old, both(b1)), m1 = mul2(g, both(a.one_minus_b1));
-        const float2 v0 = mul2(mul2(root, root), both(a.b2)), v1 = mul2(mul2(g, g), both(a.one_minus_b2));
-        m[i] = make_float2(__fadd_rn(m0.x, m1.x), __fadd_rn(m0.y, m1.y));
-        r[i] = make_float2(__fsqrt_rn(__fadd_rn(v0.x, v1.x)), __fsqrt_rn(__fadd_rn(v0.y, v1.y)));
-        mtop = max_abs(max_abs(mtop, m[i].x), m[i].y);
-        rtop = max_abs(max_abs(rtop, r[i].x), r[i].y);
-        // the update itself, in 2 ulp: it is small against the parameter that it is added to
-        const float2 den = fma2(r[i], both(a.inv_sqrt_bc2), both(a.eps));
-        const float2 step = make_float2(__fdividef(m[i].x, den.x), __fdividef(m[i].y, den.y));
-        set_pair(u.p, i, fma2(both(-a.step_size), step, mul2(pair_of(u.p, i), both(t.decay))));
+    for (int k = 0; k < kUnits; ++k) {
+        const long long e = first + k * kStateBlock;
+        us[k].p = load_raw<TP, kAccess>(t.param, e, t.n, lane);
+        us[k].g = load_raw<TG, kAccess>(t.grad, e, t.n, lane);
+        us[k].m = load_raw<code8, kAccess>(t.m, e, t.n, lane);
+        us[k].r = load_raw<code8, kAccess>(t.v, e, t.n, lane);
+        us[k].ms = __ldcg(t.m_scale + blk + k);
+        us[k].rs = __ldcg(t.v_scale + blk + k);
     }
-    store_raw<TP, kVec>(t.param, e0, t.n, u.p);
-    float msc, mover, rsc, rover;
-    block_scale(mtop, msc, mover);
-    block_scale(rtop, rsc, rover);
-    unsigned top[8];
+    uint4 pend, gend;
+    if constexpr (kAccess == kSkewed) {
+        pend = load_end<TP>(t.param, first + kUnits * kStateBlock, lane);
+        gend = load_end<TG>(t.grad, first + kUnits * kStateBlock, lane);
+    }
+    float2 m[kUnits][4], r[kUnits][4];
+    unsigned top_of = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned c = e4m3_nearest(mul2(m[i], both(mover)));
-        if (i & 1) u.m.w[i >> 1] |= c << 16;
-        else u.m.w[i >> 1] = c;
-        const float2 y = mul2(r[i], both(rover)), z = mul2(y, both(0x1p-120f));
-        if (kVec) {
-            const unsigned h = pair_hash(((unsigned)e0 >> 1) + i, seed_term);
-            top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h, 0, 0x4104));          // low half at bit 8
-            top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h, 0, 0x4324));      // high half at bit 8
-        } else {
-            const unsigned first = (unsigned)element_at<kVec>(e0, 2 * i);          // both of the lane's parity
-            const unsigned h0 = pair_hash(first >> 1, seed_term), h1 = pair_hash((first >> 1) + 16, seed_term);
-            const unsigned pick = (first & 1) ? 0x4324 : 0x4104;
-            top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h0, 0, pick));
-            top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h1, 0, pick));
+    for (int k = 0; k < kUnits; ++k) {
+        Unit8<TP, TG> &u = us[k];
+        if constexpr (kAccess == kSkewed) {
+            constexpr int kLast = kUnits - 1;
+            settle<TP>(t.param, u.p, k < kLast ? first_piece(us[k < kLast ? k + 1 : k].p) : pend, lane);
+            settle<TG>(t.grad, u.g, k < kLast ? first_piece(us[k < kLast ? k + 1 : k].g) : gend, lane);
         }
-    }
+        float mtop = 0.f, rtop = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        u.r.w[i] = __byte_perm(__byte_perm(top[4 * i], top[4 * i + 1], 0x0073), __byte_perm(top[4 * i + 2], top[4 * i + 3], 0x0073), 0x5410);
-    store_raw<code8, kVec>(t.m, e0, t.n, u.m);
-    store_raw<code8, kVec>(t.v, e0, t.n, u.r);
-    if (lane == 0) {
-        t.m_scale[blk] = msc;
-        t.v_scale[blk] = rsc;
+        for (int i = 0; i < 4; ++i) {
+            const float2 g = mul2(pair_of(u.g, i), both(gs));
+            const float2 old = mul2(e4m3_values(u.m, i), both(u.ms)), root = mul2(e4m3_values(u.r, i), both(u.rs));
+            const float2 m0 = mul2(old, both(b1)), m1 = mul2(g, both(a.one_minus_b1));
+            const float2 v0 = mul2(mul2(root, root), both(a.b2)), v1 = mul2(mul2(g, g), both(a.one_minus_b2));
+            m[k][i] = make_float2(__fadd_rn(m0.x, m1.x), __fadd_rn(m0.y, m1.y));
+            r[k][i] = sqrt2(make_float2(__fadd_rn(v0.x, v1.x), __fadd_rn(v0.y, v1.y)));
+            mtop = max_abs(max_abs(mtop, m[k][i].x), m[k][i].y);
+            rtop = max_abs(max_abs(rtop, r[k][i].x), r[k][i].y);
+            // the update itself, in 2 ulp: it is small against the parameter that it is added to
+            const float2 den = fma2(r[k][i], both(a.inv_sqrt_bc2), both(a.eps));
+            const float2 step = mul2(m[k][i], make_float2(reciprocal(den.x), reciprocal(den.y)));
+            set_pair(u.p, i, fma2(both(-a.step_size), step, mul2(pair_of(u.p, i), both(t.decay))));
+        }
+        store_raw<TP, kAccess>(t.param, first + k * kStateBlock, t.n, lane, u.p);
+        // largest magnitudes of the block (fp32 bits order as magnitudes do; NaN is above infinity)
+        const unsigned mt = __reduce_max_sync(0xffffffffu, __float_as_uint(mtop) & 0x7fffffffu), rt = __reduce_max_sync(0xffffffffu, __float_as_uint(rtop) & 0x7fffffffu);
+        if (lane == 2 * k) top_of = mt;
+        if (lane == 2 * k + 1) top_of = rt;
+    }
+    float scale = __fmul_rn(__uint_as_float(top_of), 1.0f / 448.0f);
+    if (scale < 0x1p-126f) scale = 0.f;
+    const float over = scale == 0.f ? 0.f : __fdiv_rn(1.f, scale);
+    if (lane < 2 * kUnits) ((lane & 1) ? t.v_scale : t.m_scale)[blk + (lane >> 1)] = scale;
+#pragma unroll
+    for (int k = 0; k < kUnits; ++k) {
+        Unit8<TP, TG> &u = us[k];
+        const long long e = first + k * kStateBlock;
+        const float mover = __shfl_sync(0xffffffffu, over, 2 * k), rover = __shfl_sync(0xffffffffu, over, 2 * k + 1);
+        unsigned top[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned c = e4m3_nearest(mul2(m[k][i], both(mover)));
+            if (i & 1) u.m.w[i >> 1] |= c << 16;
+            else u.m.w[i >> 1] = c;
+            const float2 y = mul2(r[k][i], both(rover)), z = mul2(y, both(0x1p-120f));
+            const unsigned pair = (unsigned)(e + lane_element<kAccess>(lane, 2 * i)) >> 1;
+            if (kAccess != kAnyAlignment) {
+                const unsigned h = pair_hash(pair, seed_term);
+                top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h, 0, 0x4104));          // low half at bit 8
+                top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h, 0, 0x4324));      // high half at bit 8
+            } else {                                                                        // 32 elements apart, both of the lane's parity
+                const unsigned h0 = pair_hash(pair, seed_term), h1 = pair_hash(pair + 16, seed_term), pick = (lane & 1) ? 0x4324 : 0x4104;
+                top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h0, 0, pick));
+                top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h1, 0, pick));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            u.r.w[i] = __byte_perm(__byte_perm(top[4 * i], top[4 * i + 1], 0x0073), __byte_perm(top[4 * i + 2], top[4 * i + 3], 0x0073), 0x5410);
+        store_raw<code8, kAccess>(t.m, e, t.n, lane, u.m);
+        store_raw<code8, kAccess>(t.v, e, t.n, lane, u.r);
     }
 }
 
 // ---------------------------------------------------------------- fp32 states
+// Units need not begin where the tensor does: with `lead` elements before its start they lie on 128-byte (else on
+// 16-byte) boundaries in all four arrays wherever the arrays' offsets allow it (tensors at the same places of packed rows).
 
-template <typename TP, typename TG, bool kVec>
-__device__ __forceinline__ void step_unit32(const TensorEntry &t, int blk, int lane, const AdamArgs &a, float gs) {
-    const long long e0 = (long long)blk * kStateBlock + (kVec ? lane * 8 : lane);
+template <typename TP, typename TG, int kAccess>
+__device__ __forceinline__ void step_unit32(const TensorEntry &t, long long first, int lane, const AdamArgs &a, float gs) {
     AdamArgs mine = a;
     mine.decay = t.decay;
-    Raw<TP> p = load_raw<TP, kVec>(t.param, e0, t.n);
-    const Raw<TG> g = load_raw<TG, kVec>(t.grad, e0, t.n);
-    Raw<float> m = load_raw<float, kVec>(t.m, e0, t.n), v = load_raw<float, kVec>(t.v, e0, t.n);
+    Raw<TP> p = load_raw<TP, kAccess>(t.param, first, t.n, lane);
+    Raw<TG> g = load_raw<TG, kAccess>(t.grad, first, t.n, lane);
+    Raw<float> m = load_raw<float, kAccess>(t.m, first, t.n, lane), v = load_raw<float, kAccess>(t.v, first, t.n, lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float2 pp = pair_of(p, i), mm = pair_of(m, i), vv = pair_of(v, i);
@@ -250,49 +367,60 @@ __device__ __forceinline__ void step_unit32(const TensorEntry &t, int blk, int l
         set_pair(m, i, mm);
         set_pair(v, i, vv);
     }
-    store_raw<TP, kVec>(t.param, e0, t.n, p);
-    store_raw<float, kVec>(t.m, e0, t.n, m);
-    store_raw<float, kVec>(t.v, e0, t.n, v);
+    store_raw<TP, kAccess>(t.param, first, t.n, lane, p);
+    store_raw<float, kAccess>(t.m, first, t.n, lane, m);
+    store_raw<float, kAccess>(t.v, first, t.n, lane, v);
 }
 
 // ---------------------------------------------------------------- the kernel
 
-template <int kBits>
-__device__ __forceinline__ bool takes_vectors(const TensorEntry &t) {
-    const uintptr_t wide = reinterpret_cast<uintptr_t>(t.param) | reinterpret_cast<uintptr_t>(t.grad);
-    const uintptr_t states = reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v);
-    return kBits == 32 ? ((wide | states) & 15u) == 0 : (wide & 15u) == 0 && (states & 7u) == 0;
-}
-
-template <typename TP, typename TG, int kBits, int kEntries>
-__global__ void __launch_bounds__(kTensorThreads, kBits == 8 ? 4 : 3)
-adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
-    const float gs = tab.grad_scale ? __ldg(tab.grad_scale) : 1.f;
-    if (!isfinite(gs)) return;                              // a step whose gradients overflowed is skipped whole
-    const int lane = threadIdx.x & 31;
-    const int stride = gridDim.x * kTensorWarps;
-    int u = blockIdx.x * kTensorWarps + (threadIdx.x >> 5);
-    if (u >= tab.units) return;
-    int k = 0, hi = tab.n;                                  // the last tensor with first_unit <= u
+// The last tensor whose first unit is not past u.
+template <int kEntries>
+__device__ __forceinline__ int find_tensor(const TensorTable<kEntries> &tab, int u) {
+    int k = 0, hi = tab.n;
     while (hi - k > 1) {
         const int mid = (k + hi) >> 1;
         if (tab.e[mid].first_unit <= u) k = mid; else hi = mid;
     }
-    for (; u < tab.units; u += stride) {
-        while (k + 1 < tab.n && tab.e[k + 1].first_unit <= u) ++k;
-        const TensorEntry &t = tab.e[k];
-        const int blk = u - t.first_unit;
-        if constexpr (kBits == 32) {
-            if (takes_vectors<kBits>(t)) step_unit32<TP, TG, true>(t, blk, lane, tab.args, gs);
-            else step_unit32<TP, TG, false>(t, blk, lane, tab.args, gs);
-        } else {
-            Unit8<TP, TG> x;
-            if (takes_vectors<kBits>(t)) {
-                load_unit8<TP, TG, true>(t, blk, lane, x);
-                step_unit8<TP, TG, true>(t, blk, lane, x, tab.args, tab.b1, gs, tab.seed_term);
+    return k;
+}
+
+template <typename TP, typename TG, int kBits, int kEntries>
+__global__ void __launch_bounds__(kTensorThreads, TensorShape<TP, TG, kBits>::kBlocks)
+adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
+    const float gs = tab.grad_scale ? __ldg(tab.grad_scale) : 1.f;
+    if (!isfinite(gs)) return;                              // a step whose gradients overflowed is skipped whole
+    const int lane = threadIdx.x & 31;
+    const int step = gridDim.x * kTensorWarps * tab.group;
+    int first = (blockIdx.x * kTensorWarps + (threadIdx.x >> 5)) * tab.group;
+    if (first >= tab.units) return;
+    int k = find_tensor(tab, first);
+    for (; first < tab.units; first += step) {
+        while (k + 1 < tab.n && tab.e[k + 1].first_unit <= first) ++k;
+        const TensorEntry *t = &tab.e[k];
+        int blk = first - t->first_unit;
+        if constexpr (kBits == 8) {
+            if (tab.group == kGroup && t->lead >= 0 && (long long)(blk + kGroup) * kStateBlock <= t->n) {
+                if (skew(t->param) | skew(t->grad)) step_units8<TP, TG, kSkewed, kGroup>(*t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+                else step_units8<TP, TG, kAligned, kGroup>(*t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+                continue;
+            }
+        }
+        int at = k;
+        const int last = min(first + tab.group, tab.units);
+        for (int u = first; u < last; ++u) {
+            while (at + 1 < tab.n && tab.e[at + 1].first_unit <= u) ++at;
+            t = &tab.e[at];
+            blk = u - t->first_unit;
+            if constexpr (kBits == 32) {
+                const long long e = (long long)blk * kStateBlock - max(t->lead, 0);
+                if (t->lead >= 0 && e >= 0 && e + kStateBlock <= t->n) step_unit32<TP, TG, kAligned>(*t, e, lane, tab.args, gs);
+                else step_unit32<TP, TG, kAnyAlignment>(*t, e, lane, tab.args, gs);
             } else {
-                load_unit8<TP, TG, false>(t, blk, lane, x);
-                step_unit8<TP, TG, false>(t, blk, lane, x, tab.args, tab.b1, gs, tab.seed_term);
+                if (t->lead >= 0 && (long long)(blk + 1) * kStateBlock <= t->n)
+                    step_units8<TP, TG, kSkewed, 1>(*t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+                else
+                    step_units8<TP, TG, kAnyAlignment, 1>(*t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
             }
         }
     }

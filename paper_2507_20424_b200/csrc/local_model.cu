@@ -175,14 +175,17 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
 // ---------------------------------------------------------------- AdamW over many tensors
 
 template <typename TP, typename TG, int kBits, int kEntries>
-int launch_tensors(const TensorTable<kEntries> &tab, int sms, cudaStream_t s) {
-    const int blocks = (tab.units + kTensorWarps - 1) / kTensorWarps, most = sms * (kBits == 8 ? 4 : 3);
-    const int grid = blocks < most ? blocks : most;
-    adamw_tensors_kernel<TP, TG, kBits, kEntries><<<grid, kTensorThreads, 0, s>>>(tab);
+int launch_tensors(TensorTable<kEntries> &tab, int sms, cudaStream_t s) {
+    constexpr int kBlocks = TensorShape<TP, TG, kBits>::kBlocks;
+    const long long most = (long long)sms * kBlocks;                 // blocks that are resident
+    // groups only while every warp still gets one
+    tab.group = kBits == 8 && tab.units >= most * kTensorWarps * kGroup ? kGroup : 1;
+    const long long warps = (tab.units + tab.group - 1) / tab.group, blocks = (warps + kTensorWarps - 1) / kTensorWarps;
+    adamw_tensors_kernel<TP, TG, kBits, kEntries><<<(unsigned)(blocks < most ? blocks : most), kTensorThreads, 0, s>>>(tab);
     return launched();
 }
 template <int kEntries>
-int launch_tensors_types(const TensorTable<kEntries> &tab, int tp, int tg, int bits, int sms, cudaStream_t s) {
+int launch_tensors_types(TensorTable<kEntries> &tab, int tp, int tg, int bits, int sms, cudaStream_t s) {
 #define DPPF_TENSORS(P, G) \
     return bits == 8 ? launch_tensors<P, G, 8, kEntries>(tab, sms, s) : launch_tensors<P, G, 32, kEntries>(tab, sms, s)
     if (tp == DPPF_FLOAT32 && tg == DPPF_FLOAT32) DPPF_TENSORS(float, float);
@@ -202,6 +205,20 @@ struct TensorScalars {
 
 int64_t units_of(int64_t n) { return (n + kStateBlock - 1) / kStateBlock; }
 
+// Elements (0 .. 63) by which units have to begin before the tensor so that they lie on 128-byte boundaries, or else
+// on 16-byte boundaries, in the parameter, the gradient and both fp32 moments; -1 if no number does.
+int common_lead(const dppf_tensor &t, int tp, int tg) {
+    const void *p[4] = {t.param, t.grad, t.exp_avg, t.exp_avg_sq};
+    const int type[4] = {tp, tg, DPPF_FLOAT32, DPPF_FLOAT32};
+    for (const size_t boundary : {(size_t)128, (size_t)16})
+        for (size_t lead = 0; lead < boundary / 2; ++lead) {
+            bool fits = true;
+            for (int i = 0; i < 4; ++i) fits = fits && (reinterpret_cast<uintptr_t>(p[i]) - lead * type_bytes(type[i])) % boundary == 0;
+            if (fits) return (int)lead;
+        }
+    return -1;
+}
+
 // Tensors [first, last) as one launch, or as many as the table and the unit count allow.
 template <int kEntries>
 int launch_table(const dppf_tensor *ts, int first, int last, const TensorScalars &p, int sms, cudaStream_t s) {
@@ -217,14 +234,17 @@ int launch_table(const dppf_tensor *ts, int first, int last, const TensorScalars
         for (; k < last && tab.n < kEntries; ++k) {
             const dppf_tensor &t = ts[k];
             if (t.numel == 0) continue;
-            if (units + units_of(t.numel) > INT_MAX / 2 && tab.n) break;
+            const int lead = p.bits == 8 ? (aligned_to(t.exp_avg, 8) && aligned_to(t.exp_avg_sq, 8) ? 0 : -1) : common_lead(t, p.tp, p.tg);
+            const int64_t more = units_of(t.numel + (lead > 0 ? lead : 0));
+            if (units + more > INT_MAX / 2 && tab.n) break;
             TensorEntry &e = tab.e[tab.n++];
             e.param = t.param; e.grad = t.grad; e.m = t.exp_avg; e.v = t.exp_avg_sq;
             e.m_scale = t.exp_avg_scale; e.v_scale = t.exp_avg_sq_scale;
             e.n = t.numel;
             e.decay = (float)(1.0 - (double)p.lr * (double)p.wd * (double)t.decay);
             e.first_unit = (int)units;
-            units += units_of(t.numel);
+            e.lead = lead;
+            units += more;
         }
         if (tab.n == 0) break;
         tab.units = (int)units;
