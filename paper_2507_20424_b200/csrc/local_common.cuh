@@ -79,8 +79,8 @@ __device__ __forceinline__ void store_vec(T *p, const float (&f)[N]) {
 }
 
 // ---------------------------------------------------------------- two fp32 operations in one instruction
-// Each result is rounded by itself.  There is no packed sum here: one that follows a packed product was
-// seen to come out as a fused multiply-add, in spite of .rn, so separately rounded sums are scalar.
+// Each result is rounded by itself.  A packed sum that follows a packed product was seen to come out as a fused
+// multiply-add, in spite of .rn: where the product has to be rounded first, the sum is written as two scalar ones.
 
 __device__ __forceinline__ unsigned long long pack2(float2 a) {
     unsigned long long r;
@@ -95,6 +95,11 @@ __device__ __forceinline__ float2 unpack2(unsigned long long a) {
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     unsigned long long r;
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)));
+    return unpack2(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)));
     return unpack2(r);
 }
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -117,6 +122,8 @@ __device__ __forceinline__ unsigned cluster_size() {
     return r;
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+// ... by a thread that has written nothing the others are to see: no fence
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // Shared-memory address of the same variable in another block of the cluster.
 __device__ __forceinline__ unsigned cluster_map(const void *p, unsigned rank) {

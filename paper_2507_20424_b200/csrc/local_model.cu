@@ -148,8 +148,8 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     if (!allow_smem(policy_kernel<T>, dev, ready, kPolicySliceMax)) return DPPF_ERR_CUDA;
     const int sms = multiprocessors(dev);
     if (sms < 0) return DPPF_ERR_CUDA;
-    // 16-byte vectors a row can span, whatever its alignment
-    const int vectors = (int)(((size_t)a.V * sizeof(T) + 15 + 15) / 16);
+    // 16-byte vectors that a row spans: one more if rows may start inside one
+    const int vectors = (int)(((size_t)a.V * sizeof(T) + 15) / 16) + (rows_on_16(a.logits, a.ld, sizeof(T) == 4 ? DPPF_FLOAT32 : DPPF_BFLOAT16) ? 0 : 1);
     int C = 1;
     auto slice_bytes = [&](int c) { return (vectors + c - 1) / c * 16; };
     while (C < kPolicyMaxCluster && slice_bytes(C) > kPolicySliceGood) C *= 2;
@@ -157,6 +157,8 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     while (C < kPolicyMaxCluster && (long long)a.T * C < 2LL * sms && slice_bytes(C) > 16 * 1024) C *= 2;
     if (slice_bytes(C) > kPolicySliceMax) return DPPF_ERR_INVALID_ARG;
     a.slice = (vectors + C - 1) / C;
+    // four chunks, in whole rounds of the block's threads
+    a.chunk = (a.slice + kPolicyChunks * kPolicyThreads - 1) / (kPolicyChunks * kPolicyThreads) * kPolicyThreads;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.T * (unsigned)C);
     cfg.blockDim = dim3(kPolicyThreads);

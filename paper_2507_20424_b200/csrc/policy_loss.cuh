@@ -18,7 +18,7 @@ namespace {
 // so that rows of the type's lowest value, and -inf entries, need no special case.
 
 constexpr int kPolicyThreads = 256;
-constexpr int kPolicyChunks = 8;
+constexpr int kPolicyChunks = 4;
 constexpr int kPolicyMaxCluster = 8;
 
 struct PolicyHeader {           // first bytes of the workspace; all zero before the first call
@@ -39,28 +39,32 @@ struct PolicyArgs {
     int T, V;
     int targets64;
     int slice;                  // 16-byte vectors of a row that each block of the cluster holds
+    int chunk;                  // ... and that a bulk copy brings
     int spin;
     float clip_lo, clip_hi, kl_coef, log2e_t, inv_t;
 };
 
-template <typename T> struct Vec16;      // the elements of a 16-byte vector
+template <typename T> struct Vec16;      // the elements of a 16-byte vector, in pairs
 template <> struct Vec16<float> {
     static constexpr int N = 4;
-    static __device__ __forceinline__ void get(uint4 u, float (&x)[4]) {
-        x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+    static __device__ __forceinline__ void get(uint4 u, float2 *x) {
+        x[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+        x[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
     }
-    static __device__ __forceinline__ uint4 put(const float (&x)[4]) {
-        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    static __device__ __forceinline__ uint4 put(const float2 *x) {
+        return make_uint4(__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[1].x), __float_as_uint(x[1].y));
     }
 };
 template <> struct Vec16<bf16> {
     static constexpr int N = 8;
-    static __device__ __forceinline__ void get(uint4 u, float (&x)[8]) {
-        x[0] = bf16_low(u.x); x[1] = bf16_high(u.x); x[2] = bf16_low(u.y); x[3] = bf16_high(u.y);
-        x[4] = bf16_low(u.z); x[5] = bf16_high(u.z); x[6] = bf16_low(u.w); x[7] = bf16_high(u.w);
+    static __device__ __forceinline__ void get(uint4 u, float2 *x) {
+        x[0] = make_float2(bf16_low(u.x), bf16_high(u.x));
+        x[1] = make_float2(bf16_low(u.y), bf16_high(u.y));
+        x[2] = make_float2(bf16_low(u.z), bf16_high(u.z));
+        x[3] = make_float2(bf16_low(u.w), bf16_high(u.w));
     }
-    static __device__ __forceinline__ uint4 put(const float (&x)[8]) {
-        return make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+    static __device__ __forceinline__ uint4 put(const float2 *x) {
+        return make_uint4(bf16_pair(x[0].x, x[0].y), bf16_pair(x[1].x, x[1].y), bf16_pair(x[2].x, x[2].y), bf16_pair(x[3].x, x[3].y));
     }
 };
 
@@ -70,6 +74,41 @@ __device__ __forceinline__ void merge(float &m, float &s, float m2, float s2, fl
     const float top = fmaxf(m, m2);
     s = s * exp2_fast((m - top) * k) + s2 * exp2_fast((m2 - top) * k);
     m = top;
+}
+
+// Running maximum m and sum s = sum 2^((x - m) k) of a thread, over G vectors at once.
+template <typename T, int G>
+__device__ __forceinline__ void take(const uint4 *v, float k, float &m, float &s) {
+    constexpr int kPairs = Vec16<T>::N / 2 * G;
+    float2 x[kPairs];
+#pragma unroll
+    for (int i = 0; i < G; ++i) Vec16<T>::get(v[i * kPolicyThreads], x + i * (Vec16<T>::N / 2));
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) top = fmaxf(fmaxf(top, x[i].x), x[i].y);
+    s *= exp2_fast((m - top) * k);
+    m = top;
+    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        const float2 t = mul2(add2(x[i], both(-top)), both(k));
+        sum = add2(sum, make_float2(exp2_fast(t.x), exp2_fast(t.y)));
+    }
+    s += sum.x + sum.y;
+}
+
+// Gradient of one vector, without the target's own term: -c exp(z - lse), cn = -c / s.
+template <typename T>
+__device__ __forceinline__ uint4 slope_vector(uint4 v, float k, float m, float cn) {
+    constexpr int kPairs = Vec16<T>::N / 2;
+    float2 x[kPairs];
+    Vec16<T>::get(v, x);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        const float2 t = mul2(add2(x[i], both(-m)), both(k));
+        x[i] = mul2(make_float2(exp2_fast(t.x), exp2_fast(t.y)), both(cn));
+    }
+    return Vec16<T>::put(x);
 }
 
 // Fixed-order sum of the rows' terms by the last block to finish.
@@ -98,7 +137,7 @@ __device__ __forceinline__ void policy_finish(const PolicyArgs &a, double *s_red
 
 template <typename T>
 __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs a) {
-    constexpr int N = Vec16<T>::N;
+    constexpr int N = Vec16<T>::N, kTake = 4;
     extern __shared__ __align__(128) uint4 s_row[];              // this block's slice, as aligned in the row
     __shared__ unsigned long long s_bar[kPolicyChunks];
     __shared__ float2 s_stats[kPolicyMaxCluster];                // one entry from each block of the cluster
@@ -116,24 +155,38 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
         for (int c = 0; c < kPolicyChunks; ++c) mbar_init(&s_bar[c], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_failed = 0;
+        s_last = 0;
     }
     const float w = __ldg(a.weight + row);
     const long long y = a.targets64 ? __ldg(static_cast<const long long *>(a.targets) + row)
                                     : (long long)__ldg(static_cast<const int *>(a.targets) + row);
     const bool live = w != 0.f && y >= 0 && y < a.V;
 
-    // Vectors of the row: 16-byte pieces of memory, the first and the last of which may reach over
-    // the row's ends (into the same 16 bytes as one of its elements; those values are not used).
+    // Vectors of the row: 16-byte pieces of memory, the first and the last of which may reach over the row's ends
+    // (into the same 16 bytes as one of its elements; those values are not used).  This block has vectors [v0, v0 + nv)
+    // of it, elements [e_first, e_last); of its vectors [lo, hi) lie wholly inside the row.
     const int before = (int)((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T));
     const int vectors = (before + a.V + N - 1) / N;
-    const int v0 = rank * a.slice, v1 = min(v0 + a.slice, vectors), nv = max(v1 - v0, 0);
-    const int e_first = max(v0 * N - before, 0), e_last = min(v1 * N - before, a.V);   // elements [e_first, e_last)
+    const int v0 = rank * a.slice, nv = max(min(a.slice, vectors - v0), 0);
+    const int e_first = max(v0 * N - before, 0), e_last = min((v0 + nv) * N - before, a.V);
+    const int lo = (rank == 0 && before) ? 1 : 0, hi = max(min(nv, (before + a.V) / N - v0), lo);
+    T *gv = g - before + (long long)v0 * N;                       // where this block's vectors go, if they are aligned there
     const bool same = a.grad && ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(x)) & 15u) == 0;
+    const T *sx = reinterpret_cast<const T *>(s_row) + before - v0 * N;   // element e of the row, for e in [e_first, e_last)
 
-    float term[3] = {0.f, 0.f, 0.f}, lp = 0.f;
+    auto count_row = [&](float lp, float loss, float kl, float part) {   // by one thread of the cluster
+        a.logp[row] = lp;
+        a.terms[row] = loss;
+        a.terms[(size_t)a.T + row] = kl;
+        a.terms[2 * (size_t)a.T + row] = part;
+        __threadfence();
+        s_last = atomicInc(&a.hdr->done, (unsigned)a.T - 1u) == (unsigned)a.T - 1u;
+        __threadfence();
+    };
+
     if (live) {
         __syncthreads();                                          // barriers initialised
-        const int per = (a.slice + kPolicyChunks - 1) / kPolicyChunks;
+        const int per = a.chunk;
         if (tid == 0) {
             const unsigned char *src = reinterpret_cast<const unsigned char *>(x - before) + (size_t)v0 * 16;
             for (int c = 0; c * per < nv; ++c) {
@@ -142,7 +195,7 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
                 bulk_load(s_row + c * per, src + (size_t)c * per * 16, bytes, &s_bar[c]);
             }
         }
-        if (C > 1) cluster_arrive();                              // this block's s_stats may be written
+        if (C > 1) cluster_arrive_relaxed();                      // this block's s_stats may be written
         const float xy = to_float(x[y]);                          // before any block writes (grad may be logits)
         const float old = __ldg(a.old_logp + row), A = __ldg(a.advantage + row);
         const float ref = a.ref_logp ? __ldg(a.ref_logp + row) : 0.f;
@@ -152,26 +205,18 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
         int bad = 0;
         for (int c = 0; c * per < nv; ++c) {
             if (!mbar_wait_bounded(&s_bar[c], 0, a.spin)) { bad = 1; break; }
-            const int stop = min(nv, (c + 1) * per);
-            for (int i = c * per + tid; i < stop; i += kPolicyThreads) {
-                float f[N];
-                Vec16<T>::get(s_row[i], f);
-                const int e = (v0 + i) * N - before;
-                if (e < 0 || e + N > a.V) {
-#pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        if (e + j < 0 || e + j >= a.V) f[j] = __int_as_float(0xff800000);
-                }
-                float top = m;
-#pragma unroll
-                for (int j = 0; j < N; ++j) top = fmaxf(top, f[j]);
-                s *= exp2_fast((m - top) * k);
-                m = top;
-#pragma unroll
-                for (int j = 0; j < N; ++j) s += exp2_fast((f[j] - m) * k);
-            }
+            const int stop = min(hi, (c + 1) * per);
+            int i = max(lo, c * per) + tid;
+            for (; i + (kTake - 1) * kPolicyThreads < stop; i += kTake * kPolicyThreads) take<T, kTake>(s_row + i, k, m, s);
+            for (; i < stop; i += kPolicyThreads) take<T, 1>(s_row + i, k, m, s);
         }
-        if (bad) {                                                // the row becomes NaN; seen by the last block
+        if (!bad) {                                               // the row's ends, element by element
+            const int head = min(lo * N + v0 * N - before, e_last), tail = max(hi * N + v0 * N - before, head);
+            int e = -1;
+            if (tid < head - e_first) e = e_first + tid;
+            else if (tid >= 32 && tid - 32 < e_last - tail) e = tail + tid - 32;
+            if (e >= 0) merge(m, s, to_float(sx[e]), 1.f, k);
+        } else {                                                  // the row becomes NaN; seen by the last block
             s = __int_as_float(0x7fc00000);
             s_failed = 1;
             atomicExch(&a.hdr->failed, 1);
@@ -183,17 +228,19 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
         if (lane == 0) s_warp[warp] = make_float2(m, s);
         __syncthreads();
         m = s_warp[0].x; s = s_warp[0].y;
+#pragma unroll
         for (int i = 1; i < kPolicyThreads / 32; ++i) merge(m, s, s_warp[i].x, s_warp[i].y, k);
         if (C > 1) {
             cluster_wait();                                       // the other blocks have started
             if (tid < C) cluster_store2(cluster_map(&s_stats[rank], tid), m, s);
-            cluster_arrive();
+            if (warp == 0) cluster_arrive();
+            else cluster_arrive_relaxed();
             cluster_wait();
             m = s_stats[0].x; s = s_stats[0].y;
             for (int i = 1; i < C; ++i) merge(m, s, s_stats[i].x, s_stats[i].y, k);
         }
 
-        lp = (xy - m) * a.inv_t - logf(s);
+        const float lp = (xy - m) * a.inv_t - logf(s);
         const float q = expf(lp - old);
         const bool clipped = (A > 0.f && q > a.clip_hi) || (A < 0.f && q < a.clip_lo);
         const float qc = fminf(fmaxf(q, a.clip_lo), a.clip_hi);
@@ -208,69 +255,48 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
             loss += a.kl_coef * kl;
             slope -= a.kl_coef * eg;
         }
-        term[0] = w * loss;
-        term[1] = w * kl;
-        term[2] = clipped ? w : 0.f;
+        // before the gradient's stores, which a fence would wait for
+        if (rank == 0 && tid == 0) count_row(lp, w * loss, w * kl, clipped ? w : 0.f);
 
         if (a.grad) {
             const float c = w * slope * a.inv_t, cn = -c / s;
-            const int yv = (int)((y + before) / N) - v0, yj = (int)((y + before) % N);   // the target's place in the slice
+            auto entry = [&](int e) {
+                const float f = exp2_fast((to_float(sx[e]) - m) * k) * cn;
+                g[e] = from_float<T>(e == y ? f + c : f);
+            };
             if (same) {
-                for (int i = tid; i < nv; i += kPolicyThreads) {
-                    float f[N];
-                    Vec16<T>::get(s_row[i], f);
-#pragma unroll
-                    for (int j = 0; j < N; ++j) f[j] = exp2_fast((f[j] - m) * k) * cn;
-                    if (i == yv) {
-#pragma unroll
-                        for (int j = 0; j < N; ++j)
-                            if (j == yj) f[j] += c;
-                    }
-                    const int e = (v0 + i) * N - before;
-                    if (e >= 0 && e + N <= a.V) {
-                        __stcs(reinterpret_cast<uint4 *>(g + e), Vec16<T>::put(f));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < N; ++j)
-                            if (e + j >= 0 && e + j < a.V) g[e + j] = from_float<T>(f[j]);
-                    }
-                }
+                uint4 *out = reinterpret_cast<uint4 *>(gv);
+#pragma unroll 4
+                for (int i = lo + tid; i < hi; i += kPolicyThreads) __stcs(out + i, slope_vector<T>(s_row[i], k, m, cn));
+                const int head = min(lo * N + v0 * N - before, e_last), tail = max(hi * N + v0 * N - before, head);
+                if (tid < head - e_first) entry(e_first + tid);
+                else if (tid >= 32 && tid - 32 < e_last - tail) entry(tail + tid - 32);
+                const int at = (int)y + before - v0 * N;          // the target's place in the slice: written over by the
+                if (at >= lo * N && at < hi * N && (at / N - lo) % kPolicyThreads == tid) entry((int)y);   // thread that wrote its vector
             } else {
-                const T *sx = reinterpret_cast<const T *>(s_row) + before - v0 * N;
-                for (int e = e_first + tid; e < e_last; e += kPolicyThreads) {
-                    float f = exp2_fast((to_float(sx[e]) - m) * k) * cn;
-                    if (e == y) f += c;
-                    g[e] = from_float<T>(f);
-                }
+                for (int e = e_first + tid; e < e_last; e += kPolicyThreads) entry(e);
             }
         }
         if (s_failed && tid == 0)                                 // copies still under way land before the block leaves
             for (int c = 0; c * per < nv; ++c) mbar_wait_bounded(&s_bar[c], 0, kSpinLimit);
-    } else if (a.grad) {
-        if (same) {
-            for (int i = tid; i < nv; i += kPolicyThreads) {
-                const int e = (v0 + i) * N - before;
-                if (e >= 0 && e + N <= a.V) {
-                    __stcs(reinterpret_cast<uint4 *>(g + e), make_uint4(0, 0, 0, 0));
-                } else {
-                    for (int j = 0; j < N; ++j)
-                        if (e + j >= 0 && e + j < a.V) g[e + j] = from_float<T>(0.f);
-                }
+    } else {
+        __syncthreads();                                          // s_last is initialised
+        if (rank == 0 && tid == 0) count_row(0.f, 0.f, 0.f, 0.f);
+        if (a.grad) {
+            const T zero = from_float<T>(0.f);
+            if (same) {
+                uint4 *out = reinterpret_cast<uint4 *>(gv);
+                for (int i = lo + tid; i < hi; i += kPolicyThreads) __stcs(out + i, make_uint4(0, 0, 0, 0));
+                const int head = min(lo * N + v0 * N - before, e_last), tail = max(hi * N + v0 * N - before, head);
+                if (tid < head - e_first) g[e_first + tid] = zero;
+                else if (tid >= 32 && tid - 32 < e_last - tail) g[tail + tid - 32] = zero;
+            } else {
+                for (int e = e_first + tid; e < e_last; e += kPolicyThreads) g[e] = zero;
             }
-        } else {
-            for (int e = e_first + tid; e < e_last; e += kPolicyThreads) g[e] = from_float<T>(0.f);
         }
     }
 
     if (rank != 0) return;
-    __syncthreads();
-    if (tid == 0) {
-        a.logp[row] = lp;
-        for (int i = 0; i < 3; ++i) a.terms[(size_t)i * a.T + row] = term[i];
-        __threadfence();
-        s_last = atomicInc(&a.hdr->done, (unsigned)a.T - 1u) == (unsigned)a.T - 1u;
-        __threadfence();
-    }
     __syncthreads();
     if (s_last) policy_finish(a, s_red);
 }
