@@ -24,287 +24,594 @@ __device__ __forceinline__ long long read_id(const void *ids, int ids64, long lo
 }
 
 constexpr int kLookupThreads = 256;
+constexpr int kLookupAhead = 4;      // rows' pieces that a thread has under way
 
-// A block takes rows_per_block rows; its threads walk the groups of those rows in memory order.
-// N = 8 needs rows of both tensors that start on 16-byte boundaries and H % 8 == 0, N = 1 takes anything.
+// A block takes rows_per_block rows; its threads walk the groups of those rows in memory order, kLookupAhead at a time.
+// N = 8 needs rows of both tensors that start on 16-byte boundaries and H % 8 == 0, N = 2 rows on boundaries of two
+// elements and an even H, N = 1 takes anything.
 template <typename TW, typename TO, int N>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs a) {
     const long long t0 = (long long)blockIdx.x * a.rows_per_block;
     const unsigned rows = (unsigned)min((long long)a.rows_per_block, a.T - t0);
     const unsigned total = rows * (unsigned)a.groups;
-    for (unsigned i = threadIdx.x; i < total; i += kLookupThreads) {
-        const unsigned r = i / (unsigned)a.groups, j = (i - r * (unsigned)a.groups) * N;
-        const long long t = t0 + r, id = read_id(a.ids, a.ids64, t);
-        float f[N];
-        if (id >= 0 && id < a.V) {
-            load_vec<TW, N>(static_cast<const TW *>(a.table) + id * a.ld_table + j, f);
+    for (unsigned i0 = threadIdx.x; i0 < total; i0 += kLookupThreads * kLookupAhead) {
+        long long id[kLookupAhead];
+        unsigned r[kLookupAhead], j[kLookupAhead];
+        float f[kLookupAhead][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) f[k] *= a.scale;
-        } else {
+        for (int u = 0; u < kLookupAhead; ++u) {
+            const unsigned i = i0 + u * kLookupThreads;
+            r[u] = i / (unsigned)a.groups;
+            j[u] = (i - r[u] * (unsigned)a.groups) * N;
+            id[u] = i < total ? read_id(a.ids, a.ids64, t0 + r[u]) : -1;
+        }
 #pragma unroll
-            for (int k = 0; k < N; ++k) f[k] = 0.f;
-        }
-        store_vec<TO, N>(static_cast<TO *>(a.out) + t * a.ld_out + j, f);
-    }
-}
-
-// ---------------------------------------------------------------- gradient: order of the tokens
-// dtable[v] = scale * sum over t with id_t = v of dout[t].  The tokens are sorted by id, stably, so
-// that equal ids stand together and each sum runs in token order: the result is the same from run to
-// run, with no atomics on floating numbers.
-//
-// Sort: least significant digit first, digits of up to 9 bits, by ONE cluster of up to 8 blocks
-// (two passes for any vocabulary up to 262,143).  Every warp owns a stretch of the input; it counts
-// its digits in a histogram of its own in shared memory, a prefix sum over (digit, block, warp) turns
-// the counts into first places, and the warp walks its stretch again and places each element:
-// rank within 32 elements by match, then the warp's running place.  Ids outside [0, V) get the key V
-// and end up last.  The other blocks of the launch write the zeros of a gradient that is written whole.
-
-constexpr int kSortThreads = 1024;
-constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kDigitBits = 9;
-constexpr int kBins = 1 << kDigitBits;
-constexpr int kSortMaxCluster = 8;
-
-struct SortArgs {
-    const void *ids;
-    int ids64;
-    long long V;
-    unsigned T;
-    unsigned *key[2], *pos[2];   // workspace: two buffers; the result is in buffer passes & 1
-    int passes, bits;            // digits and their width
-    // zero fill (rows of dtable), none if zero == null
-    void *zero;
-    long long zero_ld;           // bytes
-    long long zero_width;        // bytes of a row
-    int zero_vec;                // rows start on 16-byte boundaries and are a multiple of 16 bytes wide
-};
-
-__device__ __forceinline__ void fill_zero(const SortArgs &a, long long block, long long blocks) {
-    unsigned char *base = static_cast<unsigned char *>(a.zero);
-    if (a.zero_vec) {
-        const long long w = a.zero_width / 16;
-        if (a.zero_ld == a.zero_width) {                                     // one stretch
-            for (long long i = block * kSortThreads + threadIdx.x; i < w * a.V; i += blocks * kSortThreads)
-                __stcs(reinterpret_cast<uint4 *>(base) + i, make_uint4(0, 0, 0, 0));
-        } else {
-            for (long long v = block; v < a.V; v += blocks)
-                for (long long i = threadIdx.x; i < w; i += kSortThreads)
-                    __stcs(reinterpret_cast<uint4 *>(base + v * a.zero_ld) + i, make_uint4(0, 0, 0, 0));
-        }
-    } else {                                                                  // 2 bytes divide every element type
-        const long long w = a.zero_width / 2;
-        for (long long v = block; v < a.V; v += blocks)
-            for (long long i = threadIdx.x; i < w; i += kSortThreads)
-                reinterpret_cast<unsigned short *>(base + v * a.zero_ld)[i] = 0;
-    }
-}
-
-__device__ __forceinline__ unsigned sort_key(const SortArgs &a, int pass, unsigned i) {
-    if (pass > 0) return __ldcg(a.key[pass & 1] + i);
-    const long long id = read_id(a.ids, a.ids64, i);
-    return (unsigned)((id < 0 || id >= a.V) ? a.V : id);
-}
-
-__global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(const SortArgs a) {
-    extern __shared__ unsigned s_hist[];                      // [kSortWarps][bins]
-    __shared__ unsigned s_total[kBins], s_scan[kSortWarps];
-    const int C = (int)cluster_size(), rank = (int)cluster_rank();
-    if ((int)blockIdx.x >= C) {
-        fill_zero(a, (long long)blockIdx.x - C, (long long)gridDim.x - C);
-        return;
-    }
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int bins = 1 << a.bits;
-    const unsigned mask = (unsigned)bins - 1u;
-    const unsigned warps = (unsigned)C * kSortWarps;
-    const unsigned stretch = ((a.T + warps - 1) / warps + 31u) & ~31u;
-    const unsigned long long from = (unsigned long long)(rank * kSortWarps + warp) * stretch;
-    const unsigned i0 = (unsigned)min(from, (unsigned long long)a.T);
-    const unsigned i1 = (unsigned)min(from + stretch, (unsigned long long)a.T);
-    unsigned *hist = s_hist + warp * bins;
-
-    for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = pass * a.bits;
-        for (int b = lane; b < bins; b += 32) hist[b] = 0;
-        __syncwarp();
-#pragma unroll 4
-        for (unsigned i = i0 + lane; i < i1; i += 32) atomicAdd(&hist[(sort_key(a, pass, i) >> shift) & mask], 1u);
-        __syncthreads();
-        unsigned run = 0;                                     // elements of this block with digit tid
-        if (tid < bins) {
-            for (int w = 0; w < kSortWarps; ++w) {
-                const unsigned c = s_hist[w * bins + tid];
-                s_hist[w * bins + tid] = run;
-                run += c;
-            }
-            s_total[tid] = run;
-        }
-        if (C > 1) { cluster_arrive(); cluster_wait(); }
-        unsigned all = run, lower = 0;                        // ... of the cluster; of the blocks before this one
-        if (C > 1 && tid < bins) {
-            all = 0;
-            for (int r = 0; r < C; ++r) {
-                const unsigned c = cluster_load(cluster_map(&s_total[tid], r));
-                if (r < rank) lower += c;
-                all += c;
-            }
-        }
-        unsigned incl = all;                                  // prefix sum over the digits
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned n = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += n;
-        }
-        if (lane == 31) s_scan[warp] = incl;
-        __syncthreads();
-        if (tid < bins) {
-            unsigned first = incl - all + lower;
-            for (int w = 0; w < warp; ++w) first += s_scan[w];
-            for (int w = 0; w < kSortWarps; ++w) s_hist[w * bins + tid] += first;
-        }
-        __syncthreads();
-        unsigned *key_out = a.key[(pass + 1) & 1], *pos_out = a.pos[(pass + 1) & 1];
-        for (unsigned i = i0; i < i1; i += 32) {
-            const bool in = i + lane < i1;
-            const unsigned key = in ? sort_key(a, pass, i + lane) : 0u;
-            const unsigned pos = !in ? 0u : pass > 0 ? __ldcg(a.pos[pass & 1] + i + lane) : i + lane;
-            const unsigned digit = in ? (key >> shift) & mask : 0xffffffffu;
-            const unsigned peers = __match_any_sync(0xffffffffu, digit);
-            unsigned place = 0;
-            if (in) place = hist[digit] + __popc(peers & ((1u << lane) - 1u));
-            __syncwarp();
-            if (in && lane == 31 - __clz(peers)) hist[digit] = place + 1;
-            __syncwarp();
-            if (in) {
-                __stcg(key_out + place, key);
-                __stcg(pos_out + place, pos);
-            }
-        }
-        __threadfence();                                      // the next pass reads what other blocks wrote
-        if (C > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
-    }
-}
-
-// ---------------------------------------------------------------- gradient: sums over equal ids
-// The sorted tokens are cut into tiles of `tile` places.  A thread owns N columns of one tile and
-// walks its places, with the rows' loads ahead of the sums.  An id whose tokens all lie in the tile
-// is written at once; the part of one that reaches over a tile's end goes to the workspace (at most
-// two a tile: the first id's and the last id's), and a second launch adds such parts in tile order.
-
-constexpr int kReduceThreads = 256;
-
-struct ReduceArgs {
-    const unsigned *key, *pos;
-    const void *dout;
-    void *dtable;
-    float *part;                 // [tiles][2][H]: 0 an id that came in from the tile before, 1 one that starts here and goes on
-    long long ld_dout, ld_dtable;
-    unsigned T, V;
-    int H, groups, tile, tiles;
-    int row_threads;             // threads side by side on one tile's columns (power of two)
-    int add;
-    float scale;
-};
-
-template <typename TW, int N>
-__device__ __forceinline__ void write_row(const ReduceArgs &a, unsigned v, int j, float (&acc)[N]) {
-    TW *p = static_cast<TW *>(a.dtable) + (long long)v * a.ld_dtable + j;
-    if (a.add) {
-        float f[N];
-        load_vec<TW, N>(p, f);
-#pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] = fmaf(acc[k], a.scale, f[k]);
-    } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] *= a.scale;
-    }
-    store_vec<TW, N>(p, acc);
-}
-
-template <typename TG, typename TW, int N>
-__global__ void __launch_bounds__(kReduceThreads) embedding_reduce_kernel(const ReduceArgs a) {
-    constexpr int kAhead = 8;
-    const int sub = threadIdx.x / a.row_threads, col = threadIdx.x - sub * a.row_threads;
-    const int tile = blockIdx.x * (kReduceThreads / a.row_threads) + sub;
-    const int grp = blockIdx.y * a.row_threads + col;
-    if (tile >= a.tiles || grp >= a.groups) return;
-    const int j = grp * N;
-    const unsigned i0 = (unsigned)tile * a.tile, i1 = min(i0 + a.tile, a.T);
-    const unsigned none = 0xffffffffu;
-    const unsigned before = i0 ? __ldg(a.key + i0 - 1) : none;
-    const unsigned after = i1 < a.T ? __ldg(a.key + i1) : none;
-    unsigned cur = __ldg(a.key + i0);
-    bool open = cur == before;                               // the current id came in from the tile before
-    float acc[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) acc[k] = 0.f;
-    auto flush = [&](bool goes_on) {
-        if (cur >= a.V) return;
-        if (open || goes_on)
-            store_vec<float, N>(a.part + ((size_t)tile * 2 + (open ? 0 : 1)) * a.H + j, acc);
-        else
-            write_row<TW, N>(a, cur, j, acc);
-    };
-    for (unsigned i = i0; i < i1; i += kAhead) {
-        unsigned key[kAhead];
-        float f[kAhead][N];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            key[u] = i + u < i1 ? __ldg(a.key + i + u) : none;
-            if (key[u] < a.V) {
-                const unsigned t = __ldg(a.pos + i + u);
-                load_vec<TG, N>(static_cast<const TG *>(a.dout) + (long long)t * a.ld_dout + j, f[u]);
+        for (int u = 0; u < kLookupAhead; ++u) {
+            if (id[u] >= 0 && id[u] < a.V) {
+                load_vec<TW, N, false>(static_cast<const TW *>(a.table) + id[u] * a.ld_table + j[u], f[u]);
             } else {
 #pragma unroll
                 for (int k = 0; k < N; ++k) f[u][k] = 0.f;
             }
         }
 #pragma unroll
+        for (int u = 0; u < kLookupAhead; ++u) {
+            if (i0 + u * kLookupThreads >= total) break;
+            if (id[u] >= 0 && id[u] < a.V) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) f[u][k] *= a.scale;
+            }
+            store_vec<TO, N>(static_cast<TO *>(a.out) + (t0 + r[u]) * a.ld_out + j[u], f[u]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- gradient
+// dtable[v] = scale * sum over t with id_t = v of dout[t].  The tokens are sorted by id, stably, so that equal ids stand
+// together and each sum runs in token order: the result is the same from run to run, and no order of atomics matters.
+// The launches (count, place per digit, sums and zeros, joins) are each set up while the one before ends; up to
+// kFewTokens tokens take a single launch that sorts in every block.
+
+struct GradArgs {
+    const void *ids;
+    int ids64;
+    unsigned T, V;
+    const void *dout;
+    void *dtable;
+    long long ld_dout, ld_dtable;   // elements
+    int H, add;
+    float scale;
+    // sorted tokens (workspace); the sort's result is in buffer passes & 1
+    unsigned *key0, *pos0, *key1, *pos1;
+    unsigned *hist;              // [3][kSortBlocks][kBins]: a digit's counts, the next one's, the one's after that, in turn
+    int passes, bits;            // digits and their width
+    int sort_blocks;
+    unsigned chunk;              // tokens of a block of the sort, a multiple of kSortThreads
+    int zero_vec;                // rows of dtable start on 16-byte boundaries and are a multiple of 16 bytes wide
+    // rows of a gradient that is written whole: the last early_rows are zeroed by spare blocks of the sort's launches,
+    // the late_rows before them (where their ids do not occur) beside the joins, the others beside the sums
+    unsigned early_rows, late_rows;
+    int zero_blocks, late_blocks;   // blocks that write zeros, beside the sums and beside the joins
+    int zero_rows;               // rows that each of them looks after at a time
+    // sums
+    float *part;                 // [tiles][2][H]: 0 an id that came in from the tile before, 1 one that starts here and goes on
+    int groups, tile, tiles;
+    int row_threads;             // threads side by side on one tile's columns
+    int tile_blocks;             // blocks side by side over the tiles
+};
+
+// The dependent launch may be scheduled from here on; it waits for this one's end before it reads.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+__device__ __forceinline__ unsigned token_key(const GradArgs &a, unsigned i) {
+    const long long id = read_id(a.ids, a.ids64, i);
+    return (id < 0 || id >= (long long)a.V) ? a.V : (unsigned)id;
+}
+
+// Zeros to row v, by `threads` threads of which this is `rank`.
+template <typename TW>
+__device__ __forceinline__ void zero_row(const GradArgs &a, long long v, int rank, int threads) {
+    TW *p = static_cast<TW *>(a.dtable) + v * a.ld_dtable;
+    if (a.zero_vec) {
+        const int w = a.H * (int)sizeof(TW) / 16;
+        for (int i = rank; i < w; i += threads) __stcs(reinterpret_cast<uint4 *>(p) + i, make_uint4(0, 0, 0, 0));
+    } else {
+        for (int i = rank; i < a.H; i += threads) p[i] = from_float<TW>(0.f);
+    }
+}
+
+// ---------------------------------------------------------------- gradient: order of the tokens
+// Least significant digit first, digits of up to 9 bits (two for any vocabulary up to 262,143).  A block owns a chunk of the
+// sequence and a warp a stretch of the chunk.  The first launch counts each chunk's digits.  A launch per
+// digit then places: a block reads all chunks' counts, so that it knows where each of its digits begins, counts per
+// warp in shared memory, and its warps walk their stretches: rank within 32 elements by match, then the warp's running
+// place.  As an element is placed, its next digit is counted for the chunk that it moves to (whole
+// numbers: any order).  Ids outside [0, V) get the key V and end up last.
+
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kDigitBits = 9;
+constexpr int kBins = 1 << kDigitBits;
+constexpr int kSortBlocks = 128;     // at most
+constexpr int kSortHold = 4;         // elements a lane keeps in registers between counting and placing
+constexpr int kCountGroups = kSortThreads / (kBins / 4);
+constexpr size_t kPlaceSmem = (size_t)(kSortWarps + 2 * kCountGroups) * kBins * sizeof(unsigned);
+
+__device__ __forceinline__ unsigned *counts_of(const GradArgs &a, int pass) { return a.hist + (size_t)(pass % 3) * kSortBlocks * kBins; }
+
+__global__ void __launch_bounds__(kSortThreads) embedding_count_kernel(const GradArgs a) {
+    __shared__ unsigned s_count[kBins];
+    let_next_start();
+    const unsigned mask = (1u << a.bits) - 1u;
+    for (int b = threadIdx.x; b < kBins; b += kSortThreads) s_count[b] = 0;
+    __syncthreads();
+    const unsigned long long end = min((unsigned long long)(blockIdx.x + 1) * a.chunk, (unsigned long long)a.T);
+    for (unsigned long long i = (unsigned long long)blockIdx.x * a.chunk + threadIdx.x; i < end; i += kSortThreads)
+        atomicAdd(&s_count[token_key(a, (unsigned)i) & mask], 1u);
+    __syncthreads();
+    for (int b = threadIdx.x; b < kBins; b += kSortThreads) {
+        counts_of(a, 0)[(size_t)blockIdx.x * kBins + b] = s_count[b];
+        counts_of(a, 1)[(size_t)blockIdx.x * kBins + b] = 0;
+    }
+}
+
+template <typename TW>
+__global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const GradArgs a, int pass) {
+    extern __shared__ unsigned s_hist[];                      // [kSortWarps][kBins], then [kCountGroups][kBins] twice
+    __shared__ unsigned s_scan[kSortWarps];
+    unsigned *s_all = s_hist + kSortWarps * kBins, *s_lower = s_all + kCountGroups * kBins;
+    let_next_start();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if ((int)blockIdx.x >= a.sort_blocks) {                   // nothing else in this sequence of launches touches the table yet
+        const long long from = (long long)a.V - a.early_rows + (long long)a.early_rows * pass / a.passes, to = (long long)a.V - a.early_rows + (long long)a.early_rows * (pass + 1) / a.passes;
+        for (long long v = from + (long long)(blockIdx.x - a.sort_blocks) * kSortWarps + warp; v < to; v += (long long)(gridDim.x - a.sort_blocks) * kSortWarps)
+            zero_row<TW>(a, v, lane, 32);
+        return;
+    }
+    unsigned *hist = s_hist + warp * kBins;
+    for (int b = lane; b < kBins; b += 32) hist[b] = 0;
+    wait_for_previous();
+
+    const int shift = pass * a.bits;
+    const unsigned mask = (1u << a.bits) - 1u;
+    const bool more = pass + 1 < a.passes;
+    const unsigned *key_in = (pass & 1) ? a.key1 : a.key0, *pos_in = (pass & 1) ? a.pos1 : a.pos0;
+    unsigned *key_out = (pass & 1) ? a.key0 : a.key1, *pos_out = (pass & 1) ? a.pos0 : a.pos1;
+    const unsigned *counts = counts_of(a, pass);
+    unsigned *next_counts = counts_of(a, pass + 1);
+    if (more && tid < kBins) counts_of(a, pass + 2)[(size_t)blockIdx.x * kBins + tid] = 0;
+    const unsigned stretch = a.chunk / kSortWarps;            // a multiple of 32
+    const unsigned long long from = (unsigned long long)blockIdx.x * a.chunk + (unsigned long long)warp * stretch;
+    const unsigned i0 = (unsigned)min(from, (unsigned long long)a.T), i1 = (unsigned)min(from + stretch, (unsigned long long)a.T);
+    auto key_at = [&](unsigned i) { return pass == 0 ? token_key(a, i) : __ldcg(key_in + i); };
+    auto pos_at = [&](unsigned i) { return pass == 0 ? i : __ldcg(pos_in + i); };
+
+    unsigned key[kSortHold], pos[kSortHold];                  // of the first elements of the stretch
+#pragma unroll
+    for (int u = 0; u < kSortHold; ++u) {
+        const unsigned i = i0 + u * 32 + lane;
+        if (i < i1) { key[u] = key_at(i); pos[u] = pos_at(i); }
+    }
+    {                                                         // four digits a thread, the chunks in kCountGroups turns
+        const int q = tid % (kBins / 4), turn = tid / (kBins / 4);
+        uint4 all = make_uint4(0, 0, 0, 0), lower = all;
+#pragma unroll 8
+        for (int c = turn; c < a.sort_blocks; c += kCountGroups) {
+            const uint4 n = __ldcg(reinterpret_cast<const uint4 *>(counts + (size_t)c * kBins) + q);
+            all.x += n.x; all.y += n.y; all.z += n.z; all.w += n.w;
+            if (c < (int)blockIdx.x) { lower.x += n.x; lower.y += n.y; lower.z += n.z; lower.w += n.w; }
+        }
+        reinterpret_cast<uint4 *>(s_all + turn * kBins)[q] = all;
+        reinterpret_cast<uint4 *>(s_lower + turn * kBins)[q] = lower;
+    }
+#pragma unroll
+    for (int u = 0; u < kSortHold; ++u)
+        if (i0 + u * 32 + lane < i1) atomicAdd(&hist[(key[u] >> shift) & mask], 1u);
+    for (unsigned i = i0 + 32 * kSortHold + lane; i < i1; i += 32) atomicAdd(&hist[(key_at(i) >> shift) & mask], 1u);
+    __syncthreads();
+    unsigned all = 0, first = 0;                              // elements of digit tid; where this block's begin
+    if (tid < kBins) {
+#pragma unroll
+        for (int g = 0; g < kCountGroups; ++g) { all += s_all[g * kBins + tid]; first += s_lower[g * kBins + tid]; }
+    }
+    unsigned incl = all;                                      // prefix sum over the digits
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned n = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += n;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    __syncthreads();
+    if (tid < kBins) {
+        first += incl - all;
+        for (int w = 0; w < warp; ++w) first += s_scan[w];
+        unsigned count[kSortWarps];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) count[w] = s_hist[w * kBins + tid];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) {
+            s_hist[w * kBins + tid] = first;
+            first += count[w];
+        }
+    }
+    __syncthreads();
+    auto place = [&](bool in, unsigned k, unsigned p) {
+        const unsigned digit = in ? (k >> shift) & mask : 0xffffffffu;
+        const unsigned peers = __match_any_sync(0xffffffffu, digit);
+        unsigned at = 0;
+        if (in) at = hist[digit] + __popc(peers & ((1u << lane) - 1u));
+        __syncwarp();
+        if (in && lane == 31 - __clz(peers)) hist[digit] = at + 1;
+        __syncwarp();
+        if (in) {
+            __stcg(key_out + at, k);
+            __stcg(pos_out + at, p);
+            if (more) atomicAdd(next_counts + (size_t)(at / a.chunk) * kBins + ((k >> (shift + a.bits)) & mask), 1u);
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < kSortHold; ++u)
+        if (i0 + u * 32 < i1) place(i0 + u * 32 + lane < i1, key[u], pos[u]);
+    for (unsigned i = i0 + 32 * kSortHold; i < i1; i += 32) {
+        const bool in = i + lane < i1;
+        place(in, in ? key_at(i + lane) : 0u, in ? pos_at(i + lane) : 0u);
+    }
+}
+
+// ---------------------------------------------------------------- gradient: sums over equal ids
+// The sorted tokens are cut into tiles of `tile` places.  A thread owns N columns of one tile and walks its
+// places, kAhead rows under way.  An id that starts in a tile and ends in it or in the next is added up and
+// written by the thread of the tile where it starts (the next tile passes over it).  Of a longer one every tile leaves
+// its part in the workspace, and the last launch adds the parts in tile order.
+
+constexpr int kReduceThreads = 256;
+constexpr int kMaxTile = 32;
+constexpr int kMinRowThreads = 8;
+
+// N elements as they are stored
+template <typename T, int N> struct Stored { unsigned w[N * sizeof(T) >= 4 ? N * sizeof(T) / 4 : 1]; };
+template <typename T, int N>
+__device__ __forceinline__ Stored<T, N> load_stored(const T *p) {
+    Stored<T, N> r;
+    if constexpr (N == 1 && sizeof(T) == 2) {
+        r.w[0] = __ldcs(reinterpret_cast<const unsigned short *>(p));
+    } else {
+        constexpr int kWords = N * (int)sizeof(T) / 4, kPer = kWords < 4 ? kWords : 4;
+        using W = typename Words<kPer>::type;
+#pragma unroll
+        for (int i = 0; i < kWords / kPer; ++i) {
+            const W w = __ldcs(reinterpret_cast<const W *>(p) + i);
+            memcpy(&r.w[i * kPer], &w, sizeof(W));
+        }
+    }
+    return r;
+}
+template <int N> __device__ __forceinline__ float element_of(const Stored<float, N> &r, int k) { return __uint_as_float(r.w[k]); }
+template <int N> __device__ __forceinline__ float element_of(const Stored<bf16, N> &r, int k) { return (k & 1) ? bf16_high(r.w[k / 2]) : bf16_low(r.w[k / 2]); }
+
+// dtable[v] = scale * acc, or += that.  Every element has one writer in a launch, so adding to fp32 in memory (one
+// rounding, nothing waits for the old value) depends on no order.
+template <typename TW, int N>
+__device__ __forceinline__ void finish_row(const GradArgs &a, unsigned v, int j, const float (&acc)[N]) {
+    TW *p = static_cast<TW *>(a.dtable) + (long long)v * a.ld_dtable + j;
+    float f[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) f[k] = acc[k] * a.scale;
+    if (!a.add) {
+        store_vec<TW, N>(p, f);
+    } else if constexpr (sizeof(TW) == 4) {
+        if constexpr (N == 8) {
+            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
+            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p + 4), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) atomicAdd(reinterpret_cast<float *>(p) + k, f[k]);
+        }
+    } else {
+        float old[N];
+        load_vec<TW, N>(p, old);
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] += old[k];
+        store_vec<TW, N>(p, f);
+    }
+}
+
+// Zeros to the rows of ids that do not occur, zero_rows at a time: the sorted keys between the rows' bounds tell which.
+constexpr int kMaxZeroRows = 1024;
+
+// First place in the sorted keys that is not below v, by a warp, 33 stretches at a time.
+__device__ __forceinline__ unsigned lower_bound(const unsigned *key, unsigned T, long long v, int lane) {
+    unsigned lo = 0, hi = T;                                 // places before lo are below v, places from hi on are not
+    while (lo < hi) {
+        const unsigned step = (hi - lo + 32) / 33;
+        const unsigned long long at = (unsigned long long)lo + (unsigned long long)step * (lane + 1) - 1;
+        const int below = __popc(__ballot_sync(0xffffffffu, at < hi && (long long)__ldcg(key + (at < hi ? at : lo)) < v));
+        const unsigned end = (unsigned)min((unsigned long long)hi, (unsigned long long)lo + (unsigned long long)step * (below + 1) - 1);
+        lo += step * below;
+        hi = max(lo, end);
+    }
+    return lo;
+}
+
+template <typename TW>
+__device__ __forceinline__ void zero_absent(const GradArgs &a, const unsigned *key, long long begin, long long end, int block, int blocks) {
+    __shared__ unsigned s_seen[kMaxZeroRows / 32], s_from, s_to;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int threads = blockDim.x;
+    for (long long v0 = begin + (long long)block * a.zero_rows; v0 < end; v0 += (long long)blocks * a.zero_rows) {
+        const int rows = (int)min((long long)a.zero_rows, end - v0);
+        if (tid < kMaxZeroRows / 32) s_seen[tid] = 0;
+        if (warp < 2) {
+            const unsigned at = lower_bound(key, a.T, warp ? v0 + rows : v0, lane);
+            if (lane == 0) (warp ? s_to : s_from) = at;
+        }
+        __syncthreads();
+        for (unsigned i = s_from + tid; i < s_to; i += threads) {
+            const int r = (int)(__ldcg(key + i) - v0);
+            if (!((s_seen[r >> 5] >> (r & 31)) & 1u)) atomicOr(&s_seen[r >> 5], 1u << (r & 31));
+        }
+        __syncthreads();
+        for (int r = warp; r < rows; r += threads / 32)
+            if (!((s_seen[r >> 5] >> (r & 31)) & 1u)) zero_row<TW>(a, v0 + r, lane, 32);
+        __syncthreads();
+    }
+}
+
+template <typename TG, typename TW, int N>
+__global__ void __launch_bounds__(kReduceThreads, 4) embedding_reduce_kernel(const GradArgs a) {
+    constexpr int kAhead = N * sizeof(TG) == 32 ? 4 : 8;
+    constexpr int kMost = kReduceThreads / kMinRowThreads * kMaxTile;
+    __shared__ unsigned s_key[kMost + 2 * kMaxTile + 2], s_pos[kMost + kMaxTile];
+    let_next_start();
+    wait_for_previous();
+    // the blocks that write zeros are spread evenly among the others
+    const long long zeros_before = (long long)blockIdx.x * a.zero_blocks / gridDim.x;
+    if ((long long)(blockIdx.x + 1) * a.zero_blocks / gridDim.x > zeros_before) {
+        zero_absent<TW>(a, (a.passes & 1) ? a.key1 : a.key0, 0, (long long)a.V - a.early_rows - a.late_rows, (int)zeros_before, a.zero_blocks);
+        return;
+    }
+    const int block = (int)(blockIdx.x - zeros_before), block_x = block % a.tile_blocks, block_y = block / a.tile_blocks;
+    const int subs = kReduceThreads / a.row_threads;
+    const int sub = threadIdx.x / a.row_threads, col = threadIdx.x - sub * a.row_threads;
+    const unsigned *key_in = (a.passes & 1) ? a.key1 : a.key0, *pos_in = (a.passes & 1) ? a.pos1 : a.pos0;
+    // keys of the places from one tile (and one) before this block's to one after it; V + 1 where there is none
+    const int span = subs * a.tile;
+    const long long base = (long long)block_x * span;
+    for (int i = threadIdx.x; i < span + 2 * a.tile + 2; i += kReduceThreads) {
+        const long long at = base + i - a.tile - 1;
+        s_key[i] = at >= 0 && at < (long long)a.T ? __ldcg(key_in + at) : a.V + 1;
+    }
+    for (int i = threadIdx.x; i < span + a.tile; i += kReduceThreads)
+        if (base + i < (long long)a.T) s_pos[i] = __ldcg(pos_in + base + i);
+    __syncthreads();
+    const int tile = block_x * subs + sub;
+    const int grp = block_y * a.row_threads + col;
+    if (tile >= a.tiles || grp >= a.groups) return;
+    const int j = grp * N, L = a.tile;
+    const unsigned *key = s_key + sub * L + L + 1, *pos = s_pos + sub * L;        // key[-L - 1] .. key[2 L]
+    int i = 0, n = (int)min((long long)L, (long long)a.T - (long long)tile * L);
+    bool came = key[0] == key[-1];                           // the current id came in, and is a long one
+    if (came && key[-L - 1] != key[0] && key[L] != key[0]) { // not so long: the tile before has it
+        while (i < n && key[i] == key[-1]) ++i;
+        came = false;
+    }
+    const bool goes_on = key[n - 1] == key[n];
+    bool leaves = goes_on;                                   // the last id goes on as a long one
+    if (goes_on && key[-1] != key[n - 1] && key[2 * L] != key[n - 1]) {
+        const unsigned v = key[n - 1];
+        while (key[n] == v) ++n;
+        leaves = false;
+    }
+    float acc[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] = 0.f;
+    const TG *dout = static_cast<const TG *>(a.dout) + j;
+    for (; i < n; i += kAhead) {
+        Stored<TG, N> f[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (i + u < n && key[i + u] < a.V) f[u] = load_stored<TG, N>(dout + (long long)pos[i + u] * a.ld_dout);
+#pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (i + u >= i1) break;
-            if (key[u] != cur) {
-                flush(false);
-                cur = key[u];
-                open = false;
+            if (i + u >= n || key[i + u] >= a.V) break;      // ids outside [0, V) are last
+#pragma unroll
+            for (int k = 0; k < N; ++k) acc[k] += element_of<N>(f[u], k);
+            if (key[i + u] != key[i + u + 1]) {              // the id's last token
+                if (came) store_vec<float, N>(a.part + (size_t)tile * 2 * a.H + j, acc);
+                else finish_row<TW, N>(a, key[i + u], j, acc);
+                came = false;
 #pragma unroll
                 for (int k = 0; k < N; ++k) acc[k] = 0.f;
             }
-#pragma unroll
-            for (int k = 0; k < N; ++k) acc[k] += f[u][k];
         }
     }
-    flush(cur == after);
+    if (leaves && key[n - 1] < a.V) store_vec<float, N>(a.part + ((size_t)tile * 2 + (came ? 0 : 1)) * a.H + j, acc);
 }
 
-// One thread group per tile: if an id starts in the tile and goes on, its parts are added up here.
+// A block looks through kJoinTiles tiles for long ids that start in one of them and adds such an id's parts over 32 N
+// columns: a warp where there are up to kFewParts of them, else all warps together, each a stretch of the parts.
+constexpr int kJoinTiles = 32;
+constexpr int kFewParts = 8;
+constexpr int kJoinThreads = 256;
+constexpr int kJoinWarps = kJoinThreads / 32;
+
 template <typename TW, int N>
-__global__ void __launch_bounds__(kReduceThreads) embedding_join_kernel(const ReduceArgs a) {
-    const int sub = threadIdx.x / a.row_threads, col = threadIdx.x - sub * a.row_threads;
-    const int tile = blockIdx.x * (kReduceThreads / a.row_threads) + sub;
-    const int grp = blockIdx.y * a.row_threads + col;
-    if (tile + 1 >= a.tiles || grp >= a.groups) return;
-    const unsigned i0 = (unsigned)tile * a.tile, i1 = i0 + a.tile;
-    const unsigned v = __ldg(a.key + i1 - 1);
-    if (v >= a.V || __ldg(a.key + i1) != v) return;          // nothing goes on
-    if (__ldg(a.key + i0) == v && i0 && __ldg(a.key + i0 - 1) == v) return;   // it started before this tile
-    // tiles reached: places up to the last one with id v
-    unsigned lo = i1, hi = a.T;                              // key[lo] == v; first place past v is in (lo, hi]
-    while (hi - lo > 1) {
-        const unsigned mid = lo + (hi - lo) / 2;
-        if (__ldg(a.key + mid) == v) lo = mid; else hi = mid;
+__global__ void __launch_bounds__(kJoinThreads, 4) embedding_join_kernel(const GradArgs a) {
+    __shared__ float s_sum[kJoinWarps][32 * N];
+    wait_for_previous();
+    const unsigned *key = (a.passes & 1) ? a.key1 : a.key0;
+    const int join_blocks = (int)gridDim.x - a.late_blocks;
+    if ((int)blockIdx.x >= join_blocks) {
+        const long long end = (long long)a.V - a.early_rows;
+        zero_absent<TW>(a, key, end - a.late_rows, end, (int)blockIdx.x - join_blocks, a.late_blocks);
+        return;
     }
-    const int last = (int)(lo / (unsigned)a.tile);
-    const int j = grp * N;
-    float acc[N], f[N];
-    load_vec<float, N>(a.part + ((size_t)tile * 2 + 1) * a.H + j, acc);
-#pragma unroll 4
-    for (int t = tile + 1; t <= last; ++t) {
-        load_vec<float, N>(a.part + (size_t)t * 2 * a.H + j, f);
+    const int tile_groups = (a.tiles + kJoinTiles - 1) / kJoinTiles, block_x = blockIdx.x % tile_groups, block_y = blockIdx.x / tile_groups;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int j = (block_y * 32 + lane) * N;
+    const bool in = j < a.H;
+    const int mine = block_x * kJoinTiles + lane;         // every warp looks at the same tiles
+    auto first_key = [&](long long tile) {                   // of a tile; V + 1 past the last
+        return tile < a.tiles ? __ldcg(key + tile * a.tile) : a.V + 1;
+    };
+    unsigned v = a.V + 1;
+    bool starts = false, many = false;                       // a long id starts in this lane's tile; it has over kFewParts parts
+    if (mine + 2 < a.tiles) {                                // it reaches the tile after the next
+        v = first_key(mine + 1);
+        const unsigned i0 = (unsigned)mine * a.tile, last = __ldcg(key + i0 + a.tile - 1), before = i0 ? __ldcg(key + i0 - 1) : a.V + 1;
+        const unsigned after_next = first_key((long long)mine + 2), far = first_key((long long)mine + kFewParts);
+        starts = v < a.V && last == v && before != v && after_next == v;
+        many = starts && far == v;
+    }
+    // sum of parts p0 .. p1 - 1 of the id that starts in `tile` (part 0 is that tile's)
+    auto add_parts = [&](int tile, int p0, int p1, float (&acc)[N]) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) acc[k] += f[k];
+        for (int k = 0; k < N; ++k) acc[k] = 0.f;
+#pragma unroll 4
+        for (int p = p0; p < p1; ++p) {
+            float f[N];
+            load_vec<float, N>(a.part + ((size_t)(tile + p) * 2 + (p == 0 ? 1 : 0)) * a.H + j, f);
+#pragma unroll
+            for (int k = 0; k < N; ++k) acc[k] += f[k];
+        }
+    };
+    int turn = 0;
+    for (unsigned todo = __ballot_sync(0xffffffffu, starts && !many); todo; todo &= todo - 1, ++turn) {
+        if (turn % kJoinWarps != warp) continue;
+        const int from = __ffs(todo) - 1, tile = block_x * kJoinTiles + from;
+        const unsigned id = __shfl_sync(0xffffffffu, v, from);
+        const int parts = __popc(__ballot_sync(0xffffffffu, lane < kFewParts && (lane == 0 || first_key((long long)tile + lane) == id)));
+        float acc[N];
+        if (in) {
+            add_parts(tile, 0, parts, acc);
+            finish_row<TW, N>(a, id, j, acc);
+        }
     }
-    write_row<TW, N>(a, v, j, acc);
+    for (unsigned todo = __ballot_sync(0xffffffffu, many); todo; todo &= todo - 1) {
+        const int from = __ffs(todo) - 1, tile = block_x * kJoinTiles + from;
+        const unsigned id = __shfl_sync(0xffffffffu, v, from);
+        // tile lo begins with the id; the first tile that does not is in (lo, hi].  Two looks for up to 256 parts
+        int lo = tile + kFewParts, hi = a.tiles;
+        for (int step = 8; hi - lo > 1; step = (hi - lo + 32) / 33) {
+            const long long t = lo + (long long)step * (lane + 1);
+            const int steps = __popc(__ballot_sync(0xffffffffu, t < hi && first_key(t) == id));   // sorted: the lanes that match come first
+            if (steps < 32) hi = (int)min((long long)hi, lo + (long long)step * (steps + 1));
+            lo += step * steps;
+        }
+        const int parts = lo - tile + 1, each = (parts + kJoinWarps - 1) / kJoinWarps;
+        const int p0 = min(warp * each, parts), p1 = min(p0 + each, parts);
+        float acc[N];
+        if (in) {
+            add_parts(tile, p0, p1, acc);
+#pragma unroll
+            for (int k = 0; k < N; ++k) s_sum[warp][k * 32 + lane] = acc[k];
+        }
+        __syncthreads();
+        if (warp == 0 && in) {
+            for (int w = 1; w < kJoinWarps; ++w) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) acc[k] += s_sum[w][k * 32 + lane];
+            }
+            finish_row<TW, N>(a, id, j, acc);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- gradient: few tokens
+// One launch, no workspace.  Every block sorts all the tokens in shared memory (each thread counts the tokens that
+// come before its own).  The first column_blocks blocks take 32 N columns each: their warps walk equal
+// stretches of the sorted tokens, and an id that reaches over a stretch's end is added up by the warp where it starts, from
+// the parts that the others leave in shared memory.  The other blocks write zeros to the rows of ids that do not occur.
+
+constexpr int kFewTokens = 512;
+constexpr int kFewThreads = 512;
+constexpr int kFewWarps = kFewThreads / 32;
+
+template <typename TG, typename TW, int N>
+__global__ void __launch_bounds__(kFewThreads) embedding_few_kernel(const GradArgs a) {
+    __shared__ unsigned s_id[kFewTokens], s_key[kFewTokens + 2], s_pos[kFewTokens];
+    __shared__ float s_part[kFewWarps][32 * N];              // sum of the id that a warp's stretch begins with, if it came in
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned T = a.T;
+    const int column_blocks = (int)gridDim.x - a.zero_blocks;
+    unsigned mine = a.V;
+    if ((unsigned)tid < T) s_id[tid] = mine = token_key(a, tid);
+    if (tid == 0) { s_key[0] = a.V + 1; s_key[T + 1] = a.V + 1; }
+    __syncthreads();
+    if ((int)blockIdx.x >= column_blocks) {
+        // rows [v0, v1) of this block, 1024 at a time: which of them occur?
+        __shared__ unsigned s_seen[32];
+        const long long per = ((long long)a.V + a.zero_blocks - 1) / a.zero_blocks;
+        const long long v0 = per * ((int)blockIdx.x - column_blocks), v1 = min(v0 + per, (long long)a.V);
+        for (long long v = v0; v < v1; v += 1024) {
+            const int rows = (int)min(1024LL, v1 - v);
+            if (tid < 32) s_seen[tid] = 0;
+            __syncthreads();
+            if ((unsigned)tid < T && mine >= v && mine < v + rows) atomicOr(&s_seen[(mine - v) >> 5], 1u << ((mine - v) & 31));
+            __syncthreads();
+            for (int r = warp; r < rows; r += kFewWarps)
+                if (!((s_seen[r >> 5] >> (r & 31)) & 1u)) zero_row<TW>(a, v + r, lane, 32);
+            __syncthreads();
+        }
+        return;
+    }
+    unsigned place = 0;
+    if ((unsigned)tid < T) {
+#pragma unroll 8
+        for (unsigned i = 0; i < T; ++i) place += s_id[i] < mine || (s_id[i] == mine && i < (unsigned)tid);
+        s_key[place + 1] = mine;
+        s_pos[place] = tid;
+    }
+    __syncthreads();
+    const unsigned *key = s_key + 1;                         // key[-1] .. key[T]
+    const unsigned each = (T + kFewWarps - 1) / kFewWarps;
+    const unsigned from = min(warp * each, T), to = min(from + each, T);
+    const int j = (blockIdx.x * 32 + lane) * N;
+    const bool in = j < a.H;
+    constexpr int kAhead = 8;
+    float acc[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) acc[k] = 0.f;
+    bool open = from < to && from > 0 && key[from] == key[(int)from - 1];
+    for (unsigned i = from; i < to; i += kAhead) {
+        float f[kAhead][N];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (in && i + u < to && key[i + u] < a.V) load_vec<TG, N>(static_cast<const TG *>(a.dout) + (long long)s_pos[i + u] * a.ld_dout + j, f[u]);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u >= to || key[i + u] >= a.V) break;
+            if (in) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) acc[k] += f[u][k];
+            }
+            const bool ends = key[i + u] != key[i + u + 1];
+            if ((ends || i + u + 1 == to) && open) {         // (a part of) an id that came in
+#pragma unroll
+                for (int k = 0; k < N; ++k) s_part[warp][k * 32 + lane] = acc[k];
+                open = false;
+#pragma unroll
+                for (int k = 0; k < N; ++k) acc[k] = 0.f;
+            } else if (ends) {
+                if (in) finish_row<TW, N>(a, key[i + u], j, acc);
+#pragma unroll
+                for (int k = 0; k < N; ++k) acc[k] = 0.f;
+            }
+        }
+    }
+    __syncthreads();
+    // an id that starts in this stretch and goes on
+    if (from < to && in && key[to - 1] < a.V && key[to - 1] == key[to]) {
+        const unsigned v = key[to - 1];
+        if (from > 0 && key[from] == v && key[(int)from - 1] == v) return;       // it came in itself
+        for (int w = warp + 1; w < kFewWarps && w * each < T && key[w * each] == v; ++w) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) acc[k] += s_part[w][k * 32 + lane];
+        }
+        finish_row<TW, N>(a, v, j, acc);
+    }
 }
 
 }  // namespace

@@ -17,7 +17,7 @@ template <> __device__ __forceinline__ bf16 from_float<bf16>(float x) { return _
 
 // ---------------------------------------------------------------- N consecutive elements as fp32
 // N * sizeof(T) bytes in as few accesses as its alignment to min(16, N * sizeof(T)) bytes allows.
-// kOnce: the data is not used again (streaming loads and stores).
+// kOnce: the data is not read again soon (streaming loads; stores always are).
 
 __device__ __forceinline__ float bf16_low(unsigned u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf16_high(unsigned u) { return __uint_as_float(u & 0xffff0000u); }
@@ -31,17 +31,17 @@ template <> struct Words<1> { using type = unsigned; };
 template <> struct Words<2> { using type = uint2; };
 template <> struct Words<4> { using type = uint4; };
 
-template <typename T, int N>
+template <typename T, int N, bool kOnce = true>
 __device__ __forceinline__ void load_vec(const T *p, float (&f)[N]) {
     if constexpr (N == 1) {
-        f[0] = to_float(__ldcs(p));
+        f[0] = to_float(kOnce ? __ldcs(p) : __ldcg(p));
     } else {
         constexpr int kWords = N * (int)sizeof(T) / 4, kPer = kWords < 4 ? kWords : 4;
         using W = typename Words<kPer>::type;
         unsigned u[kWords];
 #pragma unroll
         for (int i = 0; i < kWords / kPer; ++i) {
-            const W w = __ldcs(reinterpret_cast<const W *>(p) + i);
+            const W w = kOnce ? __ldcs(reinterpret_cast<const W *>(p) + i) : __ldcg(reinterpret_cast<const W *>(p) + i);
             memcpy(&u[i * kPer], &w, sizeof(W));
         }
         if constexpr (sizeof(T) == 4) {

@@ -68,19 +68,31 @@ constexpr int64_t kMaxLd = (int64_t)1 << 40;
 
 // ---------------------------------------------------------------- embedding
 
+// Elements that a thread moves at a time (8, 2 or 1): what row starts and width allow in both matrices.
+int group_width(int H, const void *p, int64_t ldp, int tp, const void *q, int64_t ldq, int tq) {
+    for (const int n : {8, 2}) {
+        auto fits = [&](const void *x, int64_t ld, int type) {
+            const size_t boundary = n * type_bytes(type) < 16 ? n * type_bytes(type) : 16;
+            return aligned_to(x, boundary) && (size_t)ld * type_bytes(type) % boundary == 0;
+        };
+        if (H % n == 0 && fits(p, ldp, tp) && fits(q, ldq, tq)) return n;
+    }
+    return 1;
+}
+
 template <typename TW, typename TO>
-int launch_lookup(LookupArgs a, bool vec, cudaStream_t s) {
-    constexpr int kWide = 8;
-    a.groups = vec ? a.H / kWide : a.H;
-    // about eight groups a thread, at least one row a block
-    long long rows = (8LL * kLookupThreads) / a.groups;
+int launch_lookup(LookupArgs a, int n, cudaStream_t s) {
+    a.groups = a.H / n;
+    // two rounds of kLookupAhead groups a thread, at least one row a block
+    long long rows = (2LL * kLookupAhead * kLookupThreads) / a.groups;
     if (rows < 1) rows = 1;
     // short lookups: fewer rows a block, so that more blocks share the work
     while (rows > 1 && (a.T + rows - 1) / rows < 592) rows = (rows + 1) / 2;
     a.rows_per_block = (unsigned)rows;
     const long long grid = (a.T + rows - 1) / rows;
     if (grid > INT_MAX) return DPPF_ERR_INVALID_ARG;
-    if (vec) lookup_kernel<TW, TO, kWide><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
+    if (n == 8) lookup_kernel<TW, TO, 8><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
+    else if (n == 2) lookup_kernel<TW, TO, 2><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
     else lookup_kernel<TW, TO, 1><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
     return launched();
 }
@@ -89,18 +101,18 @@ int launch_lookup(LookupArgs a, bool vec, cudaStream_t s) {
 bool rows_on_16(const void *p, int64_t ld, int type) { return aligned_to(p, 16) && (size_t)ld * type_bytes(type) % 16 == 0; }
 
 // Places of the sorted tokens that a thread walks: long enough that few sums are split, short enough
-// that about 1,000 threads an SM are at work (8 to 128).
+// that about 2,000 threads an SM are at work (8 to 32).
 int reduce_tile(int64_t T, int H) {
-    const double rows = (double)T * ((H + 7) / 8) / (148.0 * 1024.0);
+    const double rows = (double)T * ((H + 7) / 8) / (148.0 * 2048.0);
     int tile = 8;
-    while (tile < 128 && tile < rows) tile *= 2;
+    while (tile < kMaxTile && tile < rows) tile *= 2;
     return tile;
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 struct EmbeddingLayout {
-    size_t key[2], pos[2], part, total;
+    size_t key[2], pos[2], hist, part, total;
     int tile, tiles;
 };
 EmbeddingLayout embedding_layout(int64_t T, int H) {
@@ -110,29 +122,87 @@ EmbeddingLayout embedding_layout(int64_t T, int H) {
     size_t at = 0;
     const size_t words = round256((size_t)T * 4);
     for (int i = 0; i < 2; ++i) { l.key[i] = at; at += words; l.pos[i] = at; at += words; }
+    l.hist = at;
+    at += (size_t)3 * kSortBlocks * kBins * 4;
     l.part = at;
     at += round256((size_t)l.tiles * 2 * (size_t)H * 4);
     l.total = at;
     return l;
 }
 
-template <typename TG, typename TW, int N>
-void launch_reduce(const ReduceArgs &a, dim3 grid, cudaStream_t s) {
-    embedding_reduce_kernel<TG, TW, N><<<grid, kReduceThreads, 0, s>>>(a);
-    if (a.tiles > 1) embedding_join_kernel<TW, N><<<grid, kReduceThreads, 0, s>>>(a);
-}
-template <int N>
-void launch_reduce_types(const ReduceArgs &a, int tg, int tw, dim3 grid, cudaStream_t s) {
-    if (tg == DPPF_FLOAT32) {
-        if (tw == DPPF_FLOAT32) launch_reduce<float, float, N>(a, grid, s);
-        else launch_reduce<float, bf16, N>(a, grid, s);
-    } else {
-        if (tw == DPPF_FLOAT32) launch_reduce<bf16, float, N>(a, grid, s);
-        else launch_reduce<bf16, bf16, N>(a, grid, s);
-    }
+// A launch that may be set up while the one before it in the stream still runs (its kernel waits by itself).
+template <typename... P, typename... A>
+bool launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess;
 }
 
-std::atomic<int> g_sort_ready[kMaxDevices];
+// Bytes of zeros written at a time by a block, beside a digit's launch of the sort and beside the joins
+constexpr long long kZeroBytes = 65536, kEarlyBytes = 32LL << 20, kLateBytes = 40LL << 20;
+
+std::atomic<int> g_place_ready[2][kMaxDevices];
+
+// Threads side by side on a row's groups: as many as possible without leaving over a sixth of them idle.
+int row_threads(int groups) {
+    for (int n = kReduceThreads; n > kMinRowThreads; n /= 2)
+        if (groups % n == 0 || (int64_t)groups * 6 >= (int64_t)((groups + n - 1) / n) * n * 5) return n;
+    return kMinRowThreads;
+}
+
+template <typename TG, typename TW, int N>
+int launch_grad(GradArgs a, int dev, int sms, cudaStream_t s) {
+    a.groups = a.H / N;
+    const long long row_bytes = (long long)a.H * (int)sizeof(TW), zero_bytes = a.add ? 0 : (long long)a.V * row_bytes;
+    if (a.T <= kFewTokens) {
+        const int column_blocks = (a.groups + 31) / 32;
+        a.zero_blocks = (int)((zero_bytes + 65535) / 65536 < 2LL * sms ? (zero_bytes + 65535) / 65536 : 2LL * sms);
+        embedding_few_kernel<TG, TW, N><<<column_blocks + a.zero_blocks, kFewThreads, 0, s>>>(a);
+        return launched();
+    }
+    if (!allow_smem(embedding_place_kernel<TW>, dev, g_place_ready[sizeof(TW) == 4 ? 0 : 1], (int)kPlaceSmem)) return DPPF_ERR_CUDA;
+    const long long per = ((long long)a.T + kSortBlocks - 1) / kSortBlocks;
+    a.chunk = (unsigned)((per + kSortThreads - 1) / kSortThreads * kSortThreads);
+    a.sort_blocks = (int)(((long long)a.T + a.chunk - 1) / a.chunk);
+    // zeros (V rows): what SMs without a part in the sort can write meanwhile, what fits beside the joins, the rest
+    const int spare = zero_bytes && a.sort_blocks < 2 * sms ? 2 * sms - a.sort_blocks : 0;
+    a.zero_rows = (int)(kZeroBytes / row_bytes < 1 ? 1 : kZeroBytes / row_bytes > kMaxZeroRows ? kMaxZeroRows : kZeroBytes / row_bytes);
+    if (zero_bytes) {
+        auto rows_of = [&](long long bytes, long long most) { return bytes / row_bytes < most ? bytes / row_bytes : most; };
+        a.early_rows = spare ? (unsigned)rows_of(kEarlyBytes * a.passes, a.V) : 0;
+        a.late_rows = (unsigned)rows_of(kLateBytes, (long long)a.V - a.early_rows);
+        auto blocks_of = [&](long long rows) { const long long n = (rows + a.zero_rows - 1) / a.zero_rows; return (int)(n < 16LL * sms ? n : 16LL * sms); };
+        a.zero_blocks = blocks_of((long long)a.V - a.early_rows - a.late_rows);
+        a.late_blocks = blocks_of(a.late_rows);
+    }
+    embedding_count_kernel<<<a.sort_blocks, kSortThreads, 0, s>>>(a);
+    bool ok = cudaPeekAtLastError() == cudaSuccess;
+    for (int pass = 0; pass < a.passes; ++pass)
+        ok = ok && launch_after(embedding_place_kernel<TW>, dim3((unsigned)(a.sort_blocks + spare)), kSortThreads, kPlaceSmem, s, a, pass);
+    a.row_threads = row_threads(a.groups);
+    const int subs = kReduceThreads / a.row_threads;
+    a.tile_blocks = (a.tiles + subs - 1) / subs;
+    const long long blocks = (long long)a.tile_blocks * ((a.groups + a.row_threads - 1) / a.row_threads);
+    if (blocks + a.zero_blocks > INT_MAX) return DPPF_ERR_INVALID_ARG;
+    ok = ok && launch_after(embedding_reduce_kernel<TG, TW, N>, dim3((unsigned)(blocks + a.zero_blocks)), kReduceThreads, 0, s, a);
+    const long long joins = (long long)((a.tiles + kJoinTiles - 1) / kJoinTiles) * ((a.groups + 31) / 32) + a.late_blocks;
+    if (joins > INT_MAX) return DPPF_ERR_INVALID_ARG;
+    ok = ok && launch_after(embedding_join_kernel<TW, N>, dim3((unsigned)joins), kJoinThreads, 0, s, a);
+    if (!ok) { cudaGetLastError(); return DPPF_ERR_CUDA; }
+    return DPPF_OK;
+}
+template <typename TG, typename TW>
+int launch_grad_width(const GradArgs &a, int n, int dev, int sms, cudaStream_t s) {
+    return n == 8 ? launch_grad<TG, TW, 8>(a, dev, sms, s) : n == 2 ? launch_grad<TG, TW, 2>(a, dev, sms, s) : launch_grad<TG, TW, 1>(a, dev, sms, s);
+}
 
 // ---------------------------------------------------------------- policy loss
 
@@ -277,10 +347,10 @@ int dppf_embedding(const void *table, int table_type, int64_t V, int H, int64_t 
     a.table = table; a.ids = ids; a.out = out;
     a.ld_table = ld_table; a.ld_out = ld_out; a.T = T; a.V = V; a.H = H; a.ids64 = id_bits == 64;
     a.scale = scale;
-    const bool vec = H % 8 == 0 && rows_on_16(table, ld_table, table_type) && rows_on_16(out, ld_out, out_type);
+    const int n = group_width(H, table, ld_table, table_type, out, ld_out, out_type);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    if (table_type == DPPF_FLOAT32) return out_type == DPPF_FLOAT32 ? launch_lookup<float, float>(a, vec, s) : launch_lookup<float, bf16>(a, vec, s);
-    return out_type == DPPF_FLOAT32 ? launch_lookup<bf16, float>(a, vec, s) : launch_lookup<bf16, bf16>(a, vec, s);
+    if (table_type == DPPF_FLOAT32) return out_type == DPPF_FLOAT32 ? launch_lookup<float, float>(a, n, s) : launch_lookup<float, bf16>(a, n, s);
+    return out_type == DPPF_FLOAT32 ? launch_lookup<bf16, float>(a, n, s) : launch_lookup<bf16, bf16>(a, n, s);
 }
 
 size_t dppf_embedding_workspace_bytes(int64_t T, int H) {
@@ -314,63 +384,31 @@ int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, cons
     const int dev = current_device();
     if (dev < 0) return DPPF_ERR_CUDA;
     const int sms = multiprocessors(dev);
-    if (sms < 0 || !allow_smem(embedding_sort_kernel, dev, g_sort_ready, kSortWarps * kBins * 4)) return DPPF_ERR_CUDA;
-
-    SortArgs a;
-    a.ids = ids; a.ids64 = id_bits == 64; a.V = V; a.T = (unsigned)T;
+    if (sms < 0) return DPPF_ERR_CUDA;
+    GradArgs a = {};
+    a.ids = ids; a.ids64 = id_bits == 64;
+    a.T = (unsigned)T; a.V = (unsigned)V; a.H = H;
+    a.dout = grad_out; a.dtable = grad_table;
+    a.ld_dout = ld_out; a.ld_dtable = ld_table;
+    a.add = accumulate ? 1 : 0;
+    a.scale = scale;
     unsigned char *base = static_cast<unsigned char *>(ws);
-    for (int i = 0; i < 2; ++i) {
-        a.key[i] = reinterpret_cast<unsigned *>(base + l.key[i]);
-        a.pos[i] = reinterpret_cast<unsigned *>(base + l.pos[i]);
-    }
+    a.key0 = reinterpret_cast<unsigned *>(base + l.key[0]);
+    a.pos0 = reinterpret_cast<unsigned *>(base + l.pos[0]);
+    a.key1 = reinterpret_cast<unsigned *>(base + l.key[1]);
+    a.pos1 = reinterpret_cast<unsigned *>(base + l.pos[1]);
+    a.hist = reinterpret_cast<unsigned *>(base + l.hist);
+    a.part = reinterpret_cast<float *>(base + l.part);
     int bits = 1;
     while (((int64_t)1 << bits) <= V) ++bits;                    // keys 0 .. V
     a.passes = (bits + kDigitBits - 1) / kDigitBits;
     a.bits = (bits + a.passes - 1) / a.passes;
-    const size_t es = type_bytes(table_type);
-    a.zero = accumulate ? nullptr : grad_table;
-    a.zero_ld = ld_table * (int64_t)es;
-    a.zero_width = (int64_t)H * (int64_t)es;
-    a.zero_vec = rows_on_16(grad_table, ld_table, table_type) && a.zero_width % 16 == 0;
-    int C = 1;
-    while (C < kSortMaxCluster && T > 2048LL * C) C *= 2;        // up to 64 tokens a warp before another block joins
-    long long fill = 0;                                          // blocks that write zeros
-    if (a.zero) {
-        fill = (V * a.zero_width + 65535) / 65536;
-        if (fill > 2LL * sms) fill = 2LL * sms;
-        fill = (fill + C - 1) / C * C;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(C + fill));
-    cfg.blockDim = dim3(kSortThreads);
-    cfg.dynamicSmemBytes = (size_t)kSortWarps * ((size_t)1 << a.bits) * 4;
-    cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)C;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, embedding_sort_kernel, a) != cudaSuccess) { cudaGetLastError(); return DPPF_ERR_CUDA; }
-
-    ReduceArgs r;
-    r.key = a.key[a.passes & 1]; r.pos = a.pos[a.passes & 1];
-    r.dout = grad_out; r.dtable = grad_table;
-    r.part = reinterpret_cast<float *>(base + l.part);
-    r.ld_dout = ld_out; r.ld_dtable = ld_table;
-    r.T = (unsigned)T; r.V = (unsigned)V; r.H = H;
-    r.tile = l.tile; r.tiles = l.tiles;
-    r.add = accumulate ? 1 : 0;
-    r.scale = scale;
-    const bool vec = H % 8 == 0 && rows_on_16(grad_table, ld_table, table_type) && rows_on_16(grad_out, ld_out, out_type);
-    r.groups = vec ? H / 8 : H;
-    r.row_threads = 1;
-    while (r.row_threads < kReduceThreads && r.row_threads < r.groups) r.row_threads *= 2;
-    const int per_block = kReduceThreads / r.row_threads;
-    const dim3 grid((unsigned)((r.tiles + per_block - 1) / per_block), (unsigned)((r.groups + r.row_threads - 1) / r.row_threads));
-    if (vec) launch_reduce_types<8>(r, out_type, table_type, grid, s);
-    else launch_reduce_types<1>(r, out_type, table_type, grid, s);
-    return launched();
+    a.zero_vec = rows_on_16(grad_table, ld_table, table_type) && (size_t)H * type_bytes(table_type) % 16 == 0;
+    a.tile = l.tile; a.tiles = l.tiles;
+    const int n = group_width(H, grad_out, ld_out, out_type, grad_table, ld_table, table_type);
+    if (out_type == DPPF_FLOAT32)
+        return table_type == DPPF_FLOAT32 ? launch_grad_width<float, float>(a, n, dev, sms, s) : launch_grad_width<float, bf16>(a, n, dev, sms, s);
+    return table_type == DPPF_FLOAT32 ? launch_grad_width<bf16, float>(a, n, dev, sms, s) : launch_grad_width<bf16, bf16>(a, n, dev, sms, s);
 }
 
 size_t dppf_policy_workspace_bytes(int64_t T) {
