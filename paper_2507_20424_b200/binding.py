@@ -430,7 +430,7 @@ def dppf_embedding(table, ids, scale=1.0, out=None, out_dtype=None):
     V, H, ld = _matrix(table, "table")
     ids = _vector(ids, ids.numel(), "ids", table.device, tuple(_ID_BITS))
     if out is None:
-        out = torch.empty((*ids.shape, H), dtype=out_dtype or table.dtype, device=table.device)
+        out = table.new_empty((*ids.shape, H), dtype=out_dtype)
     elif out.device != table.device or out.numel() != ids.numel() * H or out.shape[-1:] != (H,):
         raise ValueError("out must hold one row of H columns per id, on the table's device")
     flat = out if out.dim() == 2 else out.view(-1, H)
@@ -501,7 +501,7 @@ def dppf_policy_loss(logits, targets, old_logp, advantage, weight, ref_logp=None
         if grad_logits.dtype != logits.dtype or grad_logits.device != dev or (rows, cols) != (T, V):
             raise ValueError("grad_logits must have the type, shape and device of logits")
     ws = alloc_policy_workspace(T, dev) if ws is None else ws
-    out = torch.empty(3 + T, dtype=torch.float32, device=dev)
+    out = logits.new_empty(3 + T, dtype=torch.float32)
     sums, logp = out[:3], out[3:]
     _call(dev, load().dppf_policy_loss, "dppf_policy_loss", logits.data_ptr(), code, T, V, ld, targets.data_ptr(), _ID_BITS[targets.dtype], old_logp.data_ptr(),
           _ptr(ref_logp), advantage.data_ptr(), weight.data_ptr(), clip_low, clip_high, kl_coef, temperature, sums.data_ptr(), logp.data_ptr(), _ptr(grad_logits),

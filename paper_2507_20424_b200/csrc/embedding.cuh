@@ -100,10 +100,6 @@ struct GradArgs {
     int tile_blocks;             // blocks side by side over the tiles
 };
 
-// The dependent launch may be scheduled from here on; it waits for this one's end before it reads.
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 __device__ __forceinline__ unsigned token_key(const GradArgs &a, unsigned i) {
     const long long id = read_id(a.ids, a.ids64, i);
     return (id < 0 || id >= (long long)a.V) ? a.V : (unsigned)id;

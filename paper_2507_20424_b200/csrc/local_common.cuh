@@ -140,6 +140,11 @@ __device__ __forceinline__ unsigned cluster_load(unsigned a) {
     return v;
 }
 
+// ---------------------------------------------------------------- launches that follow one another
+// The dependent launch may be scheduled from here on; it waits for this one's end before it reads.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ float exp2_fast(float x) {   // 2 ulp; results below 2^-126 are 0
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

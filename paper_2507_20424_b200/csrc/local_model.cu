@@ -44,6 +44,22 @@ bool allow_smem(K kernel, int dev, std::atomic<int> *done, int bytes) {
 
 int launched() { return cudaGetLastError() == cudaSuccess ? DPPF_OK : DPPF_ERR_CUDA; }
 
+// A launch that may be set up while the one before it in the stream still runs (its kernel waits by itself).
+template <typename... P, typename... A>
+bool launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess;
+}
+
 bool all_finite(std::initializer_list<float> vals) {
     for (float f : vals)
         if (!std::isfinite(f)) return false;
@@ -130,22 +146,6 @@ EmbeddingLayout embedding_layout(int64_t T, int H) {
     return l;
 }
 
-// A launch that may be set up while the one before it in the stream still runs (its kernel waits by itself).
-template <typename... P, typename... A>
-bool launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess;
-}
-
 // Bytes of zeros written at a time by a block, beside a digit's launch of the sort and beside the joins
 constexpr long long kZeroBytes = 65536, kEarlyBytes = 32LL << 20, kLateBytes = 40LL << 20;
 
@@ -208,7 +208,9 @@ int launch_grad_width(const GradArgs &a, int n, int dev, int sms, cudaStream_t s
 
 constexpr size_t kPolicyHeaderBytes = 256;
 constexpr int kPolicySliceMax = 200 * 1024;        // shared memory of one block's slice at most
-constexpr int kPolicySliceGood = 72 * 1024;        // three blocks fit an SM: one loads while another writes
+// Four blocks and more fit an SM: some load while others write.  4,096 x 131,072 bf16 in slices of 64 KB (three blocks): 352 us,
+// of 32 KB: 342 us; 256 threads instead of 128 in slices of 64 KB: 359 us, of 32 KB: 424 us.
+constexpr int kPolicySliceGood = 54 * 1024;
 
 std::atomic<int> g_policy_ready[2][kMaxDevices];
 
@@ -220,19 +222,28 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     if (sms < 0) return DPPF_ERR_CUDA;
     // 16-byte vectors that a row spans: one more if rows may start inside one
     const int vectors = (int)(((size_t)a.V * sizeof(T) + 15) / 16) + (rows_on_16(a.logits, a.ld, sizeof(T) == 4 ? DPPF_FLOAT32 : DPPF_BFLOAT16) ? 0 : 1);
+    if (vectors <= 8 * 32) {
+        auto kernel = vectors <= 4 * 32 ? policy_short_kernel<T, 4> : policy_short_kernel<T, 8>;
+        const long long blocks = ((long long)a.T + kShortThreads / 32 - 1) / (kShortThreads / 32), most = 16LL * sms;
+        kernel<<<(unsigned)(blocks < most ? blocks : most), kShortThreads, 0, s>>>(a);
+        if (cudaPeekAtLastError() != cudaSuccess || !launch_after(policy_finish_kernel, dim3(3), kFinishThreads, 0, s, a)) { cudaGetLastError(); return DPPF_ERR_CUDA; }
+        return DPPF_OK;
+    }
     int C = 1;
     auto slice_bytes = [&](int c) { return (vectors + c - 1) / c * 16; };
-    while (C < kPolicyMaxCluster && slice_bytes(C) > kPolicySliceGood) C *= 2;
+    while (a.grad && C < kPolicyMaxCluster && slice_bytes(C) > kPolicySliceGood) C *= 2;
     // few rows: split them further while SMs are idle and a slice stays above 8 KB
     while (C < kPolicyMaxCluster && (long long)a.T * C < 2LL * sms && slice_bytes(C) > 16 * 1024) C *= 2;
-    if (slice_bytes(C) > kPolicySliceMax) return DPPF_ERR_INVALID_ARG;
     a.slice = (vectors + C - 1) / C;
-    // four chunks, in whole rounds of the block's threads
+    // a slice in four chunks, in whole rounds of the block's threads; a longer one goes through the ring if it is not kept
     a.chunk = (a.slice + kPolicyChunks * kPolicyThreads - 1) / (kPolicyChunks * kPolicyThreads) * kPolicyThreads;
+    if (!a.grad && a.chunk > kPolicyRing) a.chunk = kPolicyRing;
+    const int held = a.slice < kPolicyChunks * a.chunk ? a.slice : kPolicyChunks * a.chunk;
+    if (held * 16 > kPolicySliceMax) return DPPF_ERR_INVALID_ARG;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.T * (unsigned)C);
     cfg.blockDim = dim3(kPolicyThreads);
-    cfg.dynamicSmemBytes = (size_t)a.slice * 16;
+    cfg.dynamicSmemBytes = (size_t)held * 16;
     cfg.stream = s;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -240,7 +251,10 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, policy_kernel<T>, a) != cudaSuccess) { cudaGetLastError(); return DPPF_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, policy_kernel<T>, a) != cudaSuccess || !launch_after(policy_finish_kernel, dim3(3), kFinishThreads, 0, s, a)) {
+        cudaGetLastError();
+        return DPPF_ERR_CUDA;
+    }
     return DPPF_OK;
 }
 

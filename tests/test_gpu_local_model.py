@@ -272,6 +272,24 @@ def test_policy_loss_and_gradient(b, T, V, dtype):
     check_policy(b, policy_inputs(T, V, dtype, seed=T + V + 2), backward=False, temperature=1.6)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [1023, 1024, 1025, 2047, 2048, 2049, 4095, 4096, 4097, 8190])
+def test_policy_rows_around_the_size_a_warp_holds(b, V, dtype):
+    """128, 256 and 512 vectors of 16 bytes, aligned and not."""
+    check_policy(b, policy_inputs(7, V, dtype, seed=V))
+    check_policy(b, policy_inputs(7, V, dtype, seed=V + 1, stride=V + 3, offset=1), kl=False, backward=False)
+
+
+@pytest.mark.parametrize("T,V,stride,dtype", [(400, 70_001, 70_001, BF16), (330, 20_001, 20_003, F32), (600, 9_000, 9_000, BF16)])
+def test_policy_forward_streams_long_rows(b, T, V, stride, dtype):
+    i = policy_inputs(T, V, dtype, 21, stride=stride)
+    out = check_policy(b, i, backward=False)
+    kept = b.dppf_policy_loss(i["logits"], i["targets"], i["old"], i["adv"], i["weight"], grad_logits=torch.empty_like(i["logits"]))
+    # other slices, another order of the sums: 1e-6 (2 + |lp|), as against the reference
+    again = b.dppf_policy_loss(i["logits"], i["targets"], i["old"], i["adv"], i["weight"])
+    assert torch.allclose(kept.logp, again.logp, rtol=1e-6, atol=2e-6) and out.logp.shape == (T,)
+
+
 @pytest.mark.parametrize("stride,offset,gstride,goffset", [(1009, 0, 1009, 0), (1009, 3, 1009, 3), (1016, 0, 1016, 0), (1016, 1, 1016, 0), (1011, 2, 1040, 5), (1024, 0, 1009, 1)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_policy_strides_and_alignment(b, stride, offset, gstride, goffset, dtype):
@@ -390,9 +408,10 @@ def test_policy_offsets_past_32_bits(b):
     assert float(grad.float().abs().sum(1).count_nonzero()) <= 4 and abs(float(out.loss) - float(want.loss)) < 1e-4
 
 
-def test_policy_wait_that_gives_up_is_reported(b):
-    i = policy_inputs(6, 3000, BF16, 11, masked=0.0)
-    grad = torch.empty_like(i["logits"])
+@pytest.mark.parametrize("V,backward", [(40_000, True), (40_000, False), (200_000, False)])
+def test_policy_wait_that_gives_up_is_reported(b, V, backward):
+    i = policy_inputs(6, V, BF16, 11, masked=0.0)
+    grad = torch.empty_like(i["logits"]) if backward else None
     ws = b.alloc_policy_workspace(6)
     try:
         b.debug_set_poll_limits(0, -1)
@@ -401,7 +420,7 @@ def test_policy_wait_that_gives_up_is_reported(b):
     finally:
         b.debug_set_poll_limits(-1, -1)
     assert status == b.ERR_TIMEOUT and torch.isnan(out.logp).all() and torch.isnan(out.loss)
-    check_policy(b, i, ws=ws)                                  # and the workspace is good again
+    check_policy(b, i, ws=ws, backward=backward)               # and the workspace is good again
 
 
 def test_policy_refusals(b):
