@@ -9,7 +9,7 @@ namespace {
 
 // The recurrence is that of adamw1.  A work unit is 256 consecutive elements of one tensor, held by a
 // warp, eight a lane; the table of tensors travels in the launch's parameters (nothing on the device can
-// be stale).  A warp finds its first unit's tensor by bisection and walks the table from there.
+// be stale).  A warp finds a unit's tensor by bisection.
 //
 // States in 8 bits: blocks of 256 elements counted from the tensor's start, which is what a warp holds.
 //   m = code_m * scale_m,  sqrt(v) = code_r * scale_r,  codes e4m3, scale = (block's largest) / 448.
@@ -374,10 +374,11 @@ __device__ __forceinline__ void step_unit32(const TensorEntry &t, long long firs
 
 // ---------------------------------------------------------------- the kernel
 
-// The last tensor whose first unit is not past u.
+// The last tensor whose first unit is not past u, at or after tensor k.
 template <int kEntries>
-__device__ __forceinline__ int find_tensor(const TensorTable<kEntries> &tab, int u) {
-    int k = 0, hi = tab.n;
+__device__ __forceinline__ int find_tensor(const TensorTable<kEntries> &tab, int u, int k) {
+    int hi = tab.n;
+    if (k + 1 >= hi || tab.e[k + 1].first_unit > u) return k;
     while (hi - k > 1) {
         const int mid = (k + hi) >> 1;
         if (tab.e[mid].first_unit <= u) k = mid; else hi = mid;
@@ -393,10 +394,8 @@ adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
     const int lane = threadIdx.x & 31;
     const int step = gridDim.x * kTensorWarps * tab.group;
     int first = (blockIdx.x * kTensorWarps + (threadIdx.x >> 5)) * tab.group;
-    if (first >= tab.units) return;
-    int k = find_tensor(tab, first);
-    for (; first < tab.units; first += step) {
-        while (k + 1 < tab.n && tab.e[k + 1].first_unit <= first) ++k;
+    for (int k = 0; first < tab.units; first += step) {
+        k = find_tensor(tab, first, k);
         const TensorEntry *t = &tab.e[k];
         int blk = first - t->first_unit;
         if constexpr (kBits == 8) {

@@ -24,29 +24,32 @@ __device__ __forceinline__ long long read_id(const void *ids, int ids64, long lo
 }
 
 constexpr int kLookupThreads = 256;
-constexpr int kLookupAhead = 4;      // rows' pieces that a thread has under way
 
 // A block takes rows_per_block rows; its threads walk the groups of those rows in memory order, kLookupAhead at a time.
-// N = 8 needs rows of both tensors that start on 16-byte boundaries and H % 8 == 0, N = 2 rows on boundaries of two
-// elements and an even H, N = 1 takes anything.
+// N elements are 16 bytes of the output (16,384 rows of 1,024 from fp32 to bf16: 13.0 us with 8, 16.6 with 4; 26,214 of 5,120 from
+// bf16 to fp32: 117 us with 4, 136 with 8) where rows of both tensors start on 16-byte boundaries and H allows it; N = 2 needs
+// rows on boundaries of two elements and an even H, N = 1 takes anything.
+template <int N> constexpr int kLookupAhead = N == 8 ? 4 : 8;         // groups that a thread has under way
+
 template <typename TW, typename TO, int N>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs a) {
+    constexpr int kAhead = kLookupAhead<N>;
     const long long t0 = (long long)blockIdx.x * a.rows_per_block;
     const unsigned rows = (unsigned)min((long long)a.rows_per_block, a.T - t0);
     const unsigned total = rows * (unsigned)a.groups;
-    for (unsigned i0 = threadIdx.x; i0 < total; i0 += kLookupThreads * kLookupAhead) {
-        long long id[kLookupAhead];
-        unsigned r[kLookupAhead], j[kLookupAhead];
-        float f[kLookupAhead][N];
+    for (unsigned i0 = threadIdx.x; i0 < total; i0 += kLookupThreads * kAhead) {
+        long long id[kAhead];
+        unsigned r[kAhead], j[kAhead];
+        float f[kAhead][N];
 #pragma unroll
-        for (int u = 0; u < kLookupAhead; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
             const unsigned i = i0 + u * kLookupThreads;
             r[u] = i / (unsigned)a.groups;
             j[u] = (i - r[u] * (unsigned)a.groups) * N;
             id[u] = i < total ? read_id(a.ids, a.ids64, t0 + r[u]) : -1;
         }
 #pragma unroll
-        for (int u = 0; u < kLookupAhead; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
             if (id[u] >= 0 && id[u] < a.V) {
                 load_vec<TW, N, false>(static_cast<const TW *>(a.table) + id[u] * a.ld_table + j[u], f[u]);
             } else {
@@ -55,7 +58,7 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs
             }
         }
 #pragma unroll
-        for (int u = 0; u < kLookupAhead; ++u) {
+        for (int u = 0; u < kAhead; ++u) {
             if (i0 + u * kLookupThreads >= total) break;
             if (id[u] >= 0 && id[u] < a.V) {
 #pragma unroll
@@ -297,9 +300,10 @@ __device__ __forceinline__ void finish_row(const GradArgs &a, unsigned v, int j,
     if (!a.add) {
         store_vec<TW, N>(p, f);
     } else if constexpr (sizeof(TW) == 4) {
-        if constexpr (N == 8) {
-            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]) : "memory");
-            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p + 4), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
+        if constexpr (N >= 4) {
+#pragma unroll
+            for (int k = 0; k < N; k += 4)
+                asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p + k), "f"(f[k]), "f"(f[k + 1]), "f"(f[k + 2]), "f"(f[k + 3]) : "memory");
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k) atomicAdd(reinterpret_cast<float *>(p) + k, f[k]);
@@ -425,15 +429,14 @@ __global__ void __launch_bounds__(kReduceThreads, 4) embedding_reduce_kernel(con
     if (leaves && key[n - 1] < a.V) store_vec<float, N>(a.part + ((size_t)tile * 2 + (came ? 0 : 1)) * a.H + j, acc);
 }
 
-// A block looks through kJoinTiles tiles for long ids that start in one of them and adds such an id's parts over 32 N
-// columns: a warp where there are up to kFewParts of them, else all warps together, each a stretch of the parts.
+// A block looks through kJoinTiles tiles for long ids that start in one of them and adds each one's parts over 32 N columns,
+// several ids side by side: its warps are dealt out among them, and a warp takes every so manieth part.
 constexpr int kJoinTiles = 32;
-constexpr int kFewParts = 8;
 constexpr int kJoinThreads = 256;
 constexpr int kJoinWarps = kJoinThreads / 32;
 
 template <typename TW, int N>
-__global__ void __launch_bounds__(kJoinThreads, 4) embedding_join_kernel(const GradArgs a) {
+__global__ void __launch_bounds__(kJoinThreads, 3) embedding_join_kernel(const GradArgs a) {
     __shared__ float s_sum[kJoinWarps][32 * N];
     wait_for_previous();
     const unsigned *key = (a.passes & 1) ? a.key1 : a.key0;
@@ -447,67 +450,52 @@ __global__ void __launch_bounds__(kJoinThreads, 4) embedding_join_kernel(const G
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int j = (block_y * 32 + lane) * N;
     const bool in = j < a.H;
-    const int mine = block_x * kJoinTiles + lane;         // every warp looks at the same tiles
+    const int mine = block_x * kJoinTiles + lane;            // every warp looks at the same tiles
     auto first_key = [&](long long tile) {                   // of a tile; V + 1 past the last
         return tile < a.tiles ? __ldcg(key + tile * a.tile) : a.V + 1;
     };
     unsigned v = a.V + 1;
-    bool starts = false, many = false;                       // a long id starts in this lane's tile; it has over kFewParts parts
-    if (mine + 2 < a.tiles) {                                // it reaches the tile after the next
+    bool starts = false;                                     // a long id starts in this lane's tile: it reaches the tile after the next
+    if (mine + 2 < a.tiles) {
         v = first_key(mine + 1);
         const unsigned i0 = (unsigned)mine * a.tile, last = __ldcg(key + i0 + a.tile - 1), before = i0 ? __ldcg(key + i0 - 1) : a.V + 1;
-        const unsigned after_next = first_key((long long)mine + 2), far = first_key((long long)mine + kFewParts);
-        starts = v < a.V && last == v && before != v && after_next == v;
-        many = starts && far == v;
+        starts = v < a.V && last == v && before != v && first_key((long long)mine + 2) == v;
     }
-    // sum of parts p0 .. p1 - 1 of the id that starts in `tile` (part 0 is that tile's)
-    auto add_parts = [&](int tile, int p0, int p1, float (&acc)[N]) {
+    const unsigned found = __ballot_sync(0xffffffffu, starts);
+    for (int done = 0; done < __popc(found); done += kJoinWarps) {
+        const int ids = min(__popc(found) - done, kJoinWarps), share = ids > 4 ? 1 : ids > 2 ? 2 : ids > 1 ? 4 : 8;   // warps an id
+        const int mine_of = warp / share, sub = warp % share;
+        const bool busy = mine_of < ids;
+        unsigned id = a.V;
+        float acc[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) acc[k] = 0.f;
-#pragma unroll 4
-        for (int p = p0; p < p1; ++p) {
-            float f[N];
-            load_vec<float, N>(a.part + ((size_t)(tile + p) * 2 + (p == 0 ? 1 : 0)) * a.H + j, f);
+        if (busy) {
+            const int from = (int)__fns(found, 0, done + mine_of + 1), tile = block_x * kJoinTiles + from;
+            id = __shfl_sync(0xffffffffu, v, from);
+            for (int p0 = sub;; p0 += 32 * share) {          // parts p0, p0 + share, ...: as many as begin with the id
+                const int p = p0 + share * lane;
+                const int count = __popc(__ballot_sync(0xffffffffu, p == 0 || first_key((long long)tile + p) == id));
+                if (in) {
+#pragma unroll 8
+                    for (int q = 0; q < count; ++q) {
+                        float f[N];
+                        const int part = p0 + share * q;
+                        load_vec<float, N>(a.part + ((size_t)(tile + part) * 2 + (part == 0 ? 1 : 0)) * a.H + j, f);
 #pragma unroll
-            for (int k = 0; k < N; ++k) acc[k] += f[k];
-        }
-    };
-    int turn = 0;
-    for (unsigned todo = __ballot_sync(0xffffffffu, starts && !many); todo; todo &= todo - 1, ++turn) {
-        if (turn % kJoinWarps != warp) continue;
-        const int from = __ffs(todo) - 1, tile = block_x * kJoinTiles + from;
-        const unsigned id = __shfl_sync(0xffffffffu, v, from);
-        const int parts = __popc(__ballot_sync(0xffffffffu, lane < kFewParts && (lane == 0 || first_key((long long)tile + lane) == id)));
-        float acc[N];
-        if (in) {
-            add_parts(tile, 0, parts, acc);
-            finish_row<TW, N>(a, id, j, acc);
-        }
-    }
-    for (unsigned todo = __ballot_sync(0xffffffffu, many); todo; todo &= todo - 1) {
-        const int from = __ffs(todo) - 1, tile = block_x * kJoinTiles + from;
-        const unsigned id = __shfl_sync(0xffffffffu, v, from);
-        // tile lo begins with the id; the first tile that does not is in (lo, hi].  Two looks for up to 256 parts
-        int lo = tile + kFewParts, hi = a.tiles;
-        for (int step = 8; hi - lo > 1; step = (hi - lo + 32) / 33) {
-            const long long t = lo + (long long)step * (lane + 1);
-            const int steps = __popc(__ballot_sync(0xffffffffu, t < hi && first_key(t) == id));   // sorted: the lanes that match come first
-            if (steps < 32) hi = (int)min((long long)hi, lo + (long long)step * (steps + 1));
-            lo += step * steps;
-        }
-        const int parts = lo - tile + 1, each = (parts + kJoinWarps - 1) / kJoinWarps;
-        const int p0 = min(warp * each, parts), p1 = min(p0 + each, parts);
-        float acc[N];
-        if (in) {
-            add_parts(tile, p0, p1, acc);
+                        for (int k = 0; k < N; ++k) acc[k] += f[k];
+                    }
+                }
+                if (count < 32) break;
+            }
 #pragma unroll
             for (int k = 0; k < N; ++k) s_sum[warp][k * 32 + lane] = acc[k];
         }
         __syncthreads();
-        if (warp == 0 && in) {
-            for (int w = 1; w < kJoinWarps; ++w) {
+        if (busy && sub == 0 && in) {
+            for (int w = 1; w < share; ++w) {
 #pragma unroll
-                for (int k = 0; k < N; ++k) acc[k] += s_sum[w][k * 32 + lane];
+                for (int k = 0; k < N; ++k) acc[k] += s_sum[warp + w][k * 32 + lane];
             }
             finish_row<TW, N>(a, id, j, acc);
         }
@@ -522,18 +510,20 @@ __global__ void __launch_bounds__(kJoinThreads, 4) embedding_join_kernel(const G
 // the parts that the others leave in shared memory.  The other blocks write zeros to the rows of ids that do not occur.
 
 constexpr int kFewTokens = 512;
-constexpr int kFewThreads = 512;
+constexpr int kFewThreads = 1024;
 constexpr int kFewWarps = kFewThreads / 32;
 
 template <typename TG, typename TW, int N>
 __global__ void __launch_bounds__(kFewThreads) embedding_few_kernel(const GradArgs a) {
-    __shared__ unsigned s_id[kFewTokens], s_key[kFewTokens + 2], s_pos[kFewTokens];
+    __shared__ __align__(16) unsigned s_id[kFewTokens];
+    __shared__ unsigned s_key[kFewTokens + 2], s_pos[kFewTokens];
     __shared__ float s_part[kFewWarps][32 * N];              // sum of the id that a warp's stretch begins with, if it came in
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const unsigned T = a.T;
     const int column_blocks = (int)gridDim.x - a.zero_blocks;
     unsigned mine = a.V;
-    if ((unsigned)tid < T) s_id[tid] = mine = token_key(a, tid);
+    if ((unsigned)tid < T) mine = token_key(a, tid);
+    if (tid < kFewTokens) s_id[tid] = (unsigned)tid < T ? mine : 0xffffffffu;     // past the end: above every key
     if (tid == 0) { s_key[0] = a.V + 1; s_key[T + 1] = a.V + 1; }
     __syncthreads();
     if ((int)blockIdx.x >= column_blocks) {
@@ -553,12 +543,29 @@ __global__ void __launch_bounds__(kFewThreads) embedding_few_kernel(const GradAr
         }
         return;
     }
-    unsigned place = 0;
-    if ((unsigned)tid < T) {
-#pragma unroll 8
-        for (unsigned i = 0; i < T; ++i) place += s_id[i] < mine || (s_id[i] == mine && i < (unsigned)tid);
-        s_key[place + 1] = mine;
-        s_pos[place] = tid;
+    if (warp * 32 < (int)T) {
+        // tokens before this warp's count if their id is not above, those after it if it is below; the warp's own by position
+        unsigned place = 0;
+        const uint4 *ids4 = reinterpret_cast<const uint4 *>(s_id);
+#pragma unroll 4
+        for (int i = 0; i < warp * 8; ++i) {
+            const uint4 u = ids4[i];
+            place += (u.x <= mine) + (u.y <= mine) + (u.z <= mine) + (u.w <= mine);
+        }
+#pragma unroll 4
+        for (int i = warp * 8 + 8; i < ((int)T + 3) / 4; ++i) {
+            const uint4 u = ids4[i];
+            place += (u.x < mine) + (u.y < mine) + (u.z < mine) + (u.w < mine);
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const unsigned u = __shfl_sync(0xffffffffu, mine, i);
+            place += (i < lane ? u <= mine : u < mine) && warp * 32 + i < (int)T;
+        }
+        if ((unsigned)tid < T) {
+            s_key[place + 1] = mine;
+            s_pos[place] = tid;
+        }
     }
     __syncthreads();
     const unsigned *key = s_key + 1;                         // key[-1] .. key[T]
@@ -566,22 +573,22 @@ __global__ void __launch_bounds__(kFewThreads) embedding_few_kernel(const GradAr
     const unsigned from = min(warp * each, T), to = min(from + each, T);
     const int j = (blockIdx.x * 32 + lane) * N;
     const bool in = j < a.H;
-    constexpr int kAhead = 8;
+    constexpr int kAhead = N * sizeof(TG) == 32 ? 4 : 8;
     float acc[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) acc[k] = 0.f;
     bool open = from < to && from > 0 && key[from] == key[(int)from - 1];
     for (unsigned i = from; i < to; i += kAhead) {
-        float f[kAhead][N];
+        Stored<TG, N> f[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (in && i + u < to && key[i + u] < a.V) load_vec<TG, N>(static_cast<const TG *>(a.dout) + (long long)s_pos[i + u] * a.ld_dout + j, f[u]);
+            if (in && i + u < to && key[i + u] < a.V) f[u] = load_stored<TG, N>(static_cast<const TG *>(a.dout) + (long long)s_pos[i + u] * a.ld_dout + j);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (i + u >= to || key[i + u] >= a.V) break;
             if (in) {
 #pragma unroll
-                for (int k = 0; k < N; ++k) acc[k] += f[u][k];
+                for (int k = 0; k < N; ++k) acc[k] += element_of<N>(f[u], k);
             }
             const bool ends = key[i + u] != key[i + u + 1];
             if ((ends || i + u + 1 == to) && open) {         // (a part of) an id that came in

@@ -84,9 +84,9 @@ constexpr int64_t kMaxLd = (int64_t)1 << 40;
 
 // ---------------------------------------------------------------- embedding
 
-// Elements that a thread moves at a time (8, 2 or 1): what row starts and width allow in both matrices.
-int group_width(int H, const void *p, int64_t ldp, int tp, const void *q, int64_t ldq, int tq) {
-    for (const int n : {8, 2}) {
+// Elements that a thread moves at a time: `wide` (16 bytes of a type), 2 or 1, as row starts and width of both matrices allow.
+int group_width(int H, int wide, const void *p, int64_t ldp, int tp, const void *q, int64_t ldq, int tq) {
+    for (const int n : {wide, 2}) {
         auto fits = [&](const void *x, int64_t ld, int type) {
             const size_t boundary = n * type_bytes(type) < 16 ? n * type_bytes(type) : 16;
             return aligned_to(x, boundary) && (size_t)ld * type_bytes(type) % boundary == 0;
@@ -99,15 +99,16 @@ int group_width(int H, const void *p, int64_t ldp, int tp, const void *q, int64_
 template <typename TW, typename TO>
 int launch_lookup(LookupArgs a, int n, cudaStream_t s) {
     a.groups = a.H / n;
-    // two rounds of kLookupAhead groups a thread, at least one row a block
-    long long rows = (2LL * kLookupAhead * kLookupThreads) / a.groups;
+    // two rounds of a thread's groups, at least one row a block
+    long long rows = (2LL * (n == 8 ? kLookupAhead<8> : kLookupAhead<4>) * kLookupThreads) / a.groups;
     if (rows < 1) rows = 1;
     // short lookups: fewer rows a block, so that more blocks share the work
     while (rows > 1 && (a.T + rows - 1) / rows < 592) rows = (rows + 1) / 2;
     a.rows_per_block = (unsigned)rows;
     const long long grid = (a.T + rows - 1) / rows;
     if (grid > INT_MAX) return DPPF_ERR_INVALID_ARG;
-    if (n == 8) lookup_kernel<TW, TO, 8><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
+    constexpr int kWide = 16 / sizeof(TO);
+    if (n == kWide) lookup_kernel<TW, TO, kWide><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
     else if (n == 2) lookup_kernel<TW, TO, 2><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
     else lookup_kernel<TW, TO, 1><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
     return launched();
@@ -201,7 +202,8 @@ int launch_grad(GradArgs a, int dev, int sms, cudaStream_t s) {
 }
 template <typename TG, typename TW>
 int launch_grad_width(const GradArgs &a, int n, int dev, int sms, cudaStream_t s) {
-    return n == 8 ? launch_grad<TG, TW, 8>(a, dev, sms, s) : n == 2 ? launch_grad<TG, TW, 2>(a, dev, sms, s) : launch_grad<TG, TW, 1>(a, dev, sms, s);
+    constexpr int kWide = 16 / sizeof(TG);
+    return n == kWide ? launch_grad<TG, TW, kWide>(a, dev, sms, s) : n == 2 ? launch_grad<TG, TW, 2>(a, dev, sms, s) : launch_grad<TG, TW, 1>(a, dev, sms, s);
 }
 
 // ---------------------------------------------------------------- policy loss
@@ -361,7 +363,7 @@ int dppf_embedding(const void *table, int table_type, int64_t V, int H, int64_t 
     a.table = table; a.ids = ids; a.out = out;
     a.ld_table = ld_table; a.ld_out = ld_out; a.T = T; a.V = V; a.H = H; a.ids64 = id_bits == 64;
     a.scale = scale;
-    const int n = group_width(H, table, ld_table, table_type, out, ld_out, out_type);
+    const int n = group_width(H, out_type == DPPF_BFLOAT16 ? 8 : 4, table, ld_table, table_type, out, ld_out, out_type);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     if (table_type == DPPF_FLOAT32) return out_type == DPPF_FLOAT32 ? launch_lookup<float, float>(a, n, s) : launch_lookup<float, bf16>(a, n, s);
     return out_type == DPPF_FLOAT32 ? launch_lookup<bf16, float>(a, n, s) : launch_lookup<bf16, bf16>(a, n, s);
@@ -419,7 +421,7 @@ int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, cons
     a.bits = (bits + a.passes - 1) / a.passes;
     a.zero_vec = rows_on_16(grad_table, ld_table, table_type) && (size_t)H * type_bytes(table_type) % 16 == 0;
     a.tile = l.tile; a.tiles = l.tiles;
-    const int n = group_width(H, grad_out, ld_out, out_type, grad_table, ld_table, table_type);
+    const int n = group_width(H, out_type == DPPF_BFLOAT16 ? 8 : 4, grad_out, ld_out, out_type, grad_table, ld_table, table_type);
     if (out_type == DPPF_FLOAT32)
         return table_type == DPPF_FLOAT32 ? launch_grad_width<float, float>(a, n, dev, sms, s) : launch_grad_width<float, bf16>(a, n, dev, sms, s);
     return table_type == DPPF_FLOAT32 ? launch_grad_width<bf16, float>(a, n, dev, sms, s) : launch_grad_width<bf16, bf16>(a, n, dev, sms, s);
