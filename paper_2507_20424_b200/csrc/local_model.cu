@@ -214,18 +214,22 @@ constexpr int kPolicySliceMax = 200 * 1024;        // shared memory of one block
 // of 32 KB: 342 us; 256 threads instead of 128 in slices of 64 KB: 359 us, of 32 KB: 424 us.
 constexpr int kPolicySliceGood = 54 * 1024;
 
+// Rows up to this size go to blocks of 64 threads: 8,000 x 8,192 bf16 30 us (128 threads: 34), 10,000 x 4,096 21 (26); of 32 KB
+// rows 128 threads are quicker (8,000 x 16,384: 52 us, 57).
+constexpr int kPolicyShortSlice = 24 * 1024;
+
 std::atomic<int> g_policy_ready[2][kMaxDevices];
 
 template <typename T>
 int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     std::atomic<int> *ready = g_policy_ready[sizeof(T) == 4 ? 0 : 1];
-    if (!allow_smem(policy_kernel<T>, dev, ready, kPolicySliceMax)) return DPPF_ERR_CUDA;
+    if (!allow_smem(policy_kernel<T, kPolicyThreads>, dev, ready, kPolicySliceMax)) return DPPF_ERR_CUDA;
     const int sms = multiprocessors(dev);
     if (sms < 0) return DPPF_ERR_CUDA;
     // 16-byte vectors that a row spans: one more if rows may start inside one
     const int vectors = (int)(((size_t)a.V * sizeof(T) + 15) / 16) + (rows_on_16(a.logits, a.ld, sizeof(T) == 4 ? DPPF_FLOAT32 : DPPF_BFLOAT16) ? 0 : 1);
     if (vectors <= 8 * 32) {
-        auto kernel = vectors <= 4 * 32 ? policy_short_kernel<T, 4> : policy_short_kernel<T, 8>;
+        auto kernel = vectors <= 2 * 32 ? policy_short_kernel<T, 2> : vectors <= 4 * 32 ? policy_short_kernel<T, 4> : policy_short_kernel<T, 8>;
         const long long blocks = ((long long)a.T + kShortThreads / 32 - 1) / (kShortThreads / 32), most = 16LL * sms;
         kernel<<<(unsigned)(blocks < most ? blocks : most), kShortThreads, 0, s>>>(a);
         if (cudaPeekAtLastError() != cudaSuccess || !launch_after(policy_finish_kernel, dim3(3), kFinishThreads, 0, s, a)) { cudaGetLastError(); return DPPF_ERR_CUDA; }
@@ -238,13 +242,15 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     while (C < kPolicyMaxCluster && (long long)a.T * C < 2LL * sms && slice_bytes(C) > 16 * 1024) C *= 2;
     a.slice = (vectors + C - 1) / C;
     // a slice in four chunks, in whole rounds of the block's threads; a longer one goes through the ring if it is not kept
-    a.chunk = (a.slice + kPolicyChunks * kPolicyThreads - 1) / (kPolicyChunks * kPolicyThreads) * kPolicyThreads;
+    const bool shorter = C == 1 && a.slice * 16 <= kPolicyShortSlice;
+    const int threads = shorter ? kPolicyShortThreads : kPolicyThreads;
+    a.chunk = (a.slice + kPolicyChunks * threads - 1) / (kPolicyChunks * threads) * threads;
     if (!a.grad && a.chunk > kPolicyRing) a.chunk = kPolicyRing;
     const int held = a.slice < kPolicyChunks * a.chunk ? a.slice : kPolicyChunks * a.chunk;
     if (held * 16 > kPolicySliceMax) return DPPF_ERR_INVALID_ARG;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.T * (unsigned)C);
-    cfg.blockDim = dim3(kPolicyThreads);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)held * 16;
     cfg.stream = s;
     cudaLaunchAttribute attr;
@@ -252,8 +258,8 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     attr.val.clusterDim.x = (unsigned)C;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, policy_kernel<T>, a) != cudaSuccess || !launch_after(policy_finish_kernel, dim3(3), kFinishThreads, 0, s, a)) {
+    cfg.numAttrs = C > 1 ? 1 : 0;                                // a cluster of one starts slower than a plain block
+    if (cudaLaunchKernelEx(&cfg, shorter ? policy_kernel<T, kPolicyShortThreads> : policy_kernel<T, kPolicyThreads>, a) != cudaSuccess || !launch_after(policy_finish_kernel, dim3(3), kFinishThreads, 0, s, a)) {
         cudaGetLastError();
         return DPPF_ERR_CUDA;
     }

@@ -18,8 +18,7 @@ namespace {
 // type's lowest value, and -inf entries, need no special case.  The rows' terms are summed by a second launch, in a
 // fixed order (a counter of finished rows cost each block a fence: 381 us against 359 for 4,096 x 131,072).
 
-constexpr int kPolicyThreads = 128;
-constexpr int kPolicyWarps = kPolicyThreads / 32;
+constexpr int kPolicyThreads = 128, kPolicyShortThreads = 64;   // ... for rows whose blocks would not fill an SM by their memory
 constexpr int kPolicyChunks = 4;                 // buffers, and copies of a slice that is kept
 constexpr int kPolicyRing = 512;                 // vectors of a buffer of the ring
 constexpr int kPolicyMaxCluster = 8;
@@ -81,12 +80,12 @@ __device__ __forceinline__ void merge(float &m, float &s, float m2, float s2, fl
 }
 
 // Running maximum m and sum s = sum 2^((x - m) k) of a thread, over G vectors at once.
-template <typename T, int G>
+template <typename T, int G, int kThreads>
 __device__ __forceinline__ void take(const uint4 *v, float k, float &m, float &s) {
     constexpr int kPairs = Vec16<T>::N / 2 * G;
     float2 x[kPairs];
 #pragma unroll
-    for (int i = 0; i < G; ++i) Vec16<T>::get(v[i * kPolicyThreads], x + i * (Vec16<T>::N / 2));
+    for (int i = 0; i < G; ++i) Vec16<T>::get(v[i * kThreads], x + i * (Vec16<T>::N / 2));
     float top = m;
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) top = fmaxf(fmaxf(top, x[i].x), x[i].y);
@@ -125,7 +124,6 @@ __device__ __forceinline__ void warp_merge(float &m, float &s, float k) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
 }
-static_assert(kPolicyMaxCluster * kPolicyWarps <= 32, "a warp merges the pairs of all warps of a cluster");
 
 struct RowTerms { float lp, loss, kl, slope; bool clipped; };     // slope: dL/dlp
 
@@ -179,12 +177,13 @@ __global__ void __launch_bounds__(kFinishThreads) policy_finish_kernel(const Pol
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs a) {
-    constexpr int N = Vec16<T>::N, kTake = 4;
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
+    constexpr int N = Vec16<T>::N, kTake = 4, kWarps = kThreads / 32;
+    static_assert(kPolicyMaxCluster * kWarps <= 32, "a warp merges the pairs of all warps of a cluster");
     extern __shared__ __align__(128) uint4 s_row[];              // this block's slice, as aligned in the row, or the ring
     __shared__ unsigned long long s_bar[kPolicyChunks];
-    __shared__ float2 s_stats[kPolicyMaxCluster * kPolicyWarps]; // one entry from each warp of the cluster
+    __shared__ float2 s_stats[kPolicyMaxCluster * kWarps]; // one entry from each warp of the cluster
     __shared__ int s_failed;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -242,8 +241,8 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
                 const uint4 *v = s_row + (c % kPolicyChunks) * per - (size_t)c * per;                     // v[i]: vector i of the slice
                 const int stop = min(hi, (c + 1) * per);
                 int i = max(lo, c * per) + tid;
-                for (; i + (kTake - 1) * kPolicyThreads < stop; i += kTake * kPolicyThreads) take<T, kTake>(v + i, k, m, s);
-                for (; i < stop; i += kPolicyThreads) take<T, 1>(v + i, k, m, s);
+                for (; i + (kTake - 1) * kThreads < stop; i += kTake * kThreads) take<T, kTake, kThreads>(v + i, k, m, s);
+                for (; i < stop; i += kThreads) take<T, 1, kThreads>(v + i, k, m, s);
                 // the row's ends, element by element
                 const T *ve = reinterpret_cast<const T *>(v) + before - v0 * N;
                 if (c == 0 && tid < head - e_first) merge(m, s, to_float(ve[e_first + tid]), 1.f, k);
@@ -262,15 +261,15 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
         warp_merge(m, s, k);
         if (C > 1) {                                              // every warp's pair goes to every block of the cluster
             cluster_wait();                                       // the other blocks have started
-            if (lane < C) cluster_store2(cluster_map(&s_stats[rank * kPolicyWarps + warp], lane), m, s);
+            if (lane < C) cluster_store2(cluster_map(&s_stats[rank * kWarps + warp], lane), m, s);
             cluster_arrive();
             cluster_wait();
         } else {
             if (lane == 0) s_stats[warp] = make_float2(m, s);
             __syncthreads();
         }
-        m = lane < C * kPolicyWarps ? s_stats[lane].x : -FLT_MAX;
-        s = lane < C * kPolicyWarps ? s_stats[lane].y : 0.f;
+        m = lane < C * kWarps ? s_stats[lane].x : -FLT_MAX;
+        s = lane < C * kWarps ? s_stats[lane].y : 0.f;
         warp_merge(m, s, k);                                      // the same bits in every warp
 
         const RowTerms r = row_terms(a, (xy - m) * a.inv_t - logf(s), old, ref, A);
@@ -285,13 +284,13 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
             if (same) {
                 uint4 *out = reinterpret_cast<uint4 *>(gv);
 #pragma unroll 4
-                for (int i = lo + tid; i < hi; i += kPolicyThreads) __stcs(out + i, slope_vector<T>(s_row[i], k, m, cn));
+                for (int i = lo + tid; i < hi; i += kThreads) __stcs(out + i, slope_vector<T>(s_row[i], k, m, cn));
                 if (tid < head - e_first) entry(e_first + tid);
                 else if (tid >= 32 && tid - 32 < e_last - tail) entry(tail + tid - 32);
                 const int at = (int)y + before - v0 * N;          // the target's place in the slice: written over by the
-                if (at >= lo * N && at < hi * N && (at / N - lo) % kPolicyThreads == tid) entry((int)y);   // thread that wrote its vector
+                if (at >= lo * N && at < hi * N && (at / N - lo) % kThreads == tid) entry((int)y);   // thread that wrote its vector
             } else {
-                for (int e = e_first + tid; e < e_last; e += kPolicyThreads) entry(e);
+                for (int e = e_first + tid; e < e_last; e += kThreads) entry(e);
             }
         }
         if (s_failed && tid == 0)                                 // copies still under way land before the block leaves
@@ -302,12 +301,12 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
             const T zero = from_float<T>(0.f);
             if (same) {
                 uint4 *out = reinterpret_cast<uint4 *>(gv);
-                for (int i = lo + tid; i < hi; i += kPolicyThreads) __stcs(out + i, make_uint4(0, 0, 0, 0));
+                for (int i = lo + tid; i < hi; i += kThreads) __stcs(out + i, make_uint4(0, 0, 0, 0));
                 const int head = min((lo + v0) * N - before, e_last), tail = max((hi + v0) * N - before, head);
                 if (tid < head - e_first) g[e_first + tid] = zero;
                 else if (tid >= 32 && tid - 32 < e_last - tail) g[tail + tid - 32] = zero;
             } else {
-                for (int e = e_first + tid; e < e_last; e += kPolicyThreads) g[e] = zero;
+                for (int e = e_first + tid; e < e_last; e += kThreads) g[e] = zero;
             }
         }
     }
@@ -320,16 +319,24 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_kernel(const PolicyArgs
 constexpr int kShortThreads = 128;
 
 template <typename T, int kHold>
-__global__ void __launch_bounds__(kShortThreads) policy_short_kernel(const PolicyArgs a) {
+__global__ void __launch_bounds__(kShortThreads, kHold == 8 ? 4 : 8) policy_short_kernel(const PolicyArgs a) {
     constexpr int N = Vec16<T>::N, kPairs = N / 2;
     const int lane = threadIdx.x & 31;
     const float k = a.log2e_t;
-    for (long long row_l = (long long)blockIdx.x * (kShortThreads / 32) + (threadIdx.x >> 5); row_l < a.T; row_l += (long long)gridDim.x * (kShortThreads / 32)) {
+    const long long stride = (long long)gridDim.x * (kShortThreads / 32);
+    long long row_l = (long long)blockIdx.x * (kShortThreads / 32) + (threadIdx.x >> 5);
+    float w_next = row_l < a.T ? __ldg(a.weight + row_l) : 0.f;
+    long long y_next = row_l < a.T ? target_of(a, (int)row_l) : -1;
+    for (; row_l < a.T; row_l += stride) {
         const int row = (int)row_l;
+        const float w = w_next;
+        const long long y = y_next;
+        if (row_l + stride < a.T) {                               // the next row's, ahead of this one's work
+            w_next = __ldg(a.weight + row_l + stride);
+            y_next = target_of(a, (int)(row_l + stride));
+        }
         const T *x = static_cast<const T *>(a.logits) + (long long)row * a.ld;
         T *g = static_cast<T *>(a.grad) + (long long)row * a.ld_grad;
-        const float w = __ldg(a.weight + row);
-        const long long y = target_of(a, row);
         const bool live = w != 0.f && y >= 0 && y < a.V;
         const int before = (int)((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T)), vectors = (before + a.V + N - 1) / N;
         const bool same = a.grad && ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(x)) & 15u) == 0;
