@@ -27,8 +27,8 @@ constexpr int kLookupThreads = 256;
 
 // A block takes rows_per_block rows; its threads walk the groups of those rows in memory order, kLookupAhead at a time.
 // N elements are 16 bytes of the output (16,384 rows of 1,024 from fp32 to bf16: 13.0 us with 8, 16.6 with 4; 26,214 of 5,120 from
-// bf16 to fp32: 117 us with 4, 136 with 8) where rows of both tensors start on 16-byte boundaries and H allows it; N = 2 needs
-// rows on boundaries of two elements and an even H, N = 1 takes anything.
+// bf16 to fp32: 117 us with 4, 136 with 8) where rows of both tensors start on 16-byte boundaries and H allows it; 4 and 2 need
+// rows on boundaries of so many elements and such an H, 1 takes anything.
 template <int N> constexpr int kLookupAhead = N == 8 ? 4 : 8;         // groups that a thread has under way
 
 template <typename TW, typename TO, int N>

@@ -84,9 +84,9 @@ constexpr int64_t kMaxLd = (int64_t)1 << 40;
 
 // ---------------------------------------------------------------- embedding
 
-// Elements that a thread moves at a time: `wide` (16 bytes of a type), 2 or 1, as row starts and width of both matrices allow.
+// Elements that a thread moves at a time: `wide` (16 bytes of a type), 4, 2 or 1, as row starts and width of both matrices allow.
 int group_width(int H, int wide, const void *p, int64_t ldp, int tp, const void *q, int64_t ldq, int tq) {
-    for (const int n : {wide, 2}) {
+    for (const int n : {wide, 4, 2}) {
         auto fits = [&](const void *x, int64_t ld, int type) {
             const size_t boundary = n * type_bytes(type) < 16 ? n * type_bytes(type) : 16;
             return aligned_to(x, boundary) && (size_t)ld * type_bytes(type) % boundary == 0;
@@ -109,6 +109,7 @@ int launch_lookup(LookupArgs a, int n, cudaStream_t s) {
     if (grid > INT_MAX) return DPPF_ERR_INVALID_ARG;
     constexpr int kWide = 16 / sizeof(TO);
     if (n == kWide) lookup_kernel<TW, TO, kWide><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
+    else if (n == 4) lookup_kernel<TW, TO, 4><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
     else if (n == 2) lookup_kernel<TW, TO, 2><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
     else lookup_kernel<TW, TO, 1><<<(unsigned)grid, kLookupThreads, 0, s>>>(a);
     return launched();
@@ -203,7 +204,7 @@ int launch_grad(GradArgs a, int dev, int sms, cudaStream_t s) {
 template <typename TG, typename TW>
 int launch_grad_width(const GradArgs &a, int n, int dev, int sms, cudaStream_t s) {
     constexpr int kWide = 16 / sizeof(TG);
-    return n == kWide ? launch_grad<TG, TW, kWide>(a, dev, sms, s) : n == 2 ? launch_grad<TG, TW, 2>(a, dev, sms, s) : launch_grad<TG, TW, 1>(a, dev, sms, s);
+    return n == kWide ? launch_grad<TG, TW, kWide>(a, dev, sms, s) : n == 4 ? launch_grad<TG, TW, 4>(a, dev, sms, s) : n == 2 ? launch_grad<TG, TW, 2>(a, dev, sms, s) : launch_grad<TG, TW, 1>(a, dev, sms, s);
 }
 
 // ---------------------------------------------------------------- policy loss
@@ -238,8 +239,10 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     int C = 1;
     auto slice_bytes = [&](int c) { return (vectors + c - 1) / c * 16; };
     while (a.grad && C < kPolicyMaxCluster && slice_bytes(C) > kPolicySliceGood) C *= 2;
-    // few rows: split them further while SMs are idle and a slice stays above 8 KB
-    while (C < kPolicyMaxCluster && (long long)a.T * C < 2LL * sms && slice_bytes(C) > 16 * 1024) C *= 2;
+    // few rows: split them further while SMs are idle and a slice stays above 8 KB; rows that are only read also while
+    // there are fewer than 8 blocks an SM and a slice stays above 16 KB (388 x 187,236 bf16: 37 us, 41 with 2)
+    while (C < kPolicyMaxCluster && (((long long)a.T * C < 2LL * sms && slice_bytes(C) > 16 * 1024) ||
+                                     (!a.grad && (long long)a.T * C < 8LL * sms && slice_bytes(C) > 32 * 1024))) C *= 2;
     a.slice = (vectors + C - 1) / C;
     // a slice in four chunks, in whole rounds of the block's threads; a longer one goes through the ring if it is not kept
     const bool shorter = C == 1 && a.slice * 16 <= kPolicyShortSlice;
