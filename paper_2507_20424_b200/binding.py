@@ -404,7 +404,7 @@ def _matrix(t: torch.Tensor, what: str):
     if t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{what} must be a 2-D CUDA tensor with unit column stride")
     rows, cols = t.shape
-    return rows, cols, (t.stride(0) if rows > 1 else cols)
+    return rows, cols, (t.stride(0) if rows > 1 else cols)     # the stride of a single row says nothing
 
 
 def _vector(t: torch.Tensor, n: int, what: str, device, dtypes=(torch.float32,)) -> torch.Tensor:
@@ -428,15 +428,20 @@ def dppf_embedding(table, ids, scale=1.0, out=None, out_dtype=None):
     """Rows ``ids`` of ``table[V, H]`` times ``scale`` -> ``out[*ids.shape, H]`` (zeros where an id is
     outside [0, V)).  ``out_dtype`` (default: the table's) is used when ``out`` is not given."""
     V, H, ld = _matrix(table, "table")
-    ids = _vector(ids, ids.numel(), "ids", table.device, tuple(_ID_BITS))
+    dev = table.device
+    if ids.dtype not in _ID_BITS or ids.device != dev or not ids.is_contiguous():
+        _vector(ids, ids.numel(), "ids", dev, tuple(_ID_BITS))
+    T = ids.numel()
     if out is None:
-        out = table.new_empty((*ids.shape, H), dtype=out_dtype)
-    elif out.device != table.device or out.numel() != ids.numel() * H or out.shape[-1:] != (H,):
-        raise ValueError("out must hold one row of H columns per id, on the table's device")
-    flat = out if out.dim() == 2 else out.view(-1, H)
-    _, _, ld_out = _matrix(flat, "out")
-    _call(table.device, load().dppf_embedding, "dppf_embedding", table.data_ptr(), _type(table, "table"), V, H, ld, ids.data_ptr(), _ID_BITS[ids.dtype],
-          ids.numel(), scale, flat.data_ptr(), _type(flat, "out"), ld_out)
+        out = flat = table.new_empty((*ids.shape, H), dtype=out_dtype)
+        ld_out = H
+    else:
+        if out.device != dev or out.numel() != T * H or out.shape[-1:] != (H,):
+            raise ValueError("out must hold one row of H columns per id, on the table's device")
+        flat = out if out.dim() == 2 else out.view(-1, H)
+        _, _, ld_out = _matrix(flat, "out")
+    _call(dev, load().dppf_embedding, "dppf_embedding", table.data_ptr(), _type(table, "table"), V, H, ld, ids.data_ptr(), _ID_BITS[ids.dtype], T, scale,
+          flat.data_ptr(), _type(flat, "out"), ld_out)
     return out
 
 
@@ -491,21 +496,25 @@ def dppf_policy_loss(logits, targets, old_logp, advantage, weight, ref_logp=None
     gradient.  ``weight`` carries mask and normalisation; rows with weight 0 are not read."""
     T, V, ld = _matrix(logits, "logits")
     dev, code = logits.device, _type(logits, "logits")
-    targets = _vector(targets, T, "targets", dev, tuple(_ID_BITS))
-    for t, what in ((old_logp, "old_logp"), (advantage, "advantage"), (weight, "weight"), (ref_logp, "ref_logp")):
-        if t is not None:
-            _vector(t, T, what, dev)
-    ld_grad = 0
+    if targets.device != dev or targets.numel() != T or targets.dtype not in _ID_BITS or not targets.is_contiguous():
+        _vector(targets, T, "targets", dev, tuple(_ID_BITS))
+    for t in (old_logp, advantage, weight, ref_logp):             # quickly; _vector says what is wrong
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != T or t.device != dev or not t.is_contiguous()):
+            _vector(t, T, "old_logp, advantage, weight and ref_logp", dev)
+    ld_grad, grad_ptr = 0, None
     if grad_logits is not None:
         rows, cols, ld_grad = _matrix(grad_logits, "grad_logits")
-        if grad_logits.dtype != logits.dtype or grad_logits.device != dev or (rows, cols) != (T, V):
+        if grad_logits.dtype != logits.dtype or grad_logits.device != dev or rows != T or cols != V:
             raise ValueError("grad_logits must have the type, shape and device of logits")
-    ws = alloc_policy_workspace(T, dev) if ws is None else ws
+        grad_ptr = grad_logits.data_ptr()
+    if ws is None:
+        ws = alloc_policy_workspace(T, dev)
     out = logits.new_empty(3 + T, dtype=torch.float32)
-    sums, logp = out[:3], out[3:]
+    sums_ptr = out.data_ptr()
     _call(dev, load().dppf_policy_loss, "dppf_policy_loss", logits.data_ptr(), code, T, V, ld, targets.data_ptr(), _ID_BITS[targets.dtype], old_logp.data_ptr(),
-          _ptr(ref_logp), advantage.data_ptr(), weight.data_ptr(), clip_low, clip_high, kl_coef, temperature, sums.data_ptr(), logp.data_ptr(), _ptr(grad_logits),
-          ld_grad, ws.data_ptr(), ws.numel() * ws.element_size())
+          None if ref_logp is None else ref_logp.data_ptr(), advantage.data_ptr(), weight.data_ptr(), clip_low, clip_high, kl_coef, temperature, sums_ptr,
+          sums_ptr + 12, grad_ptr, ld_grad, ws.data_ptr(), ws.nbytes)
+    sums, logp = out.split_with_sizes((3, T))
     loss, kl, clipped = sums.unbind()
     return PolicyLoss(loss, kl, clipped, logp, ws)
 
