@@ -121,8 +121,7 @@ __device__ __forceinline__ unsigned cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-// ... by a thread that has written nothing the others are to see: no fence
+// Arrival of a thread that has written nothing the others are to see: no fence.
 __device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // Shared-memory address of the same variable in another block of the cluster.
@@ -131,13 +130,10 @@ __device__ __forceinline__ unsigned cluster_map(const void *p, unsigned rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
     return a;
 }
-__device__ __forceinline__ void cluster_store2(unsigned a, float x, float y) {
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(x), "f"(y) : "memory");
-}
-__device__ __forceinline__ unsigned cluster_load(unsigned a) {
-    unsigned v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
+// Asynchronous store of a pair to an address of the cluster's shared memory, counted (8 bytes) on the mbarrier `bar` of the
+// same block: who waits for that sees the pair, and no fence is needed.
+__device__ __forceinline__ void cluster_send2(unsigned a, float x, float y, unsigned bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(a), "f"(x), "f"(y), "r"(bar) : "memory");
 }
 
 // ---------------------------------------------------------------- launches that follow one another

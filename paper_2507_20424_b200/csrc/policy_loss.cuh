@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
     constexpr int N = Vec16<T>::N, kTake = 4, kWarps = kThreads / 32;
     static_assert(kPolicyMaxCluster * kWarps <= 32, "a warp merges the pairs of all warps of a cluster");
     extern __shared__ __align__(128) uint4 s_row[];              // this block's slice, as aligned in the row, or the ring
-    __shared__ unsigned long long s_bar[kPolicyChunks];
+    __shared__ unsigned long long s_bar[kPolicyChunks], s_told;  // s_told: the pairs of the cluster's warps
     __shared__ float2 s_stats[kPolicyMaxCluster * kWarps]; // one entry from each warp of the cluster
     __shared__ int s_failed;
 
@@ -194,6 +194,8 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
 
     if (tid == 0) {
         for (int c = 0; c < kPolicyChunks; ++c) mbar_init(&s_bar[c], 1);
+        mbar_init(&s_told, 1);
+        if (C > 1) mbar_expect_tx(&s_told, (unsigned)(C * kWarps * sizeof(float2)));
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_failed = 0;
     }
@@ -259,11 +261,12 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
             a.hdr->failed = 1;
         }
         warp_merge(m, s, k);
+        bool told = true;
         if (C > 1) {                                              // every warp's pair goes to every block of the cluster
             cluster_wait();                                       // the other blocks have started
-            if (lane < C) cluster_store2(cluster_map(&s_stats[rank * kWarps + warp], lane), m, s);
-            cluster_arrive();
-            cluster_wait();
+            if (lane < C) cluster_send2(cluster_map(&s_stats[rank * kWarps + warp], lane), m, s, cluster_map(&s_told, lane));
+            // a block stays until it has been told by all, so nobody writes to one that has left
+            told = mbar_wait_bounded(&s_told, 0, kSpinLimit);
         } else {
             if (lane == 0) s_stats[warp] = make_float2(m, s);
             __syncthreads();
@@ -271,6 +274,10 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
         m = lane < C * kWarps ? s_stats[lane].x : -FLT_MAX;
         s = lane < C * kWarps ? s_stats[lane].y : 0.f;
         warp_merge(m, s, k);                                      // the same bits in every warp
+        if (!told) {
+            s = __int_as_float(0x7fc00000);
+            a.hdr->failed = 1;
+        }
 
         const RowTerms r = row_terms(a, (xy - m) * a.inv_t - logf(s), old, ref, A);
         if (rank == 0 && tid == 0) put_terms(a, row, r.lp, w * r.loss, w * r.kl, r.clipped ? w : 0.f);
