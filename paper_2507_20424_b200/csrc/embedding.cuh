@@ -84,8 +84,7 @@ struct GradArgs {
     long long ld_dout, ld_dtable;   // elements
     int H, add;
     float scale;
-    // sorted tokens (workspace); the sort's result is in buffer passes & 1
-    unsigned *key0, *pos0, *key1, *pos1;
+    uint2 *order0, *order1;      // workspace: (key, token) in order; the sort's result is in buffer passes & 1
     unsigned *hist;              // [3][kSortBlocks][kBins]: a digit's counts, the next one's, the one's after that, in turn
     int passes, bits;            // digits and their width
     int sort_blocks;
@@ -175,22 +174,21 @@ __global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const Gra
     const int shift = pass * a.bits;
     const unsigned mask = (1u << a.bits) - 1u;
     const bool more = pass + 1 < a.passes;
-    const unsigned *key_in = (pass & 1) ? a.key1 : a.key0, *pos_in = (pass & 1) ? a.pos1 : a.pos0;
-    unsigned *key_out = (pass & 1) ? a.key0 : a.key1, *pos_out = (pass & 1) ? a.pos0 : a.pos1;
+    const uint2 *in_order = (pass & 1) ? a.order1 : a.order0;
+    uint2 *out_order = (pass & 1) ? a.order0 : a.order1;
     const unsigned *counts = counts_of(a, pass);
     unsigned *next_counts = counts_of(a, pass + 1);
     if (more && tid < kBins) counts_of(a, pass + 2)[(size_t)blockIdx.x * kBins + tid] = 0;
     const unsigned stretch = a.chunk / kSortWarps;            // a multiple of 32
     const unsigned long long from = (unsigned long long)blockIdx.x * a.chunk + (unsigned long long)warp * stretch;
     const unsigned i0 = (unsigned)min(from, (unsigned long long)a.T), i1 = (unsigned)min(from + stretch, (unsigned long long)a.T);
-    auto key_at = [&](unsigned i) { return pass == 0 ? token_key(a, i) : __ldcg(key_in + i); };
-    auto pos_at = [&](unsigned i) { return pass == 0 ? i : __ldcg(pos_in + i); };
+    auto element = [&](unsigned i) { return pass == 0 ? make_uint2(token_key(a, i), i) : __ldcg(in_order + i); };   // (key, token)
 
-    unsigned key[kSortHold], pos[kSortHold];                  // of the first elements of the stretch
+    uint2 held[kSortHold];                                    // the first elements of the stretch
 #pragma unroll
     for (int u = 0; u < kSortHold; ++u) {
         const unsigned i = i0 + u * 32 + lane;
-        if (i < i1) { key[u] = key_at(i); pos[u] = pos_at(i); }
+        held[u] = i < i1 ? element(i) : make_uint2(0, 0);
     }
     {                                                         // four digits a thread, the chunks in kCountGroups turns
         const int q = tid % (kBins / 4), turn = tid / (kBins / 4);
@@ -206,8 +204,8 @@ __global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const Gra
     }
 #pragma unroll
     for (int u = 0; u < kSortHold; ++u)
-        if (i0 + u * 32 + lane < i1) atomicAdd(&hist[(key[u] >> shift) & mask], 1u);
-    for (unsigned i = i0 + 32 * kSortHold + lane; i < i1; i += 32) atomicAdd(&hist[(key_at(i) >> shift) & mask], 1u);
+        if (i0 + u * 32 + lane < i1) atomicAdd(&hist[(held[u].x >> shift) & mask], 1u);
+    for (unsigned i = i0 + 32 * kSortHold + lane; i < i1; i += 32) atomicAdd(&hist[(element(i).x >> shift) & mask], 1u);
     __syncthreads();
     unsigned all = 0, first = 0;                              // elements of digit tid; where this block's begin
     if (tid < kBins) {
@@ -235,8 +233,8 @@ __global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const Gra
         }
     }
     __syncthreads();
-    auto place = [&](bool in, unsigned k, unsigned p) {
-        const unsigned digit = in ? (k >> shift) & mask : 0xffffffffu;
+    auto place = [&](bool in, uint2 e) {
+        const unsigned digit = in ? (e.x >> shift) & mask : 0xffffffffu;
         const unsigned peers = __match_any_sync(0xffffffffu, digit);
         unsigned at = 0;
         if (in) at = hist[digit] + __popc(peers & ((1u << lane) - 1u));
@@ -244,17 +242,16 @@ __global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const Gra
         if (in && lane == 31 - __clz(peers)) hist[digit] = at + 1;
         __syncwarp();
         if (in) {
-            __stcg(key_out + at, k);
-            __stcg(pos_out + at, p);
-            if (more) atomicAdd(next_counts + (size_t)(at / a.chunk) * kBins + ((k >> (shift + a.bits)) & mask), 1u);
+            __stcg(out_order + at, e);
+            if (more) atomicAdd(next_counts + (size_t)(at / a.chunk) * kBins + ((e.x >> (shift + a.bits)) & mask), 1u);
         }
     };
 #pragma unroll
     for (int u = 0; u < kSortHold; ++u)
-        if (i0 + u * 32 < i1) place(i0 + u * 32 + lane < i1, key[u], pos[u]);
+        if (i0 + u * 32 < i1) place(i0 + u * 32 + lane < i1, held[u]);
     for (unsigned i = i0 + 32 * kSortHold; i < i1; i += 32) {
         const bool in = i + lane < i1;
-        place(in, in ? key_at(i + lane) : 0u, in ? pos_at(i + lane) : 0u);
+        place(in, in ? element(i + lane) : make_uint2(0, 0));
     }
 }
 
@@ -321,12 +318,12 @@ __device__ __forceinline__ void finish_row(const GradArgs &a, unsigned v, int j,
 constexpr int kMaxZeroRows = 1024;
 
 // First place in the sorted keys that is not below v, by a warp, 33 stretches at a time.
-__device__ __forceinline__ unsigned lower_bound(const unsigned *key, unsigned T, long long v, int lane) {
+__device__ __forceinline__ unsigned lower_bound(const uint2 *order, unsigned T, long long v, int lane) {
     unsigned lo = 0, hi = T;                                 // places before lo are below v, places from hi on are not
     while (lo < hi) {
         const unsigned step = (hi - lo + 32) / 33;
         const unsigned long long at = (unsigned long long)lo + (unsigned long long)step * (lane + 1) - 1;
-        const int below = __popc(__ballot_sync(0xffffffffu, at < hi && (long long)__ldcg(key + (at < hi ? at : lo)) < v));
+        const int below = __popc(__ballot_sync(0xffffffffu, at < hi && (long long)__ldcg(&order[at < hi ? at : lo].x) < v));
         const unsigned end = (unsigned)min((unsigned long long)hi, (unsigned long long)lo + (unsigned long long)step * (below + 1) - 1);
         lo += step * below;
         hi = max(lo, end);
@@ -335,7 +332,7 @@ __device__ __forceinline__ unsigned lower_bound(const unsigned *key, unsigned T,
 }
 
 template <typename TW>
-__device__ __forceinline__ void zero_absent(const GradArgs &a, const unsigned *key, long long begin, long long end, int block, int blocks) {
+__device__ __forceinline__ void zero_absent(const GradArgs &a, const uint2 *order, long long begin, long long end, int block, int blocks) {
     __shared__ unsigned s_seen[kMaxZeroRows / 32], s_from, s_to;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int threads = blockDim.x;
@@ -343,12 +340,12 @@ __device__ __forceinline__ void zero_absent(const GradArgs &a, const unsigned *k
         const int rows = (int)min((long long)a.zero_rows, end - v0);
         if (tid < kMaxZeroRows / 32) s_seen[tid] = 0;
         if (warp < 2) {
-            const unsigned at = lower_bound(key, a.T, warp ? v0 + rows : v0, lane);
+            const unsigned at = lower_bound(order, a.T, warp ? v0 + rows : v0, lane);
             if (lane == 0) (warp ? s_to : s_from) = at;
         }
         __syncthreads();
         for (unsigned i = s_from + tid; i < s_to; i += threads) {
-            const int r = (int)(__ldcg(key + i) - v0);
+            const int r = (int)(__ldcg(&order[i].x) - v0);
             if (!((s_seen[r >> 5] >> (r & 31)) & 1u)) atomicOr(&s_seen[r >> 5], 1u << (r & 31));
         }
         __syncthreads();
@@ -368,22 +365,22 @@ __global__ void __launch_bounds__(kReduceThreads, 4) embedding_reduce_kernel(con
     // the blocks that write zeros are spread evenly among the others
     const long long zeros_before = (long long)blockIdx.x * a.zero_blocks / gridDim.x;
     if ((long long)(blockIdx.x + 1) * a.zero_blocks / gridDim.x > zeros_before) {
-        zero_absent<TW>(a, (a.passes & 1) ? a.key1 : a.key0, 0, (long long)a.V - a.early_rows - a.late_rows, (int)zeros_before, a.zero_blocks);
+        zero_absent<TW>(a, (a.passes & 1) ? a.order1 : a.order0, 0, (long long)a.V - a.early_rows - a.late_rows, (int)zeros_before, a.zero_blocks);
         return;
     }
     const int block = (int)(blockIdx.x - zeros_before), block_x = block % a.tile_blocks, block_y = block / a.tile_blocks;
     const int subs = kReduceThreads / a.row_threads;
     const int sub = threadIdx.x / a.row_threads, col = threadIdx.x - sub * a.row_threads;
-    const unsigned *key_in = (a.passes & 1) ? a.key1 : a.key0, *pos_in = (a.passes & 1) ? a.pos1 : a.pos0;
+    const uint2 *order = (a.passes & 1) ? a.order1 : a.order0;
     // keys of the places from one tile (and one) before this block's to one after it; V + 1 where there is none
     const int span = subs * a.tile;
     const long long base = (long long)block_x * span;
     for (int i = threadIdx.x; i < span + 2 * a.tile + 2; i += kReduceThreads) {
         const long long at = base + i - a.tile - 1;
-        s_key[i] = at >= 0 && at < (long long)a.T ? __ldcg(key_in + at) : a.V + 1;
+        const uint2 e = at >= 0 && at < (long long)a.T ? __ldcg(order + at) : make_uint2(a.V + 1, 0);
+        s_key[i] = e.x;
+        if (i > a.tile && i - a.tile - 1 < span + a.tile) s_pos[i - a.tile - 1] = e.y;
     }
-    for (int i = threadIdx.x; i < span + a.tile; i += kReduceThreads)
-        if (base + i < (long long)a.T) s_pos[i] = __ldcg(pos_in + base + i);
     __syncthreads();
     const int tile = block_x * subs + sub;
     const int grp = block_y * a.row_threads + col;
@@ -439,11 +436,11 @@ template <typename TW, int N>
 __global__ void __launch_bounds__(kJoinThreads, 3) embedding_join_kernel(const GradArgs a) {
     __shared__ float s_sum[kJoinWarps][32 * N];
     wait_for_previous();
-    const unsigned *key = (a.passes & 1) ? a.key1 : a.key0;
+    const uint2 *order = (a.passes & 1) ? a.order1 : a.order0;
     const int join_blocks = (int)gridDim.x - a.late_blocks;
     if ((int)blockIdx.x >= join_blocks) {
         const long long end = (long long)a.V - a.early_rows;
-        zero_absent<TW>(a, key, end - a.late_rows, end, (int)blockIdx.x - join_blocks, a.late_blocks);
+        zero_absent<TW>(a, order, end - a.late_rows, end, (int)blockIdx.x - join_blocks, a.late_blocks);
         return;
     }
     const int tile_groups = (a.tiles + kJoinTiles - 1) / kJoinTiles, block_x = blockIdx.x % tile_groups, block_y = blockIdx.x / tile_groups;
@@ -452,13 +449,13 @@ __global__ void __launch_bounds__(kJoinThreads, 3) embedding_join_kernel(const G
     const bool in = j < a.H;
     const int mine = block_x * kJoinTiles + lane;            // every warp looks at the same tiles
     auto first_key = [&](long long tile) {                   // of a tile; V + 1 past the last
-        return tile < a.tiles ? __ldcg(key + tile * a.tile) : a.V + 1;
+        return tile < a.tiles ? __ldcg(&order[tile * a.tile].x) : a.V + 1;
     };
     unsigned v = a.V + 1;
     bool starts = false;                                     // a long id starts in this lane's tile: it reaches the tile after the next
     if (mine + 2 < a.tiles) {
         v = first_key(mine + 1);
-        const unsigned i0 = (unsigned)mine * a.tile, last = __ldcg(key + i0 + a.tile - 1), before = i0 ? __ldcg(key + i0 - 1) : a.V + 1;
+        const unsigned i0 = (unsigned)mine * a.tile, last = __ldcg(&order[i0 + a.tile - 1].x), before = i0 ? __ldcg(&order[i0 - 1].x) : a.V + 1;
         starts = v < a.V && last == v && before != v && first_key((long long)mine + 2) == v;
     }
     const unsigned found = __ballot_sync(0xffffffffu, starts);

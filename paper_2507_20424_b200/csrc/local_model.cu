@@ -130,7 +130,7 @@ int reduce_tile(int64_t T, int H) {
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 struct EmbeddingLayout {
-    size_t key[2], pos[2], hist, part, total;
+    size_t order[2], hist, part, total;
     int tile, tiles;
 };
 EmbeddingLayout embedding_layout(int64_t T, int H) {
@@ -138,8 +138,7 @@ EmbeddingLayout embedding_layout(int64_t T, int H) {
     l.tile = reduce_tile(T, H);
     l.tiles = (int)((T + l.tile - 1) / l.tile);
     size_t at = 0;
-    const size_t words = round256((size_t)T * 4);
-    for (int i = 0; i < 2; ++i) { l.key[i] = at; at += words; l.pos[i] = at; at += words; }
+    for (int i = 0; i < 2; ++i) { l.order[i] = at; at += round256((size_t)T * sizeof(uint2)); }
     l.hist = at;
     at += (size_t)3 * kSortBlocks * kBins * 4;
     l.part = at;
@@ -211,9 +210,9 @@ int launch_grad_width(const GradArgs &a, int n, int dev, int sms, cudaStream_t s
 
 constexpr size_t kPolicyHeaderBytes = 256;
 constexpr int kPolicySliceMax = 200 * 1024;        // shared memory of one block's slice at most
-// Four blocks and more fit an SM: some load while others write.  4,096 x 131,072 bf16 in slices of 64 KB (three blocks): 352 us,
-// of 32 KB: 342 us; 256 threads instead of 128 in slices of 64 KB: 359 us, of 32 KB: 424 us.
-constexpr int kPolicySliceGood = 54 * 1024;
+// Six blocks and more fit an SM: some load while others write.  4,096 x 131,072 bf16 in slices of 32 KB: 317 us, of 64 KB:
+// 343 us; with 64 threads a block 350, with 96 344 (slices of 32 KB).
+constexpr int kPolicySliceGood = 36 * 1024;
 
 // Rows up to this size go to blocks of 64 threads: 8,000 x 8,192 bf16 30 us (128 threads: 34), 10,000 x 4,096 21 (26); of 32 KB
 // rows 128 threads are quicker (8,000 x 16,384: 52 us, 57).
@@ -418,10 +417,8 @@ int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, cons
     a.add = accumulate ? 1 : 0;
     a.scale = scale;
     unsigned char *base = static_cast<unsigned char *>(ws);
-    a.key0 = reinterpret_cast<unsigned *>(base + l.key[0]);
-    a.pos0 = reinterpret_cast<unsigned *>(base + l.pos[0]);
-    a.key1 = reinterpret_cast<unsigned *>(base + l.key[1]);
-    a.pos1 = reinterpret_cast<unsigned *>(base + l.pos[1]);
+    a.order0 = reinterpret_cast<uint2 *>(base + l.order[0]);
+    a.order1 = reinterpret_cast<uint2 *>(base + l.order[1]);
     a.hist = reinterpret_cast<unsigned *>(base + l.hist);
     a.part = reinterpret_cast<float *>(base + l.part);
     int bits = 1;
