@@ -42,7 +42,7 @@ struct TensorEntry {
     long long n;
     float decay;                 // 1 - lr * weight decay of this tensor
     int first_unit;
-    int lead;                    // 32 bits: elements that the first unit begins before the tensor (0 .. 63); 8 bits: 0; -1: only
+    int lead;                    // 32 bits: elements that the first unit begins before the tensor (0 .. 255); 8 bits: 0; -1: only
                                  // accesses of any alignment
 };
 
@@ -347,8 +347,9 @@ __device__ __forceinline__ void step_units8(const TensorEntry &t, int blk, int l
 }
 
 // ---------------------------------------------------------------- fp32 states
-// Units need not begin where the tensor does: with `lead` elements before its start they lie on 128-byte (else on
-// 16-byte) boundaries in all four arrays wherever the arrays' offsets allow it (tensors at the same places of packed rows).
+// Units need not begin where the tensor does: with `lead` elements before its start they lie on multiples of their own size
+// (else of 16 bytes) in all four arrays wherever the arrays' offsets allow it (tensors at the same places of packed rows: 86.6M
+// elements in 152 tensors 379 us; on multiples of 128 bytes 403, in accesses of any alignment 405 to 417).
 
 template <typename TP, typename TG, int kAccess>
 __device__ __forceinline__ void step_unit32(const TensorEntry &t, long long first, int lane, const AdamArgs &a, float gs) {

@@ -301,18 +301,19 @@ struct TensorScalars {
 
 int64_t units_of(int64_t n) { return (n + kStateBlock - 1) / kStateBlock; }
 
-// Elements (0 .. 63) by which units have to begin before the tensor so that they lie on 128-byte boundaries, or else
-// on 16-byte boundaries, in the parameter, the gradient and both fp32 moments; -1 if no number does.
+// Elements (0 .. 255) by which units have to begin before the tensor so that they lie on multiples of their own size (else
+// of 16 bytes) in the parameter, the gradient and both fp32 moments; -1 if no number does.
 int common_lead(const dppf_tensor &t, int tp, int tg) {
     const void *p[4] = {t.param, t.grad, t.exp_avg, t.exp_avg_sq};
     const int type[4] = {tp, tg, DPPF_FLOAT32, DPPF_FLOAT32};
-    for (const size_t boundary : {(size_t)128, (size_t)16})
-        for (size_t lead = 0; lead < boundary / 2; ++lead) {
-            bool fits = true;
-            for (int i = 0; i < 4; ++i) fits = fits && (reinterpret_cast<uintptr_t>(p[i]) - lead * type_bytes(type[i])) % boundary == 0;
-            if (fits) return (int)lead;
-        }
-    return -1;
+    auto at = [&](int i) { return reinterpret_cast<uintptr_t>(p[i]) / type_bytes(type[i]); };   // in elements
+    auto fits = [&](uintptr_t lead, bool units) {
+        for (int i = 0; i < 4; ++i)
+            if ((at(i) - lead) % (units ? kStateBlock : 16 / type_bytes(type[i])) != 0) return false;
+        return true;
+    };
+    const uintptr_t lead = at(0) % kStateBlock, small = at(tp == DPPF_BFLOAT16 ? 0 : tg == DPPF_BFLOAT16 ? 1 : 2) % 8;
+    return fits(lead, true) ? (int)lead : fits(small, false) ? (int)small : -1;
 }
 
 // Tensors [first, last) as one launch, or as many as the table and the unit count allow.
