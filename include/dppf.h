@@ -395,7 +395,7 @@ int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld,
  *   A gradient that is not finite makes its whole block of 256 states NaN (with 32 bits: one element).
  * bf16 parameters are rounded to nearest after the step (updates below half their spacing are lost; keep
  * fp32 parameters where that matters).  The arrays of one tensor must not overlap each other, and no two
- * tensors may overlap.  Tensors with numel 0 are skipped.
+ * tensors may overlap.  Tensors with numel 0 are skipped; numel is at most 2^37.
  */
 typedef struct {
     void *param;

@@ -484,7 +484,10 @@ int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld,
     a.clip_lo = (float)(1.0 - (double)clip_low);
     a.clip_hi = (float)(1.0 + (double)clip_high);
     a.kl_coef = kl_coef;
-    a.log2e_t = (float)(1.4426950408889634 / (double)temperature);
+    const double log2e_t = 1.4426950408889634 / (double)temperature;
+    a.log2e_t = (float)log2e_t;
+    if ((double)a.log2e_t >= log2e_t) a.log2e_t = std::nextafterf(a.log2e_t, 0.f);
+    a.log2e_t_rest = (float)(log2e_t - (double)a.log2e_t);
     a.inv_t = (float)(1.0 / (double)temperature);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     return type == DPPF_FLOAT32 ? launch_policy<float>(a, dev, s) : launch_policy<bf16>(a, dev, s);
@@ -501,7 +504,7 @@ int dppf_adamw_tensors(const dppf_tensor *tensors_host, int n_tensors, int param
     int present = 0;
     for (int k = 0; k < n_tensors; ++k) {
         const dppf_tensor &t = tensors_host[k];
-        if (t.numel < 0 || t.numel > ((int64_t)1 << 40) || !std::isfinite(t.decay)) return DPPF_ERR_INVALID_ARG;
+        if (t.numel < 0 || t.numel > ((int64_t)1 << 37) || !std::isfinite(t.decay)) return DPPF_ERR_INVALID_ARG;
         if (t.numel == 0) continue;
         ++present;
         const size_t n = (size_t)t.numel, scales = state_bits == 8 ? (n + kStateBlock - 1) / kStateBlock * 4 : 0;

@@ -44,7 +44,8 @@ struct PolicyArgs {
     int slice;                  // 16-byte vectors of a row that each block of the cluster holds
     int chunk;                  // ... and that a bulk copy brings, into one of kPolicyChunks buffers (in turn, without a gradient)
     int spin;
-    float clip_lo, clip_hi, kl_coef, log2e_t, inv_t;
+    float clip_lo, clip_hi, kl_coef, inv_t;
+    float log2e_t, log2e_t_rest;                             // log2(e) / temperature = their sum, both above zero
 };
 
 template <typename T> struct Vec16;      // the elements of a 16-byte vector, in pairs
@@ -81,9 +82,16 @@ __device__ __forceinline__ void merge(float &m, float &s, float m2, float s2, fl
     m = top;
 }
 
+// (x - m) k for the sums: with the part of k below its fp32 value, since that error would be the same in all of a row's
+// terms (as much as 1e-6 of a log-probability).  The rest is above zero, so that -inf stays -inf.
+__device__ __forceinline__ float2 scaled2(float2 x, float m, float k, float rest) {
+    const float2 d = add2(x, both(-m));
+    return fma2(d, both(rest), mul2(d, both(k)));
+}
+
 // Running maximum m and sum s = sum 2^((x - m) k) of a thread, over G vectors at once.
 template <typename T, int G, int kThreads>
-__device__ __forceinline__ void take(const uint4 *v, float k, float &m, float &s) {
+__device__ __forceinline__ void take(const uint4 *v, float k, float rest, float &m, float &s) {
     constexpr int kPairs = Vec16<T>::N / 2 * G;
     float2 x[kPairs];
 #pragma unroll
@@ -96,7 +104,7 @@ __device__ __forceinline__ void take(const uint4 *v, float k, float &m, float &s
     float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-        const float2 t = mul2(add2(x[i], both(-top)), both(k));
+        const float2 t = scaled2(x[i], top, k, rest);
         sum = add2(sum, make_float2(exp2_fast(t.x), exp2_fast(t.y)));
     }
     s += sum.x + sum.y;
@@ -234,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
         const float ref = a.ref_logp ? __ldg(a.ref_logp + row) : 0.f;
 
         float m = -FLT_MAX, s = 0.f;
-        const float k = a.log2e_t;
+        const float k = a.log2e_t, rest = a.log2e_t_rest;
         const int head = min((lo + v0) * N - before, e_last), tail = max((hi + v0) * N - before, head);   // whole vectors: elements [head, tail)
         int landed = 0, bad = 0;                                  // chunks whose copies this thread has waited for
         for (int c = 0; c < chunks && !bad; ++c) {
@@ -245,8 +253,8 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
                 const uint4 *v = s_row + (c % kPolicyChunks) * per - (size_t)c * per;                     // v[i]: vector i of the slice
                 const int stop = min(hi, (c + 1) * per);
                 int i = max(lo, c * per) + tid;
-                for (; i + (kTake - 1) * kThreads < stop; i += kTake * kThreads) take<T, kTake, kThreads>(v + i, k, m, s);
-                for (; i < stop; i += kThreads) take<T, 1, kThreads>(v + i, k, m, s);
+                for (; i + (kTake - 1) * kThreads < stop; i += kTake * kThreads) take<T, kTake, kThreads>(v + i, k, rest, m, s);
+                for (; i < stop; i += kThreads) take<T, 1, kThreads>(v + i, k, rest, m, s);
                 // the row's ends, element by element
                 const T *ve = reinterpret_cast<const T *>(v) + before - v0 * N;
                 if (c == 0 && tid < head - e_first) merge(m, s, to_float(ve[e_first + tid]), 1.f, k);
@@ -407,7 +415,7 @@ __global__ void __launch_bounds__(kShortThreads, kHold == 8 ? 4 : 8) policy_shor
             Vec16<T>::get(v[h], f);
 #pragma unroll
             for (int j = 0; j < kPairs; ++j) {
-                const float2 t = mul2(add2(f[j], both(-m)), both(k));
+                const float2 t = scaled2(f[j], m, k, a.log2e_t_rest);
                 sum = add2(sum, make_float2(exp2_fast(t.x), exp2_fast(t.y)));
             }
             s += sum.x + sum.y;

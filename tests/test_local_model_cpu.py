@@ -95,7 +95,7 @@ def test_adamw_tensors_refusals(b):
     nan = float("nan")
     for bad in (dict(null=True), dict(n=-1), dict(tp=2), dict(tg=5), dict(bits=16), dict(lr=nan), dict(b1=1.0), dict(b2=-0.1), dict(eps=nan), dict(wd=nan), dict(step=0),
                 dict(param=None), dict(grad=None), dict(exp_avg=None), dict(exp_avg_sq=None), dict(bits=8, exp_avg_scale=None), dict(bits=8, exp_avg_sq_scale=None),
-                dict(numel=-1), dict(decay=nan), dict(grad=P[0] + 4), dict(exp_avg=P[3] + 400), dict(bits=8, exp_avg_scale=P[5]), dict(bits=8, exp_avg_scale=P[2] + 4)):
+                dict(numel=-1), dict(numel=2**38), dict(decay=nan), dict(grad=P[0] + 4), dict(exp_avg=P[3] + 400), dict(bits=8, exp_avg_scale=P[5]), dict(bits=8, exp_avg_scale=P[2] + 4)):
         assert call(**bad) == b.ERR_INVALID_ARG, bad
     for bad in (dict(param=P[0] + 2), dict(tg=1, grad=P[1] + 1), dict(exp_avg=P[2] + 1), dict(bits=8, exp_avg_scale=P[4] + 2), dict(gs=P[6] + 2)):
         assert call(**bad) == b.ERR_ALIGNMENT, bad
