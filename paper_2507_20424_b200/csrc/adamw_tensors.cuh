@@ -9,7 +9,7 @@ namespace {
 
 // The recurrence is that of adamw1.  A work unit is 256 consecutive elements of one tensor, held by a
 // warp, eight a lane; the table of tensors travels in the launch's parameters (nothing on the device can
-// be stale).  A warp finds a unit's tensor by bisection.
+// be stale).  A warp finds a unit's tensor in it.
 //
 // States in 8 bits: blocks of 256 elements counted from the tensor's start, which is what a warp holds.
 //   m = code_m * scale_m,  sqrt(v) = code_r * scale_r,  codes e4m3, scale = (block's largest) / 448.
@@ -375,11 +375,13 @@ __device__ __forceinline__ void step_unit32(const TensorEntry &t, long long firs
 
 // ---------------------------------------------------------------- the kernel
 
-// The last tensor whose first unit is not past u, at or after tensor k.
+// The last tensor whose first unit is not past u, at or after tensor k: a few steps, or else bisection (few large tensors lie
+// between a warp's units, or many small ones).
 template <int kEntries>
 __device__ __forceinline__ int find_tensor(const TensorTable<kEntries> &tab, int u, int k) {
+    for (int i = 0; i < 4; ++i, ++k)
+        if (k + 1 >= tab.n || tab.e[k + 1].first_unit > u) return k;
     int hi = tab.n;
-    if (k + 1 >= hi || tab.e[k + 1].first_unit > u) return k;
     while (hi - k > 1) {
         const int mid = (k + hi) >> 1;
         if (tab.e[mid].first_unit <= u) k = mid; else hi = mid;
