@@ -662,3 +662,76 @@ def test_operators_on_a_side_stream_and_in_a_graph(b):
         reset()
         graph.replay()
         assert all(same_bits(x, y) for x, y in zip(plain, answers()))
+
+
+def test_longer_paths_on_a_side_stream_and_in_a_graph(b):
+    """The gradient's chain of launches (sort, sums, joins), rows split over a cluster, rows streamed forward."""
+    T, V, H = 5000, 3000 + 71, 136
+    ids, go = some_ids(T, V, torch.int64, 31), torch.randn(T, H, generator=gen(32), device="cuda").to(BF16)
+    whole, added = torch.empty(V, H, device="cuda"), torch.zeros(V, H, dtype=BF16, device="cuda")
+    i, j = policy_inputs(24, 60_001, BF16, 33), policy_inputs(700, 50_000, BF16, 34)
+    gx = torch.empty_like(i["logits"])
+    ws_e, ws_p = b.alloc_embedding_workspace(T, H), b.alloc_policy_workspace(700)
+    res = {}
+
+    def step():
+        b.dppf_embedding_grad(go, ids, whole, ws=ws_e)
+        b.dppf_embedding_grad(go, ids, added, accumulate=True, ws=ws_e)
+        res["a"] = b.dppf_policy_loss(i["logits"], i["targets"], i["old"], i["adv"], i["weight"], grad_logits=gx, ws=ws_p).logp
+        res["b"] = b.dppf_policy_loss(j["logits"], j["targets"], j["old"], j["adv"], j["weight"], ws=ws_p).loss
+
+    def answers():
+        torch.cuda.synchronize()
+        out = [t.clone() for t in (whole, added, gx, res["a"], res["b"])]
+        whole.fill_(float("nan")), gx.fill_(float("nan")), added.zero_()
+        return out
+
+    step()
+    plain = answers()
+    assert torch.isfinite(plain[0]).all() and torch.isfinite(plain[4])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    assert all(same_bits(x, y) for x, y in zip(plain, answers()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        graph.replay()
+        assert all(same_bits(x, y) for x, y in zip(plain, answers()))
+
+
+# ---------------------------------------------------------------- seeded random shapes
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_shapes(b, seed):
+    rng = np.random.default_rng(seed)
+    size = lambda low, high: int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))  # noqa: E731
+    pick = lambda *x: x[rng.integers(len(x))]  # noqa: E731
+    for _ in range(4):
+        check_grad(b, size(1, 30_000), size(1, 20_000), size(1, 700), pick(F32, BF16), pick(F32, BF16), pick(torch.int32, torch.int64), bool(rng.integers(2)), seed=size(1, 10_000))
+        V = size(2, 150_000)
+        T = size(1, max(2, min(400, 3_000_000 // V)))
+        i = policy_inputs(T, V, pick(F32, BF16), size(1, 10_000), stride=V + int(rng.integers(0, 20)), offset=int(rng.integers(0, 9)), masked=pick(0.0, 0.3, 0.8))
+        check_policy(b, i, kl=bool(rng.integers(2)), temperature=pick(0.6, 1.0, 1.7), backward=bool(rng.integers(2)))
+    # many tensors at random offsets of one row, 8-bit states: the plain sequence's codes
+    sizes = [size(1, 5000) for _ in range(pick(3, 40, 90))]
+    lead = int(rng.integers(0, 9))
+    g = gen(seed)
+    rows = [torch.randn(lead + sum(sizes), generator=g, device="cuda")[lead:] * s for s in (0.02, 1e-2)]
+    p, gr = list(rows[0].split(sizes)), list(rows[1].to(pick(F32, BF16)).split(sizes))
+    t = b.AdamWTensors(p, gr, state_bits=8)
+    for step in (1, 2):
+        st = [(t.exp_avgs[k].view(torch.uint8).cpu().numpy(), t.exp_avg_sqs[k].view(torch.uint8).cpu().numpy(), t.exp_avg_scales[k].cpu().numpy(),
+               t.exp_avg_sq_scales[k].cpu().numpy()) for k in range(len(sizes))]
+        old = [x.double().cpu().numpy() for x in p]
+        b.dppf_adamw_tensors(t, step=step, seed=seed + step, **HP)
+        for k, n in enumerate(sizes):
+            gk = gr[k].float().cpu().numpy()
+            wm, wms, wr, wrs = ref.adamw8_states(gk, *st[k], HP["beta1"], HP["beta2"], seed + step)
+            assert np.array_equal(t.exp_avgs[k].view(torch.uint8).cpu().numpy(), wm) and np.array_equal(t.exp_avg_sqs[k].view(torch.uint8).cpu().numpy(), wr)
+            assert np.array_equal(t.exp_avg_scales[k].cpu().numpy(), wms) and np.array_equal(t.exp_avg_sq_scales[k].cpu().numpy(), wrs)
+            wp, _, _ = ref.adamw(old[k], gk.astype(np.float64), ref.decode(st[k][0], st[k][2], n), ref.decode(st[k][1], st[k][3], n) ** 2, step=step, **HP)
+            got = p[k].double().cpu().numpy()
+            assert np.all(np.abs(got - wp) <= EPS * np.abs(wp) + 2e-6 * (np.abs(wp) + np.abs(wp - old[k])) + 1e-9)
