@@ -100,7 +100,7 @@ template <typename TW, typename TO>
 int launch_lookup(LookupArgs a, int n, cudaStream_t s) {
     a.groups = a.H / n;
     // two rounds of a thread's groups, at least one row a block
-    long long rows = (2LL * (n == 8 ? kLookupAhead<8> : kLookupAhead<4>) * kLookupThreads) / a.groups;
+    long long rows = (2LL * kLookupAhead * kLookupThreads) / a.groups;
     if (rows < 1) rows = 1;
     // short lookups: fewer rows a block, so that more blocks share the work
     while (rows > 1 && (a.T + rows - 1) / rows < 592) rows = (rows + 1) / 2;
