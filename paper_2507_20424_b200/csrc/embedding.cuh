@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kReduceThreads, 4) embedding_reduce_kernel(con
     __syncthreads();
     const int tile = block_x * subs + sub;
     const int grp = block_y * a.row_threads + col;
-    if (tile >= a.tiles || grp >= a.groups) return;
+    if (sub >= subs || tile >= a.tiles || grp >= a.groups) return;
     const int j = grp * N, L = a.tile;
     const unsigned *key = s_key + sub * L + L + 1, *pos = s_pos + sub * L;        // key[-L - 1] .. key[2 L]
     int i = 0, n = (int)min((long long)L, (long long)a.T - (long long)tile * L);
