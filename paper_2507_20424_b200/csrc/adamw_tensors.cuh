@@ -28,9 +28,9 @@ constexpr int kGroup = 4;                              // units that a warp take
 constexpr int kSmallTable = 50, kLargeTable = 440;     // table sizes: under 4 KB and 32 KB of launch parameters
 
 // Resident blocks an SM.  Fewer loads in flight run faster once there are enough of them, since reads and writes
-// share the memory: fp32 states with fp32 parameters and gradients 2 blocks (86.6M elements: 371 us; 3: 425 us), with
+// share the memory: fp32 states with fp32 parameters and gradients 2 blocks (86.6M elements: 365 us; 3: 425 us), with
 // bf16 ones 3 (295 us; 2: 364 us, 4: 336 us), with one of each 3.  8-bit states are bound by instructions and registers: 2 blocks of
-// 128 registers and groups of four units (300M bf16: 535 us; groups of 2, 80 registers: 587 us; single units: 675 to 780 us).
+// 128 registers and groups of four units (300M bf16: 531 us; groups of 2, 80 registers: 587 us; single units: 675 to 780 us).
 template <typename TP, typename TG, int kBits>
 struct TensorShape { static constexpr int kBlocks = kBits == 8 || sizeof(TP) + sizeof(TG) == 8 ? 2 : 3; };
 
@@ -41,9 +41,12 @@ struct TensorEntry {
     float *m_scale, *v_scale;
     long long n;
     float decay;                 // 1 - lr * weight decay of this tensor
-    int first_unit;
-    int lead;                    // 32 bits: elements that the first unit begins before the tensor (0 .. 255); 8 bits: 0; -1: only
-                                 // accesses of any alignment
+    int first_unit;              // 8 bits: of those that are taken one at a time
+    union {
+        int lead;                // 32 bits: elements that the first unit begins before the tensor (0 .. 255); -1: only accesses of
+                                 // any alignment
+        int first_group;         // 8 bits
+    };
 };
 
 template <int kEntries>
@@ -53,8 +56,7 @@ struct TensorTable {
     AdamArgs args;               // scalars only
     float b1;
     unsigned seed_term;
-    int n, units;
-    int group;                   // units a warp takes at a time: 1, or (8-bit states) kGroup
+    int n, units, groups;        // 8 bits: a tensor begins with its groups of kGroup units, the units are the rest
 };
 
 // ---------------------------------------------------------------- eight elements of a lane, as stored
@@ -375,18 +377,23 @@ __device__ __forceinline__ void step_unit32(const TensorEntry &t, long long firs
 
 // ---------------------------------------------------------------- the kernel
 
-// The last tensor whose first unit is not past u, at or after tensor k: a few steps, or else bisection (few large tensors lie
-// between a warp's units, or many small ones).
-template <int kEntries>
+// The last tensor whose first unit (or group) is not past u, at or after tensor k: a few steps, or else bisection (few large
+// tensors lie between a warp's units, or many small ones).
+template <bool kGroups>
+__device__ __forceinline__ int first_of(const TensorEntry &t) { return kGroups ? t.first_group : t.first_unit; }
+template <bool kGroups, int kEntries>
 __device__ __forceinline__ int find_tensor(const TensorTable<kEntries> &tab, int u, int k) {
     for (int i = 0; i < 4; ++i, ++k)
-        if (k + 1 >= tab.n || tab.e[k + 1].first_unit > u) return k;
+        if (k + 1 >= tab.n || first_of<kGroups>(tab.e[k + 1]) > u) return k;
     int hi = tab.n;
     while (hi - k > 1) {
         const int mid = (k + hi) >> 1;
-        if (tab.e[mid].first_unit <= u) k = mid; else hi = mid;
+        if (first_of<kGroups>(tab.e[mid]) <= u) k = mid; else hi = mid;
     }
     return k;
+}
+__host__ __device__ __forceinline__ bool codes_on_8(const TensorEntry &t) {
+    return ((reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v)) & 7u) == 0;
 }
 
 template <typename TP, typename TG, int kBits, int kEntries>
@@ -395,35 +402,34 @@ adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
     const float gs = tab.grad_scale ? __ldg(tab.grad_scale) : 1.f;
     if (!isfinite(gs)) return;                              // a step whose gradients overflowed is skipped whole
     const int lane = threadIdx.x & 31;
-    const int step = gridDim.x * kTensorWarps * tab.group;
-    int first = (blockIdx.x * kTensorWarps + (threadIdx.x >> 5)) * tab.group;
-    for (int k = 0; first < tab.units; first += step) {
-        k = find_tensor(tab, first, k);
-        const TensorEntry *t = &tab.e[k];
-        int blk = first - t->first_unit;
-        if constexpr (kBits == 8) {
-            if (tab.group == kGroup && t->lead >= 0 && (long long)(blk + kGroup) * kStateBlock <= t->n) {
-                if (skew(t->param) | skew(t->grad)) step_units8<TP, TG, kSkewed, kGroup>(*t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
-                else step_units8<TP, TG, kAligned, kGroup>(*t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
-                continue;
-            }
+    const int step = gridDim.x * kTensorWarps, warp = blockIdx.x * kTensorWarps + (threadIdx.x >> 5);
+    int u = warp;
+    for (int k = 0; u < tab.units; u += step) {
+        k = find_tensor<false>(tab, u, k);
+        const TensorEntry &t = tab.e[k];
+        if constexpr (kBits == 32) {
+            const long long e = (long long)(u - t.first_unit) * kStateBlock - max(t.lead, 0);
+            if (t.lead >= 0 && e >= 0 && e + kStateBlock <= t.n) step_unit32<TP, TG, kAligned>(t, e, lane, tab.args, gs);
+            else step_unit32<TP, TG, kAnyAlignment>(t, e, lane, tab.args, gs);
+        } else {
+            const int grouped = ((k + 1 < tab.n ? tab.e[k + 1].first_group : tab.groups) - t.first_group) * kGroup;
+            const int blk = grouped + u - t.first_unit;
+            if (codes_on_8(t) && (long long)(blk + 1) * kStateBlock <= t.n)
+                step_units8<TP, TG, kSkewed, 1>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+            else
+                step_units8<TP, TG, kAnyAlignment, 1>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
         }
-        int at = k;
-        const int last = min(first + tab.group, tab.units);
-        for (int u = first; u < last; ++u) {
-            while (at + 1 < tab.n && tab.e[at + 1].first_unit <= u) ++at;
-            t = &tab.e[at];
-            blk = u - t->first_unit;
-            if constexpr (kBits == 32) {
-                const long long e = (long long)blk * kStateBlock - max(t->lead, 0);
-                if (t->lead >= 0 && e >= 0 && e + kStateBlock <= t->n) step_unit32<TP, TG, kAligned>(*t, e, lane, tab.args, gs);
-                else step_unit32<TP, TG, kAnyAlignment>(*t, e, lane, tab.args, gs);
-            } else {
-                if (t->lead >= 0 && (long long)(blk + 1) * kStateBlock <= t->n)
-                    step_units8<TP, TG, kSkewed, 1>(*t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
-                else
-                    step_units8<TP, TG, kAnyAlignment, 1>(*t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
-            }
+    }
+    if constexpr (kBits == 8) {
+        // Groups go on from the warp after the last unit's.  Groups hold whole units of one tensor only: taken across the tensors' ends,
+        // a unit at a time there, the warps that met an end finished late (25.7M bf16 in 150 tensors 65 us, now 54; 4.4M in 116 27, 16).
+        u -= tab.units;
+        for (int k = 0; u < tab.groups; u += step) {
+            k = find_tensor<true>(tab, u, k);
+            const TensorEntry &t = tab.e[k];
+            const int blk = (u - t.first_group) * kGroup;
+            if (skew(t.param) | skew(t.grad)) step_units8<TP, TG, kSkewed, kGroup>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+            else step_units8<TP, TG, kAligned, kGroup>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
         }
     }
 }

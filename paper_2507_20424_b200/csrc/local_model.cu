@@ -278,13 +278,29 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
 
 // ---------------------------------------------------------------- AdamW over many tensors
 
+int64_t units_of(int64_t n) { return (n + kStateBlock - 1) / kStateBlock; }
+
 template <typename TP, typename TG, int kBits, int kEntries>
 int launch_tensors(TensorTable<kEntries> &tab, int sms, cudaStream_t s) {
     constexpr int kBlocks = TensorShape<TP, TG, kBits>::kBlocks;
     const long long most = (long long)sms * kBlocks;                 // blocks that are resident
-    // groups only while every warp still gets one
-    tab.group = kBits == 8 && tab.units >= most * kTensorWarps * kGroup ? kGroup : 1;
-    const long long warps = (tab.units + tab.group - 1) / tab.group, blocks = (warps + kTensorWarps - 1) / kTensorWarps;
+    tab.groups = 0;
+    if (kBits == 8) {
+        auto groups_of = [](const TensorEntry &e) { return codes_on_8(e) ? (int)(e.n / (kStateBlock * kGroup)) : 0; };
+        long long groups = 0;
+        for (int k = 0; k < tab.n; ++k) groups += groups_of(tab.e[k]);
+        const bool grouped = groups >= most * kTensorWarps;          // every warp gets one
+        tab.units = 0;
+        for (int k = 0; k < tab.n; ++k) {
+            TensorEntry &e = tab.e[k];
+            const int mine = grouped ? groups_of(e) : 0;
+            e.first_unit = tab.units;
+            e.first_group = tab.groups;
+            tab.units += (int)units_of(e.n) - mine * kGroup;
+            tab.groups += mine;
+        }
+    }
+    const long long warps = (long long)tab.units + tab.groups, blocks = (warps + kTensorWarps - 1) / kTensorWarps;
     adamw_tensors_kernel<TP, TG, kBits, kEntries><<<(unsigned)(blocks < most ? blocks : most), kTensorThreads, 0, s>>>(tab);
     return launched();
 }
@@ -306,8 +322,6 @@ struct TensorScalars {
     unsigned seed_term;
     int tp, tg, bits;
 };
-
-int64_t units_of(int64_t n) { return (n + kStateBlock - 1) / kStateBlock; }
 
 // Elements (0 .. 255) by which units have to begin before the tensor so that they lie on multiples of their own size (else
 // of 16 bytes) in the parameter, the gradient and both fp32 moments; -1 if no number does.
@@ -339,7 +353,7 @@ int launch_table(const dppf_tensor *ts, int first, int last, const TensorScalars
         for (; k < last && tab.n < kEntries; ++k) {
             const dppf_tensor &t = ts[k];
             if (t.numel == 0) continue;
-            const int lead = p.bits == 8 ? (aligned_to(t.exp_avg, 8) && aligned_to(t.exp_avg_sq, 8) ? 0 : -1) : common_lead(t, p.tp, p.tg);
+            const int lead = p.bits == 8 ? 0 : common_lead(t, p.tp, p.tg);
             const int64_t more = units_of(t.numel + (lead > 0 ? lead : 0));
             if (units + more > INT_MAX / 2 && tab.n) break;
             TensorEntry &e = tab.e[tab.n++];
