@@ -1,0 +1,40 @@
+"""Orders, extremes and longer paths of a local step's operators on the GPU (the plain cases are in test_gpu_local_model.py)."""
+import pytest
+import torch
+
+from gpu_util import require_gpu
+from test_gpu_local_model import BF16, F32, gen, policy_inputs, same_bits
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def b():
+    return require_gpu()[1]
+
+
+# ---------------------------------------------------------------- policy loss
+
+def edge_targets(V, count, seed):
+    """Targets at the row's ends, around the ends of halves, quarters and eighths of it, and anywhere."""
+    at = [0, 1, V - 2, V - 1] + [min(max(V * k // 8 + o, 0), V - 1) for k in range(1, 8) for o in range(-9, 10)]
+    some = torch.randint(0, V, (count,), generator=gen(seed), device="cuda")
+    n = min(count, len(at))
+    some[:n] = torch.tensor(at[:n], device="cuda")
+    return some
+
+
+@pytest.mark.parametrize("dtype,T,V,stride", [(BF16, 700, 131_072, 131_072), (BF16, 500, 100_001, 100_001), (F32, 300, 74_003, 74_003), (F32, 150, 262_144, 262_144), (BF16, 9, 32_000, 32_000)])
+def test_policy_gradient_in_place_over_clusters(b, dtype, T, V, stride):
+    """The gradient replaces the logits while the blocks of a row's cluster still need the target's logit."""
+    i = policy_inputs(T, V, dtype, 41, stride=stride, masked=0.0)
+    i["targets"] = edge_targets(V, T, 42)
+    i["old"] = torch.log_softmax(i["logits"].float(), 1).gather(1, i["targets"][:, None])[:, 0]
+    keep, sep = i["logits"].clone(), torch.empty_like(i["logits"])
+    args = (i["targets"], i["old"], i["adv"], i["weight"])
+    a = b.dppf_policy_loss(keep, *args, grad_logits=sep)
+    for _ in range(3):
+        i["logits"].copy_(keep)
+        c = b.dppf_policy_loss(i["logits"], *args, grad_logits=i["logits"])
+        assert same_bits(i["logits"], sep) and same_bits(a.logp, c.logp) and same_bits(a.loss, c.loss)
+    assert torch.allclose(a.logp, i["old"], rtol=0, atol=8e-5)    # two fp32 log-softmaxes, 1e-6 (2 + |lp| + log V) each
