@@ -169,6 +169,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const Gra
     }
     unsigned *hist = s_hist + warp * kBins;
     for (int b = lane; b < kBins; b += 32) hist[b] = 0;
+    __syncwarp();                                             // the zeros, before any lane counts into them
     wait_for_previous();
 
     const int shift = pass * a.bits;

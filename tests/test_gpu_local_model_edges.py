@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from gpu_util import require_gpu
-from test_gpu_local_model import BF16, F32, gen, policy_inputs, same_bits
+from test_gpu_local_model import BF16, F32, check_grad, gen, policy_inputs, same_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -11,6 +11,16 @@ pytestmark = pytest.mark.gpu
 @pytest.fixture(scope="module")
 def b():
     return require_gpu()[1]
+
+
+# ---------------------------------------------------------------- embedding gradient
+
+@pytest.mark.parametrize("T", [140_000, 600_001])
+@pytest.mark.parametrize("V,H,alike", [(300, 3, False), (40_000, 8, False), (300_000, 2, False), (5000, 8, True)])
+def test_lookup_gradient_sorts_long_sequences(b, T, V, H, alike):
+    """A warp of the sort has more than 32 places, and more than it holds in registers; one, two and three digits."""
+    check_grad(b, T, V, H, F32, F32, torch.int64, False, seed=T + V, alike=alike)
+    check_grad(b, T, V, H, BF16, BF16, torch.int32, True, seed=T + V + 1, alike=alike)
 
 
 # ---------------------------------------------------------------- policy loss
