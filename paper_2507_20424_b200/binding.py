@@ -413,6 +413,13 @@ def _vector(t: torch.Tensor, n: int, what: str, device, dtypes=(torch.float32,))
     return t
 
 
+def _workspace(ws: torch.Tensor, device) -> torch.Tensor:
+    """ws, whose bytes the kernels will use: they must be memory of this device, and all of them there."""
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous tensor on {device}")
+    return ws
+
+
 def _call(device, fn, where, *args):
     """fn(*args, stream) with `device` current; raises on a status other than OK."""
     if device.index == torch._C._cuda_getDevice():            # the calls behind torch.cuda.current_device() and
@@ -467,7 +474,9 @@ def dppf_embedding_grad(grad_out, ids, grad_table, scale=1.0, accumulate=False, 
         raise ValueError("grad_out must hold one row of H columns per id, on the table's device")
     flat = grad_out if grad_out.dim() == 2 else grad_out.view(-1, H)
     _, _, ld_out = _matrix(flat, "grad_out")
-    if ws is None and T:
+    if ws is not None:
+        _workspace(ws, dev)
+    elif T:
         ws = alloc_embedding_workspace(T, H, dev)
     _call(dev, load().dppf_embedding_grad, "dppf_embedding_grad", flat.data_ptr(), _type(flat, "grad_out"), ld_out, ids.data_ptr(), _ID_BITS[ids.dtype], T, scale,
           grad_table.data_ptr(), _type(grad_table, "grad_table"), V, H, ld, int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
@@ -507,8 +516,7 @@ def dppf_policy_loss(logits, targets, old_logp, advantage, weight, ref_logp=None
         if grad_logits.dtype != logits.dtype or grad_logits.device != dev or rows != T or cols != V:
             raise ValueError("grad_logits must have the type, shape and device of logits")
         grad_ptr = grad_logits.data_ptr()
-    if ws is None:
-        ws = alloc_policy_workspace(T, dev)
+    ws = alloc_policy_workspace(T, dev) if ws is None else _workspace(ws, dev)
     out = logits.new_empty(3 + T, dtype=torch.float32)
     sums_ptr = out.data_ptr()
     _call(dev, load().dppf_policy_loss, "dppf_policy_loss", logits.data_ptr(), code, T, V, ld, targets.data_ptr(), _ID_BITS[targets.dtype], old_logp.data_ptr(),

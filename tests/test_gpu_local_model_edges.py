@@ -48,3 +48,19 @@ def test_policy_gradient_in_place_over_clusters(b, dtype, T, V, stride):
         c = b.dppf_policy_loss(i["logits"], *args, grad_logits=i["logits"])
         assert same_bits(i["logits"], sep) and same_bits(a.logp, c.logp) and same_bits(a.loss, c.loss)
     assert torch.allclose(a.logp, i["old"], rtol=0, atol=8e-5)    # two fp32 log-softmaxes, 1e-6 (2 + |lp| + log V) each
+
+
+# ---------------------------------------------------------------- refusals
+
+def test_workspaces_have_to_be_memory_of_the_device(b):
+    i = policy_inputs(6, 64, BF16, 12)
+    args = (i["logits"], i["targets"], i["old"], i["adv"], i["weight"])
+    ids, go, t = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.ones(4, 8, device="cuda"), torch.zeros(3, 8, device="cuda")
+    for alloc, call in ((lambda: b.alloc_policy_workspace(6), lambda ws: b.dppf_policy_loss(*args, ws=ws)),
+                        (lambda: b.alloc_embedding_workspace(4, 8), lambda ws: b.dppf_embedding_grad(go, ids, t, ws=ws))):
+        ws = alloc()
+        for bad in (ws.cpu(), ws[:1].expand(ws.numel()), ws.repeat(2)[::2]):      # host memory; one byte said to be many; bytes with gaps
+            with pytest.raises(ValueError):
+                call(bad)
+        call(ws)
+    assert bool((t[0] == 4).all())
