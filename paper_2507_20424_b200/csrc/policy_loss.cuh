@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
         float m = -FLT_MAX, s = 0.f;
         const float k = a.log2e_t, rest = a.log2e_t_rest;
         const int head = min((lo + v0) * N - before, e_last), tail = max((hi + v0) * N - before, head);   // whole vectors: elements [head, tail)
-        int landed = 0, bad = 0;                                  // chunks whose copies this thread has waited for
+        int landed = 0, issued = min(chunks, kPolicyChunks), bad = 0;   // chunks whose copies this thread has waited for, has started (thread 0)
         for (int c = 0; c < chunks && !bad; ++c) {
             if (!mbar_wait_bounded(&s_bar[c % kPolicyChunks], (c / kPolicyChunks) & 1, a.spin)) {
                 bad = 1;
@@ -267,7 +267,10 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
             }
             if (chunks > kPolicyChunks) {                         // the ring: the chunk's buffer is free
                 bad = __syncthreads_or(bad);
-                if (tid == 0 && !bad && c + kPolicyChunks < chunks) fetch(c + kPolicyChunks);
+                if (tid == 0 && !bad && c + kPolicyChunks < chunks) {
+                    fetch(c + kPolicyChunks);
+                    issued = c + kPolicyChunks + 1;
+                }
             }
         }
         if (bad) {                                                // the row becomes NaN
@@ -320,7 +323,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
             }
         }
         if (s_failed && tid == 0)                                 // copies still under way land before the block leaves
-            for (int c = landed; c < min(landed + kPolicyChunks, chunks); ++c) mbar_wait_bounded(&s_bar[c % kPolicyChunks], (c / kPolicyChunks) & 1, kSpinLimit);
+            for (int c = landed; c < issued; ++c) mbar_wait_bounded(&s_bar[c % kPolicyChunks], (c / kPolicyChunks) & 1, kSpinLimit);
     } else {
         if (rank == 0 && tid == 0) put_terms(a, row, 0.f, 0.f, 0.f, 0.f);
         if (a.grad) {

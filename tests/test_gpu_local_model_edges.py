@@ -50,6 +50,29 @@ def test_policy_gradient_in_place_over_clusters(b, dtype, T, V, stride):
     assert torch.allclose(a.logp, i["old"], rtol=0, atol=8e-5)    # two fp32 log-softmaxes, 1e-6 (2 + |lp| + log V) each
 
 
+@pytest.mark.parametrize("polls", [0, 1, 2])
+def test_policy_rows_through_the_ring_give_up_soon(b, polls):
+    """A block whose threads disagree on whether a copy arrived in time waits for the copies that were started, and no others
+    (for one that never was, the wait would run to its limit of about a second)."""
+    i = policy_inputs(600, 131_072, BF16, 43, masked=0.0)
+    args = (i["logits"], i["targets"], i["old"], i["adv"], i["weight"])
+    good = b.dppf_policy_loss(*args)
+    ws, a, z = b.alloc_policy_workspace(600), torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    try:
+        b.debug_set_poll_limits(polls, -1)
+        a.record()
+        out = b.dppf_policy_loss(*args, ws=ws)
+        z.record()
+        status = b.dppf_device_status(ws)
+    finally:
+        b.debug_set_poll_limits(-1, -1)
+    late = torch.isnan(out.logp)
+    assert status == (b.ERR_TIMEOUT if bool(late.any()) else b.OK) and (polls or bool(late.all()))
+    assert same_bits(out.logp[~late], good.logp[~late]) and a.elapsed_time(z) < 100
+    again = b.dppf_policy_loss(*args, ws=ws)
+    assert same_bits(again.logp, good.logp) and same_bits(again.loss, good.loss)
+
+
 # ---------------------------------------------------------------- refusals
 
 def test_workspaces_have_to_be_memory_of_the_device(b):
