@@ -531,7 +531,10 @@ class AdamWTensors:
     """The tensors of :func:`dppf_adamw_tensors`: parameters, gradients and optimiser state, held for as long as
     the object lives.  ``state_bits`` 32: fp32 moments; 8: e4m3 codes with one fp32 scale per 256 elements (of the
     first moment, and of the root of the second).  State that is not given starts at zero.  ``decay``: factor on the
-    weight decay per tensor (default 1)."""
+    weight decay per tensor (default 1).
+
+    The step writes to the memory that the tensors have when the object is made (and reads the gradients' when they are
+    bound).  That memory is kept alive: a tensor that is given other memory later, as by ``p.data = q``, is not followed."""
 
     def __init__(self, params, grads, state_bits=32, exp_avgs=None, exp_avg_sqs=None, exp_avg_scales=None, exp_avg_sq_scales=None, decay=None):
         if state_bits not in (8, 32):
@@ -551,12 +554,13 @@ class AdamWTensors:
             given = list(given)
             if len(given) != n:
                 raise ValueError(f"{what} must have one entry per tensor")
-            return [_vector(t, c, what, self.device, (kind,)) for t, c in zip(given, counts)]
+            return [_vector(t, c, what, self.device, (kind,)).detach() for t, c in zip(given, counts)]
 
         for p in self.params:
             _vector(p, p.numel(), "params", self.device, (self.params[0].dtype,))
         if not self.params[0].is_cuda:
             raise ValueError("params must be CUDA tensors")
+        self.params = [p.detach() for p in self.params]           # aliases: they hold the memory even if p gets another
         self.exp_avgs = state(exp_avgs, sizes, dtype, "exp_avgs")
         self.exp_avg_sqs = state(exp_avg_sqs, sizes, dtype, "exp_avg_sqs")
         self.exp_avg_scales = self.exp_avg_sq_scales = None
@@ -582,7 +586,7 @@ class AdamWTensors:
         self.grad_type = _type(grads[0], "grads")
         for p, g in zip(self.params, grads):
             _vector(g, p.numel(), "grads", self.device, (grads[0].dtype,))
-        self.grads = grads
+        self.grads = [g.detach() for g in grads]
         for e, g in zip(self._table, grads):
             e.grad = g.data_ptr()
 

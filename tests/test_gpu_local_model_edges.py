@@ -73,6 +73,20 @@ def test_policy_rows_through_the_ring_give_up_soon(b, polls):
     assert same_bits(again.logp, good.logp) and same_bits(again.loss, good.loss)
 
 
+# ---------------------------------------------------------------- AdamW over many tensors
+
+def test_adamw_tensors_keep_the_memory_that_they_write(b):
+    p, g, m, v = (torch.full((1000,), x, device="cuda") for x in (1.0, 0.5, 0.0, 0.0))
+    t = b.AdamWTensors([p], [g], exp_avgs=[m], exp_avg_sqs=[v])
+    keep = [x.data_ptr() for x in (p, g, m, v)]
+    for x in (p, g, m, v):
+        x.data = torch.full_like(x, 7.0)                       # other memory; the old would be free
+    held = (t.params[0], t.grads[0], t.exp_avgs[0], t.exp_avg_sqs[0])
+    assert [x.data_ptr() for x in held] == keep
+    b.dppf_adamw_tensors(t, 0.1, 0.9, 0.999, 1e-8, 0.0, 1)
+    assert torch.allclose(t.params[0], torch.full_like(p, 0.9)) and bool((p == 7).all())
+
+
 # ---------------------------------------------------------------- refusals
 
 def test_workspaces_have_to_be_memory_of_the_device(b):
