@@ -567,6 +567,12 @@ class AdamWTensors:
         if state_bits == 8:
             self.exp_avg_scales = state(exp_avg_scales, blocks, torch.float32, "exp_avg_scales")
             self.exp_avg_sq_scales = state(exp_avg_sq_scales, blocks, torch.float32, "exp_avg_sq_scales")
+        # what the step writes, in order of address: all tensors are updated side by side, so none may share memory (as tied weights
+        # listed twice would)
+        written = sorted((t.data_ptr(), t.nbytes) for ts in (self.params, self.exp_avgs, self.exp_avg_sqs, self.exp_avg_scales, self.exp_avg_sq_scales)
+                         for t in ts or () if t.numel())
+        if any(at + size > after for (at, size), (after, _) in zip(written, written[1:])):
+            raise ValueError("parameters and optimiser states must not overlap")
         self.decay = [1.0] * n if decay is None else [float(d) for d in decay]
         if len(self.decay) != n:
             raise ValueError("decay must have one entry per tensor")

@@ -101,3 +101,15 @@ def test_workspaces_have_to_be_memory_of_the_device(b):
                 call(bad)
         call(ws)
     assert bool((t[0] == 4).all())
+
+
+def test_adamw_tensors_refuse_shared_memory(b):
+    row, states = torch.zeros(100, device="cuda"), [torch.zeros(40, device="cuda") for _ in range(4)]
+    a, c = row[:40], row[60:]
+    g = [torch.zeros(40, device="cuda")] * 2                   # gradients are read only: they may be one
+    b.AdamWTensors([a, row[:0], c], [g[0], row[:0], g[1]])
+    b.AdamWTensors([a, row[40:80]], g, exp_avgs=states[:2], exp_avg_sqs=states[2:])
+    for params, more in (([a, a], {}), ([a, row[39:79]], {}), ([a, c], dict(exp_avgs=[states[0], states[0]])), ([a, c], dict(exp_avgs=states[:2], exp_avg_sqs=[states[2], states[1]])),
+                         ([a, c], dict(exp_avgs=[states[0], a]))):
+        with pytest.raises(ValueError):
+            b.AdamWTensors(params, g, **more)
