@@ -30,7 +30,7 @@ constexpr int kSmallTable = 50, kLargeTable = 440;     // table sizes: under 4 K
 // Resident blocks an SM.  Fewer loads in flight run faster once there are enough of them, since reads and writes
 // share the memory: fp32 states with fp32 parameters and gradients 2 blocks (86.6M elements: 365 us; 3: 425 us), with
 // bf16 ones 3 (295 us; 2: 364 us, 4: 336 us), with one of each 3.  8-bit states are bound by instructions and registers: 2 blocks of
-// 128 registers and groups of four units (300M bf16: 531 us; groups of 2, 80 registers: 587 us; single units: 675 to 780 us).
+// 128 registers and groups of four units (300M bf16: 534 us; groups of 2, 80 registers: 587 us; single units: 675 to 780 us).
 template <typename TP, typename TG, int kBits>
 struct TensorShape { static constexpr int kBlocks = kBits == 8 || sizeof(TP) + sizeof(TG) == 8 ? 2 : 3; };
 
@@ -231,9 +231,10 @@ __device__ __forceinline__ unsigned e4m3_random_top(float y, float z, unsigned r
     const unsigned t = (__float_as_uint(z) << 4) + random_at_8;
     return y > 0.f ? max(t, 1u << 24) : t;
 }
-// Correctly rounded square roots of two numbers that are zero or at least 2^-100 (smaller ones: 1 ulp), without the
-// range branch of the library's: an approximate root s = v y, y ~ 1/sqrt(v), corrected by its exact residual,
-// s + (v - s s) y / 2 (Markstein, IBM J. Res. Dev. 34, 1990).  Infinity gives NaN.
+// Square roots: an approximate root s = v y, y ~ 1/sqrt(v), corrected by its residual, s + (v - s s) y / 2 (Markstein, IBM J. Res.
+// Dev. 34, 1990).  The residual's last bits are 2^-46 of v: down to 2^-102 it is exact and the roots are correctly rounded.  Smaller
+// numbers come out near enough as long as they are normal, and below 2^-126, where y stays at 2^63, as something above 0 (0 as 0)
+// that is below 2^-62, as their roots are.  Infinity gives NaN.
 __device__ __forceinline__ float2 sqrt2(float2 v) {
     float2 y;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, 0x1p-126f)));
@@ -242,6 +243,19 @@ __device__ __forceinline__ float2 sqrt2(float2 v) {
     const float2 rest = fma2(make_float2(-s.x, -s.y), s, v);
     return fma2(rest, half, s);
 }
+// Correctly rounded for every v: small ones are multiplied by 2^64 (exactly) and their roots by 2^-32.
+__device__ __forceinline__ float2 sqrt2_any(float2 v) {
+    const bool a = v.x < 0x1p-100f, b = v.y < 0x1p-100f;
+    const float2 s = sqrt2(mul2(v, make_float2(a ? 0x1p64f : 1.f, b ? 0x1p64f : 1.f)));
+    return mul2(s, make_float2(a ? 0x1p-32f : 1.f, b ? 0x1p-32f : 1.f));
+}
+// sqrt2 stands for it in two cases, which is nearly always (300M bf16: 565 us with sqrt2_any everywhere, 534 so, 531 with sqrt2
+// alone; a branch on the smallest of a lane's second moments 573 to 595).  For the parameters' update, where eps is large enough
+// (kExactRoots is false): it divides by root * inv_sqrt_bc2 + eps, in which roots below 2^-62 do not show.
+__host__ __forceinline__ bool sqrt2_is_enough(float eps, float inv_sqrt_bc2) { return eps >= 0x1p-36f * inv_sqrt_bc2; }
+// For the states, where a block's largest root is at least this: what is below 2^-51 is below half of the smallest code's value then, and
+// gets code 1 whatever it is.  The other blocks' states are done once more.
+constexpr float kTopRoot = 0x1p-32f;
 __device__ __forceinline__ float reciprocal(float x) {                            // 1 ulp; infinity below 2^-126
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -251,6 +265,79 @@ __device__ __forceinline__ float max_abs(float a, float b) {                    
     float d;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(fabsf(b)));
     return d;
+}
+__device__ __forceinline__ float2 first_moment(float2 g, float2 old, const AdamArgs &a, float b1) {
+    const float2 m0 = mul2(old, both(b1)), m1 = mul2(g, both(a.one_minus_b1));
+    return make_float2(__fadd_rn(m0.x, m1.x), __fadd_rn(m0.y, m1.y));
+}
+__device__ __forceinline__ float2 second_moment(float2 g, float2 root, const AdamArgs &a) {
+    const float2 v0 = mul2(mul2(root, root), both(a.b2)), v1 = mul2(mul2(g, g), both(a.one_minus_b2));
+    return make_float2(__fadd_rn(v0.x, v1.x), __fadd_rn(v0.y, v1.y));
+}
+// A block's largest magnitude from its lanes' (fp32 bits order as magnitudes do; NaN is above infinity)
+__device__ __forceinline__ unsigned block_top(float top) { return __reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu); }
+__device__ __forceinline__ float scale_of(unsigned top) {
+    const float scale = __fmul_rn(__uint_as_float(top), 1.0f / 448.0f);
+    return scale < 0x1p-126f ? 0.f : scale;
+}
+__device__ __forceinline__ float one_over(float scale) { return scale == 0.f ? 0.f : __fdiv_rn(1.f, scale); }
+__device__ __forceinline__ Raw<code8> moment_codes(const float2 (&m)[4], float over) {
+    Raw<code8> c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned two = e4m3_nearest(mul2(m[i], both(over)));
+        if (i & 1) c.w[i >> 1] |= two << 16;
+        else c.w[i >> 1] = two;
+    }
+    return c;
+}
+// Codes of a lane's roots; e: the unit's first element.
+template <int kAccess>
+__device__ __forceinline__ Raw<code8> root_codes(const float2 (&r)[4], float over, long long e, int lane, unsigned seed_term) {
+    unsigned top[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 y = mul2(r[i], both(over)), z = mul2(y, both(0x1p-120f));
+        const unsigned pair = (unsigned)(e + lane_element<kAccess>(lane, 2 * i)) >> 1;
+        if (kAccess != kAnyAlignment) {
+            const unsigned h = pair_hash(pair, seed_term);
+            top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h, 0, 0x4104));              // low half at bit 8
+            top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h, 0, 0x4324));          // high half at bit 8
+        } else {                                                                            // 32 elements apart, both of the lane's parity
+            const unsigned h0 = pair_hash(pair, seed_term), h1 = pair_hash(pair + 16, seed_term), pick = (lane & 1) ? 0x4324 : 0x4104;
+            top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h0, 0, pick));
+            top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h1, 0, pick));
+        }
+    }
+    Raw<code8> c;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        c.w[i] = __byte_perm(__byte_perm(top[4 * i], top[4 * i + 1], 0x0073), __byte_perm(top[4 * i + 2], top[4 * i + 3], 0x0073), 0x5410);
+    return c;
+}
+// New states of block blk, of which the parameters have had their step, with roots by sqrt2_any.  Seldom called: not in line, so that
+// the registers of the caller are its own.
+template <typename TG>
+__device__ __noinline__ void step_states8(const TensorEntry &t, int blk, int lane, const AdamArgs &a, float b1, float gs, unsigned seed_term) {
+    const long long first = (long long)blk * kStateBlock;
+    const Raw<TG> grad = load_raw<TG, kAnyAlignment>(t.grad, first, t.n, lane);
+    Raw<code8> mc = load_raw<code8, kAnyAlignment>(t.m, first, t.n, lane);
+    const Raw<code8> rc = load_raw<code8, kAnyAlignment>(t.v, first, t.n, lane);
+    const float ms = __ldcg(t.m_scale + blk), rs = __ldcg(t.v_scale + blk);
+    float2 m[4], r[4];
+    float mtop = 0.f, rtop = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 g = mul2(pair_of(grad, i), both(gs));
+        m[i] = first_moment(g, mul2(e4m3_values(mc, i), both(ms)), a, b1);
+        r[i] = sqrt2_any(second_moment(g, mul2(e4m3_values(rc, i), both(rs)), a));
+        mtop = max_abs(max_abs(mtop, m[i].x), m[i].y);
+        rtop = max_abs(max_abs(rtop, r[i].x), r[i].y);
+    }
+    const float mscale = scale_of(block_top(mtop)), rscale = scale_of(block_top(rtop));
+    if (lane == 0) { t.m_scale[blk] = mscale; t.v_scale[blk] = rscale; }
+    store_raw<code8, kAnyAlignment>(t.m, first, t.n, lane, moment_codes(m, one_over(mscale)));
+    store_raw<code8, kAnyAlignment>(t.v, first, t.n, lane, root_codes<kAnyAlignment>(r, one_over(rscale), first, lane, seed_term));
 }
 template <typename TP, typename TG>
 struct Unit8 {
@@ -262,7 +349,7 @@ struct Unit8 {
 
 // kUnits consecutive units of one tensor, so that constants, addresses and the division behind a unit's two scales
 // are shared: lane i works out the i-th scale of the 2 kUnits.
-template <typename TP, typename TG, int kAccess, int kUnits>
+template <typename TP, typename TG, int kAccess, int kUnits, bool kExactRoots>
 __device__ __forceinline__ void step_units8(const TensorEntry &t, int blk, int lane, const AdamArgs &a, float b1, float gs, unsigned seed_term) {
     const long long first = (long long)blk * kStateBlock;
     Unit8<TP, TG> us[kUnits];
@@ -296,10 +383,9 @@ __device__ __forceinline__ void step_units8(const TensorEntry &t, int blk, int l
         for (int i = 0; i < 4; ++i) {
             const float2 g = mul2(pair_of(u.g, i), both(gs));
             const float2 old = mul2(e4m3_values(u.m, i), both(u.ms)), root = mul2(e4m3_values(u.r, i), both(u.rs));
-            const float2 m0 = mul2(old, both(b1)), m1 = mul2(g, both(a.one_minus_b1));
-            const float2 v0 = mul2(mul2(root, root), both(a.b2)), v1 = mul2(mul2(g, g), both(a.one_minus_b2));
-            m[k][i] = make_float2(__fadd_rn(m0.x, m1.x), __fadd_rn(m0.y, m1.y));
-            r[k][i] = sqrt2(make_float2(__fadd_rn(v0.x, v1.x), __fadd_rn(v0.y, v1.y)));
+            const float2 v = second_moment(g, root, a);
+            m[k][i] = first_moment(g, old, a, b1);
+            r[k][i] = kExactRoots ? sqrt2_any(v) : sqrt2(v);
             mtop = max_abs(max_abs(mtop, m[k][i].x), m[k][i].y);
             rtop = max_abs(max_abs(rtop, r[k][i].x), r[k][i].y);
             // the update itself, in 2 ulp: it is small against the parameter that it is added to
@@ -308,43 +394,24 @@ __device__ __forceinline__ void step_units8(const TensorEntry &t, int blk, int l
             set_pair(u.p, i, fma2(both(-a.step_size), step, mul2(pair_of(u.p, i), both(t.decay))));
         }
         store_raw<TP, kAccess>(t.param, first + k * kStateBlock, t.n, lane, u.p);
-        // largest magnitudes of the block (fp32 bits order as magnitudes do; NaN is above infinity)
-        const unsigned mt = __reduce_max_sync(0xffffffffu, __float_as_uint(mtop) & 0x7fffffffu), rt = __reduce_max_sync(0xffffffffu, __float_as_uint(rtop) & 0x7fffffffu);
+        const unsigned mt = block_top(mtop), rt = block_top(rtop);
         if (lane == 2 * k) top_of = mt;
         if (lane == 2 * k + 1) top_of = rt;
     }
-    float scale = __fmul_rn(__uint_as_float(top_of), 1.0f / 448.0f);
-    if (scale < 0x1p-126f) scale = 0.f;
-    const float over = scale == 0.f ? 0.f : __fdiv_rn(1.f, scale);
+    if constexpr (!kExactRoots) {
+        if (__any_sync(0xffffffffu, (lane & 1) && lane < 2 * kUnits && top_of != 0 && top_of < __float_as_uint(kTopRoot))) {
+            for (int k = 0; k < kUnits; ++k) step_states8<TG>(t, blk + k, lane, a, b1, gs, seed_term);
+            return;
+        }
+    }
+    const float scale = scale_of(top_of), over = one_over(scale);
     if (lane < 2 * kUnits) ((lane & 1) ? t.v_scale : t.m_scale)[blk + (lane >> 1)] = scale;
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        Unit8<TP, TG> &u = us[k];
         const long long e = first + k * kStateBlock;
         const float mover = __shfl_sync(0xffffffffu, over, 2 * k), rover = __shfl_sync(0xffffffffu, over, 2 * k + 1);
-        unsigned top[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned c = e4m3_nearest(mul2(m[k][i], both(mover)));
-            if (i & 1) u.m.w[i >> 1] |= c << 16;
-            else u.m.w[i >> 1] = c;
-            const float2 y = mul2(r[k][i], both(rover)), z = mul2(y, both(0x1p-120f));
-            const unsigned pair = (unsigned)(e + lane_element<kAccess>(lane, 2 * i)) >> 1;
-            if (kAccess != kAnyAlignment) {
-                const unsigned h = pair_hash(pair, seed_term);
-                top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h, 0, 0x4104));          // low half at bit 8
-                top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h, 0, 0x4324));      // high half at bit 8
-            } else {                                                                        // 32 elements apart, both of the lane's parity
-                const unsigned h0 = pair_hash(pair, seed_term), h1 = pair_hash(pair + 16, seed_term), pick = (lane & 1) ? 0x4324 : 0x4104;
-                top[2 * i] = e4m3_random_top(y.x, z.x, __byte_perm(h0, 0, pick));
-                top[2 * i + 1] = e4m3_random_top(y.y, z.y, __byte_perm(h1, 0, pick));
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            u.r.w[i] = __byte_perm(__byte_perm(top[4 * i], top[4 * i + 1], 0x0073), __byte_perm(top[4 * i + 2], top[4 * i + 3], 0x0073), 0x5410);
-        store_raw<code8, kAccess>(t.m, e, t.n, lane, u.m);
-        store_raw<code8, kAccess>(t.v, e, t.n, lane, u.r);
+        store_raw<code8, kAccess>(t.m, e, t.n, lane, moment_codes(m[k], mover));
+        store_raw<code8, kAccess>(t.v, e, t.n, lane, root_codes<kAccess>(r[k], rover, e, lane, seed_term));
     }
 }
 
@@ -396,7 +463,7 @@ __host__ __device__ __forceinline__ bool codes_on_8(const TensorEntry &t) {
     return ((reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v)) & 7u) == 0;
 }
 
-template <typename TP, typename TG, int kBits, int kEntries>
+template <typename TP, typename TG, int kBits, bool kExactRoots, int kEntries>
 __global__ void __launch_bounds__(kTensorThreads, TensorShape<TP, TG, kBits>::kBlocks)
 adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
     const float gs = tab.grad_scale ? __ldg(tab.grad_scale) : 1.f;
@@ -415,9 +482,9 @@ adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
             const int grouped = ((k + 1 < tab.n ? tab.e[k + 1].first_group : tab.groups) - t.first_group) * kGroup;
             const int blk = grouped + u - t.first_unit;
             if (codes_on_8(t) && (long long)(blk + 1) * kStateBlock <= t.n)
-                step_units8<TP, TG, kSkewed, 1>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+                step_units8<TP, TG, kSkewed, 1, kExactRoots>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
             else
-                step_units8<TP, TG, kAnyAlignment, 1>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+                step_units8<TP, TG, kAnyAlignment, 1, kExactRoots>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
         }
     }
     if constexpr (kBits == 8) {
@@ -428,8 +495,8 @@ adamw_tensors_kernel(const __grid_constant__ TensorTable<kEntries> tab) {
             k = find_tensor<true>(tab, u, k);
             const TensorEntry &t = tab.e[k];
             const int blk = (u - t.first_group) * kGroup;
-            if (skew(t.param) | skew(t.grad)) step_units8<TP, TG, kSkewed, kGroup>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
-            else step_units8<TP, TG, kAligned, kGroup>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+            if (skew(t.param) | skew(t.grad)) step_units8<TP, TG, kSkewed, kGroup, kExactRoots>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
+            else step_units8<TP, TG, kAligned, kGroup, kExactRoots>(t, blk, lane, tab.args, tab.b1, gs, tab.seed_term);
         }
     }
 }

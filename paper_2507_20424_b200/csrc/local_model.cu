@@ -301,7 +301,9 @@ int launch_tensors(TensorTable<kEntries> &tab, int sms, cudaStream_t s) {
         }
     }
     const long long warps = (long long)tab.units + tab.groups, blocks = (warps + kTensorWarps - 1) / kTensorWarps;
-    adamw_tensors_kernel<TP, TG, kBits, kEntries><<<(unsigned)(blocks < most ? blocks : most), kTensorThreads, 0, s>>>(tab);
+    const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+    if (kBits == 32 || sqrt2_is_enough(tab.args.eps, tab.args.inv_sqrt_bc2)) adamw_tensors_kernel<TP, TG, kBits, false, kEntries><<<grid, kTensorThreads, 0, s>>>(tab);
+    else adamw_tensors_kernel<TP, TG, kBits, kBits == 8, kEntries><<<grid, kTensorThreads, 0, s>>>(tab);
     return launched();
 }
 template <int kEntries>

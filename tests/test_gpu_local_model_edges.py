@@ -1,9 +1,11 @@
 """Orders, extremes and longer paths of a local step's operators on the GPU (the plain cases are in test_gpu_local_model.py)."""
+import numpy as np
 import pytest
 import torch
 
+import local_model_ref as ref
 from gpu_util import require_gpu
-from test_gpu_local_model import BF16, F32, check_grad, gen, policy_inputs, same_bits
+from test_gpu_local_model import BF16, F32, HP, check_grad, gen, policy_inputs, same_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -85,6 +87,38 @@ def test_adamw_tensors_keep_the_memory_that_they_write(b):
     assert [x.data_ptr() for x in held] == keep
     b.dppf_adamw_tensors(t, 0.1, 0.9, 0.999, 1e-8, 0.0, 1)
     assert torch.allclose(t.params[0], torch.full_like(p, 0.9)) and bool((p == 7).all())
+
+
+@pytest.mark.parametrize("size", [1e-22, 1e-20, 1e-19, 2e-18, 1e-17, 1e-16, 1e-15, 1e-12, 1e-9, 1e-8, 1e-6])
+@pytest.mark.parametrize("shift,spread", [(0, False), (1, False), (0, True)])
+@pytest.mark.parametrize("eps", [1e-30, 1e-8])
+def test_adamw_tensors_8_bits_of_tiny_gradients(b, size, shift, spread, eps):
+    """Second moments below the smallest normal number: codes and scales are the plain fp32 sequence's bit for bit, and the
+    update is that of its moments (rounded operations: 2e-6 relative, as for the other sizes)."""
+    n, f = 5000, np.float32
+    hp = dict(HP, eps=eps, weight_decay=0.0)
+    g = (torch.randn(n + shift, generator=gen(51), device="cuda") * size)[shift:]
+    if spread:                                                 # within a block, over twenty orders of magnitude
+        g *= torch.exp(-46 * torch.rand(n, generator=gen(52), device="cuda"))
+    p = torch.zeros(n + shift, device="cuda")[shift:]
+    t = b.AdamWTensors([p], [g], state_bits=8)
+    codes = lambda x: x.view(torch.uint8).cpu().numpy()  # noqa: E731
+    for step in (1, 2, 3):
+        old = codes(t.exp_avgs[0]), codes(t.exp_avg_sqs[0]), t.exp_avg_scales[0].cpu().numpy(), t.exp_avg_sq_scales[0].cpu().numpy()
+        p.zero_()
+        b.dppf_adamw_tensors(t, step=step, seed=step, **hp)
+        gk = g.cpu().numpy()
+        want = ref.adamw8_states(gk, *old, HP["beta1"], HP["beta2"], step)
+        for got, w in zip((codes(t.exp_avgs[0]), t.exp_avg_scales[0].cpu().numpy(), codes(t.exp_avg_sqs[0]), t.exp_avg_sq_scales[0].cpu().numpy()), want):
+            assert np.array_equal(got, w)
+        gb, b1, b2 = ref.blocks_of(gk), f(HP["beta1"]), f(HP["beta2"])
+        m = ref.blocks_of(ref.E4M3[old[0]].astype(f)) * old[2][:, None] * b1 + gb * f(1 - float(b1))
+        root = ref.blocks_of(ref.E4M3[old[1]].astype(f)) * old[3][:, None]
+        r = np.sqrt(root * root * b2 + gb * gb * f(1 - float(b2))).astype(np.float64)
+        want = -float(f(HP["lr"])) / (1 - float(b1) ** step) * m.astype(np.float64) / (r / np.sqrt(1 - float(b2) ** step) + float(f(hp["eps"])))
+        want = want.reshape(-1)[:n]
+        err = np.abs(p.double().cpu().numpy() - want)
+        assert np.all(err <= 2e-6 * np.abs(want) + 2.0 ** -149), float((err / np.abs(want).clip(2.0 ** -149)).max())
 
 
 # ---------------------------------------------------------------- refusals
