@@ -361,7 +361,8 @@ int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, cons
  * q < 1 - clip_low.  A == 0 leaves the KL term alone.  weight carries the mask and the normalisation
  * (e.g. mask / number of tokens); a row with weight 0, or with a target outside [0, V), is not read:
  * its logp is 0, its gradient row 0 and it adds nothing, whatever the row holds.
- * ref_logp NULL: no KL term (kl_coef must be 0, sums_out[1] is 0).  grad_logits NULL: forward only.
+ * ref_logp NULL: no KL term (kl_coef must be 0, sums_out[1] is 0).  ref_logp with kl_coef 0: k is summed and has no part
+ * in loss and gradient, even where it is infinite (a target of probability 0, a gap above 88).  grad_logits NULL: forward only.
  * grad_logits may be logits itself (same ld): the logits are replaced by their gradient; other overlaps
  * are refused.  Logits of -inf have probability 0; a row that holds NaN or +inf, or nothing but -inf,
  * gives NaN.  old_logp, ref_logp, advantage, weight, logp_out: device fp32[T]; sums_out: device fp32[3].

@@ -147,9 +147,11 @@ __device__ __forceinline__ RowTerms row_terms(const PolicyArgs &a, float lp, flo
     r.kl = 0.f;
     if (a.ref_logp) {
         const float gap = ref - lp, eg = expm1f(gap);
-        r.kl = eg - gap;
-        r.loss += a.kl_coef * r.kl;
-        r.slope -= a.kl_coef * eg;
+        r.kl = isinf(eg) ? eg : eg - gap;                         // (a gap of infinity is infinitely far, not NaN)
+        if (a.kl_coef != 0.f) {                                   // watched only: no part in either, however large it is
+            r.loss += a.kl_coef * r.kl;
+            r.slope -= a.kl_coef * eg;
+        }
     }
     return r;
 }

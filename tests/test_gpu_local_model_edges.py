@@ -75,6 +75,26 @@ def test_policy_rows_through_the_ring_give_up_soon(b, polls):
     assert same_bits(again.logp, good.logp) and same_bits(again.loss, good.loss)
 
 
+@pytest.mark.parametrize("V", [300, 9000, 40_000])
+def test_policy_kl_that_is_only_watched_leaves_loss_and_gradient_alone(b, V):
+    """kl_coef 0 with reference log-probabilities: however far they are away, the KL estimate alone shows it."""
+    i = policy_inputs(6, V, F32, 44, masked=0.0)
+    i["adv"][:] = torch.tensor([1.0, -1.0, 0.5, 2.0, 0.0, -0.3])
+    i["ref"][1] = i["old"][1] + 130.0                         # e^gap is beyond fp32
+    i["logits"][3, i["targets"][3]] = float("-inf")           # a target of probability 0
+    i["ref"][4] = float("-inf")
+    args, grads = (i["logits"], i["targets"], i["old"], i["adv"], i["weight"]), [torch.empty_like(i["logits"]) for _ in range(3)]
+    plain = b.dppf_policy_loss(*args, grad_logits=grads[0])
+    out = b.dppf_policy_loss(*args, ref_logp=i["ref"], kl_coef=0.0, grad_logits=grads[1])
+    assert same_bits(out.loss, plain.loss) and same_bits(out.logp, plain.logp) and same_bits(*grads[:2])
+    assert torch.isfinite(out.loss) and torch.isfinite(grads[1]).all() and float(out.kl) == float("inf")
+    near = torch.where(torch.isfinite(i["ref"]), i["ref"], i["old"])
+    near[1], near[3] = i["old"][1], i["old"][3]
+    counted = b.dppf_policy_loss(*args, ref_logp=near, kl_coef=0.1, grad_logits=grads[2])      # only the row of probability 0 is infinitely far
+    assert float(counted.kl) == float("inf") and float(counted.loss) == float("inf")
+    assert torch.isfinite(grads[2][[0, 1, 2, 4, 5]]).all()
+
+
 # ---------------------------------------------------------------- AdamW over many tensors
 
 def test_adamw_tensors_keep_the_memory_that_they_write(b):
