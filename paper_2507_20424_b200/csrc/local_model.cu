@@ -5,6 +5,8 @@
 //   adamw_tensors.cuh  AdamW over many tensors, optimiser state in fp32 or in 8 bits
 #include "dppf.h"
 
+#include <limits>
+
 #include "adamw_tensors.cuh"
 #include "embedding.cuh"
 #include "policy_loss.cuh"
@@ -470,7 +472,7 @@ int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld,
     if (T < 1 || T > DPPF_MAX_POLICY_TOKENS || V < 1 || V > DPPF_MAX_VOCABULARY || ld < V || ld > kMaxLd) return DPPF_ERR_INVALID_ARG;
     if (grad_logits && (ld_grad < V || ld_grad > kMaxLd)) return DPPF_ERR_INVALID_ARG;
     if (!all_finite({clip_low, clip_high, kl_coef, temperature}) || clip_low < 0.f || clip_low > 1.f || clip_high < 0.f || !(temperature > 0.f) ||
-        !std::isfinite(1.4426950408889634 / temperature))
+        1.4426950408889634 / (double)temperature > (double)FLT_MAX)         // neither that nor 1 / temperature is an fp32 number
         return DPPF_ERR_INVALID_ARG;
     if (!logits || !targets || !old_logp || !advantage || !weight || !sums_out || !logp_out || !ws) return DPPF_ERR_INVALID_ARG;
     if (kl_coef != 0.f && !ref_logp) return DPPF_ERR_INVALID_ARG;
@@ -511,6 +513,7 @@ int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld,
     a.log2e_t = (float)log2e_t;
     if ((double)a.log2e_t >= log2e_t) a.log2e_t = std::nextafterf(a.log2e_t, 0.f);
     a.log2e_t_rest = (float)(log2e_t - (double)a.log2e_t);
+    if (a.log2e_t_rest == 0.f) a.log2e_t_rest = std::numeric_limits<float>::denorm_min();   // 0 * -inf would be NaN
     a.inv_t = (float)(1.0 / (double)temperature);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     return type == DPPF_FLOAT32 ? launch_policy<float>(a, dev, s) : launch_policy<bf16>(a, dev, s);

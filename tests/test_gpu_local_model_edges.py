@@ -95,6 +95,30 @@ def test_policy_kl_that_is_only_watched_leaves_loss_and_gradient_alone(b, V):
     assert torch.isfinite(grads[2][[0, 1, 2, 4, 5]]).all()
 
 
+@pytest.mark.parametrize("V", [300, 9000, 40_000])
+@pytest.mark.parametrize("temperature", [1e30, 1e38, 1.7e38, 2.2e38, 3e38, 1e-38, 4.3e-39])
+def test_policy_at_extreme_temperatures(b, V, temperature):
+    """Towards infinity every logit above -inf is equally likely, towards zero the largest alone is."""
+    T = 4
+    x = (torch.randn(T, V, generator=gen(45), device="cuda") * 3).clamp(max=11)
+    x[:, ::3] = float("-inf")
+    y = torch.tensor([1, 2, 4, V - 1 if (V - 1) % 3 else V - 2], device="cuda")
+    if temperature < 1:
+        x[torch.arange(T), y] = 12.0
+    want = -np.log(V - len(range(0, V, 3))) if temperature > 1 else 0.0
+    one, grad = torch.ones(T, device="cuda"), torch.empty_like(x)
+    out = b.dppf_policy_loss(x, y, torch.full((T,), float(want), device="cuda"), one, one, temperature=temperature, grad_logits=grad)
+    assert torch.allclose(out.logp.cpu().double(), torch.full((T,), want, dtype=torch.float64), rtol=2e-6, atol=1e-6)
+    # e^lp - 1 at the target, e^lp elsewhere, over the temperature (fp32 has three digits left of 1e-38 / 200)
+    if 1 < temperature < 1e31:
+        p = np.exp(want)
+        d = torch.where(torch.isfinite(x), -p, 0.0).double()
+        d[torch.arange(T), y] += 1.0
+        assert torch.allclose(grad.double(), -d / temperature, rtol=1e-5, atol=0)
+    elif temperature > 1:
+        assert torch.isfinite(grad).all()
+
+
 # ---------------------------------------------------------------- AdamW over many tensors
 
 def test_adamw_tensors_keep_the_memory_that_they_write(b):
