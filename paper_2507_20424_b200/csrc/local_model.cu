@@ -510,7 +510,7 @@ int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld,
     a.clip_hi = (float)(1.0 + (double)clip_high);
     a.kl_coef = kl_coef;
     const double log2e_t = 1.4426950408889634 / (double)temperature;
-    a.log2e_t = (float)log2e_t;
+    a.log2e_t = a.log2e_t_near = (float)log2e_t;
     if ((double)a.log2e_t >= log2e_t) a.log2e_t = std::nextafterf(a.log2e_t, 0.f);
     a.log2e_t_rest = (float)(log2e_t - (double)a.log2e_t);
     if (a.log2e_t_rest == 0.f) a.log2e_t_rest = std::numeric_limits<float>::denorm_min();   // 0 * -inf would be NaN

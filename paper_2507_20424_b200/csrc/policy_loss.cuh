@@ -45,7 +45,8 @@ struct PolicyArgs {
     int chunk;                  // ... and that a bulk copy brings, into one of kPolicyChunks buffers (in turn, without a gradient)
     int spin;
     float clip_lo, clip_hi, kl_coef, inv_t;
-    float log2e_t, log2e_t_rest;                             // log2(e) / temperature = their sum, both above zero
+    float log2e_t, log2e_t_rest;                             // log2(e) / temperature = their sum, both above zero: for the sums
+    float log2e_t_near;                                      // ... to the nearest: for single exponentials
 };
 
 template <typename T> struct Vec16;      // the elements of a 16-byte vector, in pairs
@@ -307,15 +308,15 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
         if (rank == 0 && tid == 0) put_terms(a, row, r.lp, w * r.loss, w * r.kl, r.clipped ? w : 0.f);
 
         if (a.grad) {
-            const float c = w * r.slope * a.inv_t, cn = -c / s;
+            const float c = w * r.slope * a.inv_t, cn = -c / s, near = a.log2e_t_near;
             auto entry = [&](int e) {
-                const float f = exp2_fast((to_float(sx[e]) - m) * k) * cn;
+                const float f = exp2_fast((to_float(sx[e]) - m) * near) * cn;
                 g[e] = from_float<T>(e == y ? f + c : f);
             };
             if (same) {
                 uint4 *out = reinterpret_cast<uint4 *>(gv);
 #pragma unroll 4
-                for (int i = lo + tid; i < hi; i += kThreads) __stcs(out + i, slope_vector<T>(s_row[i], k, m, cn));
+                for (int i = lo + tid; i < hi; i += kThreads) __stcs(out + i, slope_vector<T>(s_row[i], near, m, cn));
                 if (tid < head - e_first) entry(e_first + tid);
                 else if (tid >= 32 && tid - 32 < e_last - tail) entry(tail + tid - 32);
                 const int at = (int)y + before - v0 * N;          // the target's place in the slice: written over by the
@@ -439,7 +440,7 @@ __global__ void __launch_bounds__(kShortThreads, kHold == 8 ? 4 : 8) policy_shor
         const RowTerms r = row_terms(a, (xy - m) * a.inv_t - logf(s), old, ref, A);
         if (lane == 0) put_terms(a, row, r.lp, w * r.loss, w * r.kl, r.clipped ? w : 0.f);
         if (a.grad) {
-            const float c = w * r.slope * a.inv_t, cn = -c / s;
+            const float c = w * r.slope * a.inv_t, cn = -c / s, near = a.log2e_t_near;
             const int at = (int)y + before;
 #pragma unroll
             for (int h = 0; h < kHold; ++h) {
@@ -449,7 +450,7 @@ __global__ void __launch_bounds__(kShortThreads, kHold == 8 ? 4 : 8) policy_shor
                 Vec16<T>::get(v[h], f);
 #pragma unroll
                 for (int j = 0; j < kPairs; ++j) {
-                    const float2 t = mul2(add2(f[j], both(-m)), both(k));
+                    const float2 t = mul2(add2(f[j], both(-m)), both(near));
                     f[j] = mul2(make_float2(exp2_fast(t.x), exp2_fast(t.y)), both(cn));
                 }
                 if (at / N == i) {

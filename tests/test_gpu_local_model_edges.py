@@ -119,6 +119,28 @@ def test_policy_at_extreme_temperatures(b, V, temperature):
         assert torch.isfinite(grad).all()
 
 
+@pytest.mark.parametrize("V", [1000, 9000, 40_000])
+def test_policy_gradient_far_below_the_maximum(b, V):
+    """Entries of e^-30 to e^-44 of the largest, at a temperature whose log2(e)/T lies just below an fp32 number (with a
+    significand near 1, where a whole step is 1.2e-7).  Relative error by the formula's steps: half a step of the exponent
+    below 64, 2^-19 log 2 = 1.32e-6; log2(e)/T to the nearest number, here 0.05 steps, 44 * 6e-9 = 2.6e-7; the exponential
+    2^-22 = 2.4e-7; the row's coefficient and the product four roundings, 2.4e-7: 2.1e-6 in all."""
+    temps = np.arange(np.float32(1.4421), np.float32(1.4426), np.float32(2.0) ** -23, dtype=np.float64).astype(np.float32)
+    k = 1.4426950408889634 / temps.astype(np.float64)
+    steps = (k - 1.0) * 2.0 ** 23
+    temps = temps[(steps % 1.0 > 0.95) & (steps % 1.0 < 0.99)][:4]
+    assert len(temps) == 4
+    for n, T in enumerate(temps.tolist()):
+        x = -(30 + 14 * torch.rand(1, V, generator=gen(46 + n), device="cuda")) * T
+        x[0, 17] = 0.0
+        one, grad = torch.ones(1, device="cuda"), torch.empty_like(x)
+        b.dppf_policy_loss(x, torch.tensor([17], device="cuda"), torch.zeros(1, device="cuda"), one, one, temperature=T, grad_logits=grad)
+        want = torch.exp(x.double() / T - torch.logsumexp(x.double() / T, 1, keepdim=True)) / T
+        off = ((grad.double() - want).abs() / want)[0]
+        off[17] = 0
+        assert float(off.max()) <= 2.1e-6, float(off.max())
+
+
 # ---------------------------------------------------------------- AdamW over many tensors
 
 def test_adamw_tensors_keep_the_memory_that_they_write(b):
