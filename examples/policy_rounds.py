@@ -33,6 +33,12 @@ def views(row):
     return {k: t.view(s) for (k, s), t in zip(SHAPES.items(), row[:sum(SIZES)].split(SIZES))}
 
 
+def clip_scale(norm):
+    """What gradients of this norm are multiplied by, as one CUDA number: a norm that is not finite goes on as it is, so that the
+    step is skipped (1 / inf would be 0, and the step a decay of everything, or NaN for an infinite gradient)."""
+    return torch.where(torch.isfinite(norm), 1.0 / norm.clamp(min=1.0), norm).view(1)
+
+
 class Worker:
     def __init__(self, row, grad_row, tokens, scale):
         self.p, self.g, self.tokens, self.scale = views(row), views(grad_row), tokens, scale
@@ -57,7 +63,7 @@ class Worker:
         binding.dppf_embedding_grad(dh @ self.p["hidden"].t(), context, self.g["embedding"], scale=self.scale, ws=self.embedding_ws)
         norm = torch.stack([t.norm() for t in self.g.values()]).norm()
         self.steps += 1
-        binding.dppf_adamw_tensors(self.optimiser, lr, 0.9, 0.99, 1e-8, 0.01, self.steps, grad_scale=(1.0 / norm.clamp(min=1.0)).view(1), seed=self.steps)
+        binding.dppf_adamw_tensors(self.optimiser, lr, 0.9, 0.99, 1e-8, 0.01, self.steps, grad_scale=clip_scale(norm), seed=self.steps)
         return out
 
 
