@@ -366,7 +366,8 @@ int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, cons
  * grad_logits may be logits itself (same ld): the logits are replaced by their gradient; other overlaps
  * are refused.  Logits of -inf have probability 0; a row that holds NaN or +inf, or nothing but -inf,
  * gives NaN.  old_logp, ref_logp, advantage, weight, logp_out: device fp32[T]; sums_out: device fp32[3].
- * clip_low in [0, 1], clip_high >= 0, temperature at least 4.24e-39 (1.4427 / FLT_MAX); 1 <= V <= DPPF_MAX_VOCABULARY.
+ * clip_low in [0, 1], clip_high >= 0, temperature at least 4.24e-39 (1.4427 / FLT_MAX); 1 <= V <= DPPF_MAX_VOCABULARY,
+ * 1 <= T <= DPPF_MAX_POLICY_TOKENS (the binding answers for no tokens).
  * ws: dppf_policy_workspace_bytes(T) bytes, 128-byte aligned, its first 256 bytes ZERO before the first
  * call (every call leaves them ready for the next; T may change).  dppf_device_status(ws, stream):
  * DPPF_ERR_TIMEOUT if a bounded wait on an asynchronous copy gave up (the rows concerned are NaN).

@@ -488,7 +488,7 @@ class PolicyLoss(NamedTuple):
     kl: torch.Tensor            # 0-d: sum of weight * KL estimate
     clipped: torch.Tensor       # 0-d: sum of weight over clipped tokens
     logp: torch.Tensor          # [T]
-    ws: torch.Tensor
+    ws: torch.Tensor            # the workspace used; what was given (or None) where there was no token
 
 
 def alloc_policy_workspace(T: int, device="cuda") -> torch.Tensor:
@@ -502,7 +502,7 @@ def alloc_policy_workspace(T: int, device="cuda") -> torch.Tensor:
 def dppf_policy_loss(logits, targets, old_logp, advantage, weight, ref_logp=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0,
                      temperature=1.0, grad_logits=None, ws=None) -> PolicyLoss:
     """Clipped policy loss with a KL term from ``logits[T, V]``; with ``grad_logits`` (may be ``logits``) also its
-    gradient.  ``weight`` carries mask and normalisation; rows with weight 0 are not read."""
+    gradient.  ``weight`` carries mask and normalisation; rows with weight 0 are not read.  No tokens: zero sums, no launch."""
     T, V, ld = _matrix(logits, "logits")
     dev, code = logits.device, _type(logits, "logits")
     if targets.device != dev or targets.numel() != T or targets.dtype not in _ID_BITS or not targets.is_contiguous():
@@ -516,6 +516,9 @@ def dppf_policy_loss(logits, targets, old_logp, advantage, weight, ref_logp=None
         if grad_logits.dtype != logits.dtype or grad_logits.device != dev or rows != T or cols != V:
             raise ValueError("grad_logits must have the type, shape and device of logits")
         grad_ptr = grad_logits.data_ptr()
+    if T == 0:
+        none = torch.zeros(3, dtype=torch.float32, device=dev)
+        return PolicyLoss(*none.unbind(), none[:0], ws)
     ws = alloc_policy_workspace(T, dev) if ws is None else _workspace(ws, dev)
     out = logits.new_empty(3 + T, dtype=torch.float32)
     sums_ptr = out.data_ptr()

@@ -52,6 +52,16 @@ def test_policy_gradient_in_place_over_clusters(b, dtype, T, V, stride):
     assert torch.allclose(a.logp, i["old"], rtol=0, atol=8e-5)    # two fp32 log-softmaxes, 1e-6 (2 + |lp| + log V) each
 
 
+def test_policy_loss_of_no_tokens(b):
+    x, z = torch.empty(0, 70, dtype=BF16, device="cuda"), torch.empty(0, device="cuda")
+    y = torch.empty(0, dtype=torch.int64, device="cuda")
+    for ws in (None, b.alloc_policy_workspace(5)):
+        out = b.dppf_policy_loss(x, y, z, z, z, ref_logp=z, kl_coef=0.1, grad_logits=x, ws=ws)
+        assert float(out.loss) == 0 and float(out.kl) == 0 and float(out.clipped) == 0 and out.logp.shape == (0,) and out.ws is ws
+    with pytest.raises(ValueError):
+        b.dppf_policy_loss(x, y, z, z, torch.empty(1, device="cuda"))
+
+
 @pytest.mark.parametrize("polls", [0, 1, 2])
 def test_policy_rows_through_the_ring_give_up_soon(b, polls):
     """A block whose threads disagree on whether a copy arrived in time waits for the copies that were started, and no others
