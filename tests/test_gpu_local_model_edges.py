@@ -5,7 +5,7 @@ import torch
 
 import local_model_ref as ref
 from gpu_util import require_gpu
-from test_gpu_local_model import BF16, F32, HP, check_grad, gen, policy_inputs, same_bits
+from test_gpu_local_model import BF16, EPS, F32, HALF, HP, check_grad, check_policy, gen, policy_inputs, same_bits, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -23,6 +23,40 @@ def test_lookup_gradient_sorts_long_sequences(b, T, V, H, alike):
     """A warp of the sort has more than 32 places, and more than it holds in registers; one, two and three digits."""
     check_grad(b, T, V, H, F32, F32, torch.int64, False, seed=T + V, alike=alike)
     check_grad(b, T, V, H, BF16, BF16, torch.int32, True, seed=T + V + 1, alike=alike)
+
+
+def large_ids(kind, T, V, seed):
+    g = gen(seed)
+    if kind == "padding":
+        return torch.full((T,), -1, device="cuda")
+    if kind == "dense":                                        # every row, or every so manieth, once or more
+        return (torch.randperm(T, generator=g, device="cuda") * V // T).clamp(max=V - 1)
+    if kind == "ends":                                         # a few rows at the table's ends and where its stretches meet
+        at = torch.tensor([0, 1, V // 4, V // 2, V - 20_000, V - 2, V - 1], device="cuda").clamp(min=0)
+        return at[torch.randint(0, len(at), (T,), generator=g, device="cuda")]
+    return (torch.exp(torch.rand(T, generator=g, device="cuda") * np.log(V + 1)) - 1).long().clamp(0, V - 1)
+
+
+@pytest.mark.parametrize("kind", ["dense", "some", "ends", "padding"])
+@pytest.mark.parametrize("T,V,H,ld,gt,tt", [(3000, 50_000, 1024, 1024, BF16, F32), (3001, 50_000, 1021, 1021, F32, F32), (1000, 300_007, 200, 208, F32, F32), (60_000, 60_000, 1024, 1024, BF16, BF16),
+                                            (70_000, 70_000, 513, 515, F32, BF16), (600, 400, 65_536, 65_536, BF16, F32)])
+def test_lookup_gradient_writes_every_row_of_a_large_table(b, kind, T, V, H, ld, gt, tt):
+    """Tables of more bytes than are zeroed beside the sort and the joins: rows are zeroed beside the sums too, except where their
+    ids occur."""
+    ids, go = large_ids(kind, T, V, T + H), torch.randn(T, H, generator=gen(T), device="cuda").to(gt)
+    table = torch.full((V, ld), float("nan"), dtype=tt, device="cuda")
+    b.dppf_embedding_grad(go, ids, table[:, :H], scale=0.75)
+    assert torch.isnan(table[:, H:]).all()
+    ok = ids >= 0
+    count = torch.bincount(ids[ok], minlength=V)
+    for a in range(0, V, 20_000):                              # a stretch of rows at a time
+        n = min(20_000, V - a)
+        here = ok & (ids >= a) & (ids < a + n)
+        rows = go[here].double() * 0.75
+        want, mags = (torch.zeros(n, H, dtype=torch.float64, device="cuda").index_add_(0, ids[here] - a, x) for x in (rows, rows.abs()))
+        got, c = table[a:a + n, :H].double(), count[a:a + n, None]
+        assert bool(((got - want).abs() <= (c + 3) * EPS * mags + HALF[tt] * want.abs()).all())
+        assert bool((got[c[:, 0] == 0] == 0).all())
 
 
 # ---------------------------------------------------------------- policy loss
@@ -50,6 +84,16 @@ def test_policy_gradient_in_place_over_clusters(b, dtype, T, V, stride):
         c = b.dppf_policy_loss(i["logits"], *args, grad_logits=i["logits"])
         assert same_bits(i["logits"], sep) and same_bits(a.logp, c.logp) and same_bits(a.loss, c.loss)
     assert torch.allclose(a.logp, i["old"], rtol=0, atol=8e-5)    # two fp32 log-softmaxes, 1e-6 (2 + |lp| + log V) each
+
+
+@pytest.mark.parametrize("stride,offset,gstride,goffset", [(100_001, 0, 100_008, 1), (100_008, 3, 100_001, 3), (100_008, 8, 100_016, 0)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_policy_gradient_rows_laid_out_otherwise_over_clusters(b, stride, offset, gstride, goffset, dtype):
+    i = policy_inputs(7, 100_001, dtype, 47, stride=stride, offset=offset)
+    grad = strided(7, 100_001, gstride, goffset, dtype)
+    check_policy(b, i, grad=grad)
+    grad.fill_(float("nan"))
+    assert torch.isnan(torch.empty(0, dtype=dtype, device="cuda").set_(grad.untyped_storage())).all()      # gaps untouched
 
 
 def test_policy_loss_of_no_tokens(b):
@@ -195,6 +239,60 @@ def test_adamw_tensors_8_bits_of_tiny_gradients(b, size, shift, spread, eps):
         want = want.reshape(-1)[:n]
         err = np.abs(p.double().cpu().numpy() - want)
         assert np.all(err <= 2e-6 * np.abs(want) + 2.0 ** -149), float((err / np.abs(want).clip(2.0 ** -149)).max())
+
+
+@pytest.mark.parametrize("pt,gt,eps", [(F32, F32, 1e-8), (F32, BF16, 1e-8), (BF16, F32, 1e-8), (BF16, BF16, 1e-8), (F32, F32, 1e-15), (BF16, BF16, 1e-15)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_adamw_tensors_8_bits_of_a_large_model(b, pt, gt, eps, packed):
+    """Enough elements that warps take four units at a time, and the rest of each tensor one at a time: codes and scales of two
+    steps are the plain fp32 sequence's bit for bit, the parameters those of the formula in 64 bits; what lies between the
+    tensors stays as it is.  Among them small tensors, one whose codes are not 8-byte aligned, one of tiny gradients."""
+    hp = dict(HP, eps=eps)
+    sizes = [1_300_007, 5, 900_001, 1023, 1024, 256, 70_001, 700_000, 1, 307_200, 4096 + 255]
+    odd, tiny = 6, 9
+    assert sum(n // 1024 for k, n in enumerate(sizes) if k != odd) >= 16 * torch.cuda.get_device_properties(0).multi_processor_count
+    g = gen(61)
+
+    def row_of(dtype, std, fill):
+        """Views at odd places of one row with a guard between them, or each on a boundary of 256; the row."""
+        starts, at = [], 1 if packed else 0
+        for n in sizes:
+            starts.append(at)
+            at += n + 1 if packed else -(-(n + 1) // 256) * 256
+        row = torch.full((at,), fill, dtype=dtype, device="cuda")
+        for a, n in zip(starts, sizes):
+            row[a:a + n] = (torch.randn(n, generator=g, device="cuda") * std).to(dtype)
+        inside = torch.zeros(at, dtype=torch.bool, device="cuda")
+        for a, n in zip(starts, sizes):
+            inside[a:a + n] = True
+        return row, [row[a:a + n] for a, n in zip(starts, sizes)], ~inside
+
+    prow, p, outside = row_of(pt, 0.02, 7.0)
+    grow, gr, _ = row_of(gt, 1e-2, float("nan"))
+    gr[tiny].copy_((gr[tiny].float() * 1e-17).to(gt))
+    code = lambda n, lead: torch.zeros(n + 8, dtype=torch.uint8, device="cuda")[lead:lead + n].view(torch.float8_e4m3fn)  # noqa: E731
+    states = [[code(n, 3 if k == odd else 0) for k, n in enumerate(sizes)] for _ in range(2)]
+    t = b.AdamWTensors(p, gr, state_bits=8, exp_avgs=states[0], exp_avg_sqs=states[1])
+    codes = lambda x: x.view(torch.uint8).cpu().numpy()  # noqa: E731
+    clip = torch.tensor([0.5], device="cuda")
+    for step in (1, 2):
+        old, st = [x.double().cpu().numpy() for x in p], [[codes(t.exp_avgs[k]), codes(t.exp_avg_sqs[k]), t.exp_avg_scales[k].cpu().numpy(), t.exp_avg_sq_scales[k].cpu().numpy()]
+                                                          for k in range(len(sizes))]
+        b.dppf_adamw_tensors(t, step=step, seed=step + 9, grad_scale=clip, **hp)
+        for k, n in enumerate(sizes):
+            gk = gr[k].float().cpu().numpy() * np.float32(0.5)
+            want = ref.adamw8_states(gk, *st[k], HP["beta1"], HP["beta2"], step + 9)
+            for got, w in zip((codes(t.exp_avgs[k]), t.exp_avg_scales[k].cpu().numpy(), codes(t.exp_avg_sqs[k]), t.exp_avg_sq_scales[k].cpu().numpy()), want):
+                assert np.array_equal(got, w), (k, n)
+            wp, _, _ = ref.adamw(old[k], gk.astype(np.float64), ref.decode(st[k][0], st[k][2], n), ref.decode(st[k][1], st[k][3], n) ** 2, step=step, **hp)
+            got = p[k].double().cpu().numpy()
+            assert np.all(np.abs(got - wp) <= HALF[pt] * np.abs(wp) + 2e-6 * (np.abs(wp) + np.abs(wp - old[k])) + 1e-9), (k, n)
+    assert bool((prow[outside] == 7).all()) and bool(torch.isnan(grow[outside]).all())
+    for ts in states:
+        for k, x in enumerate(ts):
+            whole = torch.empty(0, dtype=torch.uint8, device="cuda").set_(x.untyped_storage())
+            lead = 3 if k == odd else 0
+            assert not whole[:lead].any() and not whole[lead + sizes[k]:].any()
 
 
 # ---------------------------------------------------------------- refusals
