@@ -394,6 +394,11 @@ int dppf_policy_loss(const void *logits, int type, int64_t T, int V, int64_t ld,
  *   (largest magnitude of the block) / 448; m is rounded to nearest, sqrt(v) up or down in
  *   proportion by a hash of (element, seed) -- pass another seed each step, e.g. the step -- and never to
  *   zero unless it is zero.  The parameters are updated from the moments before they are rounded.
+ *   What rounding m to nearest costs: a step that changes m by less than half of e4m3's spacing (3 to 6 % of m) leaves it as
+ *   it is, so that after a gradient falls m stays above the average that it stands for.  Gradients that drop to 0.3 of their
+ *   size without any noise leave m at 1.8 times that average with beta1 = 0.9, 3.3 times (never moved) with 0.95, 2.6 times with 0.99;
+ *   noise of 30 % of the gradient undoes that with 0.9 (within 1 % in the median) and mostly with 0.95 (9 % above), with 0.99 it takes
+ *   noise of three times the gradient.  Where beta1 is above 0.95 take 32 bits.
  *   A gradient that is not finite makes its whole block of 256 states NaN (with 32 bits: one element).
  * bf16 parameters are rounded to nearest after the step (updates below half their spacing are lost; keep
  * fp32 parameters where that matters).  The arrays of one tensor must not overlap each other, and no two

@@ -533,8 +533,8 @@ def dppf_policy_loss(logits, targets, old_logp, advantage, weight, ref_logp=None
 class AdamWTensors:
     """The tensors of :func:`dppf_adamw_tensors`: parameters, gradients and optimiser state, held for as long as
     the object lives.  ``state_bits`` 32: fp32 moments; 8: e4m3 codes with one fp32 scale per 256 elements (of the
-    first moment, and of the root of the second).  State that is not given starts at zero.  ``decay``: factor on the
-    weight decay per tensor (default 1).
+    first moment, and of the root of the second; for beta1 up to 0.95, above which the first moment follows falling
+    gradients too slowly).  State that is not given starts at zero.  ``decay``: factor on the weight decay per tensor (default 1).
 
     The step writes to the memory that the tensors have when the object is made (and reads the gradients' when they are
     bound).  That memory is kept alive: a tensor that is given other memory later, as by ``p.data = q``, is not followed."""

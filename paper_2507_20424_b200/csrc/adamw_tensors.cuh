@@ -16,7 +16,9 @@ namespace {
 // The root is stored because e4m3 spans 2^18: of v itself that would be nine binary orders of the
 // gradient's size.  m is rounded to nearest.  sqrt(v) is rounded up or down at random (in proportion,
 // from a hash of element number and seed): with beta2 = 0.999 a step changes sqrt(v) by less than half
-// of e4m3's spacing, and rounded to nearest it would never move.  A root that is not zero is never
+// of e4m3's spacing, and rounded to nearest it would never move.  (m stops short in the same way where
+// (1 - beta1) |g - m| stays below half of its spacing, 3 to 6 % of m, and the gradients bring no noise of their own: 1.8
+// times its average after a drop to 0.3 with beta1 = 0.9, not at all with noise of 30 %.)  A root that is not zero is never
 // stored as zero, so no update is divided by eps alone.  The parameters' update uses the new
 // moments before they are rounded.  The state arithmetic is a fixed sequence of separately rounded fp32
 // operations (no fused multiply-adds), so that a few lines of plain code give the same codes.
