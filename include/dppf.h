@@ -316,8 +316,8 @@ int dppf_static_device_status(void *cuda_stream);
  *
  * The operators that a worker needs between two rounds when the replica is a language model.  They
  * work on ordinary tensors (any address that is aligned to the element type, any row stride; 16-byte
- * aligned rows run faster) of fp32 or bf16, in fp32 arithmetic with one rounding at the end; sums run
- * in a fixed order.  Streams, return values and "arguments are checked before any CUDA call" are as
+ * aligned rows run faster) of fp32 or bf16, in fp32 arithmetic, rounded to the result's type at the end; sums run
+ * in an order that the inputs' ids and sizes fix.  Streams, workspaces (calls that share one must be ordered on one stream), return values and "arguments are checked before any CUDA call" are as
  * above.  Type arguments are DPPF_FLOAT32 or DPPF_BFLOAT16; ids and targets are signed 32- or 64-bit
  * integers (id_bits, target_bits: 32 or 64), contiguous.
  */
@@ -328,7 +328,7 @@ int dppf_static_device_status(void *cuda_stream);
 #define DPPF_MAX_POLICY_TOKENS 16777216
 
 /*
- * Embedding lookup with a scale: out[t, 0..H) = scale * table[ids[t], 0..H), one rounding to out's
+ * Embedding lookup with a scale: out[t, 0..H) = scale * table[ids[t], 0..H), the fp32 product rounded to out's
  * type; zeros where ids[t] is outside [0, V) (padding).  table[V, ld_table], out[T, ld_out].
  * T == 0 does nothing.
  */
@@ -339,10 +339,12 @@ int dppf_embedding(const void *table, int table_type, int64_t V, int H, int64_t 
  * Its gradient: grad_table[v] = scale * (sum over t with ids[t] == v of grad_out[t]), or, with
  * accumulate != 0, that sum added to what grad_table holds.  Without accumulate every row of
  * grad_table is written (zeros for ids that do not occur); with it only the rows of ids that occur
- * are touched.  Ids outside [0, V) contribute nothing.  The tokens are sorted by id (stably), each sum
- * runs in token order in fp32 and is rounded once; results are the same from run to run for given sizes.
+ * are touched.  Ids outside [0, V) contribute nothing.  The tokens are sorted by id (stably) and each sum is
+ * formed in fp32 from parts that run in token order; in which order a long sum's parts are added depends on the ids and
+ * sizes alone, so results are the same from run to run.  The sum times scale is rounded to fp32 and then to the table's
+ * type; with accumulate it is rounded to fp32, and the addition rounds again.
  * Columns H..ld-1 are not touched.  ws: dppf_embedding_workspace_bytes(T, H) bytes, 128-byte aligned, no
- * initialisation (may be null when T == 0).  The helper returns 0 for invalid T or H.
+ * initialisation (may be null when T == 0; up to 512 tokens it is asked for but not used).  The helper returns 0 for invalid T or H.
  */
 size_t dppf_embedding_workspace_bytes(int64_t T, int H);
 int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, const void *ids, int id_bits, int64_t T,

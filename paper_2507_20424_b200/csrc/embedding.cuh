@@ -5,7 +5,7 @@
 namespace {
 
 // ---------------------------------------------------------------- lookup
-// out[t] = scale * table[id_t], zeros where id_t is outside [0, V).  One fp32 product, rounded once.
+// out[t] = scale * table[id_t], zeros where id_t is outside [0, V).  The fp32 product, rounded to out's type.
 // Bound by the bytes of the distinct rows and of the output.
 
 struct LookupArgs {
@@ -13,7 +13,7 @@ struct LookupArgs {
     void *out;
     long long ld_table, ld_out;   // elements
     long long T, V;
-    int groups;                   // groups of N elements in a row (the last may be short)
+    int groups;                   // groups of N elements in a row
     int H, ids64;
     unsigned rows_per_block;
     float scale;
@@ -71,7 +71,8 @@ __global__ void __launch_bounds__(kLookupThreads, 8) lookup_kernel(const LookupA
 
 // ---------------------------------------------------------------- gradient
 // dtable[v] = scale * sum over t with id_t = v of dout[t].  The tokens are sorted by id, stably, so that equal ids stand
-// together and each sum runs in token order: the result is the same from run to run, and no order of atomics matters.
+// together.  A sum runs in token order within a part (a tile, or a warp's stretch of few tokens); how a long sum's parts are added
+// depends on the ids and sizes alone: the result is the same from run to run, and no order of atomics matters.
 // The launches (count, place per digit, sums and zeros, joins) are each set up while the one before ends; up to
 // kFewTokens tokens take a single launch that sorts in every block.
 
@@ -260,7 +261,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_place_kernel(const Gra
 // The sorted tokens are cut into tiles of `tile` places.  A thread owns N columns of one tile and walks its
 // places, kAhead rows under way.  An id that starts in a tile and ends in it or in the next is added up and
 // written by the thread of the tile where it starts (the next tile passes over it).  Of a longer one every tile leaves
-// its part in the workspace, and the last launch adds the parts in tile order.
+// its part in the workspace, and the last launch adds the parts.
 
 constexpr int kReduceThreads = 256;
 constexpr int kMaxTile = 32;
@@ -428,7 +429,8 @@ __global__ void __launch_bounds__(kReduceThreads, 4) embedding_reduce_kernel(con
 }
 
 // A block looks through kJoinTiles tiles for long ids that start in one of them and adds each one's parts over 32 N columns,
-// several ids side by side: its warps are dealt out among them, and a warp takes every so manieth part.
+// several ids side by side: its warps are dealt out among them (1, 2, 4 or 8 an id, by how many long ids start in these tiles), a
+// warp adds every so manieth part, in tile order, and the warps' sums are added in theirs.
 constexpr int kJoinTiles = 32;
 constexpr int kJoinThreads = 256;
 constexpr int kJoinWarps = kJoinThreads / 32;

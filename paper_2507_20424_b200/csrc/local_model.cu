@@ -99,13 +99,13 @@ int group_width(int H, int wide, const void *p, int64_t ldp, int tp, const void 
 }
 
 template <typename TW, typename TO>
-int launch_lookup(LookupArgs a, int n, cudaStream_t s) {
+int launch_lookup(LookupArgs a, int n, int sms, cudaStream_t s) {
     a.groups = a.H / n;
     // two rounds of a thread's groups, at least one row a block
     long long rows = (2LL * kLookupAhead * kLookupThreads) / a.groups;
     if (rows < 1) rows = 1;
-    // short lookups: fewer rows a block, so that more blocks share the work
-    while (rows > 1 && (a.T + rows - 1) / rows < 592) rows = (rows + 1) / 2;
+    // short lookups: fewer rows a block, so that four blocks an SM share the work
+    while (rows > 1 && (a.T + rows - 1) / rows < 4LL * sms) rows = (rows + 1) / 2;
     a.rows_per_block = (unsigned)rows;
     const long long grid = (a.T + rows - 1) / rows;
     if (grid > INT_MAX) return DPPF_ERR_INVALID_ARG;
@@ -121,7 +121,8 @@ int launch_lookup(LookupArgs a, int n, cudaStream_t s) {
 bool rows_on_16(const void *p, int64_t ld, int type) { return aligned_to(p, 16) && (size_t)ld * type_bytes(type) % 16 == 0; }
 
 // Places of the sorted tokens that a thread walks: long enough that few sums are split, short enough that about
-// 2,000 threads an SM are at work, each on one of a row's `groups` (8 to 32).
+// 2,000 threads an SM are at work, each on one of a row's `groups` (8 to 32).  The SMs are a B200's 148 whatever the device: the
+// workspace is laid out by this, and its size is asked for without one.
 int reduce_tile(int64_t T, int groups) {
     const double rows = (double)T * groups / (148.0 * 2048.0);
     int tile = 8;
@@ -393,15 +394,16 @@ int dppf_embedding(const void *table, int table_type, int64_t V, int H, int64_t 
     const size_t out_bytes = matrix_bytes(T, H, ld_out, out_type);
     if (ranges_meet(out, out_bytes, table, matrix_bytes(V, H, ld_table, table_type)) || ranges_meet(out, out_bytes, ids, (size_t)T * (id_bits / 8)))
         return DPPF_ERR_INVALID_ARG;
-    if (current_device() < 0) return DPPF_ERR_CUDA;
+    const int dev = current_device(), sms = dev < 0 ? -1 : multiprocessors(dev);
+    if (sms < 0) return DPPF_ERR_CUDA;
     LookupArgs a;
     a.table = table; a.ids = ids; a.out = out;
     a.ld_table = ld_table; a.ld_out = ld_out; a.T = T; a.V = V; a.H = H; a.ids64 = id_bits == 64;
     a.scale = scale;
     const int n = group_width(H, out_type == DPPF_BFLOAT16 ? 8 : 4, table, ld_table, table_type, out, ld_out, out_type);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    if (table_type == DPPF_FLOAT32) return out_type == DPPF_FLOAT32 ? launch_lookup<float, float>(a, n, s) : launch_lookup<float, bf16>(a, n, s);
-    return out_type == DPPF_FLOAT32 ? launch_lookup<bf16, float>(a, n, s) : launch_lookup<bf16, bf16>(a, n, s);
+    if (table_type == DPPF_FLOAT32) return out_type == DPPF_FLOAT32 ? launch_lookup<float, float>(a, n, sms, s) : launch_lookup<float, bf16>(a, n, sms, s);
+    return out_type == DPPF_FLOAT32 ? launch_lookup<bf16, float>(a, n, sms, s) : launch_lookup<bf16, bf16>(a, n, sms, s);
 }
 
 size_t dppf_embedding_workspace_bytes(int64_t T, int H) {
