@@ -135,9 +135,6 @@ __device__ __forceinline__ unsigned cluster_map(const void *p, unsigned rank) {
 __device__ __forceinline__ void cluster_send2(unsigned a, float x, float y, unsigned bar) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(a), "f"(x), "f"(y), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void cluster_send1(unsigned a, float x, unsigned bar) {     // the same, 4 bytes
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(a), "f"(x), "r"(bar) : "memory");
-}
 
 // ---------------------------------------------------------------- launches that follow one another
 // The dependent launch may be scheduled from here on; it waits for this one's end before it reads.

@@ -13,7 +13,7 @@ namespace {
 // memory between the two, so that the row is read once and its gradient written once: the pass is bound by those bytes.
 // Each block copies its slice in with bulk asynchronous copies (each with its own mbarrier, so that the first is
 // used while the last is under way), forms a running maximum and sum per thread, and the warps of the cluster tell one
-// another a pair of numbers (and the target's logit), by asynchronous stores that the receiver counts (a cluster barrier instead, whose arrival
+// another a pair of numbers, by asynchronous stores that the receiver counts (a cluster barrier instead, whose arrival
 // is a fence behind all of a block's traffic: 350 us instead of 317 for 4,096 x 131,072 bf16, a quarter masked).  Without a
 // gradient nothing is kept: the chunks go through a ring of buffers.
 // Exponentials are base 2: e_v = 2^((x_v - max) log2e / temperature), with the difference formed first, so that rows of the
@@ -197,7 +197,6 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
     extern __shared__ __align__(128) uint4 s_row[];              // this block's slice, as aligned in the row, or the ring
     __shared__ unsigned long long s_bar[kPolicyChunks], s_told;  // s_told: the pairs of the cluster's warps
     __shared__ float2 s_stats[kPolicyMaxCluster * kWarps]; // one entry from each warp of the cluster
-    __shared__ float s_target;                                   // in a cluster that writes a gradient: the target's logit
     __shared__ int s_failed;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -209,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
     if (tid == 0) {
         for (int c = 0; c < kPolicyChunks; ++c) mbar_init(&s_bar[c], 1);
         mbar_init(&s_told, 1);
-        if (C > 1) mbar_expect_tx(&s_told, (unsigned)(C * kWarps * sizeof(float2) + (a.grad ? sizeof(float) : 0)));
+        if (C > 1) mbar_expect_tx(&s_told, (unsigned)(C * kWarps * sizeof(float2)));
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_failed = 0;
     }
@@ -241,11 +240,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
         if (tid == 0)
             for (int c = 0; c < min(chunks, kPolicyChunks); ++c) fetch(c);
         if (C > 1) cluster_arrive_relaxed();                      // this block's s_stats may be written
-        // The target's logit, before it is written over (grad may be logits): one block's threads meet at a barrier before they
-        // write; in a cluster the block that holds it sends it from its shared memory, with its pairs.  A read of it by the
-        // other blocks would not be ordered before the owner's write: what they send does not wait for their loads.
-        const bool told_target = C > 1 && a.grad;
-        float xy = told_target ? 0.f : to_float(x[y]);
+        const float xy = to_float(x[y]);                          // before it is written over (grad may be logits): see below
         const float old = __ldg(a.old_logp + row), A = __ldg(a.advantage + row);
         const float ref = a.ref_logp ? __ldg(a.ref_logp + row) : 0.f;
 
@@ -285,13 +280,13 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyArgs a) {
         bool told = true;
         if (C > 1) {                                              // every warp's pair goes to every block of the cluster
             cluster_wait();                                       // the other blocks have started
-            if (lane < C) {
-                cluster_send2(cluster_map(&s_stats[rank * kWarps + warp], lane), m, s, cluster_map(&s_told, lane));
-                if (told_target && warp == 0 && y >= e_first && y < e_last) cluster_send1(cluster_map(&s_target, lane), to_float(sx[y]), cluster_map(&s_told, lane));
-            }
+            // The block that holds the target's logit may write over it once it has all pairs, so a pair must not leave before the
+            // read of xy in its warp has come back.  The vote makes it wait: what is sent depends on every lane's xy (which,
+            // if it is NaN, makes the row NaN in any case).
+            if (__any_sync(0xffffffffu, isnan(xy))) s = __int_as_float(0x7fc00000);
+            if (lane < C) cluster_send2(cluster_map(&s_stats[rank * kWarps + warp], lane), m, s, cluster_map(&s_told, lane));
             // a block stays until it has been told by all, so nobody writes to one that has left
             told = mbar_wait_bounded(&s_told, 0, kSpinLimit);
-            if (told_target) xy = s_target;
         } else {
             if (lane == 0) s_stats[warp] = make_float2(m, s);
             __syncthreads();
