@@ -30,9 +30,11 @@ constexpr int kGroup = 4;                              // units that a warp take
 constexpr int kSmallTable = 50, kLargeTable = 440;     // table sizes: under 4 KB and 32 KB of launch parameters
 
 // Resident blocks an SM.  Fewer loads in flight run faster once there are enough of them, since reads and writes
-// share the memory: fp32 states with fp32 parameters and gradients 2 blocks (86.6M elements: 365 us; 3: 425 us), with
-// bf16 ones 3 (295 us; 2: 364 us, 4: 336 us), with one of each 3.  8-bit states are bound by instructions and registers: 2 blocks of
-// 128 registers and groups of four units (300M bf16: 534 us; groups of 2, 80 registers: 587 us; single units: 675 to 780 us).
+// share the memory: fp32 states with fp32 parameters and gradients 2 blocks (86.6M elements: 365 us; 3: 433 us, 4: 445), with
+// bf16 ones 3 (297 us; 2 and 4: 333 us), with one of each 3 as well, although fp32 parameters with bf16 gradients take 393 us so and
+// 355 with 2 (4: 422).  8-bit states are bound by instructions and registers: 2 blocks of 128 registers and groups of four units
+// (300M bf16: 534 us; 3 blocks and groups of 2: 587 us; 4 blocks and single units: 726 us).  fp32 parameters with fp32 gradients
+// are 28 bytes a thread short of registers there (86.6M in packed rows: 266 us; groups of 2: 299).
 template <typename TP, typename TG, int kBits>
 struct TensorShape { static constexpr int kBlocks = kBits == 8 || sizeof(TP) + sizeof(TG) == 8 ? 2 : 3; };
 
@@ -420,7 +422,7 @@ __device__ __forceinline__ void step_units8(const TensorEntry &t, int blk, int l
 // ---------------------------------------------------------------- fp32 states
 // Units need not begin where the tensor does: with `lead` elements before its start they lie on multiples of their own size
 // (else of 16 bytes) in all four arrays wherever the arrays' offsets allow it (tensors at the same places of packed rows: 86.6M
-// elements in 152 tensors 379 us; on multiples of 128 bytes 403, in accesses of any alignment 405 to 417).
+// elements in 152 tensors 365 us; on multiples of 16 bytes 390, in accesses of any alignment 420).
 
 template <typename TP, typename TG, int kAccess>
 __device__ __forceinline__ void step_unit32(const TensorEntry &t, long long first, int lane, const AdamArgs &a, float gs) {

@@ -26,10 +26,12 @@ __device__ __forceinline__ long long read_id(const void *ids, int ids64, long lo
 constexpr int kLookupThreads = 256;
 
 // A block takes rows_per_block rows; its threads walk the groups of those rows in memory order, kLookupAhead at a time.
-// N elements are 16 bytes of the output (16,384 rows of 1,024 from fp32 to bf16: 8 elements 13.0 us, 4 16.6; 26,214 of 5,120 from
-// bf16 to fp32: 4 elements 117 us, 8 136; both at half the occupancy of now) where rows of both tensors start on 16-byte boundaries and H allows it; 4 and 2 need
-// rows on boundaries of so many elements and such an H, 1 takes anything.
-constexpr int kLookupAhead = 2;      // groups that a thread has under way: full occupancy hides more than longer runs (4 and 8 ahead: 13.2 us, 153 us; 2: 11.9, 134)
+// N elements are 16 bytes of the output (16,384 rows of 1,024 from fp32 to bf16: 8 elements 11.9 us, 4 14.2; 26,214 of 5,120 from
+// bf16 to fp32: 4 elements 104 us, 8 130) where rows of both tensors start on 16-byte boundaries and H allows it; 4 and 2 need rows
+// on boundaries of so many elements and such an H, 1 takes anything.
+// Groups that a thread has under way, for the same two: 2 at full occupancy (32 registers) 11.9 and 104 us; 1 11.9 and 107; 4 at half
+// the occupancy 13.2 and 120, at full occupancy, out of registers, 25.6 and 116.
+constexpr int kLookupAhead = 2;
 
 template <typename TW, typename TO, int N>
 __global__ void __launch_bounds__(kLookupThreads, 8) lookup_kernel(const LookupArgs a) {

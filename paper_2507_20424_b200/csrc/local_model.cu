@@ -154,7 +154,7 @@ constexpr long long kZeroBytes = 65536, kEarlyBytes = 32LL << 20, kLateBytes = 4
 std::atomic<int> g_place_ready[2][kMaxDevices];
 
 // Threads side by side on a row's groups: a whole part of them that leaves the fewest of a block's threads idle.
-// Rows of 50 groups in 50 threads, tiles by the groups that a row has: 91,096 tokens of 200 fp32 45 us (in 64 threads
+// Rows of 50 groups in 50 threads, tiles by the groups that a row has: 91,096 tokens of 200 fp32 44 us (in 64 threads
 // and tiles by the width 55); of 473 groups, one element each, 20,011 tokens 37 us (44).
 int row_threads(int groups) {
     int best = kMinRowThreads;
@@ -221,12 +221,12 @@ int launch_grad_width(const GradArgs &a, int n, int dev, int sms, cudaStream_t s
 
 constexpr size_t kPolicyHeaderBytes = 256;
 constexpr int kPolicySliceMax = 200 * 1024;        // shared memory of one block's slice at most
-// Six blocks and more fit an SM: some load while others write.  4,096 x 131,072 bf16 in slices of 32 KB: 317 us, of 64 KB:
-// 343 us; with 64 threads a block 350, with 96 344 (slices of 32 KB).
+// Six blocks and more fit an SM: some load while others write.  4,096 x 131,072 bf16, a quarter masked, in slices of 32 KB: 319 us,
+// of 64 KB: 345 us; with 64 threads a block (slices of 32 KB) 352.
 constexpr int kPolicySliceGood = 36 * 1024;
 
-// Rows up to this size go to blocks of 64 threads: 8,000 x 8,192 bf16 30 us (128 threads: 34), 10,000 x 4,096 21 (26); of 32 KB
-// rows 128 threads are quicker (8,000 x 16,384: 52 us, 57).
+// Rows up to this size go to blocks of 64 threads (with a gradient, a quarter masked): 8,000 x 8,192 bf16 47 us (128 threads: 51),
+// 10,000 x 4,096 37 (47); for rows of 32 KB 128 threads are quicker (8,000 x 16,384: 83 us, 90).
 constexpr int kPolicyShortSlice = 24 * 1024;
 
 std::atomic<int> g_policy_ready[2][kMaxDevices];
@@ -250,7 +250,7 @@ int launch_policy(PolicyArgs a, int dev, cudaStream_t s) {
     auto slice_bytes = [&](int c) { return (vectors + c - 1) / c * 16; };
     while (a.grad && C < kPolicyMaxCluster && slice_bytes(C) > kPolicySliceGood) C *= 2;
     // few rows: split them further while SMs are idle and a slice stays above 8 KB; rows that are only read also while
-    // there are fewer than 8 blocks an SM and a slice stays above 16 KB (388 x 187,236 bf16: 37 us, 41 with 2)
+    // there are fewer than 8 blocks an SM and a slice stays above 16 KB (388 x 187,236 bf16: 36 us, 41 with 2)
     while (C < kPolicyMaxCluster && (((long long)a.T * C < 2LL * sms && slice_bytes(C) > 16 * 1024) ||
                                      (!a.grad && (long long)a.T * C < 8LL * sms && slice_bytes(C) > 32 * 1024))) C *= 2;
     a.slice = (vectors + C - 1) / C;
