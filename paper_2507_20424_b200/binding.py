@@ -557,34 +557,42 @@ class AdamWTensors:
             given = list(given)
             if len(given) != n:
                 raise ValueError(f"{what} must have one entry per tensor")
-            return [_vector(t, c, what, self.device, (kind,)).detach() for t, c in zip(given, counts)]
+            return [_vector(t, c, what, self.device, (kind,)) for t, c in zip(given, counts)]
 
         for p in self.params:
             _vector(p, p.numel(), "params", self.device, (self.params[0].dtype,))
         if not self.params[0].is_cuda:
             raise ValueError("params must be CUDA tensors")
-        self.params = [p.detach() for p in self.params]           # aliases: they hold the memory even if p gets another
         self.exp_avgs = state(exp_avgs, sizes, dtype, "exp_avgs")
         self.exp_avg_sqs = state(exp_avg_sqs, sizes, dtype, "exp_avg_sqs")
         self.exp_avg_scales = self.exp_avg_sq_scales = None
         if state_bits == 8:
             self.exp_avg_scales = state(exp_avg_scales, blocks, torch.float32, "exp_avg_scales")
             self.exp_avg_sq_scales = state(exp_avg_sq_scales, blocks, torch.float32, "exp_avg_sq_scales")
-        # what the step writes, in order of address: all tensors are updated side by side, so none may share memory (as tied weights
-        # listed twice would)
-        written = sorted((t.data_ptr(), t.nbytes) for ts in (self.params, self.exp_avgs, self.exp_avg_sqs, self.exp_avg_scales, self.exp_avg_sq_scales)
-                         for t in ts or () if t.numel())
-        if any(at + size > after for (at, size), (after, _) in zip(written, written[1:])):
-            raise ValueError("parameters and optimiser states must not overlap")
         self.decay = [1.0] * n if decay is None else [float(d) for d in decay]
         if len(self.decay) != n:
             raise ValueError("decay must have one entry per tensor")
-        self._table = (_Tensor * n)()
-        for k, e in enumerate(self._table):
-            e.param, e.numel, e.decay = self.params[k].data_ptr(), sizes[k], self.decay[k]
-            e.exp_avg, e.exp_avg_sq = self.exp_avgs[k].data_ptr(), self.exp_avg_sqs[k].data_ptr()
-            if state_bits == 8:
-                e.exp_avg_scale, e.exp_avg_sq_scale = self.exp_avg_scales[k].data_ptr(), self.exp_avg_sq_scales[k].data_ptr()
+        width, code = self.params[0].element_size(), state_bits // 8
+        arrays = [("param", self.params, sizes, width), ("exp_avg", self.exp_avgs, sizes, code), ("exp_avg_sq", self.exp_avg_sqs, sizes, code)]
+        if state_bits == 8:
+            arrays += [("exp_avg_scale", self.exp_avg_scales, blocks, 4), ("exp_avg_sq_scale", self.exp_avg_sq_scales, blocks, 4)]
+        self._table, self._sizes, self._memory = (_Tensor * n)(), sizes, []
+        for e, count, d in zip(self._table, sizes, self.decay):
+            e.numel, e.decay = count, d
+        starts, ends = [], []                                     # of what the step writes
+        for field, ts, counts, each in arrays:
+            at = [t.data_ptr() for t in ts]
+            for e, pointer in zip(self._table, at):
+                setattr(e, field, pointer)
+            self._memory += [t.untyped_storage() for t in ts]     # stays, even if a tensor is given other memory
+            starts += [a for a, c in zip(at, counts) if c]
+            ends += [a + c * each for a, c in zip(at, counts) if c]
+        # All tensors are updated side by side, so none may share memory (as tied weights listed twice would): in order, each start is
+        # past the end before it.
+        starts.sort()
+        ends.sort()
+        if any(after < end for after, end in zip(starts[1:], ends)):
+            raise ValueError("parameters and optimiser states must not overlap")
         self.bind_grads(grads)
 
     def bind_grads(self, grads) -> None:
@@ -593,9 +601,11 @@ class AdamWTensors:
         if len(grads) != len(self.params):
             raise ValueError("grads must have one entry per tensor")
         self.grad_type = _type(grads[0], "grads")
-        for p, g in zip(self.params, grads):
-            _vector(g, p.numel(), "grads", self.device, (grads[0].dtype,))
-        self.grads = [g.detach() for g in grads]
+        kind, dev = grads[0].dtype, self.device
+        for n, g in zip(self._sizes, grads):                      # quickly; _vector says what is wrong
+            if g.dtype is not kind or g.numel() != n or g.device != dev or not g.is_contiguous():
+                _vector(g, n, "grads", dev, (kind,))
+        self.grads, self._grad_memory = grads, [g.untyped_storage() for g in grads]
         for e, g in zip(self._table, grads):
             e.grad = g.data_ptr()
 

@@ -198,15 +198,18 @@ def test_policy_gradient_far_below_the_maximum(b, V):
 # ---------------------------------------------------------------- AdamW over many tensors
 
 def test_adamw_tensors_keep_the_memory_that_they_write(b):
-    p, g, m, v = (torch.full((1000,), x, device="cuda") for x in (1.0, 0.5, 0.0, 0.0))
+    n = 5_000_000                                              # blocks of their own in the allocator
+    p, g, m, v = (torch.full((n,), x, device="cuda") for x in (1.0, 0.5, 0.0, 0.0))
     t = b.AdamWTensors([p], [g], exp_avgs=[m], exp_avg_sqs=[v])
-    keep = [x.data_ptr() for x in (p, g, m, v)]
+    keep = {x.data_ptr() for x in (p, g, m, v)}
     for x in (p, g, m, v):
-        x.data = torch.full_like(x, 7.0)                       # other memory; the old would be free
-    held = (t.params[0], t.grads[0], t.exp_avgs[0], t.exp_avg_sqs[0])
-    assert [x.data_ptr() for x in held] == keep
+        x.data = torch.zeros(1, device="cuda")                 # other memory; the old would be free
+    others = [torch.full((n,), 7.0, device="cuda") for _ in range(8)]
+    assert not keep & {x.data_ptr() for x in others}
     b.dppf_adamw_tensors(t, 0.1, 0.9, 0.999, 1e-8, 0.0, 1)
-    assert torch.allclose(t.params[0], torch.full_like(p, 0.9)) and bool((p == 7).all())
+    assert all(bool((x == 7).all()) for x in others)
+    del t
+    assert keep & {torch.empty(n, device="cuda").data_ptr() for _ in range(1)}                # and lets it go with the object
 
 
 @pytest.mark.parametrize("size", [1e-22, 1e-20, 1e-19, 2e-18, 1e-17, 1e-16, 1e-15, 1e-12, 1e-9, 1e-8, 1e-6])
