@@ -437,6 +437,7 @@ __global__ void __launch_bounds__(kShortThreads, kHold == 8 ? 4 : 8) policy_shor
         if (a.grad) {
             const float c = w * r.slope * a.inv_t, cn = -c / s, near = a.log2e_t_near;
             const int at = (int)y + before;
+            __syncwarp();                                         // every lane has its xy before one writes over it (grad may be logits)
 #pragma unroll
             for (int h = 0; h < kHold; ++h) {
                 const int i = lane + 32 * h;

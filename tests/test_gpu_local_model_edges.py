@@ -129,6 +129,21 @@ def test_policy_rows_through_the_ring_give_up_soon(b, polls):
     assert same_bits(again.logp, good.logp) and same_bits(again.loss, good.loss)
 
 
+@pytest.mark.parametrize("dtype,T,V,stride", [(BF16, 20_000, 1000, 1000), (F32, 5000, 1021, 1025), (BF16, 9000, 257, 259), (F32, 3000, 4001, 4001)])
+def test_policy_gradient_in_place_of_short_rows(b, dtype, T, V, stride):
+    i = policy_inputs(T, V, dtype, 48, stride=stride)
+    live = i["weight"] != 0
+    i["targets"][live] = edge_targets(V, int(live.sum()), 49)
+    keep, sep = strided(T, V, stride, 0, dtype), torch.empty_like(i["logits"])
+    keep.copy_(i["logits"])
+    args = (i["targets"], i["old"], i["adv"], i["weight"])
+    a = b.dppf_policy_loss(keep, *args, grad_logits=sep)
+    for _ in range(3):
+        i["logits"].copy_(keep)
+        c = b.dppf_policy_loss(i["logits"], *args, grad_logits=i["logits"])
+        assert same_bits(i["logits"], sep) and same_bits(a.logp, c.logp) and same_bits(a.loss, c.loss)
+
+
 @pytest.mark.parametrize("V", [300, 9000, 40_000])
 def test_policy_kl_that_is_only_watched_leaves_loss_and_gradient_alone(b, V):
     """kl_coef 0 with reference log-probabilities: however far they are away, the KL estimate alone shows it."""
