@@ -312,7 +312,7 @@ int dppf_consensus_static(float *x, int M, int64_t d, int64_t ld, float alpha, f
 int dppf_static_device_status(void *cuda_stream);
 
 /*
- * ---- A worker's local step on a language model: first layer, loss, optimiser -------------------
+ * ---- A worker's local step on a language model: layers, loss, optimiser ------------------------
  *
  * The operators that a worker needs between two rounds when the replica is a language model.  They
  * work on ordinary tensors (any address that is aligned to the element type, any row stride; 16-byte
@@ -350,6 +350,65 @@ size_t dppf_embedding_workspace_bytes(int64_t T, int H);
 int dppf_embedding_grad(const void *grad_out, int out_type, int64_t ld_out, const void *ids, int id_bits, int64_t T,
                         float scale, void *grad_table, int table_type, int64_t V, int H, int64_t ld_table,
                         int accumulate, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Layer norm after a residual addition.  For row t of x[T, ld_x] (H columns), with weight w[H] and bias b[H] (NULL: none):
+ *   h = x + branch, rounded to x's type and written to sum_out   (branch NULL: h = x, and sum_out is NULL)
+ *   mean_out[t] = mu = mean h;   rstd_out[t] = r = (mean (h - mu)^2 + eps)^(-1/2);   out[t] = (h - mu) r w + b
+ * sum_out has x's type and may be x itself (same ld); other overlaps of what is written are refused.  branch, out and the weight
+ * (bias: the weight's type) have types of their own.  mean_out, rstd_out: device fp32[T], for the gradient.  The mean is taken
+ * first and the squares about it; deviations above 1e18 overflow.  eps >= 0; with eps 0 a row of equal values has no defined result.  A row
+ * that holds NaN or an infinity is NaN, the others are as they are.  T == 0 does nothing.
+ */
+int dppf_layer_norm(const void *x, int x_type, int64_t ld_x, const void *branch, int branch_type, int64_t ld_branch,
+                    const void *weight, const void *bias, int weight_type, int64_t T, int H, float eps, void *sum_out,
+                    int64_t ld_sum, void *out, int out_type, int64_t ld_out, float *mean_out, float *rstd_out, void *cuda_stream);
+
+/*
+ * Its gradient, from x (the h of above), mean and rstd:  u = w grad_out, xh = (x - mu) r,
+ *   grad_x = r (u - mean u - xh mean(u xh)) + grad_sum,   grad_weight = sum_t grad_out xh,   grad_bias = sum_t grad_out
+ * grad_sum (NULL: none; x's type): the gradient that reaches h past the norm.  grad_x (x's type) is the gradient of x and of
+ * branch; it may be grad_sum or, where the types agree, grad_out itself (same ld).  grad_weight[H] and grad_bias[H] (NULL: not
+ * wanted) are of grad_type, written or, with accumulate != 0, added to.  The sums over tokens are formed in fp32, in an order that T and H
+ * fix, and rounded to grad_type at the end (accumulate: once more by the addition).  T == 0: zeros (accumulate: nothing).
+ * ws: dppf_layer_norm_workspace_bytes(T, H) bytes, 128-byte aligned, no initialisation.  The helper returns 0 for invalid T or H.
+ */
+size_t dppf_layer_norm_workspace_bytes(int64_t T, int H);
+int dppf_layer_norm_grad(const void *grad_out, int out_type, int64_t ld_out, const void *x, int x_type, int64_t ld_x,
+                         const float *mean, const float *rstd, const void *weight, int weight_type, int64_t T, int H,
+                         const void *grad_sum, int64_t ld_grad_sum, void *grad_x, int64_t ld_grad_x, void *grad_weight,
+                         void *grad_bias, int grad_type, int accumulate, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Rotary positions.  Element i of head h of token t of x lies at x[t * ld_x + h * head_x + i] (heads side by side in a token's
+ * row, or each head's tokens in a block of their own).  Of a head's D elements the first `turned` (even) form pairs: (2i, 2i + 1)
+ * if interleaved != 0, else (i, i + turned / 2).  With a = positions[t] * frequencies[i]:
+ *   (x1, x2) -> scale (x1 cos a - x2 sin a, x2 cos a + x1 sin a);   inverse != 0: a is negated.
+ * The inverse with the same scale is the gradient.  The rest of a head is copied.  out may be x (same strides: in place).
+ * positions: int32 or int64 [T] (position_bits); frequencies: device fp64[turned / 2].  The angle is formed and reduced in fp64, the
+ * rest computed in fp32.  x and out are of one type.  T == 0 does nothing.
+ */
+#define DPPF_MAX_HEADS 1024
+#define DPPF_MAX_HEAD_WIDTH 1024
+int dppf_rotary(const void *x, int type, int64_t ld_x, int64_t head_x, int64_t T, int heads, int D, int turned, int interleaved,
+                const void *positions, int position_bits, const double *frequencies, float scale, int inverse, void *out,
+                int64_t ld_out, int64_t head_out, void *cuda_stream);
+
+/*
+ * Host side: frequencies_host[i] = base^(-2i / turned) for i < turned / 2, adapted to contexts `factor` times as long as those
+ * that a model was trained with, and the scale to pass on (1 but for BY_PARTS).  No CUDA call.
+ *   PLAIN         as they are
+ *   INTERPOLATED  divided by factor (arXiv 2306.15595)
+ *   STRETCHED     of the base times factor^(turned / (turned - 2)): the slowest is divided by factor, the fastest stays
+ *   BY_PARTS      those that turn less than once over original_length are divided by factor, those that turn 32 times and more stay,
+ *                 in between linearly; scale 0.1 ln(factor) + 1 (arXiv 2309.00071)
+ */
+#define DPPF_POSITIONS_PLAIN 0
+#define DPPF_POSITIONS_INTERPOLATED 1
+#define DPPF_POSITIONS_STRETCHED 2
+#define DPPF_POSITIONS_BY_PARTS 3
+int dppf_rotary_frequencies(int turned, double base, int scaling, double factor, int64_t original_length, double *frequencies_host,
+                            float *scale_host);
 
 /*
  * Clipped policy loss with a KL term, from logits[T, ld] (V columns of `type`), with its gradient.

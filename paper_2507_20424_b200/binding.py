@@ -26,6 +26,7 @@ EXPORTS = ("dppf_workspace_bytes", "dppf_consensus", "dppf_consensus_ex", "dppf_
            "dppf_consensus_rounds", "dppf_consensus_rounds_ex", "dppf_debug_set_poll_limits",
            "dppf_adamw_step", "dppf_adamw_step_and_consensus",
            "dppf_embedding", "dppf_embedding_grad", "dppf_embedding_workspace_bytes",
+           "dppf_layer_norm", "dppf_layer_norm_grad", "dppf_layer_norm_workspace_bytes", "dppf_rotary", "dppf_rotary_frequencies",
            "dppf_policy_loss", "dppf_policy_workspace_bytes", "dppf_adamw_tensors",
            "dppf_lambda_schedule", "dppf_lr_cosine", "dppf_qsr_period", "dppf_round_metrics")
 
@@ -119,6 +120,16 @@ def load(rebuild_if_stale: bool = False) -> ctypes.CDLL:
     lib.dppf_embedding_workspace_bytes.restype = sz
     lib.dppf_embedding_grad.argtypes = [vp, i32, i64, vp, i32, i64, f32, vp, i32, i64, i32, i64, i32, vp, sz, vp]
     lib.dppf_embedding_grad.restype = i32
+    lib.dppf_layer_norm.argtypes = [vp, i32, i64, vp, i32, i64, vp, vp, i32, i64, i32, f32, vp, i64, vp, i32, i64, vp, vp, vp]
+    lib.dppf_layer_norm.restype = i32
+    lib.dppf_layer_norm_workspace_bytes.argtypes = [i64, i32]
+    lib.dppf_layer_norm_workspace_bytes.restype = sz
+    lib.dppf_layer_norm_grad.argtypes = [vp, i32, i64, vp, i32, i64, vp, vp, vp, i32, i64, i32, vp, i64, vp, i64, vp, vp, i32, i32, vp, sz, vp]
+    lib.dppf_layer_norm_grad.restype = i32
+    lib.dppf_rotary.argtypes = [vp, i32, i64, i64, i64, i32, i32, i32, i32, vp, i32, vp, f32, i32, vp, i64, i64, vp]
+    lib.dppf_rotary.restype = i32
+    lib.dppf_rotary_frequencies.argtypes = [i32, ctypes.c_double, i32, ctypes.c_double, i64, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(f32)]
+    lib.dppf_rotary_frequencies.restype = i32
     lib.dppf_policy_workspace_bytes.argtypes = [i64]
     lib.dppf_policy_workspace_bytes.restype = sz
     lib.dppf_policy_loss.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, i64, vp, sz, vp]
@@ -481,6 +492,130 @@ def dppf_embedding_grad(grad_out, ids, grad_table, scale=1.0, accumulate=False, 
     _call(dev, load().dppf_embedding_grad, "dppf_embedding_grad", flat.data_ptr(), _type(flat, "grad_out"), ld_out, ids.data_ptr(), _ID_BITS[ids.dtype], T, scale,
           grad_table.data_ptr(), _type(grad_table, "grad_table"), V, H, ld, int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
     return ws
+
+
+class LayerNorm(NamedTuple):
+    out: torch.Tensor           # [..., H]
+    sum: torch.Tensor           # x + branch, the row that was normalised (x itself without a branch)
+    mean: torch.Tensor          # fp32, one entry a row
+    rstd: torch.Tensor
+
+
+def _rows(t: torch.Tensor, shape, what: str, device, dtype=None):
+    """(pointer, row stride) of the rows of t, which has this shape (the last dimension its columns), this device and, if given, this type."""
+    if t.shape != shape or t.device != device or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{what} must be a tensor of shape {tuple(shape)}{'' if dtype is None else f' and type {dtype}'} on {device}")
+    _, _, ld = _matrix(t if t.dim() == 2 else t.view(-1, shape[-1]), what)
+    return t.data_ptr(), ld
+
+
+def dppf_layer_norm(x, weight, bias=None, eps=1e-5, branch=None, sum_out=None, out=None, out_dtype=None) -> LayerNorm:
+    """Layer norm of the rows of ``x[..., H]`` or, with ``branch``, of ``x + branch``, which is written to ``sum_out`` (may be ``x``;
+    new if not given).  ``out_dtype`` (default: x's) is used when ``out`` is not given."""
+    shape, dev, H = x.shape, x.device, x.shape[-1] if x.dim() else 0
+    px, ld_x = _rows(x, shape, "x", dev)
+    T = x.numel() // H if H else 0
+    for t in (weight, bias):
+        if t is not None and (t.dtype != weight.dtype or t.numel() != H or t.device != dev or not t.is_contiguous()):
+            _vector(t, H, "weight and bias", dev, (weight.dtype,))
+    pb, tb, ld_b, ps, ld_s = None, FLOAT32, 0, None, 0
+    if branch is not None:
+        pb, ld_b = _rows(branch, shape, "branch", dev)
+        tb = _type(branch, "branch")
+        if sum_out is None:
+            sum_out = x.new_empty(shape)
+        ps, ld_s = _rows(sum_out, shape, "sum_out", dev, x.dtype)
+    elif sum_out is not None:
+        raise ValueError("sum_out is for the sum with a branch")
+    if out is None:
+        out = x.new_empty(shape, dtype=out_dtype)
+    po, ld_o = _rows(out, shape, "out", dev)
+    stats = x.new_empty((2, *shape[:-1]), dtype=torch.float32)
+    at = stats.data_ptr()
+    _call(dev, load().dppf_layer_norm, "dppf_layer_norm", px, _type(x, "x"), ld_x, pb, tb, ld_b, weight.data_ptr(), _ptr(bias), _type(weight, "weight"), T, H, eps, ps, ld_s,
+          po, _type(out, "out"), ld_o, at, at + 4 * T)
+    mean, rstd = stats.unbind()
+    return LayerNorm(out, x if sum_out is None else sum_out, mean, rstd)
+
+
+def alloc_layer_norm_workspace(T: int, H: int, device="cuda") -> torch.Tensor:
+    n = int(load().dppf_layer_norm_workspace_bytes(int(T), int(H)))
+    if n == 0:
+        raise ValueError("invalid T or H")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def dppf_layer_norm_grad(grad_out, x, mean, rstd, weight, grad_weight, grad_bias=None, grad_sum=None, grad_x=None, accumulate=False, ws=None):
+    """Gradient of :func:`dppf_layer_norm` from its ``sum`` (here ``x``), ``mean`` and ``rstd``: written to (or, with ``accumulate``, added
+    to) ``grad_weight`` and ``grad_bias``; returns that of x and of the branch, in ``grad_x`` (may be ``grad_sum`` or ``grad_out``; new if
+    not given), with ``grad_sum``, the gradient that reaches the sum past the norm, added."""
+    shape, dev, H = x.shape, x.device, x.shape[-1] if x.dim() else 0
+    px, ld_x = _rows(x, shape, "x", dev)
+    T = x.numel() // H if H else 0
+    pg, ld_g = _rows(grad_out, shape, "grad_out", dev)
+    for t in (mean, rstd):
+        if t.dtype is not torch.float32 or t.numel() != T or t.device != dev or not t.is_contiguous():
+            _vector(t, T, "mean and rstd", dev)
+    _vector(weight, H, "weight", dev, tuple(_TYPES))
+    for t in (grad_weight, grad_bias):
+        if t is not None and (t.dtype != grad_weight.dtype or t.numel() != H or t.device != dev or not t.is_contiguous()):
+            _vector(t, H, "grad_weight and grad_bias", dev, (grad_weight.dtype,))
+    ps, ld_s = (None, 0) if grad_sum is None else _rows(grad_sum, shape, "grad_sum", dev, x.dtype)
+    if grad_x is None:
+        grad_x = x.new_empty(shape)
+    pd, ld_d = _rows(grad_x, shape, "grad_x", dev, x.dtype)
+    if ws is not None:
+        _workspace(ws, dev)
+    elif T:
+        ws = alloc_layer_norm_workspace(T, H, dev)
+    _call(dev, load().dppf_layer_norm_grad, "dppf_layer_norm_grad", pg, _type(grad_out, "grad_out"), ld_g, px, _type(x, "x"), ld_x, mean.data_ptr(), rstd.data_ptr(),
+          weight.data_ptr(), _type(weight, "weight"), T, H, ps, ld_s, pd, ld_d, grad_weight.data_ptr(), _ptr(grad_bias), _type(grad_weight, "grad_weight"),
+          int(bool(accumulate)), _ptr(ws), 0 if ws is None else ws.nbytes)
+    return grad_x
+
+
+POSITIONS = {"plain": 0, "interpolated": 1, "stretched": 2, "by parts": 3}
+
+
+def rotary_frequencies(turned, base=10000.0, scaling="plain", factor=1.0, original_length=0, device="cuda"):
+    """(frequencies, scale) for :func:`dppf_rotary`: fp64 tensor of ``turned / 2`` entries, and a number.  ``scaling``: how they are
+    adapted to contexts ``factor`` times as long as the model's (``original_length`` tokens; for "by parts")."""
+    if scaling not in POSITIONS:
+        raise ValueError(f"scaling must be one of {', '.join(POSITIONS)}")
+    values, scale = (ctypes.c_double * max(1, int(turned) // 2))(), ctypes.c_float()
+    _check(load().dppf_rotary_frequencies(int(turned), base, POSITIONS[scaling], factor, int(original_length), values, ctypes.byref(scale)), "dppf_rotary_frequencies")
+    return torch.tensor(list(values), dtype=torch.float64, device=device), scale.value
+
+
+def _heads(t: torch.Tensor, what: str):
+    """(tokens, heads, width, token stride, head stride) of a 3-D CUDA tensor with unit stride within a head."""
+    if t.dim() != 3 or not t.is_cuda or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what} must be a 3-D CUDA tensor [tokens, heads, width] with unit stride within a head")
+    T, heads, D = t.shape
+    ld, head, _ = t.stride()
+    if heads <= 1:
+        head = D                                              # the stride of a single head, or token, says nothing
+    return T, heads, D, ld if T > 1 else (heads - 1) * head + D, head
+
+
+def dppf_rotary(x, positions, frequencies, scale=1.0, interleaved=False, inverse=False, out=None):
+    """Turns the first ``2 * len(frequencies)`` elements of every head of ``x[T, heads, D]`` by position times frequency, pairs side by
+    side (``interleaved``) or half and half; ``inverse`` turns back, which is the gradient.  ``out`` may be ``x``; new if not given."""
+    T, heads, D, ld, head = _heads(x, "x")
+    dev = x.device
+    if positions.dtype not in _ID_BITS or positions.device != dev or positions.numel() != T or not positions.is_contiguous():
+        _vector(positions, T, "positions", dev, tuple(_ID_BITS))
+    half = frequencies.numel()
+    if frequencies.dtype is not torch.float64 or frequencies.device != dev or not frequencies.is_contiguous():
+        _vector(frequencies, half, "frequencies", dev, (torch.float64,))
+    if out is None:
+        out = x.new_empty(x.shape)
+    elif out.shape != x.shape or out.dtype != x.dtype or out.device != dev:
+        raise ValueError("out must have the shape, type and device of x")
+    _, _, _, ld_o, head_o = _heads(out, "out")
+    _call(dev, load().dppf_rotary, "dppf_rotary", x.data_ptr(), _type(x, "x"), ld, head, T, heads, D, 2 * half, int(bool(interleaved)), positions.data_ptr(),
+          _ID_BITS[positions.dtype], frequencies.data_ptr(), scale, int(bool(inverse)), out.data_ptr(), ld_o, head_o)
+    return out
 
 
 class PolicyLoss(NamedTuple):

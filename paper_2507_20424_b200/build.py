@@ -12,8 +12,9 @@ _ROOT = os.path.dirname(_PKG)
 UNITS = {
     "dppf.cu": ("common.cuh", "round_register.cuh", "adamw_element.cuh", "adamw.cuh", "chunk_ring.cuh", "round_staged.cuh",
                 "round_multi.cuh", "round_fused_staged.cuh", "round_general.cuh", "round_generic.cuh", "round_worker.cuh"),
-    "local_model.cu": ("common.cuh", "chunk_ring.cuh", "adamw_element.cuh", "local_common.cuh", "embedding.cuh",
+    "local_model.cu": ("common.cuh", "chunk_ring.cuh", "adamw_element.cuh", "local_common.cuh", "local_host.cuh", "embedding.cuh",
                        "policy_loss.cuh", "adamw_tensors.cuh"),
+    "block.cu": ("common.cuh", "chunk_ring.cuh", "local_common.cuh", "local_host.cuh", "layer_norm.cuh", "rotary.cuh"),
 }
 ABI_HEADER = os.path.join(_ROOT, "include", "dppf.h")
 

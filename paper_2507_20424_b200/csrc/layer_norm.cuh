@@ -1,0 +1,376 @@
+// Layer norm after a residual addition, and its gradient with the weight's and bias's.
+//
+//   h = x + branch (rounded to x's type);  mu = mean h;  r = (mean (h - mu)^2 + eps)^-1/2;  y = (h - mu) r w + b
+//   u = w dy;  xh = (h - mu) r;  dx = r (u - mean u - xh mean(u xh)) + dsum;  dw = sum_t dy xh;  db = sum_t dy
+//
+// Both are bound by memory: a row is read once, stays in registers (sixteen elements a thread) for the statistics, the second
+// moment taken about the mean, and is written once.  Rows of up to 512 elements take a warp each, longer ones a block; above
+// kNormRow elements (kNormGradRow for the gradient) a block walks the row several times, the later ones from L2.
+//
+// The gradient's blocks stay: each walks rows blockIdx.x, + gridDim.x, ... and keeps its columns' sums of dy xh and dy in registers;
+// they go to the workspace once a block, and a second launch adds the blocks' sums in block order.  No atomics: the sums' order
+// depends on T, H and the device's SMs alone.
+#pragma once
+#include "local_common.cuh"
+
+namespace {
+
+constexpr int kNormElements = 16;                         // of a row in one thread
+constexpr int kNormWarpRow = 32 * kNormElements;          // longest row of a warp
+constexpr int kNormRow = 1024 * kNormElements;            // longest row that a block holds
+constexpr int kNormGradRow = 512 * kNormElements;         // ... with the columns' sums beside it
+constexpr int kNormWarps = 8;                             // rows side by side in a block, a warp each
+constexpr int kNormWideThreads = 512;
+constexpr int kNormJoinThreads = 256;
+
+struct NormArgs {
+    const void *x, *branch, *weight, *bias;
+    void *sum, *out;
+    float *mean, *rstd;
+    long long ld_x, ld_branch, ld_sum, ld_out, T;
+    int H, groups;               // groups: of N elements
+    int branch32, weight32;      // fp32 (else bf16)
+    float eps;
+};
+
+struct NormGradArgs {
+    const void *dy, *x, *weight, *dsum;
+    const float *mean, *rstd;
+    void *dx, *dweight, *dbias;
+    float *part;                 // [blocks][2][H]
+    long long ld_dy, ld_x, ld_dsum, ld_dx, T;
+    int H, groups, blocks;
+    int weight32, grad32, add;   // types of the weight and of its gradient; add to the gradients
+    float inv_h;
+};
+
+// N elements of an array whose type is known at run time; weights are read again by every row: kept in the caches.
+template <int N, bool kOnce>
+__device__ __forceinline__ void load_either(const void *p, int is32, long long at, float (&f)[N]) {
+    if (is32) load_vec<float, N, kOnce>(static_cast<const float *>(p) + at, f);
+    else load_vec<bf16, N, kOnce>(static_cast<const bf16 *>(p) + at, f);
+}
+
+// Sums of K values over the threads of a row: a warp, or the block.  `s` is used by one call in two (the caller alternates), so
+// that one barrier is enough.
+template <bool kWarp, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float (*s)[32]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    if constexpr (!kWarp) {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+        if (lane == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[k][warp] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = lane < warps ? s[k][lane] : 0.f;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        }
+    }
+}
+
+template <typename TX, typename TO, int N, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int G = kNormElements / N;
+    __shared__ float s_sum[2][1][32];
+    const int L = kWarp ? 32 : blockDim.x, t = kWarp ? threadIdx.x & 31 : threadIdx.x;
+    const long long row = kWarp ? (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5) : blockIdx.x;
+    if (kWarp && row >= a.T) return;
+    const TX *x = static_cast<const TX *>(a.x) + row * a.ld_x;
+    float h[G][N], sum[1] = {0.f};
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const int at = g * L + t;
+        if (at < a.groups) load_vec<TX, N>(x + (long long)at * N, h[g]);
+        else
+#pragma unroll
+            for (int i = 0; i < N; ++i) h[g][i] = 0.f;
+    }
+    if (a.branch) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int at = g * L + t;
+            if (at >= a.groups) continue;
+            float b[N];
+            load_either<N, true>(a.branch, a.branch32, row * a.ld_branch + (long long)at * N, b);
+#pragma unroll
+            for (int i = 0; i < N; ++i) h[g][i] = to_float(from_float<TX>(h[g][i] + b[i]));
+            store_vec<TX, N>(static_cast<TX *>(a.sum) + row * a.ld_sum + (long long)at * N, h[g]);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[0] += h[g][i];
+    row_sums<kWarp, 1>(sum, s_sum[0]);
+    const float mean = sum[0] / (float)a.H;
+    sum[0] = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+        if (g * L + t < a.groups)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                h[g][i] -= mean;
+                sum[0] = fmaf(h[g][i], h[g][i], sum[0]);
+            }
+    row_sums<kWarp, 1>(sum, s_sum[1]);
+    const float rstd = 1.0f / sqrtf(sum[0] / (float)a.H + a.eps);
+    if (t == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const int at = g * L + t;
+        if (at >= a.groups) continue;
+        float w[N], b[N];
+        load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
+        if (a.bias) load_either<N, false>(a.bias, a.weight32, (long long)at * N, b);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = h[g][i] * rstd;
+            h[g][i] = a.bias ? fmaf(y, w[i], b[i]) : y * w[i];
+        }
+        store_vec<TO, N>(static_cast<TO *>(a.out) + row * a.ld_out + (long long)at * N, h[g]);
+    }
+}
+
+// Rows longer than a block holds: h is formed (and written) in the first walk and read again in two more.
+template <typename TX, typename TO, int N>
+__global__ void __launch_bounds__(kNormWideThreads) norm_wide_kernel(const __grid_constant__ NormArgs a) {
+    __shared__ float s_sum[2][1][32];
+    const long long row = blockIdx.x;
+    const TX *x = static_cast<const TX *>(a.x) + row * a.ld_x;
+    float sum[1] = {0.f};
+    for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
+        float h[N];
+        load_vec<TX, N, false>(x + (long long)at * N, h);
+        if (a.branch) {
+            float b[N];
+            load_either<N, true>(a.branch, a.branch32, row * a.ld_branch + (long long)at * N, b);
+#pragma unroll
+            for (int i = 0; i < N; ++i) h[i] = to_float(from_float<TX>(h[i] + b[i]));
+            store_vec<TX, N>(static_cast<TX *>(a.sum) + row * a.ld_sum + (long long)at * N, h);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[0] += h[i];
+    }
+    row_sums<false, 1>(sum, s_sum[0]);
+    const float mean = sum[0] / (float)a.H;
+    const TX *from = a.branch ? static_cast<const TX *>(a.sum) + row * a.ld_sum : x;     // each thread reads what it wrote itself
+    sum[0] = 0.f;
+    for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
+        float h[N];
+        load_vec<TX, N, false>(from + (long long)at * N, h);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[0] = fmaf(h[i] - mean, h[i] - mean, sum[0]);
+    }
+    row_sums<false, 1>(sum, s_sum[1]);
+    const float rstd = 1.0f / sqrtf(sum[0] / (float)a.H + a.eps);
+    if (threadIdx.x == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
+    for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
+        float h[N], w[N], b[N];
+        load_vec<TX, N>(from + (long long)at * N, h);
+        load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
+        if (a.bias) load_either<N, false>(a.bias, a.weight32, (long long)at * N, b);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = (h[i] - mean) * rstd;
+            h[i] = a.bias ? fmaf(y, w[i], b[i]) : y * w[i];
+        }
+        store_vec<TO, N>(static_cast<TO *>(a.out) + row * a.ld_out + (long long)at * N, h);
+    }
+}
+
+// ---------------------------------------------------------------- gradient
+
+// dx of N elements, from dy -> u and xh
+template <typename TX, int N>
+__device__ __forceinline__ void norm_dx(const NormGradArgs &a, long long row, int at, const float (&u)[N], const float (&xh)[N], float rstd, float mu, float mx) {
+    float d[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) d[i] = rstd * (u[i] - mu - xh[i] * mx);
+    if (a.dsum) {
+        float b[N];
+        load_vec<TX, N>(static_cast<const TX *>(a.dsum) + row * a.ld_dsum + (long long)at * N, b);
+#pragma unroll
+        for (int i = 0; i < N; ++i) d[i] += b[i];
+    }
+    store_vec<TX, N>(static_cast<TX *>(a.dx) + row * a.ld_dx + (long long)at * N, d);
+}
+
+// Block `b` writes its columns' sums; threads that share columns (the warps of a block with a warp a row) add theirs in warp order.
+template <int N, bool kWarp>
+__device__ __forceinline__ void put_sums(const NormGradArgs &a, int L, int t, float (&dw)[kNormElements / N][N], float (&db)[kNormElements / N][N]) {
+    constexpr int G = kNormElements / N;
+    float *part = a.part + (long long)blockIdx.x * 2 * a.H;
+    if constexpr (kWarp) {
+        __shared__ float s_all[2][kNormWarpRow];
+        const int warp = threadIdx.x >> 5;
+        for (int w = 0; w < kNormWarps; ++w) {
+            if (warp == w)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const int at = g * L + t;
+                    if (at < a.groups)
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int c = at * N + i;
+                            s_all[0][c] = (w ? s_all[0][c] : 0.f) + dw[g][i];
+                            s_all[1][c] = (w ? s_all[1][c] : 0.f) + db[g][i];
+                        }
+                }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < a.H; c += kNormWarps * 32) {
+            __stcg(part + c, s_all[0][c]);
+            __stcg(part + a.H + c, s_all[1][c]);
+        }
+    } else {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int at = g * L + t;
+            if (at < a.groups)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    __stcg(part + at * N + i, dw[g][i]);
+                    __stcg(part + a.H + at * N + i, db[g][i]);
+                }
+        }
+    }
+}
+
+template <typename TX, typename TO, int N, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512) norm_grad_kernel(const __grid_constant__ NormGradArgs a) {
+    constexpr int G = kNormElements / N;
+    __shared__ float s_sum[2][2][32];
+    const int L = kWarp ? 32 : blockDim.x, t = kWarp ? threadIdx.x & 31 : threadIdx.x;
+    float dw[G][N], db[G][N];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int i = 0; i < N; ++i) dw[g][i] = db[g][i] = 0.f;
+    const long long step = (long long)gridDim.x * (kWarp ? kNormWarps : 1);
+    int odd = 0;
+    for (long long row = kWarp ? (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5) : blockIdx.x; row < a.T; row += step) {
+        float u[G][N], xh[G][N], sums[2] = {0.f, 0.f};
+        const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int at = g * L + t;
+            if (at < a.groups) {
+                load_vec<TO, N>(static_cast<const TO *>(a.dy) + row * a.ld_dy + (long long)at * N, u[g]);
+                load_vec<TX, N>(static_cast<const TX *>(a.x) + row * a.ld_x + (long long)at * N, xh[g]);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int at = g * L + t;
+            if (at >= a.groups) continue;
+            float w[N];
+            load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                xh[g][i] = (xh[g][i] - mean) * rstd;
+                dw[g][i] = fmaf(u[g][i], xh[g][i], dw[g][i]);
+                db[g][i] += u[g][i];
+                u[g][i] *= w[i];
+                sums[0] += u[g][i];
+                sums[1] = fmaf(u[g][i], xh[g][i], sums[1]);
+            }
+        }
+        row_sums<kWarp, 2>(sums, s_sum[odd]);
+        odd ^= 1;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int at = g * L + t;
+            if (at < a.groups) norm_dx<TX, N>(a, row, at, u[g], xh[g], rstd, sums[0] * a.inv_h, sums[1] * a.inv_h);
+        }
+    }
+    put_sums<N, kWarp>(a, L, t, dw, db);
+    let_next_start();
+}
+
+// Longer rows: the columns' sums first (dx may replace dy), a block for a stretch of columns and every gridDim.y-th row, then dx.
+template <typename TX, typename TO, int N>
+__global__ void __launch_bounds__(kNormWideThreads) norm_grad_columns_kernel(const __grid_constant__ NormGradArgs a) {
+    const int at = blockIdx.x * kNormWideThreads + threadIdx.x;
+    if (at >= a.groups) return;
+    float dw[N], db[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
+    for (long long row = blockIdx.y; row < a.T; row += gridDim.y) {
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float dy[N], x[N];
+        load_vec<TO, N, false>(static_cast<const TO *>(a.dy) + row * a.ld_dy + (long long)at * N, dy);
+        load_vec<TX, N, false>(static_cast<const TX *>(a.x) + row * a.ld_x + (long long)at * N, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            dw[i] = fmaf(dy[i], (x[i] - mean) * rstd, dw[i]);
+            db[i] += dy[i];
+        }
+    }
+    float *part = a.part + (long long)blockIdx.y * 2 * a.H + (long long)at * N;
+#pragma unroll
+    for (int i = 0; i < N; ++i) { __stcg(part + i, dw[i]); __stcg(part + a.H + i, db[i]); }
+}
+
+template <typename TX, typename TO, int N>
+__global__ void __launch_bounds__(kNormWideThreads) norm_grad_wide_kernel(const __grid_constant__ NormGradArgs a) {
+    __shared__ float s_sum[2][32];
+    const long long row = blockIdx.x;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    const TO *dy = static_cast<const TO *>(a.dy) + row * a.ld_dy;
+    const TX *x = static_cast<const TX *>(a.x) + row * a.ld_x;
+    float sums[2] = {0.f, 0.f}, u[N], xh[N], w[N];
+    auto load = [&](int at) {
+        load_vec<TO, N, false>(dy + (long long)at * N, u);
+        load_vec<TX, N, false>(x + (long long)at * N, xh);
+        load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) { xh[i] = (xh[i] - mean) * rstd; u[i] *= w[i]; }
+    };
+    for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
+        load(at);
+#pragma unroll
+        for (int i = 0; i < N; ++i) { sums[0] += u[i]; sums[1] = fmaf(u[i], xh[i], sums[1]); }
+    }
+    row_sums<false, 2>(sums, s_sum);
+    for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
+        load(at);
+        norm_dx<TX, N>(a, row, at, u, xh, rstd, sums[0] * a.inv_h, sums[1] * a.inv_h);
+    }
+}
+
+// The blocks' sums, added in block order by eight threads a column (every eighth block each) and then those eight.
+// blockIdx.y: 0 the weight's gradient, 1 the bias's.
+__global__ void __launch_bounds__(kNormJoinThreads) norm_join_kernel(const __grid_constant__ NormGradArgs a) {
+    constexpr int kParts = kNormJoinThreads / 32;
+    __shared__ float s_part[kParts][32];
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    wait_for_previous();
+    float sum = 0.f;
+    if (c < a.H) {
+        const float *p = a.part + (long long)blockIdx.y * a.H + c;
+#pragma unroll 4
+        for (int b = part; b < a.blocks; b += kParts) sum += __ldcg(p + (long long)b * 2 * a.H);
+    }
+    s_part[part][lane] = sum;
+    __syncthreads();
+    if (part || c >= a.H) return;
+    sum = s_part[0][lane];
+#pragma unroll
+    for (int k = 1; k < kParts; ++k) sum += s_part[k][lane];
+    void *to = blockIdx.y ? a.dbias : a.dweight;
+    if (a.grad32) {
+        float *d = static_cast<float *>(to) + c;
+        *d = a.add ? *d + sum : sum;
+    } else {
+        bf16 *d = static_cast<bf16 *>(to) + c;
+        *d = from_float<bf16>(a.add ? to_float(*d) + sum : sum);
+    }
+}
+
+}  // namespace

@@ -2,6 +2,7 @@
 //   local_common.cuh   element types, vectors of eight elements, cluster accesses
 //   embedding.cuh      lookup with a scale; the table's gradient by sorted tokens
 //   policy_loss.cuh    clipped policy loss with a KL term, forward and backward, from logits
+//   local_host.cuh     devices, launches, checks of arguments
 //   adamw_tensors.cuh  AdamW over many tensors, optimiser state in fp32 or in 8 bits
 #include "dppf.h"
 
@@ -9,80 +10,10 @@
 
 #include "adamw_tensors.cuh"
 #include "embedding.cuh"
+#include "local_host.cuh"
 #include "policy_loss.cuh"
 
-namespace dppf_internal {
-int first_pass_polls();          // poll budget set by dppf_debug_set_poll_limits
-}
-
 namespace {
-
-constexpr int kMaxDevices = 64;
-
-int current_device() {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return -1;
-    return dev;
-}
-
-int multiprocessors(int dev) {
-    static std::atomic<int> known[kMaxDevices];
-    int n = known[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return -1;
-        known[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
-
-// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
-template <typename K>
-bool allow_smem(K kernel, int dev, std::atomic<int> *done, int bytes) {
-    if (done[dev].load(std::memory_order_relaxed)) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-    done[dev].store(1, std::memory_order_relaxed);
-    return true;
-}
-
-int launched() { return cudaGetLastError() == cudaSuccess ? DPPF_OK : DPPF_ERR_CUDA; }
-
-// A launch that may be set up while the one before it in the stream still runs (its kernel waits by itself).
-template <typename... P, typename... A>
-bool launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess;
-}
-
-bool all_finite(std::initializer_list<float> vals) {
-    for (float f : vals)
-        if (!std::isfinite(f)) return false;
-    return true;
-}
-
-bool ranges_meet(const void *a, size_t abytes, const void *b, size_t bbytes) {
-    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
-    return a && b && abytes && bbytes && pa < pb + bbytes && pb < pa + abytes;
-}
-
-bool known_type(int t) { return t == DPPF_FLOAT32 || t == DPPF_BFLOAT16; }
-size_t type_bytes(int t) { return t == DPPF_FLOAT32 ? 4 : 2; }
-bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-// Bytes from the first element of row 0 to the last one of row rows - 1.
-size_t matrix_bytes(int64_t rows, int64_t cols, int64_t ld, int type) {
-    return rows > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * type_bytes(type) : 0;
-}
-
-constexpr int64_t kMaxLd = (int64_t)1 << 40;
 
 // ---------------------------------------------------------------- embedding
 
@@ -117,9 +48,6 @@ int launch_lookup(LookupArgs a, int n, int sms, cudaStream_t s) {
     return launched();
 }
 
-// Rows of a matrix start on 16-byte boundaries.
-bool rows_on_16(const void *p, int64_t ld, int type) { return aligned_to(p, 16) && (size_t)ld * type_bytes(type) % 16 == 0; }
-
 // Places of the sorted tokens that a thread walks: long enough that few sums are split, short enough that about
 // 2,000 threads an SM are at work, each on one of a row's `groups` (8 to 32).  The SMs are a B200's 148 whatever the device: the
 // workspace is laid out by this, and its size is asked for without one.
@@ -129,8 +57,6 @@ int reduce_tile(int64_t T, int groups) {
     while (tile < kMaxTile && tile < rows) tile *= 2;
     return tile;
 }
-
-size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 struct EmbeddingLayout {
     size_t order[2], hist, part, total;
