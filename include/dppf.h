@@ -411,6 +411,37 @@ int dppf_rotary_frequencies(int turned, double base, int scaling, double factor,
                             float *scale_host);
 
 /*
+ * Attention within the sequences of a packed batch.  Rows starts[b] .. starts[b + 1] - 1 of T token rows are sequence b (b < B); the
+ * others are rows of no sequence: they are not read, and what is written for them is zero (lse: -infinity).
+ *
+ * The plan, made once for a batch and used by every layer, forward and backward: starts (device int32 or int64 [B + 1],
+ * start_bits) -> tiles of rows.  Starts that fall back, or lie outside [0, T], are pulled to the largest before them and into [0, T]. A
+ * sequence may be empty.  plan: dppf_attention_plan_bytes(T, B) bytes of device memory, 128-byte aligned, no initialisation; the
+ * calls that use it only read it (but for its status word), so they may run side by side.  The helper returns 0 for invalid T or B.
+ */
+#define DPPF_MAX_ATTENTION_TOKENS 16777216
+#define DPPF_MAX_SEQUENCES 1048576
+#define DPPF_MAX_ATTENTION_WIDTH 128
+size_t dppf_attention_plan_bytes(int64_t T, int64_t B);
+int dppf_attention_plan(const void *starts, int start_bits, int64_t T, int64_t B, void *plan, size_t plan_bytes, void *cuda_stream);
+
+/*
+ * For query row i and head h, with the keys j of i's sequence -- causal: j <= i; window > 0 (with causal only): j > i - window --
+ * and key head h / (heads / kv_heads):
+ *   S_ij = scale q_i . k_j;   lse_out[h T + i] = log sum_j exp S_ij;   out_i = sum_j exp(S_ij - lse_i) v_j
+ * q, out: heads heads, k, v: kv_heads heads (a divisor) of D elements (a multiple of 8, up to DPPF_MAX_ATTENTION_WIDTH), bf16, laid
+ * out as for dppf_rotary, starts and strides multiples of 16 bytes.  Products of bf16, sums and softmax in fp32; the
+ * probabilities (relative to about the largest) are rounded to bf16 for the product with v, out at the end.  scale > 0.  A key or value row that is not finite
+ * spoils the queries that see it and those after it in its tile of 128, never another sequence's.  T == 0 does nothing.
+ * dppf_device_status(plan, stream): DPPF_ERR_TIMEOUT if a bounded wait gave up (the rows concerned are NaN), DPPF_ERR_WORKSPACE
+ * if the plan was not one of T rows (nothing is written).
+ */
+int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, int64_t ld_k, int64_t head_k, const void *v,
+                   int64_t ld_v, int64_t head_v, int64_t T, int64_t B, int heads, int kv_heads, int D, int causal, int window,
+                   float scale, void *out, int64_t ld_out, int64_t head_out, float *lse_out, void *plan, size_t plan_bytes,
+                   void *cuda_stream);
+
+/*
  * Clipped policy loss with a KL term, from logits[T, ld] (V columns of `type`), with its gradient.
  * For token t with z = logits[t] / temperature and y = targets[t]:
  *   lp = z_y - log sum_v exp z_v;   q = exp(lp - old_logp[t]);   A = advantage[t]

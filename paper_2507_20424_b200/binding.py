@@ -27,6 +27,7 @@ EXPORTS = ("dppf_workspace_bytes", "dppf_consensus", "dppf_consensus_ex", "dppf_
            "dppf_adamw_step", "dppf_adamw_step_and_consensus",
            "dppf_embedding", "dppf_embedding_grad", "dppf_embedding_workspace_bytes",
            "dppf_layer_norm", "dppf_layer_norm_grad", "dppf_layer_norm_workspace_bytes", "dppf_rotary", "dppf_rotary_frequencies",
+           "dppf_attention_plan_bytes", "dppf_attention_plan", "dppf_attention",
            "dppf_policy_loss", "dppf_policy_workspace_bytes", "dppf_adamw_tensors",
            "dppf_lambda_schedule", "dppf_lr_cosine", "dppf_qsr_period", "dppf_round_metrics")
 
@@ -130,6 +131,12 @@ def load(rebuild_if_stale: bool = False) -> ctypes.CDLL:
     lib.dppf_rotary.restype = i32
     lib.dppf_rotary_frequencies.argtypes = [i32, ctypes.c_double, i32, ctypes.c_double, i64, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(f32)]
     lib.dppf_rotary_frequencies.restype = i32
+    lib.dppf_attention_plan_bytes.argtypes = [i64, i64]
+    lib.dppf_attention_plan_bytes.restype = sz
+    lib.dppf_attention_plan.argtypes = [vp, i32, i64, i64, vp, sz, vp]
+    lib.dppf_attention_plan.restype = i32
+    lib.dppf_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, i64, i64, i32, i32, i32, i32, i32, f32, vp, i64, i64, vp, vp, sz, vp]
+    lib.dppf_attention.restype = i32
     lib.dppf_policy_workspace_bytes.argtypes = [i64]
     lib.dppf_policy_workspace_bytes.restype = sz
     lib.dppf_policy_loss.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, i64, vp, sz, vp]
@@ -616,6 +623,68 @@ def dppf_rotary(x, positions, frequencies, scale=1.0, interleaved=False, inverse
     _call(dev, load().dppf_rotary, "dppf_rotary", x.data_ptr(), _type(x, "x"), ld, head, T, heads, D, 2 * half, int(bool(interleaved)), positions.data_ptr(),
           _ID_BITS[positions.dtype], frequencies.data_ptr(), scale, int(bool(inverse)), out.data_ptr(), ld_o, head_o)
     return out
+
+
+class AttentionPlan:
+    """The tiles of a packed batch: ``starts[B + 1]`` (int32 or int64, on the device), sequence b being rows ``starts[b]`` to
+    ``starts[b + 1] - 1`` of ``tokens``.  Made once a batch, on the current stream, and used by every layer."""
+
+    def __init__(self, starts, tokens):
+        self.tokens, self.sequences, self.device = int(tokens), starts.numel() - 1, starts.device
+        if not starts.is_cuda:
+            raise ValueError("starts must be a CUDA tensor")
+        n = int(load().dppf_attention_plan_bytes(self.tokens, self.sequences))
+        if n == 0:
+            raise ValueError("invalid number of tokens or sequences")
+        self.buffer = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self.renew(starts)
+
+    def renew(self, starts) -> None:
+        """The plan of another batch with as many tokens and sequences, in the same memory (for captured graphs)."""
+        _vector(starts, self.sequences + 1, "starts", self.device, tuple(_ID_BITS))
+        _call(self.device, load().dppf_attention_plan, "dppf_attention_plan", starts.data_ptr(), _ID_BITS[starts.dtype], self.tokens, self.sequences,
+              self.buffer.data_ptr(), self.buffer.nbytes)
+
+
+class Attention(NamedTuple):
+    out: torch.Tensor           # [T, heads, D]
+    lse: torch.Tensor           # fp32 [heads, T]
+
+
+def _attention_heads(t, what, device, tokens):
+    if t.dtype is not torch.bfloat16 or t.device != device:
+        raise ValueError(f"{what} must be bf16 on {device}")
+    T, heads, D, ld, head = _heads(t, what)
+    if T != tokens:
+        raise ValueError(f"{what} must have the plan's {tokens} tokens")
+    return heads, D, (t.data_ptr(), ld, head)
+
+
+def _attention_inputs(q, k, v, plan, scale):
+    heads, D, at_q = _attention_heads(q, "q", plan.device, plan.tokens)
+    kv_heads, Dk, at_k = _attention_heads(k, "k", plan.device, plan.tokens)
+    kv2, Dv, at_v = _attention_heads(v, "v", plan.device, plan.tokens)
+    if Dk != D or Dv != D or kv2 != kv_heads:
+        raise ValueError("q, k and v must have heads of one width, k and v as many heads")
+    return heads, kv_heads, D, at_q, at_k, at_v, (D ** -0.5 if scale is None else scale)
+
+
+def dppf_attention(q, k, v, plan: AttentionPlan, causal=True, window=0, scale=None, out=None, lse=None) -> Attention:
+    """Attention of ``q[T, heads, D]`` over the keys ``k`` and values ``v[T, kv_heads, D]`` of the same sequence (``causal``: up to the
+    token itself; ``window``: the last so many).  ``scale``: default 1 / sqrt(D).  bf16; ``out``, ``lse``: new if not given."""
+    heads, kv_heads, D, at_q, at_k, at_v, scale = _attention_inputs(q, k, v, plan, scale)
+    if out is None:
+        out = q.new_empty(q.shape)
+    elif out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    _, _, at_o = _attention_heads(out, "out", plan.device, plan.tokens)
+    if lse is None:
+        lse = q.new_empty((heads, plan.tokens), dtype=torch.float32)
+    else:
+        _vector(lse, heads * plan.tokens, "lse", plan.device)
+    _call(plan.device, load().dppf_attention, "dppf_attention", *at_q, *at_k, *at_v, plan.tokens, plan.sequences, heads, kv_heads, D, int(bool(causal)), int(window), scale,
+          *at_o, lse.data_ptr(), plan.buffer.data_ptr(), plan.buffer.nbytes)
+    return Attention(out, lse)
 
 
 class PolicyLoss(NamedTuple):

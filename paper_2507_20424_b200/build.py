@@ -15,6 +15,7 @@ UNITS = {
     "local_model.cu": ("common.cuh", "chunk_ring.cuh", "adamw_element.cuh", "local_common.cuh", "local_host.cuh", "embedding.cuh",
                        "policy_loss.cuh", "adamw_tensors.cuh"),
     "block.cu": ("common.cuh", "chunk_ring.cuh", "local_common.cuh", "local_host.cuh", "layer_norm.cuh", "rotary.cuh"),
+    "attention.cu": ("common.cuh", "chunk_ring.cuh", "local_common.cuh", "local_host.cuh", "tensor_core.cuh", "attention.cuh"),
 }
 ABI_HEADER = os.path.join(_ROOT, "include", "dppf.h")
 

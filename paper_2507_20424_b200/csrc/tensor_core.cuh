@@ -1,0 +1,155 @@
+// Tensor cores of sm_100a as the attention kernels use them: tiles of 128 rows brought in by tensor copies, products issued by one
+// thread with their sums in tensor memory, and bounded waits.
+//
+// Shared memory: a tile of 128 rows by 64 or 128 bf16 columns lies as one or two blocks of 64 columns (kBlockBytes each), a row of
+// a block in 128 bytes, 16-byte pieces swizzled within 1,024 bytes (the copies' 128-byte swizzle).  As an operand whose rows are
+// its M or N index ("rows") a step of 16 columns is 32 bytes further on; as one whose rows are summed over ("columns": M or N
+// is the tile's column) a step of 16 rows is 2,048 bytes further on and the next 64 columns are a block further on.
+// Tensor memory: 128 lanes (rows of a product) of 512 32-bit columns; a warp reaches the 32 lanes of its number modulo 4.
+#pragma once
+#include "local_common.cuh"
+#include <cuda.h>
+
+namespace {
+
+constexpr int kTile = 128;                       // rows of a tile
+constexpr unsigned kBlockBytes = kTile * 128;    // 64 columns of bf16
+
+// ---------------------------------------------------------------- waits
+// Every wait is bounded; the first that gives up makes all others of the block give up soon.
+
+struct Waits {
+    volatile int *dead;      // shared, one for the block
+    int limit;
+    __device__ __forceinline__ bool operator()(unsigned long long *bar, unsigned parity) const {
+        for (int i = 0; i < limit; ++i) {
+            if (mbar_try_wait(bar, parity)) return true;
+            if ((i & 63) == 63 && *dead) return false;
+        }
+        *dead = 1;
+        return false;
+    }
+    // by a whole warp, which goes on together
+    __device__ __forceinline__ bool together(unsigned long long *bar, unsigned parity) const { return __all_sync(0xffffffffu, (*this)(bar, parity)); }
+};
+
+__device__ __forceinline__ void mbar_arrive(unsigned long long *bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+// ---------------------------------------------------------------- copies
+
+// Box at (column, head, row) of a tensor [rows][heads][columns]; what lies outside the tensor is zero.  column * 2 is a multiple of 16.
+__device__ __forceinline__ void tensor_load(unsigned dst, const CUtensorMap *map, int column, int head, int row, unsigned long long *bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(column), "r"(head), "r"(row), "r"(smem_addr(bar)) : "memory");
+}
+// A tile: its blocks of 64 columns, announced to `bar` by the caller.
+template <int kBlocks>
+__device__ __forceinline__ void tile_load(unsigned dst, const CUtensorMap *map, int head, int row, unsigned long long *bar) {
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) tensor_load(dst + c * kBlockBytes, map, 64 * c, head, row, bar);
+}
+// Rows first .. 127 of a tile become zeros (a warp): rows of other sequences must not reach a sum over rows, where 0 times NaN is NaN.
+template <int kBlocks>
+__device__ __forceinline__ void zero_rows(unsigned tile, int first) {
+    const int lane = threadIdx.x & 31, pieces = (kTile - first) * 8;
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c)
+        for (int i = lane; i < pieces; i += 32)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + c * kBlockBytes + first * 128 + i * 16), "r"(0) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the products read through the asynchronous proxy
+    __syncwarp();
+}
+
+// ---------------------------------------------------------------- products
+
+__device__ __forceinline__ unsigned long long operand(unsigned addr, unsigned leading_bytes) {
+    // bits 0-13 address / 16, 16-29 leading offset / 16, 32-45 stride of eight rows / 16, 46-48 one, 61-63 128-byte swizzle
+    return (unsigned long long)((addr & 0x3ffff) >> 4) | (unsigned long long)(leading_bytes >> 4) << 16 | (unsigned long long)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+__device__ __forceinline__ unsigned long long operand_rows(unsigned tile) { return operand(tile, 16); }
+__device__ __forceinline__ unsigned long long operand_columns(unsigned tile) { return operand(tile, kBlockBytes); }
+
+// Instruction descriptor: fp32 sums, bf16 operands, M = 128; kColumns: the second operand's rows are summed over.
+template <int N, bool kColumns>
+__device__ __forceinline__ constexpr unsigned product_kind() {
+    return 1u << 4 | 1u << 7 | 1u << 10 | (kColumns ? 1u << 16 : 0u) | (unsigned)(N >> 3) << 17 | (unsigned)(kTile >> 4) << 24;
+}
+// d[128, N] (+)= a b over 16 elements; one thread.
+__device__ __forceinline__ void product16(unsigned d, unsigned long long a, unsigned long long b, unsigned kind, bool add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((unsigned)add) : "memory");
+}
+// The same with the first operand in tensor memory.
+__device__ __forceinline__ void product16_tmem(unsigned d, unsigned a, unsigned long long b, unsigned kind, bool add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"((unsigned)add) : "memory");
+}
+// d[128, 128] = rows of tile a times rows of tile b, summed over 64 * kBlocks columns.
+template <int kBlocks>
+__device__ __forceinline__ void product_rows(unsigned d, unsigned a, unsigned b) {
+    const unsigned long long da = operand_rows(a), db = operand_rows(b);
+#pragma unroll
+    for (int k = 0; k < 4 * kBlocks; ++k) {
+        const unsigned at = ((k / 4) * kBlockBytes + (k % 4) * 32) >> 4;
+        product16(d, da + at, db + at, product_kind<kTile, false>(), k > 0);
+    }
+}
+// d[128, 64 * kBlocks] (+)= p[128, 128] times tile b, summed over b's rows.  p: bf16 pairs in tensor memory, rows 0-63 of the sum
+// from column `low` on, 64-127 from column `high` on.
+template <int kBlocks>
+__device__ __forceinline__ void product_columns(unsigned d, unsigned low, unsigned high, unsigned b, bool add) {
+    const unsigned long long db = operand_columns(b);
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k)
+        product16_tmem(d, (k < 4 ? low : high) + (k % 4) * 8, db + ((k * 2048) >> 4), product_kind<64 * kBlocks, true>(), add || k > 0);
+}
+// Arrives on `bar` when all products that this thread has issued are done.
+__device__ __forceinline__ void products_done(unsigned long long *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+// ---------------------------------------------------------------- tensor memory
+
+__device__ __forceinline__ void tmem_alloc(unsigned *where, int columns) {      // a warp; waits for other blocks' columns
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(where)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(unsigned at, int columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+#define DPPF_R4(v, i) "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3])
+#define DPPF_R16(v, i) DPPF_R4(v, i), DPPF_R4(v, i + 4), DPPF_R4(v, i + 8), DPPF_R4(v, i + 12)
+#define DPPF_M4(v, i) "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3])
+#define DPPF_M16(v, i) DPPF_M4(v, i), DPPF_M4(v, i + 4), DPPF_M4(v, i + 8), DPPF_M4(v, i + 12)
+#define DPPF_U4(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3])
+#define DPPF_U16(v, i) DPPF_U4(v, i), DPPF_U4(v, i + 4), DPPF_U4(v, i + 8), DPPF_U4(v, i + 12)
+
+// 32 columns of the thread's lane; the values are there after tmem_loaded(v).
+__device__ __forceinline__ void tmem_load32(unsigned at, float (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+                 "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : DPPF_R16(v, 0), DPPF_R16(v, 16) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_loaded(float (&v)[32]) {       // waits for all loads before it; ties v's uses to the wait
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : DPPF_M16(v, 0), DPPF_M16(v, 16)::"memory");
+}
+__device__ __forceinline__ void tmem_store32(unsigned at, const float (&f)[32]) {
+    unsigned v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(f[i]);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+                 "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(at), DPPF_U16(v, 0), DPPF_U16(v, 16) : "memory");
+}
+__device__ __forceinline__ void tmem_store16(unsigned at, const unsigned (&v)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(at), DPPF_U16(v, 0) : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+}  // namespace
