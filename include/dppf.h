@@ -442,6 +442,25 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
                    void *cuda_stream);
 
 /*
+ * Its gradient: the probabilities are formed again from q, k and lse.  With P_ij = exp(S_ij - lse_i), D_i = grad_out_i . out_i and
+ * dS_ij = P_ij (grad_out_i . v_j - D_i):
+ *   grad_q_i = scale sum_j dS_ij k_j;   grad_k_j = scale sum_i dS_ij q_i;   grad_v_j = sum_i P_ij grad_out_i
+ * the last two over the query heads that share the key head as well.  All three are written whole (zeros for rows of no
+ * sequence).  P and dS are rounded to bf16 for their products, sums run in fp32 in an order that the batch fixes, results
+ * are rounded at the end.  Arguments as above; grad_out and out as q, grad_q as q, grad_k and grad_v as k; gradients may be heads
+ * of the same rows (as those of one product are) but must not overlap each other or an input.
+ * ws: dppf_attention_workspace_bytes(T, heads) bytes, 128-byte aligned, no initialisation.
+ */
+size_t dppf_attention_workspace_bytes(int64_t T, int heads);
+int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_grad_out, const void *q, int64_t ld_q,
+                        int64_t head_q, const void *k, int64_t ld_k, int64_t head_k, const void *v, int64_t ld_v, int64_t head_v,
+                        const void *out, int64_t ld_out, int64_t head_out, const float *lse, int64_t T, int64_t B, int heads,
+                        int kv_heads, int D, int causal, int window, float scale, void *grad_q, int64_t ld_grad_q,
+                        int64_t head_grad_q, void *grad_k, int64_t ld_grad_k, int64_t head_grad_k, void *grad_v,
+                        int64_t ld_grad_v, int64_t head_grad_v, void *plan, size_t plan_bytes, void *ws, size_t ws_bytes,
+                        void *cuda_stream);
+
+/*
  * Clipped policy loss with a KL term, from logits[T, ld] (V columns of `type`), with its gradient.
  * For token t with z = logits[t] / temperature and y = targets[t]:
  *   lp = z_y - log sum_v exp z_v;   q = exp(lp - old_logp[t]);   A = advantage[t]

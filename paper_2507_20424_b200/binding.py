@@ -27,7 +27,7 @@ EXPORTS = ("dppf_workspace_bytes", "dppf_consensus", "dppf_consensus_ex", "dppf_
            "dppf_adamw_step", "dppf_adamw_step_and_consensus",
            "dppf_embedding", "dppf_embedding_grad", "dppf_embedding_workspace_bytes",
            "dppf_layer_norm", "dppf_layer_norm_grad", "dppf_layer_norm_workspace_bytes", "dppf_rotary", "dppf_rotary_frequencies",
-           "dppf_attention_plan_bytes", "dppf_attention_plan", "dppf_attention",
+           "dppf_attention_plan_bytes", "dppf_attention_plan", "dppf_attention", "dppf_attention_grad", "dppf_attention_workspace_bytes",
            "dppf_policy_loss", "dppf_policy_workspace_bytes", "dppf_adamw_tensors",
            "dppf_lambda_schedule", "dppf_lr_cosine", "dppf_qsr_period", "dppf_round_metrics")
 
@@ -137,6 +137,10 @@ def load(rebuild_if_stale: bool = False) -> ctypes.CDLL:
     lib.dppf_attention_plan.restype = i32
     lib.dppf_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, i64, i64, i32, i32, i32, i32, i32, f32, vp, i64, i64, vp, vp, sz, vp]
     lib.dppf_attention.restype = i32
+    lib.dppf_attention_workspace_bytes.argtypes = [i64, i32]
+    lib.dppf_attention_workspace_bytes.restype = sz
+    lib.dppf_attention_grad.argtypes = [vp, i64, i64] * 5 + [vp, i64, i64, i32, i32, i32, i32, i32, f32] + [vp, i64, i64] * 3 + [vp, sz, vp, sz, vp]
+    lib.dppf_attention_grad.restype = i32
     lib.dppf_policy_workspace_bytes.argtypes = [i64]
     lib.dppf_policy_workspace_bytes.restype = sz
     lib.dppf_policy_loss.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, i64, vp, sz, vp]
@@ -685,6 +689,42 @@ def dppf_attention(q, k, v, plan: AttentionPlan, causal=True, window=0, scale=No
     _call(plan.device, load().dppf_attention, "dppf_attention", *at_q, *at_k, *at_v, plan.tokens, plan.sequences, heads, kv_heads, D, int(bool(causal)), int(window), scale,
           *at_o, lse.data_ptr(), plan.buffer.data_ptr(), plan.buffer.nbytes)
     return Attention(out, lse)
+
+
+class AttentionGrads(NamedTuple):
+    q: torch.Tensor
+    k: torch.Tensor
+    v: torch.Tensor
+
+
+def alloc_attention_workspace(T: int, heads: int, device="cuda") -> torch.Tensor:
+    n = int(load().dppf_attention_workspace_bytes(int(T), int(heads)))
+    if n == 0:
+        raise ValueError("invalid T or number of heads")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def dppf_attention_grad(grad_out, q, k, v, out, lse, plan: AttentionPlan, causal=True, window=0, scale=None, grad_q=None, grad_k=None, grad_v=None,
+                        ws=None) -> AttentionGrads:
+    """Gradients of :func:`dppf_attention` with respect to ``q``, ``k`` and ``v``, from its ``out`` and ``lse``, written whole to ``grad_q``,
+    ``grad_k`` and ``grad_v`` (new if not given)."""
+    heads, kv_heads, D, at_q, at_k, at_v, scale = _attention_inputs(q, k, v, plan, scale)
+    given = []
+    for t, like, what in ((grad_out, q, "grad_out"), (out, q, "out"), (grad_q, q, "grad_q"), (grad_k, k, "grad_k"), (grad_v, v, "grad_v")):
+        if t is None and what.startswith("grad_") and what != "grad_out":
+            t = like.new_empty(like.shape)
+        elif t.shape != like.shape:
+            raise ValueError(f"{what} has not the shape that goes with q, k and v")
+        given.append((t, _attention_heads(t, what, plan.device, plan.tokens)[2]))
+    (_, at_go), (_, at_o), (grad_q, at_dq), (grad_k, at_dk), (grad_v, at_dv) = given
+    _vector(lse, heads * plan.tokens, "lse", plan.device)
+    if ws is not None:
+        _workspace(ws, plan.device)
+    elif plan.tokens:
+        ws = alloc_attention_workspace(plan.tokens, heads, plan.device)
+    _call(plan.device, load().dppf_attention_grad, "dppf_attention_grad", *at_go, *at_q, *at_k, *at_v, *at_o, lse.data_ptr(), plan.tokens, plan.sequences, heads, kv_heads, D,
+          int(bool(causal)), int(window), scale, *at_dq, *at_dk, *at_dv, plan.buffer.data_ptr(), plan.buffer.nbytes, _ptr(ws), 0 if ws is None else ws.nbytes)
+    return AttentionGrads(grad_q, grad_k, grad_v)
 
 
 class PolicyLoss(NamedTuple):

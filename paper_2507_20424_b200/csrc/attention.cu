@@ -80,6 +80,18 @@ int launch_attention(const AttentionArgs &a, long long blocks, int dev, cudaStre
     return launched();
 }
 
+std::atomic<int> g_query_ready[2][kMaxDevices], g_key_ready[2][kMaxDevices];
+
+template <int kBlocks>
+int launch_attention_grad(const AttentionGradArgs &a, long long query_blocks, long long key_blocks, int dev, cudaStream_t s) {
+    constexpr int kQuerySmem = (int)QueryGradShape<kBlocks>::kSmem, kKeySmem = (int)KeyGradShape<kBlocks>::kSmem;
+    if (!allow_smem(attention_grad_query_kernel<kBlocks>, dev, g_query_ready[kBlocks - 1], kQuerySmem) || !allow_smem(attention_grad_key_kernel<kBlocks>, dev, g_key_ready[kBlocks - 1], kKeySmem))
+        return DPPF_ERR_CUDA;
+    attention_grad_query_kernel<kBlocks><<<(unsigned)query_blocks, kGradThreads, kQuerySmem, s>>>(a);
+    if (cudaPeekAtLastError() == cudaSuccess) attention_grad_key_kernel<kBlocks><<<(unsigned)key_blocks, kGradThreads, kKeySmem, s>>>(a);
+    return launched();
+}
+
 }  // namespace
 
 extern "C" {
@@ -146,6 +158,71 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
     if (blocks > INT_MAX) return DPPF_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     return D <= 64 ? launch_attention<1>(a, blocks, dev, s) : launch_attention<2>(a, blocks, dev, s);
+}
+
+size_t dppf_attention_workspace_bytes(int64_t T, int heads) {
+    return T >= 1 && T <= DPPF_MAX_ATTENTION_TOKENS && heads >= 1 && heads <= DPPF_MAX_HEADS ? round256((size_t)T * (size_t)heads * sizeof(float)) : 0;
+}
+
+int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_grad_out, const void *q, int64_t ld_q, int64_t head_q, const void *k, int64_t ld_k,
+                        int64_t head_k, const void *v, int64_t ld_v, int64_t head_v, const void *out, int64_t ld_out, int64_t head_out, const float *lse, int64_t T,
+                        int64_t B, int heads, int kv_heads, int D, int causal, int window, float scale, void *grad_q, int64_t ld_grad_q, int64_t head_grad_q,
+                        void *grad_k, int64_t ld_grad_k, int64_t head_grad_k, void *grad_v, int64_t ld_grad_v, int64_t head_grad_v, void *plan, size_t plan_bytes,
+                        void *ws, size_t ws_bytes, void *cuda_stream) {
+    const AttentionShape shape = {T, B, heads, kv_heads, D, causal, window, scale};
+    if (!shape.fine()) return DPPF_ERR_INVALID_ARG;
+    if (T == 0) return DPPF_OK;
+    const HeadRows in[] = {{grad_out, ld_grad_out, head_grad_out, T, heads, D, DPPF_BFLOAT16}, {q, ld_q, head_q, T, heads, D, DPPF_BFLOAT16}, {k, ld_k, head_k, T, kv_heads, D, DPPF_BFLOAT16},
+                           {v, ld_v, head_v, T, kv_heads, D, DPPF_BFLOAT16}, {out, ld_out, head_out, T, heads, D, DPPF_BFLOAT16}};
+    const HeadRows written[] = {{grad_q, ld_grad_q, head_grad_q, T, heads, D, DPPF_BFLOAT16}, {grad_k, ld_grad_k, head_grad_k, T, kv_heads, D, DPPF_BFLOAT16},
+                                {grad_v, ld_grad_v, head_grad_v, T, kv_heads, D, DPPF_BFLOAT16}};
+    if (!lse || !plan || !ws) return DPPF_ERR_INVALID_ARG;
+    for (const HeadRows &h : in)
+        if (!h.p || !heads_strides(h)) return DPPF_ERR_INVALID_ARG;
+    for (const HeadRows &h : written)
+        if (!h.p || !heads_strides(h)) return DPPF_ERR_INVALID_ARG;
+    for (const HeadRows &h : in)
+        if (!heads_aligned(h)) return DPPF_ERR_ALIGNMENT;
+    for (const HeadRows &h : written)
+        if (!heads_aligned(h)) return DPPF_ERR_ALIGNMENT;
+    if (!aligned_to(lse, 4) || !aligned_to(plan, 128) || !aligned_to(ws, 128)) return DPPF_ERR_ALIGNMENT;
+    const PlanLayout l = plan_layout(T, B);
+    const size_t need = dppf_attention_workspace_bytes(T, heads), lse_bytes = (size_t)heads * (size_t)T * 4;
+    if (plan_bytes < l.total || ws_bytes < need) return DPPF_ERR_WORKSPACE;
+    for (int i = 0; i < 3; ++i) {
+        for (const HeadRows &h : in)
+            if (written[i].meets(h)) return DPPF_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (written[i].meets(written[j])) return DPPF_ERR_INVALID_ARG;
+        const void *p = written[i].p;
+        const size_t n = written[i].bytes();
+        if (ranges_meet(p, n, lse, lse_bytes) || ranges_meet(p, n, plan, l.total) || ranges_meet(p, n, ws, need)) return DPPF_ERR_INVALID_ARG;
+    }
+    for (const HeadRows &h : in)
+        if (ranges_meet(h.p, h.bytes(), ws, need)) return DPPF_ERR_INVALID_ARG;
+    if (ranges_meet(ws, need, lse, lse_bytes) || ranges_meet(ws, need, plan, l.total)) return DPPF_ERR_INVALID_ARG;
+    const int dev = current_device();
+    if (dev < 0) return DPPF_ERR_CUDA;
+    AttentionGradArgs a;
+    if (!heads_map(&a.grad_out, in[0]) || !heads_map(&a.q, in[1]) || !heads_map(&a.k, in[2]) || !heads_map(&a.v, in[3])) return DPPF_ERR_CUDA;
+    unsigned char *base = static_cast<unsigned char *>(plan);
+    a.hdr = reinterpret_cast<PlanHeader *>(base);
+    a.query_tiles = reinterpret_cast<const PlanTile *>(base + l.list[kByQuery]);
+    a.key_tiles = reinterpret_cast<const PlanTile *>(base + l.list[kByKey]);
+    a.out = static_cast<const bf16 *>(out); a.dout = static_cast<const bf16 *>(grad_out);
+    a.lse = lse; a.delta = static_cast<float *>(ws);
+    a.dq = static_cast<bf16 *>(grad_q); a.dk = static_cast<bf16 *>(grad_k); a.dv = static_cast<bf16 *>(grad_v);
+    a.ld_out = ld_out; a.head_out = head_out; a.ld_dout = ld_grad_out; a.head_dout = head_grad_out;
+    a.ld_dq = ld_grad_q; a.head_dq = head_grad_q; a.ld_dk = ld_grad_k; a.head_dk = head_grad_k; a.ld_dv = ld_grad_v; a.head_dv = head_grad_v;
+    a.T = T; a.heads = heads; a.kv_heads = kv_heads; a.share = heads / kv_heads; a.D = D;
+    a.causal = causal; a.window = window;
+    a.scale = scale;
+    a.scale2 = (float)((double)scale * 1.4426950408889634);
+    a.spin = dppf_internal::first_pass_polls();
+    const long long query_blocks = (long long)heads * l.most[kByQuery], key_blocks = (long long)kv_heads * l.most[kByKey];
+    if (query_blocks > INT_MAX) return DPPF_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    return D <= 64 ? launch_attention_grad<1>(a, query_blocks, key_blocks, dev, s) : launch_attention_grad<2>(a, query_blocks, key_blocks, dev, s);
 }
 
 }  // extern "C"

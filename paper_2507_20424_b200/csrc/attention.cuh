@@ -402,4 +402,420 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     if (tid == 0 && s_dead) a.hdr->status = DPPF_ERR_TIMEOUT;
 }
 
+// ---------------------------------------------------------------- gradient
+//   P = exp(S - lse);  D_i = do_i . o_i;  dP = do v^T;  dS = P (dP - D);  dq = scale dS k;  dk = scale dS^T q;  dv = P^T do
+// Two kernels, each of which forms S and dP anew: one goes over the keys for a tile of queries (D and dq), one over the queries and the heads
+// that share a key head for a tile of keys (dk, dv).  Seven products in place of the five that a single kernel needs, whose
+// sums of dq would be additions in memory by many blocks, in another order each time; here every sum has one owner and one order.
+
+struct AttentionGradArgs {
+    CUtensorMap q, k, v, grad_out;
+    PlanHeader *hdr;
+    const PlanTile *query_tiles, *key_tiles;
+    const bf16 *out, *dout;
+    const float *lse;
+    float *delta;                // [heads][T]
+    bf16 *dq, *dk, *dv;
+    long long ld_out, head_out, ld_dout, head_dout, ld_dq, head_dq, ld_dk, head_dk, ld_dv, head_dv, T;
+    int heads, kv_heads, share, D;
+    int causal, window;
+    float scale, scale2;
+    int spin;
+};
+
+constexpr int kGradThreads = 384;          // two warpgroups that halve a tile's columns, one of copies and products
+
+// Sixteen pairs of 32 values as bf16.
+__device__ __forceinline__ void put_pairs(unsigned at, const float (&v)[32]) {
+    unsigned u[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+    tmem_store16(at, u);
+}
+
+template <int kBlocks>
+struct QueryGradShape {
+    static constexpr int kKeys = 3, kValues = 2;             // stages: a tile of keys is needed until dq has it, one of values until dP has it
+    static constexpr unsigned kSmem = (2 + kKeys + kValues) * kBlocks * kBlockBytes + 1024;
+};
+
+// dq of a tile of queries, and D.  Scores have two places in tensor memory: those of the next tile of keys are there when this one's are done.
+template <int kBlocks>
+__global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(const __grid_constant__ AttentionGradArgs a) {
+    using Shape = QueryGradShape<kBlocks>;
+    constexpr int kKeys = Shape::kKeys, kValues = Shape::kValues, kColumns = 512;
+    constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ unsigned long long q_full, k_full[kKeys], k_empty[kKeys], v_full[kValues], v_empty[kValues], s_full[2], dp_full, ds_full, o_full, drained;
+    __shared__ unsigned s_tmem;
+    __shared__ volatile int s_dead;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int head = (int)(blockIdx.x % a.heads), kv_head = head / a.share;
+    const unsigned index = blockIdx.x / a.heads;
+    if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T) {
+        if (blockIdx.x == 0 && tid == 0) a.hdr->status = DPPF_ERR_WORKSPACE;
+        return;
+    }
+    if (index >= (unsigned)a.hdr->tiles[kByQuery]) return;
+    const PlanTile t = a.query_tiles[index];
+    if (t.begin == t.end) {
+        fill_rows(a.dq + (long long)t.row * a.ld_dq + head * a.head_dq, a.ld_dq, t.rows, a.D, 0.f, tid, kGradThreads);
+        return;
+    }
+    const int lo = a.window ? max(0, t.row - a.window + 1 - t.begin) / kTile : 0;
+    const int hi = ((a.causal ? min(t.end, t.row + kTile) : t.end) - t.begin + kTile - 1) / kTile, n = hi - lo;
+    const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_q = smem, s_do = s_q + kTileBytes, s_k = s_do + kTileBytes, s_v = s_k + kKeys * kTileBytes;
+    const Waits wait{&s_dead, a.spin};
+
+    if (tid == 0) {
+        for (unsigned long long *bar : {&q_full, &s_full[0], &s_full[1], &dp_full, &o_full, &drained}) mbar_init(bar, 1);
+        mbar_init(&ds_full, 256);
+        for (int i = 0; i < kKeys; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
+        for (int i = 0; i < kValues; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
+        s_dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) tmem_alloc(&s_tmem, kColumns);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const unsigned tmem = s_tmem, DP = tmem + 256, DQ = tmem + 384;      // scores at 0 and 128
+
+    if (warp == 8) {
+        if (lane == 0) {
+            mbar_expect_tx(&q_full, 2 * kTileBytes);
+            tile_load<kBlocks>(s_q, &a.q, head, t.row, &q_full);
+            tile_load<kBlocks>(s_do, &a.grad_out, head, t.row, &q_full);
+            int keys = 0, values = 0;
+            for (int j = 0; j < n; ++j) {
+                const int sk = j % kKeys, sv = j % kValues, row = t.begin + (lo + j) * kTile;
+                if (j >= kKeys && !wait(&k_empty[sk], (j / kKeys - 1) & 1)) break;
+                mbar_expect_tx(&k_full[sk], kTileBytes);
+                tile_load<kBlocks>(s_k + sk * kTileBytes, &a.k, kv_head, row, &k_full[sk]);
+                ++keys;
+                if (j >= kValues && !wait(&v_empty[sv], (j / kValues - 1) & 1)) break;
+                mbar_expect_tx(&v_full[sv], kTileBytes);
+                tile_load<kBlocks>(s_v + sv * kTileBytes, &a.v, kv_head, row, &v_full[sv]);
+                ++values;
+            }
+            mbar_wait_bounded(&q_full, 0, kSpinLimit);                   // the copies in flight land before the block leaves
+            for (int i = max(0, keys - kKeys); i < keys; ++i) mbar_wait_bounded(&k_full[i % kKeys], (i / kKeys) & 1, kSpinLimit);
+            for (int i = max(0, values - kValues); i < values; ++i) mbar_wait_bounded(&v_full[i % kValues], (i / kValues) & 1, kSpinLimit);
+        }
+    } else if (warp == 9) {
+        auto scores = [&](int j) {
+            const unsigned tile = s_k + j % kKeys * kTileBytes;
+            if (!wait.together(&k_full[j % kKeys], (j / kKeys) & 1)) return false;
+            const int there = t.end - (t.begin + (lo + j) * kTile);
+            if (there < kTile) zero_rows<kBlocks>(tile, there);
+            if (lane == 0) {
+                product_rows<kBlocks>(tmem + (j & 1) * 128, s_q, tile);
+                products_done(&s_full[j & 1]);
+            }
+            return true;
+        };
+        auto dps = [&](int j) {
+            if (!wait.together(&v_full[j % kValues], (j / kValues) & 1)) return false;
+            if (lane == 0) {
+                product_rows<kBlocks>(DP, s_do, s_v + j % kValues * kTileBytes);
+                products_done(&dp_full);
+                products_done(&v_empty[j % kValues]);
+            }
+            return true;
+        };
+        bool ok = wait.together(&q_full, 0) && scores(0) && dps(0) && (n < 2 || scores(1));
+        for (int j = 0; ok && j < n; ++j) {
+            ok = wait.together(&ds_full, j & 1);
+            if (!ok) break;
+            tmem_fence_after();
+            if (lane == 0) {
+                product_columns<kBlocks>(DQ, DP, DP + 64, s_k + j % kKeys * kTileBytes, j > 0);
+                products_done(&k_empty[j % kKeys]);
+                if (j + 1 == n) products_done(&o_full);
+            }
+            ok = (j + 1 >= n || dps(j + 1)) && (j + 2 >= n || scores(j + 2));
+        }
+        if (lane == 0) {
+            products_done(&drained);
+            mbar_wait_bounded(&drained, 0, kSpinLimit);
+        }
+    } else if (warp < 8) {
+        const int half = warp >> 2, r = tid & 127, row = t.row + r;
+        const bool mine = r < t.rows;
+        const unsigned lanes = (unsigned)(warp & 3) << 21;
+        float delta = 0.f, lse2 = 0.f;
+        if (mine) {
+            const bf16 *o = a.out + (long long)row * a.ld_out + head * a.head_out, *d = a.dout + (long long)row * a.ld_dout + head * a.head_dout;
+            for (int c = 0; c < a.D; c += 8) {
+                float x[8], y[8];
+                load_vec<bf16, 8, false>(o + c, x);
+                load_vec<bf16, 8, false>(d + c, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) delta = fmaf(x[i], y[i], delta);
+            }
+            lse2 = a.lse[head * a.T + row] * kLog2e;
+            if (half == 0) a.delta[head * a.T + row] = delta;
+        }
+        const int see_lo = a.window ? max(t.begin, row - a.window + 1) : t.begin, see_hi = a.causal ? min(t.end, row + 1) : t.end;
+        bool ok = true;
+        for (int j = 0; j < n; ++j) {
+            const int key0 = t.begin + (lo + j) * kTile + 64 * half;
+            const bool whole = (a.causal ? t.row + 1 : t.end) >= key0 + 64 && (!a.window || t.row + kTile - a.window <= key0) && key0 + 64 <= t.end;
+            const int from = see_lo - key0, to = see_hi - key0;
+            ok = wait.together(&s_full[j & 1], (j >> 1) & 1);
+            if (!ok) break;
+            tmem_fence_after();
+            float p[2][32], d[32];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) tmem_load32(tmem + lanes + (j & 1) * 128 + 64 * half + 32 * c, p[c]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) tmem_loaded(p[c]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) p[c][i] = exp2_fast(fmaf(p[c][i], a.scale2, -lse2));
+            ok = wait.together(&dp_full, j & 1);
+            if (!ok) break;
+            tmem_fence_after();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                tmem_load32(DP + lanes + 64 * half + 32 * c, d);
+                tmem_loaded(d);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) p[c][i] *= d[i] - delta;
+            }
+            if (!whole)                                                  // a select: what is masked may be NaN
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c * 32 + i < from || c * 32 + i >= to) p[c][i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) put_pairs(DP + lanes + 64 * half + 16 * c, p[c]);
+            tmem_stored();
+            tmem_fence_before();
+            mbar_arrive(&ds_full);
+        }
+        ok = ok && wait.together(&o_full, 0);
+        tmem_fence_after();
+        const float by = ok ? a.scale : __int_as_float(0x7fc00000);
+        bf16 *dq = a.dq + (long long)row * a.ld_dq + head * a.head_dq;
+        for (int c = half * kBlocks; c < (half + 1) * kBlocks; ++c) {
+            float o[32];
+            tmem_load32(DQ + lanes + c * 32, o);
+            tmem_loaded(o);
+            if (mine) put_columns(dq, c * 32, a.D, o, by);
+        }
+        tmem_fence_before();
+    }
+    __syncthreads();
+    tmem_fence_after();
+    if (warp == 9) tmem_free(tmem, kColumns);
+    if (tid == 0 && s_dead) a.hdr->status = DPPF_ERR_TIMEOUT;
+}
+
+template <int kBlocks>
+struct KeyGradShape {
+    static constexpr int kStages = 2;                        // of a tile of queries and one of grad_out
+    static constexpr unsigned kSmem = (2 + 2 * kStages) * kBlocks * kBlockBytes + 1024;
+};
+
+// dk and dv of a tile of keys: a row of the transposed scores is a key.  Scores and dP take turns: while the exponentials of one
+// tile are taken, the tensor cores form dk and dP, and dv and the next scores while dS is.
+template <int kBlocks>
+__global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(const __grid_constant__ AttentionGradArgs a) {
+    using Shape = KeyGradShape<kBlocks>;
+    constexpr int kStages = Shape::kStages, kColumns = 512;
+    constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(16) float s_stat[kStages][2][kTile];            // lse in powers of two, and D, of a tile of queries
+    __shared__ unsigned long long kv_full, q_full[kStages], stat_full[kStages], empty[kStages], s_full, dp_full, p_full, ds_full, o_full, drained;
+    __shared__ unsigned s_tmem;
+    __shared__ volatile int s_dead;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int kv_head = (int)(blockIdx.x % a.kv_heads);
+    const unsigned index = blockIdx.x / a.kv_heads;
+    if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T || index >= (unsigned)a.hdr->tiles[kByKey]) return;      // the status is the first kernel's
+    const PlanTile t = a.key_tiles[index];
+    if (t.begin == t.end) {
+        fill_rows(a.dk + (long long)t.row * a.ld_dk + kv_head * a.head_dk, a.ld_dk, t.rows, a.D, 0.f, tid, kGradThreads);
+        fill_rows(a.dv + (long long)t.row * a.ld_dv + kv_head * a.head_dv, a.ld_dv, t.rows, a.D, 0.f, tid, kGradThreads);
+        return;
+    }
+    // blocks of queries [lo, hi) that see any of these keys, of each head in turn
+    const int lo = a.causal ? (t.row - t.begin) / kTile : 0;
+    const int hi = ((a.window ? (int)min((long long)t.end, (long long)t.row + t.rows - 1 + a.window) : t.end) - t.begin + kTile - 1) / kTile;
+    const int each = hi - lo, n = each * a.share;
+    const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_k = smem, s_v = s_k + kTileBytes, s_q = s_v + kTileBytes;   // a stage: queries, grad_out
+    const Waits wait{&s_dead, a.spin};
+
+    if (tid == 0) {
+        for (unsigned long long *bar : {&kv_full, &s_full, &dp_full, &o_full, &drained}) mbar_init(bar, 1);
+        mbar_init(&p_full, 256);
+        mbar_init(&ds_full, 256);
+        for (int i = 0; i < kStages; ++i) { mbar_init(&q_full[i], 1); mbar_init(&stat_full[i], 32); mbar_init(&empty[i], 1); }
+        s_dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) tmem_alloc(&s_tmem, kColumns);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const unsigned tmem = s_tmem, DP = tmem + 128, DV = tmem + 256, DK = tmem + 384;     // scores at 0
+
+    if (warp == 8) {
+        int issued = 0;
+        if (lane == 0) {
+            mbar_expect_tx(&kv_full, 2 * kTileBytes);
+            tile_load<kBlocks>(s_k, &a.k, kv_head, t.row, &kv_full);
+            tile_load<kBlocks>(s_v, &a.v, kv_head, t.row, &kv_full);
+        }
+        for (int i = 0; i < n; ++i) {
+            const int st = i % kStages, head = kv_head * a.share + i / each, row = t.begin + (lo + i % each) * kTile;
+            if (i >= kStages && !wait.together(&empty[st], (i / kStages - 1) & 1)) break;
+            if (lane == 0) {
+                mbar_expect_tx(&q_full[st], 2 * kTileBytes);
+                tile_load<kBlocks>(s_q + 2 * st * kTileBytes, &a.q, head, row, &q_full[st]);
+                tile_load<kBlocks>(s_q + (2 * st + 1) * kTileBytes, &a.grad_out, head, row, &q_full[st]);
+            }
+            ++issued;
+#pragma unroll
+            for (int k = lane; k < kTile; k += 32) {
+                const bool there = row + k < t.end;
+                const long long at = head * a.T + row + k;
+                s_stat[st][0][k] = there ? a.lse[at] * kLog2e : 0.f;
+                s_stat[st][1][k] = there ? a.delta[at] : 0.f;
+            }
+            mbar_arrive(&stat_full[st]);
+        }
+        if (lane == 0) {                                                 // the copies in flight land before the block leaves
+            mbar_wait_bounded(&kv_full, 0, kSpinLimit);
+            for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait_bounded(&q_full[i % kStages], (i / kStages) & 1, kSpinLimit);
+        }
+    } else if (warp == 9) {
+        auto tile_q = [&](int i) { return s_q + 2 * (i % kStages) * kTileBytes; };
+        auto scores = [&](int i) {
+            if (!wait.together(&q_full[i % kStages], (i / kStages) & 1)) return false;
+            const int there = t.end - (t.begin + (lo + i % each) * kTile);
+            if (there < kTile) {
+                zero_rows<kBlocks>(tile_q(i), there);
+                zero_rows<kBlocks>(tile_q(i) + kTileBytes, there);
+            }
+            if (lane == 0) {
+                product_rows<kBlocks>(tmem, s_k, tile_q(i));
+                products_done(&s_full);
+            }
+            return true;
+        };
+        auto dps = [&](int i) {
+            if (lane == 0) {
+                product_rows<kBlocks>(DP, s_v, tile_q(i) + kTileBytes);
+                products_done(&dp_full);
+            }
+        };
+        bool ok = wait.together(&kv_full, 0) && scores(0);
+        if (ok) dps(0);
+        for (int i = 0; ok && i < n; ++i) {
+            ok = wait.together(&p_full, i & 1);
+            if (!ok) break;
+            tmem_fence_after();
+            if (lane == 0) product_columns<kBlocks>(DV, tmem, tmem + 64, tile_q(i) + kTileBytes, i > 0);
+            ok = (i + 1 >= n || scores(i + 1)) && wait.together(&ds_full, i & 1);
+            if (!ok) break;
+            tmem_fence_after();
+            if (lane == 0) {
+                product_columns<kBlocks>(DK, DP, DP + 64, tile_q(i), i > 0);
+                products_done(&empty[i % kStages]);
+                if (i + 1 == n) products_done(&o_full);
+            }
+            if (i + 1 < n) dps(i + 1);
+        }
+        if (lane == 0) {
+            products_done(&drained);
+            mbar_wait_bounded(&drained, 0, kSpinLimit);
+        }
+    } else if (warp < 8) {
+        const int half = warp >> 2, r = tid & 127, key = t.row + r;
+        const unsigned lanes = (unsigned)(warp & 3) << 21;
+        bool ok = true;
+        for (int i = 0; i < n; ++i) {
+            const int st = i % kStages, q0 = t.begin + (lo + i % each) * kTile + 64 * half;
+            const bool whole = q0 + 64 <= t.end && (!a.causal || q0 >= t.row + kTile - 1) && (!a.window || q0 + 63 < t.row + a.window);
+            const int from = a.causal ? key - q0 : 0, to = (a.window ? (int)min((long long)t.end, (long long)key + a.window) : t.end) - q0;
+            ok = wait.together(&s_full, i & 1) && wait.together(&stat_full[st], (i / kStages) & 1);
+            if (!ok) break;
+            tmem_fence_after();
+            float p[2][32], d[32];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) tmem_load32(tmem + lanes + 64 * half + 32 * c, p[c]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) tmem_loaded(p[c]);
+            const float4 *lse2 = reinterpret_cast<const float4 *>(&s_stat[st][0][64 * half]), *delta = reinterpret_cast<const float4 *>(&s_stat[st][1][64 * half]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                    const float4 l = lse2[c * 8 + k / 4];
+                    p[c][k] = exp2_fast(fmaf(p[c][k], a.scale2, -l.x));
+                    p[c][k + 1] = exp2_fast(fmaf(p[c][k + 1], a.scale2, -l.y));
+                    p[c][k + 2] = exp2_fast(fmaf(p[c][k + 2], a.scale2, -l.z));
+                    p[c][k + 3] = exp2_fast(fmaf(p[c][k + 3], a.scale2, -l.w));
+                }
+            if (!whole)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (c * 32 + k < from || c * 32 + k >= to) p[c][k] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) put_pairs(tmem + lanes + 64 * half + 16 * c, p[c]);
+            tmem_stored();
+            tmem_fence_before();
+            mbar_arrive(&p_full);
+            ok = wait.together(&dp_full, i & 1);
+            if (!ok) break;
+            tmem_fence_after();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                tmem_load32(DP + lanes + 64 * half + 32 * c, d);
+                tmem_loaded(d);
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                    const float4 l = delta[c * 8 + k / 4];
+                    p[c][k] *= d[k] - l.x;
+                    p[c][k + 1] *= d[k + 1] - l.y;
+                    p[c][k + 2] *= d[k + 2] - l.z;
+                    p[c][k + 3] *= d[k + 3] - l.w;
+                }
+            }
+            if (!whole)                                                  // a select: what is masked may be NaN
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (c * 32 + k < from || c * 32 + k >= to) p[c][k] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) put_pairs(DP + lanes + 64 * half + 16 * c, p[c]);
+            tmem_stored();
+            tmem_fence_before();
+            mbar_arrive(&ds_full);
+        }
+        ok = ok && wait.together(&o_full, 0);
+        tmem_fence_after();
+        const float by = !ok ? __int_as_float(0x7fc00000) : half ? a.scale : 1.0f;
+        bf16 *to = half ? a.dk + (long long)key * a.ld_dk + kv_head * a.head_dk : a.dv + (long long)key * a.ld_dv + kv_head * a.head_dv;
+        for (int c = 0; c < 2 * kBlocks; ++c) {
+            float o[32];
+            tmem_load32((half ? DK : DV) + lanes + c * 32, o);
+            tmem_loaded(o);
+            if (r < t.rows) put_columns(to, c * 32, a.D, o, by);
+        }
+        tmem_fence_before();
+    }
+    __syncthreads();
+    tmem_fence_after();
+    if (warp == 9) tmem_free(tmem, kColumns);
+    if (tid == 0 && s_dead) a.hdr->status = DPPF_ERR_TIMEOUT;
+}
+
 }  // namespace

@@ -141,3 +141,35 @@ def test_forward_heads(b, heads, kv_heads, D, causal, window):
     assert not got.out[:7].any() and not got.out[-131:].any() and torch.isinf(got.lse[:, -131:]).all()
     again = b.dppf_attention(q, k, v, plan, causal=causal, window=window, scale=0.11)
     assert same_bits(again.out, got.out) and same_bits(again.lse, got.lse)
+
+
+def check_grads(b, lens, heads, kv_heads, D, causal, window, scale=None, lead=0, tail=0, seed=3):
+    starts = starts_of(lens, lead)
+    T = int(starts[-1]) + tail
+    q, k, v = inputs(T, heads, kv_heads, D, seed)
+    scale = D ** -0.5 if scale is None else scale
+    plan = b.AttentionPlan(starts, T)
+    fwd = b.dppf_attention(q, k, v, plan, causal=causal, window=window, scale=scale)
+    grad_out = randn((T, heads, D), seed + 1, 0.5)
+    got = b.dppf_attention_grad(grad_out, q, k, v, fwd.out, fwd.lse, plan, causal=causal, window=window, scale=scale)
+    assert b.dppf_device_status(plan.buffer) == b.OK
+    want = reference(q, k, v, starts, causal, window, scale, (grad_out, fwd.out, fwd.lse))
+    for name in ("v", "q", "k"):
+        within(getattr(got, name), *want[name], name)
+        x = getattr(got, name)
+        assert not x[:lead].any() and not x[T - tail:].any()
+    again = b.dppf_attention_grad(grad_out, q, k, v, fwd.out, fwd.lse, plan, causal=causal, window=window, scale=scale)
+    assert all(same_bits(x, y) for x, y in zip(got, again))
+
+
+@pytest.mark.parametrize("lens", LENGTHS, ids=str)
+@pytest.mark.parametrize("heads,kv_heads,D", [(2, 1, 128), (3, 3, 64)])
+@pytest.mark.parametrize("causal,window", MASKS)
+def test_backward_lengths(b, lens, heads, kv_heads, D, causal, window):
+    check_grads(b, lens, heads, kv_heads, D, causal, window)
+
+
+@pytest.mark.parametrize("heads,kv_heads,D", HEADS)
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 77)])
+def test_backward_heads(b, heads, kv_heads, D, causal, window):
+    check_grads(b, [150, 1, 333], heads, kv_heads, D, causal, window, scale=0.11, lead=7, tail=131)
