@@ -156,6 +156,9 @@ struct AttentionArgs {
 };
 
 constexpr int kForwardThreads = 384;       // two warpgroups of a slot each, one of copies and products
+// Of the 168 registers a thread that a block of 384 starts with: a row of scores stays in a softmax thread's.
+constexpr int kSoftmaxRegisters = 208, kControlRegisters = 80;
+static_assert(256 * kSoftmaxRegisters + 128 * kControlRegisters <= kForwardThreads * 168, "no more registers than the block has");
 template <int kBlocks>
 struct ForwardShape {
     static constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
@@ -183,6 +186,12 @@ __device__ __forceinline__ void fill_rows(bf16 *p, long long ld, int rows, int D
         const int r = i / (D / 8), c = i - r * (D / 8);
         *reinterpret_cast<uint4 *>(p + r * ld + c * 8) = make_uint4(u, u, u, u);
     }
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float m;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
 }
 
 // S = scale q k^T over the keys that a query sees; out = softmax(S) v; lse = log sum exp S.
@@ -240,6 +249,8 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     tmem_fence_after();
     const unsigned tmem = s_tmem;                                        // scores of slot s at 128 s, its output at 256 + 128 s
 
+    if (warp >= 8) {
+    give_registers<kControlRegisters>();
     if (warp == 8) {
         // ---- copies
         if (lane == 0) {
@@ -309,8 +320,10 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
             products_done(&drained);
             mbar_wait_bounded(&drained, 0, kSpinLimit);
         }
-    } else if (warp < 8) {
+    }
+    } else {
         // ---- softmax: a row a thread
+        take_registers<kSoftmaxRegisters>();
         const int s = warp >> 2, r = tid & 127, row = slot_row(s) + r;
         const int first = s ? lo1 : lo0, last = s ? hi1 : hi0;
         const unsigned lanes = (unsigned)(warp & 3) << 21, S = tmem + lanes + s * 128, O = tmem + lanes + 256 + s * 128;
@@ -340,9 +353,11 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
             }
             float m[4] = {v[0][0], v[1][0], v[2][0], v[3][0]};
 #pragma unroll
-            for (int i = 1; i < 32; ++i)
+            for (int i = 1; i < 31; i += 2)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) m[c] = fmaxf(m[c], v[c][i]);
+                for (int c = 0; c < 4; ++c) m[c] = max3(m[c], v[c][i], v[c][i + 1]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) m[c] = fmaxf(m[c], v[c][31]);
             const float now = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * a.scale2;
             // The sums stay relative to an older maximum until one is 2^8 above it: then no exponential is above 2^8, and fp32 sums
             // of bf16 products lose nothing.

@@ -37,6 +37,11 @@ __device__ __forceinline__ void mbar_arrive(unsigned long long *bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
+// Registers of a warpgroup's threads from here on.  A block starts with kThreads times as many as it was compiled for; what one
+// warpgroup gives up another may take, never more than that in all.
+template <int kRegisters> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
+template <int kRegisters> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
+
 // ---------------------------------------------------------------- copies
 
 // Box at (column, head, row) of a tensor [rows][heads][columns]; what lies outside the tensor is zero.  column * 2 is a multiple of 16.
