@@ -25,6 +25,8 @@ struct PlanHeader {          // first bytes of the plan
 };
 struct PlanTile { int row, rows, begin, end; };       // first row, rows of this tile; its sequence's rows (begin == end: no sequence)
 
+__device__ __forceinline__ PlanTile uniform(const PlanTile &t) { return {uniform(t.row), uniform(t.rows), uniform(t.begin), uniform(t.end)}; }
+
 struct PlanArgs {
     const void *starts;
     PlanHeader *hdr;
@@ -208,14 +210,14 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     __shared__ unsigned long long q_full[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2], drained;
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const unsigned unit = blockIdx.x % a.units, index = blockIdx.x / a.units;
     if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T) {                 // not a plan of these rows
         if (blockIdx.x == 0 && tid == 0) a.hdr->status = DPPF_ERR_WORKSPACE;
         return;
     }
     if (index >= (unsigned)a.hdr->tiles[a.list]) return;
-    const PlanTile t = a.tiles[index];
+    const PlanTile t = uniform(a.tiles[index]);
     // slots: query rows [row, row + rows) of a head
     const int head0 = a.by_head ? 2 * unit : unit, kv_head = head0 / a.share;
     auto slot_row = [&](int s) { return a.by_head ? t.row : t.row + s * kTile; };
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const unsigned tmem = s_tmem;                                        // scores of slot s at 128 s, its output at 256 + 128 s
+    const unsigned tmem = uniform(s_tmem);                                        // scores of slot s at 128 s, its output at 256 + 128 s
 
     if (warp >= 8) {
     give_registers<kControlRegisters>();
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
         auto full = [&](int n) { return wait.together(&kv_full[n % kStages], (n / kStages) & 1); };
         auto active = [&](int s, int j) { return s == 0 ? j >= lo0 && j < hi0 : j >= lo1 && j < hi1; };
         auto scores = [&](int s, int j) {
-            if (lane == 0) {
+            if (elect()) {
                 product_rows<kBlocks>(tmem + s * 128, s_q + s * kTileBytes, s_kv + (2 * (j - lo)) % kStages * kTileBytes);
                 products_done(&s_full[s]);
             }
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
         if (ok) {
             for (int s = 0; s < 2; ++s)
                 if (active(s, lo)) scores(s, lo);
-            if (lane == 0) products_done(&kv_empty[0]);
+            if (elect()) products_done(&kv_empty[0]);
         }
         for (int j = lo; ok && j < hi; ++j) {
             const int nv = 2 * (j - lo) + 1, nk = nv + 1;
@@ -304,7 +306,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
                     ok = wait.together(&p_full[s], (j - (s ? lo1 : lo0)) & 1);
                     if (!ok) break;
                     tmem_fence_after();
-                    if (lane == 0) {
+                    if (elect()) {
                         product_columns<kBlocks>(tmem + 256 + s * 128, tmem + s * 128, tmem + s * 128 + 32, tile, j > (s ? lo1 : lo0));
                         if (j + 1 == (s ? hi1 : hi0)) products_done(&o_full[s]);
                     }
@@ -316,7 +318,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
                 if (j + 1 < hi) products_done(&kv_empty[nk % kStages]);
             }
         }
-        if (lane == 0) {                                                 // nothing is in flight when the block leaves
+        if (elect()) {                                                 // nothing is in flight when the block leaves
             products_done(&drained);
             mbar_wait_bounded(&drained, 0, kSpinLimit);
         }
@@ -464,7 +466,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     __shared__ unsigned long long q_full, k_full[kKeys], k_empty[kKeys], v_full[kValues], v_empty[kValues], s_full[2], dp_full, ds_full, o_full, drained;
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int head = (int)(blockIdx.x % a.heads), kv_head = head / a.share;
     const unsigned index = blockIdx.x / a.heads;
     if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T) {
@@ -472,7 +474,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
         return;
     }
     if (index >= (unsigned)a.hdr->tiles[kByQuery]) return;
-    const PlanTile t = a.query_tiles[index];
+    const PlanTile t = uniform(a.query_tiles[index]);
     if (t.begin == t.end) {
         fill_rows(a.dq + (long long)t.row * a.ld_dq + head * a.head_dq, a.ld_dq, t.rows, a.D, 0.f, tid, kGradThreads);
         return;
@@ -494,7 +496,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const unsigned tmem = s_tmem, DP = tmem + 256, DQ = tmem + 384;      // scores at 0 and 128
+    const unsigned tmem = uniform(s_tmem), DP = tmem + 256, DQ = tmem + 384;      // scores at 0 and 128
 
     if (warp == 8) {
         if (lane == 0) {
@@ -523,7 +525,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
             if (!wait.together(&k_full[j % kKeys], (j / kKeys) & 1)) return false;
             const int there = t.end - (t.begin + (lo + j) * kTile);
             if (there < kTile) zero_rows<kBlocks>(tile, there);
-            if (lane == 0) {
+            if (elect()) {
                 product_rows<kBlocks>(tmem + (j & 1) * 128, s_q, tile);
                 products_done(&s_full[j & 1]);
             }
@@ -531,7 +533,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
         };
         auto dps = [&](int j) {
             if (!wait.together(&v_full[j % kValues], (j / kValues) & 1)) return false;
-            if (lane == 0) {
+            if (elect()) {
                 product_rows<kBlocks>(DP, s_do, s_v + j % kValues * kTileBytes);
                 products_done(&dp_full);
                 products_done(&v_empty[j % kValues]);
@@ -543,14 +545,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
             ok = wait.together(&ds_full, j & 1);
             if (!ok) break;
             tmem_fence_after();
-            if (lane == 0) {
+            if (elect()) {
                 product_columns<kBlocks>(DQ, DP, DP + 64, s_k + j % kKeys * kTileBytes, j > 0);
                 products_done(&k_empty[j % kKeys]);
                 if (j + 1 == n) products_done(&o_full);
             }
             ok = (j + 1 >= n || dps(j + 1)) && (j + 2 >= n || scores(j + 2));
         }
-        if (lane == 0) {
+        if (elect()) {
             products_done(&drained);
             mbar_wait_bounded(&drained, 0, kSpinLimit);
         }
@@ -647,11 +649,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     __shared__ unsigned long long kv_full, q_full[kStages], stat_full[kStages], empty[kStages], s_full, dp_full, p_full, ds_full, o_full, drained;
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int kv_head = (int)(blockIdx.x % a.kv_heads);
     const unsigned index = blockIdx.x / a.kv_heads;
     if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T || index >= (unsigned)a.hdr->tiles[kByKey]) return;      // the status is the first kernel's
-    const PlanTile t = a.key_tiles[index];
+    const PlanTile t = uniform(a.key_tiles[index]);
     if (t.begin == t.end) {
         fill_rows(a.dk + (long long)t.row * a.ld_dk + kv_head * a.head_dk, a.ld_dk, t.rows, a.D, 0.f, tid, kGradThreads);
         fill_rows(a.dv + (long long)t.row * a.ld_dv + kv_head * a.head_dv, a.ld_dv, t.rows, a.D, 0.f, tid, kGradThreads);
@@ -676,7 +678,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const unsigned tmem = s_tmem, DP = tmem + 128, DV = tmem + 256, DK = tmem + 384;     // scores at 0
+    const unsigned tmem = uniform(s_tmem), DP = tmem + 128, DV = tmem + 256, DK = tmem + 384;     // scores at 0
 
     if (warp == 8) {
         int issued = 0;
@@ -716,14 +718,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
                 zero_rows<kBlocks>(tile_q(i), there);
                 zero_rows<kBlocks>(tile_q(i) + kTileBytes, there);
             }
-            if (lane == 0) {
+            if (elect()) {
                 product_rows<kBlocks>(tmem, s_k, tile_q(i));
                 products_done(&s_full);
             }
             return true;
         };
         auto dps = [&](int i) {
-            if (lane == 0) {
+            if (elect()) {
                 product_rows<kBlocks>(DP, s_v, tile_q(i) + kTileBytes);
                 products_done(&dp_full);
             }
@@ -734,18 +736,18 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             ok = wait.together(&p_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
-            if (lane == 0) product_columns<kBlocks>(DV, tmem, tmem + 64, tile_q(i) + kTileBytes, i > 0);
+            if (elect()) product_columns<kBlocks>(DV, tmem, tmem + 64, tile_q(i) + kTileBytes, i > 0);
             ok = (i + 1 >= n || scores(i + 1)) && wait.together(&ds_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
-            if (lane == 0) {
+            if (elect()) {
                 product_columns<kBlocks>(DK, DP, DP + 64, tile_q(i), i > 0);
                 products_done(&empty[i % kStages]);
                 if (i + 1 == n) products_done(&o_full);
             }
             if (i + 1 < n) dps(i + 1);
         }
-        if (lane == 0) {
+        if (elect()) {
             products_done(&drained);
             mbar_wait_bounded(&drained, 0, kSpinLimit);
         }

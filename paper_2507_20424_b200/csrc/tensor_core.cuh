@@ -68,6 +68,17 @@ __device__ __forceinline__ void zero_rows(unsigned tile, int first) {
 }
 
 // ---------------------------------------------------------------- products
+// An instruction's operands lie in uniform registers.  Values that the compiler knows to be the same in all lanes stay there; of
+// others it moves every one over before each instruction, which held the products up (about 100 cycles an instruction, of 64).
+// So what they are formed from passes through uniform(), and their thread is the one that elect() names.
+
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ unsigned uniform(unsigned x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ bool elect() {                            // true in one lane of the warp, always the same
+    unsigned is;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(is));
+    return is != 0;
+}
 
 __device__ __forceinline__ unsigned long long operand(unsigned addr, unsigned leading_bytes) {
     // bits 0-13 address / 16, 16-29 leading offset / 16, 32-45 stride of eight rows / 16, 46-48 one, 61-63 128-byte swizzle
