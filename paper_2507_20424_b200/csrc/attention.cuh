@@ -164,8 +164,9 @@ static_assert(256 * kSoftmaxRegisters + 128 * kControlRegisters <= kForwardThrea
 template <int kBlocks>
 struct ForwardShape {
     static constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
-    static constexpr int kStages = kBlocks == 2 ? 4 : 6;                 // of keys and values in turn
-    static constexpr unsigned kSmem = (2 + kStages) * kTileBytes + 1024;
+    static constexpr int kStages = kBlocks == 2 ? 2 : 4;                 // of a tile of keys and one of values
+    static constexpr int kPolynomial = kBlocks == 2 ? 8 : 4;             // one in so many exponentials is a polynomial
+    static constexpr unsigned kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
 };
 
 // Eight bf16 columns a store, those below D, of 32 columns from `at` on.
@@ -196,6 +197,22 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return m;
 }
 
+// 2^x of two numbers on the multiply-add pipes, for a part of the exponentials: the special function unit gives 16 a cycle and SM,
+// as many as the products of a tile ask for in their time.  x = n + f with n whole and |f| <= 1/2: the fp32 sum x + 1.5 2^23 ends in n,
+// a polynomial of degree 4 (least relative error with p(0) = 1 on the interval: 2.9e-6, far below the 2^-8 of the bf16 result) gives 2^f,
+// and n is added to its exponent.  x <= -127 gives 0.
+__device__ __forceinline__ float2 exp2_polynomial(float2 x) {
+    const float kRound = 12582912.0f;
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.0f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-127.0f));
+    const float2 t = add2(x, both(kRound)), n = add2(t, both(-kRound)), f = fma2(n, both(-1.0f), x);
+    float2 p = fma2(f, both(0.009582852944731712f), both(0.055906426161527634f));
+    p = fma2(p, f, both(0.24024099111557007f));
+    p = fma2(p, f, both(0.6931241750717163f));
+    p = fma2(p, f, both(1.0f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
 // S = scale q k^T over the keys that a query sees; out = softmax(S) v; lse = log sum exp S.
 // One pass over the keys with a running maximum and sum.  A block has two slots of 128 queries that share their keys and values:
 // while one slot's warpgroup takes the exponentials of its scores (a row a thread), the tensor cores work for the other.
@@ -203,11 +220,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 template <int kBlocks>
 __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __grid_constant__ AttentionArgs a) {
     using Shape = ForwardShape<kBlocks>;
-    constexpr int kStages = Shape::kStages;
+    constexpr int kStages = Shape::kStages, kPolynomial = Shape::kPolynomial;
     constexpr unsigned kTileBytes = Shape::kTileBytes;
     constexpr int kColumns = 512;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ unsigned long long q_full[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2], drained;
+    __shared__ unsigned long long q_full[2], k_full[kStages], v_full[kStages], empty[kStages], v_fixed, s_full[2], p_half[2], p_full[2], o_full[2], drained;
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
@@ -238,9 +255,15 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_q = smem, s_kv = smem + 2 * kTileBytes;
     const Waits wait{&s_dead, a.spin};
 
+    const int slots = hi1 ? 2 : 1;
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) { mbar_init(&q_full[s], 1); mbar_init(&s_full[s], 1); mbar_init(&p_full[s], 128); mbar_init(&o_full[s], 1); }
-        for (int i = 0; i < kStages; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); }
+        for (int s = 0; s < 2; ++s) {
+            for (unsigned long long *bar : {&q_full[s], &s_full[s], &o_full[s]}) mbar_init(bar, 1);
+            mbar_init(&p_half[s], 128);
+            mbar_init(&p_full[s], 128);
+        }
+        for (int i = 0; i < kStages; ++i) { mbar_init(&k_full[i], 1); mbar_init(&v_full[i], 1); mbar_init(&empty[i], 1); }
+        mbar_init(&v_fixed, 1);
         mbar_init(&drained, 1);
         s_dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -252,77 +275,82 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     const unsigned tmem = uniform(s_tmem);                                        // scores of slot s at 128 s, its output at 256 + 128 s
 
     if (warp >= 8) {
-    give_registers<kControlRegisters>();
-    if (warp == 8) {
-        // ---- copies
-        if (lane == 0) {
-            unsigned issued = 0;
+        give_registers<kControlRegisters>();
+        const int last = hi - 1, there = t.end - (t.begin + last * kTile);       // rows of the last tile that are the sequence's
+        if (warp == 8) {
+            // ---- copies
+            int issued = 0;                                              // key tiles; the same or one less of values
             bool ok = true;
-            auto load = [&](const CUtensorMap *map, int block) {
-                const unsigned st = issued % kStages;
-                ok = ok && (issued < kStages || wait(&kv_empty[st], (issued / kStages - 1) & 1));
-                if (!ok) return;
-                mbar_expect_tx(&kv_full[st], kTileBytes);
-                tile_load<kBlocks>(s_kv + st * kTileBytes, map, kv_head, t.begin + block * kTile, &kv_full[st]);
-                ++issued;
-            };
-            for (int s = 0; s < (hi1 ? 2 : 1); ++s) {
-                mbar_expect_tx(&q_full[s], kTileBytes);
-                tile_load<kBlocks>(s_q + s * kTileBytes, &a.q, slot_head(s), slot_row(s), &q_full[s]);
-                if (s == 0) load(&a.k, lo);
-            }
-            load(&a.v, lo);
-            for (int j = lo + 1; j < hi; ++j) { load(&a.k, j); load(&a.v, j); }
-            // the copies in flight land before the block leaves
-            for (int s = 0; s < (hi1 ? 2 : 1); ++s) mbar_wait_bounded(&q_full[s], 0, kSpinLimit);
-            for (unsigned i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait_bounded(&kv_full[i % kStages], (i / kStages) & 1, kSpinLimit);
-        }
-    } else if (warp == 9) {
-        // ---- products, issued by lane 0; the warp waits together
-        auto full = [&](int n) { return wait.together(&kv_full[n % kStages], (n / kStages) & 1); };
-        auto active = [&](int s, int j) { return s == 0 ? j >= lo0 && j < hi0 : j >= lo1 && j < hi1; };
-        auto scores = [&](int s, int j) {
             if (elect()) {
-                product_rows<kBlocks>(tmem + s * 128, s_q + s * kTileBytes, s_kv + (2 * (j - lo)) % kStages * kTileBytes);
-                products_done(&s_full[s]);
-            }
-        };
-        bool ok = wait.together(&q_full[0], 0) && (!hi1 || wait.together(&q_full[1], 0)) && full(0);
-        if (ok) {
-            for (int s = 0; s < 2; ++s)
-                if (active(s, lo)) scores(s, lo);
-            if (elect()) products_done(&kv_empty[0]);
-        }
-        for (int j = lo; ok && j < hi; ++j) {
-            const int nv = 2 * (j - lo) + 1, nk = nv + 1;
-            const unsigned tile = s_kv + nv % kStages * kTileBytes;
-            ok = full(nv);
-            if (!ok) break;
-            const int there = t.end - (t.begin + j * kTile);
-            if (there < kTile) zero_rows<kBlocks>(tile, there);
-            if (j + 1 < hi && !(ok = full(nk))) break;
-            for (int s = 0; s < 2; ++s) {
-                if (active(s, j)) {
-                    ok = wait.together(&p_full[s], (j - (s ? lo1 : lo0)) & 1);
-                    if (!ok) break;
-                    tmem_fence_after();
-                    if (elect()) {
-                        product_columns<kBlocks>(tmem + 256 + s * 128, tmem + s * 128, tmem + s * 128 + 32, tile, j > (s ? lo1 : lo0));
-                        if (j + 1 == (s ? hi1 : hi0)) products_done(&o_full[s]);
+                for (int s = 0; s < slots; ++s) {
+                    mbar_expect_tx(&q_full[s], kTileBytes);
+                    tile_load<kBlocks>(s_q + s * kTileBytes, &a.q, slot_head(s), slot_row(s), &q_full[s]);
+                    if (s == 0) {
+                        mbar_expect_tx(&k_full[0], kTileBytes);
+                        tile_load<kBlocks>(s_kv, &a.k, kv_head, t.begin + lo * kTile, &k_full[0]);
                     }
                 }
-                if (active(s, j + 1)) scores(s, j + 1);
+                for (int j = lo; j < hi; ++j, ++issued) {
+                    const int st = issued % kStages, row = t.begin + j * kTile;
+                    if (issued >= kStages && !(ok = wait(&empty[st], (issued / kStages - 1) & 1))) break;
+                    if (issued) {
+                        mbar_expect_tx(&k_full[st], kTileBytes);
+                        tile_load<kBlocks>(s_kv + 2 * st * kTileBytes, &a.k, kv_head, row, &k_full[st]);
+                    }
+                    mbar_expect_tx(&v_full[st], kTileBytes);
+                    tile_load<kBlocks>(s_kv + (2 * st + 1) * kTileBytes, &a.v, kv_head, row, &v_full[st]);
+                }
             }
-            if (ok && lane == 0) {
-                products_done(&kv_empty[nv % kStages]);
-                if (j + 1 < hi) products_done(&kv_empty[nk % kStages]);
+            issued = __reduce_max_sync(0xffffffffu, issued);             // the elected lane's
+            if (there < kTile && issued == hi - lo) {                    // values of other sequences must not reach a sum
+                const int st = (issued - 1) % kStages;
+                if (wait.together(&v_full[st], ((issued - 1) / kStages) & 1)) zero_rows<kBlocks>(s_kv + (2 * st + 1) * kTileBytes, there);
+                if (lane == 0) mbar_arrive(&v_fixed);
+            }
+            if (lane == 0) {                                             // the copies in flight land before the block leaves
+                for (int s = 0; s < slots; ++s) mbar_wait_bounded(&q_full[s], 0, kSpinLimit);
+                if (issued == 0) mbar_wait_bounded(&k_full[0], 0, kSpinLimit);
+                for (int i = max(0, issued - kStages); i < issued; ++i) {
+                    mbar_wait_bounded(&k_full[i % kStages], (i / kStages) & 1, kSpinLimit);
+                    mbar_wait_bounded(&v_full[i % kStages], (i / kStages) & 1, kSpinLimit);
+                }
+            }
+        } else if (warp == 9) {
+            // ---- products: of one slot the probabilities times the values of tile j, then the scores of tile j + 1; then of the other
+            bool ok = wait.together(&q_full[0], 0) && (slots == 1 || wait.together(&q_full[1], 0));
+            for (int j = lo - 1; ok && j < hi; ++j) {
+                const int n = j - lo, st = n % kStages, to = (n + 1) % kStages;
+                const unsigned tile = s_kv + (2 * st + 1) * kTileBytes;
+                ok = (n < 0 || (wait.together(&v_full[st], (n / kStages) & 1) && (j < last || there >= kTile || wait.together(&v_fixed, 0)))) &&
+                     (j + 1 >= hi || wait.together(&k_full[to], ((n + 1) / kStages) & 1));
+                for (int s = 0; ok && s < slots; ++s) {
+                    const int first = s ? lo1 : lo0, end = s ? hi1 : hi0, nth = j - first;
+                    const unsigned S = tmem + s * 128, O = tmem + 256 + s * 128;
+                    if (nth >= 0 && j < end) {
+                        ok = wait.together(&p_half[s], nth & 1);
+                        if (!ok) break;
+                        tmem_fence_after();
+                        if (elect()) product_columns<kBlocks>(O, S, tile, 0, nth > 0);
+                        ok = wait.together(&p_full[s], nth & 1);
+                        if (!ok) break;
+                        tmem_fence_after();
+                        if (elect()) {
+                            product_columns<kBlocks>(O, S + 32, tile, 1, true);
+                            if (j + 1 == end) products_done(&o_full[s]);
+                        }
+                    }
+                    if (n >= 0 && s + 1 == slots && elect()) products_done(&empty[st]);
+                    if (nth >= -1 && j + 1 < end && elect()) {
+                        product_rows<kBlocks>(S, s_q + s * kTileBytes, s_kv + 2 * to * kTileBytes);
+                        products_done(&s_full[s]);
+                    }
+                }
+            }
+            if (elect()) {                                               // nothing is in flight when the block leaves
+                products_done(&drained);
+                mbar_wait_bounded(&drained, 0, kSpinLimit);
             }
         }
-        if (elect()) {                                                 // nothing is in flight when the block leaves
-            products_done(&drained);
-            mbar_wait_bounded(&drained, 0, kSpinLimit);
-        }
-    }
     } else {
         // ---- softmax: a row a thread
         take_registers<kSoftmaxRegisters>();
@@ -353,45 +381,66 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
                     for (int i = 0; i < 32; ++i)
                         if (c * 32 + i < from || c * 32 + i >= to) v[c][i] = -INFINITY;
             }
-            float m[4] = {v[0][0], v[1][0], v[2][0], v[3][0]};
-#pragma unroll
-            for (int i = 1; i < 31; i += 2)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) m[c] = max3(m[c], v[c][i], v[c][i + 1]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) m[c] = fmaxf(m[c], v[c][31]);
-            const float now = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * a.scale2;
-            // The sums stay relative to an older maximum until one is 2^8 above it: then no exponential is above 2^8, and fp32 sums
-            // of bf16 products lose nothing.
-            const bool grow = now > top + 8.0f || top == -INFINITY;
-            if (j > first && __any_sync(0xffffffffu, grow && now > top)) {
-                const float f = grow && now > top ? exp2_fast(top - now) : 1.0f;
-                sum *= f;
-                for (int c = 0; c < 2 * kBlocks; ++c) {
-                    float o[32];
-                    tmem_load32(O + c * 32, o);
-                    tmem_loaded(o);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] *= f;
-                    tmem_store32(O + c * 32, o);
-                }
-            }
-            if (grow && now > top) top = now;
-            const float2 by = both(a.scale2), off = both(top == -INFINITY ? 0.f : -top);
-            float2 sums = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                unsigned p[16];
+            unsigned p[2][16];
+            auto exponentials = [&](int c, float2 &sums, unsigned (&to)[16], float &high) {      // of 32 columns
+                const float2 by = both(a.scale2), off = both(top == -INFINITY ? 0.f : -top);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     float2 e = fma2(make_float2(v[c][2 * i], v[c][2 * i + 1]), by, off);
-                    e.x = exp2_fast(e.x);
-                    e.y = exp2_fast(e.y);
+                    if (i % kPolynomial == 3) { high = max3(high, e.x, e.y); e = exp2_polynomial(e); }
+                    else { e.x = exp2_fast(e.x); e.y = exp2_fast(e.y); }
                     sums = add2(sums, e);
-                    p[i] = bf16_pair(e.x, e.y);
+                    to[i] = bf16_pair(e.x, e.y);
                 }
-                tmem_store16(S + c * 16, p);
+            };
+            // The sums stay relative to the maximum of the first tile until an exponential would be above 2^60, which is rare: fp32 and
+            // bf16 keep their relative precision up to 2^127.  So no maximum is taken of what the first half's sum tells: it is at least
+            // the largest of them.  (A polynomial's argument above 128 would come out as any number: those are looked at.)
+            float2 sums = make_float2(0.f, 0.f);
+            float high = -INFINITY;                                      // of the second half, and of the first's polynomials
+            if (j > first) {
+                exponentials(0, sums, p[0], high);
+                exponentials(1, sums, p[1], high);
             }
+            float m[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < 32; i += 2)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) m[c] = max3(m[c], v[c + 2][i], v[c + 2][i + 1]);
+            const float most = fmaxf(m[0], m[1]) * a.scale2;
+            const bool grow = top == -INFINITY || sums.x + sums.y > 0x1p60f || fmaxf(high, most - top) > 60.0f;
+            if (j == first || __any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 2)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) m[c] = max3(m[c], v[c][i], v[c][i + 1]);
+                const float now = fmaxf(m[0], m[1]) * a.scale2;
+                if (j > first) {
+                    const float f = now > top ? exp2_fast(top - now) : 1.0f;
+                    sum *= f;
+                    for (int c = 0; c < 4 * kBlocks; ++c) {
+                        float o[16];
+                        unsigned u[16];
+                        tmem_load16(O + c * 16, o);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(o[i] * f);
+                        tmem_store16(O + c * 16, u);
+                    }
+                }
+                top = fmaxf(top, now);
+                sums = make_float2(0.f, 0.f);
+                exponentials(0, sums, p[0], high);
+                exponentials(1, sums, p[1], high);
+            }
+            tmem_store16(S, p[0]);
+            tmem_store16(S + 16, p[1]);
+            tmem_stored();
+            tmem_fence_before();
+            mbar_arrive(&p_half[s]);
+            exponentials(2, sums, p[0], high);
+            tmem_store16(S + 32, p[0]);
+            exponentials(3, sums, p[1], high);
+            tmem_store16(S + 48, p[1]);
             sum += sums.x + sums.y;
             tmem_stored();
             tmem_fence_before();
@@ -546,7 +595,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
-                product_columns<kBlocks>(DQ, DP, DP + 64, s_k + j % kKeys * kTileBytes, j > 0);
+                product_columns<kBlocks>(DQ, DP, s_k + j % kKeys * kTileBytes, 0, j > 0);
+                product_columns<kBlocks>(DQ, DP + 64, s_k + j % kKeys * kTileBytes, 1, true);
                 products_done(&k_empty[j % kKeys]);
                 if (j + 1 == n) products_done(&o_full);
             }
@@ -736,12 +786,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             ok = wait.together(&p_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
-            if (elect()) product_columns<kBlocks>(DV, tmem, tmem + 64, tile_q(i) + kTileBytes, i > 0);
+            if (elect()) {
+                product_columns<kBlocks>(DV, tmem, tile_q(i) + kTileBytes, 0, i > 0);
+                product_columns<kBlocks>(DV, tmem + 64, tile_q(i) + kTileBytes, 1, true);
+            }
             ok = (i + 1 >= n || scores(i + 1)) && wait.together(&ds_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
-                product_columns<kBlocks>(DK, DP, DP + 64, tile_q(i), i > 0);
+                product_columns<kBlocks>(DK, DP, tile_q(i), 0, i > 0);
+                product_columns<kBlocks>(DK, DP + 64, tile_q(i), 1, true);
                 products_done(&empty[i % kStages]);
                 if (i + 1 == n) products_done(&o_full);
             }

@@ -42,6 +42,15 @@ __device__ __forceinline__ void mbar_arrive(unsigned long long *bar) {
 template <int kRegisters> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
 template <int kRegisters> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
 
+// Barrier `id` (1 .. 15) of `threads` threads; true in all if `any` is in one.
+__device__ __forceinline__ bool group_any(int id, int threads, bool any) {
+    unsigned r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %3, 0;\n bar.red.or.pred p, %1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(r) : "r"(id), "r"(threads), "r"((unsigned)any) : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ void group_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
 // ---------------------------------------------------------------- copies
 
 // Box at (column, head, row) of a tensor [rows][heads][columns]; what lies outside the tensor is zero.  column * 2 is a multiple of 16.
@@ -112,14 +121,13 @@ __device__ __forceinline__ void product_rows(unsigned d, unsigned a, unsigned b)
         product16(d, da + at, db + at, product_kind<kTile, false>(), k > 0);
     }
 }
-// d[128, 64 * kBlocks] (+)= p[128, 128] times tile b, summed over b's rows.  p: bf16 pairs in tensor memory, rows 0-63 of the sum
-// from column `low` on, 64-127 from column `high` on.
+// d[128, 64 * kBlocks] (+)= p[128, 64] times rows [64 half, 64 half + 64) of tile b, summed over them.  p: bf16 pairs in 32 columns of tensor
+// memory.
 template <int kBlocks>
-__device__ __forceinline__ void product_columns(unsigned d, unsigned low, unsigned high, unsigned b, bool add) {
-    const unsigned long long db = operand_columns(b);
+__device__ __forceinline__ void product_columns(unsigned d, unsigned p, unsigned b, int half, bool add) {
+    const unsigned long long db = operand_columns(b + half * 8192);
 #pragma unroll
-    for (int k = 0; k < kTile / 16; ++k)
-        product16_tmem(d, (k < 4 ? low : high) + (k % 4) * 8, db + ((k * 2048) >> 4), product_kind<64 * kBlocks, true>(), add || k > 0);
+    for (int k = 0; k < 4; ++k) product16_tmem(d, p + k * 8, db + ((k * 2048) >> 4), product_kind<64 * kBlocks, true>(), add || k > 0);
 }
 // Arrives on `bar` when all products that this thread has issued are done.
 __device__ __forceinline__ void products_done(unsigned long long *bar) {
@@ -154,13 +162,10 @@ __device__ __forceinline__ void tmem_load32(unsigned at, float (&v)[32]) {
 __device__ __forceinline__ void tmem_loaded(float (&v)[32]) {       // waits for all loads before it; ties v's uses to the wait
     asm volatile("tcgen05.wait::ld.sync.aligned;" : DPPF_M16(v, 0), DPPF_M16(v, 16)::"memory");
 }
-__device__ __forceinline__ void tmem_store32(unsigned at, const float (&f)[32]) {
-    unsigned v[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(f[i]);
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
-                 "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(at), DPPF_U16(v, 0), DPPF_U16(v, 16) : "memory");
+__device__ __forceinline__ void tmem_load16(unsigned at, float (&v)[16]) {          // 16 columns, waited for
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : DPPF_R16(v, 0) : "r"(at) : "memory");
 }
 __device__ __forceinline__ void tmem_store16(unsigned at, const unsigned (&v)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
