@@ -70,25 +70,25 @@ struct AttentionShape {
     }
 };
 
-std::atomic<int> g_forward_ready[2][kMaxDevices];
+std::atomic<int> g_forward_ready[3][kMaxDevices];
 
-template <int kBlocks>
+template <int kSteps>
 int launch_attention(const AttentionArgs &a, long long blocks, int dev, cudaStream_t s) {
-    constexpr int kSmem = (int)ForwardShape<kBlocks>::kSmem;
-    if (!allow_smem(attention_kernel<kBlocks>, dev, g_forward_ready[kBlocks - 1], kSmem)) return DPPF_ERR_CUDA;
-    attention_kernel<kBlocks><<<(unsigned)blocks, kForwardThreads, kSmem, s>>>(a);
+    constexpr int kSmem = (int)ForwardShape<kSteps>::kSmem;
+    if (!allow_smem(attention_kernel<kSteps>, dev, g_forward_ready[kSteps / 2 - 2], kSmem)) return DPPF_ERR_CUDA;
+    attention_kernel<kSteps><<<(unsigned)blocks, kForwardThreads, kSmem, s>>>(a);
     return launched();
 }
 
-std::atomic<int> g_query_ready[2][kMaxDevices], g_key_ready[2][kMaxDevices];
+std::atomic<int> g_query_ready[3][kMaxDevices], g_key_ready[3][kMaxDevices];
 
-template <int kBlocks>
+template <int kSteps>
 int launch_attention_grad(const AttentionGradArgs &a, long long query_blocks, long long key_blocks, int dev, cudaStream_t s) {
-    constexpr int kQuerySmem = (int)QueryGradShape<kBlocks>::kSmem, kKeySmem = (int)KeyGradShape<kBlocks>::kSmem;
-    if (!allow_smem(attention_grad_query_kernel<kBlocks>, dev, g_query_ready[kBlocks - 1], kQuerySmem) || !allow_smem(attention_grad_key_kernel<kBlocks>, dev, g_key_ready[kBlocks - 1], kKeySmem))
+    constexpr int kQuerySmem = (int)QueryGradShape<kSteps>::kSmem, kKeySmem = (int)KeyGradShape<kSteps>::kSmem;
+    if (!allow_smem(attention_grad_query_kernel<kSteps>, dev, g_query_ready[kSteps / 2 - 2], kQuerySmem) || !allow_smem(attention_grad_key_kernel<kSteps>, dev, g_key_ready[kSteps / 2 - 2], kKeySmem))
         return DPPF_ERR_CUDA;
-    attention_grad_query_kernel<kBlocks><<<(unsigned)query_blocks, kGradThreads, kQuerySmem, s>>>(a);
-    if (cudaPeekAtLastError() == cudaSuccess) attention_grad_key_kernel<kBlocks><<<(unsigned)key_blocks, kGradThreads, kKeySmem, s>>>(a);
+    attention_grad_query_kernel<kSteps><<<(unsigned)query_blocks, kGradThreads, kQuerySmem, s>>>(a);
+    if (cudaPeekAtLastError() == cudaSuccess) attention_grad_key_kernel<kSteps><<<(unsigned)key_blocks, kGradThreads, kKeySmem, s>>>(a);
     return launched();
 }
 
@@ -157,7 +157,8 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
     const long long blocks = (long long)a.units * l.most[a.list];
     if (blocks > INT_MAX) return DPPF_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    return D <= 64 ? launch_attention<1>(a, blocks, dev, s) : launch_attention<2>(a, blocks, dev, s);
+    // heads as wide as 64, 96 or 128: what a product sums over, or has as columns
+    return D <= 64 ? launch_attention<4>(a, blocks, dev, s) : D <= 96 ? launch_attention<6>(a, blocks, dev, s) : launch_attention<8>(a, blocks, dev, s);
 }
 
 size_t dppf_attention_workspace_bytes(int64_t T, int heads) {
@@ -204,15 +205,13 @@ int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_
     const int dev = current_device();
     if (dev < 0) return DPPF_ERR_CUDA;
     AttentionGradArgs a;
-    if (!heads_map(&a.grad_out, in[0]) || !heads_map(&a.q, in[1]) || !heads_map(&a.k, in[2]) || !heads_map(&a.v, in[3])) return DPPF_ERR_CUDA;
+    if (!heads_map(&a.grad_out, in[0]) || !heads_map(&a.q, in[1]) || !heads_map(&a.k, in[2]) || !heads_map(&a.v, in[3]) || !heads_map(&a.out, in[4])) return DPPF_ERR_CUDA;
     unsigned char *base = static_cast<unsigned char *>(plan);
     a.hdr = reinterpret_cast<PlanHeader *>(base);
     a.query_tiles = reinterpret_cast<const PlanTile *>(base + l.list[kByQuery]);
     a.key_tiles = reinterpret_cast<const PlanTile *>(base + l.list[kByKey]);
-    a.out = static_cast<const bf16 *>(out); a.dout = static_cast<const bf16 *>(grad_out);
     a.lse = lse; a.delta = static_cast<float *>(ws);
     a.dq = static_cast<bf16 *>(grad_q); a.dk = static_cast<bf16 *>(grad_k); a.dv = static_cast<bf16 *>(grad_v);
-    a.ld_out = ld_out; a.head_out = head_out; a.ld_dout = ld_grad_out; a.head_dout = head_grad_out;
     a.ld_dq = ld_grad_q; a.head_dq = head_grad_q; a.ld_dk = ld_grad_k; a.head_dk = head_grad_k; a.ld_dv = ld_grad_v; a.head_dv = head_grad_v;
     a.T = T; a.heads = heads; a.kv_heads = kv_heads; a.share = heads / kv_heads; a.D = D;
     a.causal = causal; a.window = window;
@@ -222,7 +221,8 @@ int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_
     const long long query_blocks = (long long)heads * l.most[kByQuery], key_blocks = (long long)kv_heads * l.most[kByKey];
     if (query_blocks > INT_MAX) return DPPF_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    return D <= 64 ? launch_attention_grad<1>(a, query_blocks, key_blocks, dev, s) : launch_attention_grad<2>(a, query_blocks, key_blocks, dev, s);
+    if (D <= 64) return launch_attention_grad<4>(a, query_blocks, key_blocks, dev, s);
+    return D <= 96 ? launch_attention_grad<6>(a, query_blocks, key_blocks, dev, s) : launch_attention_grad<8>(a, query_blocks, key_blocks, dev, s);
 }
 
 }  // extern "C"

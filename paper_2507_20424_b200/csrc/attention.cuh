@@ -159,10 +159,11 @@ struct AttentionArgs {
 
 constexpr int kForwardThreads = 384;       // two warpgroups of a slot each, one of copies and products
 // Of the 168 registers a thread that a block of 384 starts with: a row of scores stays in a softmax thread's.
-constexpr int kSoftmaxRegisters = 208, kControlRegisters = 80;
+constexpr int kSoftmaxRegisters = 208, kControlRegisters = 88;
 static_assert(256 * kSoftmaxRegisters + 128 * kControlRegisters <= kForwardThreads * 168, "no more registers than the block has");
-template <int kBlocks>
+template <int kSteps>
 struct ForwardShape {
+    static constexpr int kBlocks = (kSteps + 3) / 4;
     static constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
     static constexpr int kStages = kBlocks == 2 ? 2 : 4;                 // of a tile of keys and one of values
     static constexpr int kPolynomial = kBlocks == 2 ? 8 : 4;             // one in so many exponentials is a polynomial
@@ -217,9 +218,10 @@ __device__ __forceinline__ float2 exp2_polynomial(float2 x) {
 // One pass over the keys with a running maximum and sum.  A block has two slots of 128 queries that share their keys and values:
 // while one slot's warpgroup takes the exponentials of its scores (a row a thread), the tensor cores work for the other.
 // Scores and output sums stay in tensor memory; the probabilities replace the scores there as bf16, the first operand of the second product.
-template <int kBlocks>
+template <int kSteps>
 __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __grid_constant__ AttentionArgs a) {
-    using Shape = ForwardShape<kBlocks>;
+    using Shape = ForwardShape<kSteps>;
+    constexpr int kBlocks = Shape::kBlocks;
     constexpr int kStages = Shape::kStages, kPolynomial = Shape::kPolynomial;
     constexpr unsigned kTileBytes = Shape::kTileBytes;
     constexpr int kColumns = 512;
@@ -330,18 +332,18 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
                         ok = wait.together(&p_half[s], nth & 1);
                         if (!ok) break;
                         tmem_fence_after();
-                        if (elect()) product_columns<kBlocks>(O, S, tile, 0, nth > 0);
+                        if (elect()) product_columns<kSteps>(O, S, tile, 0, nth > 0);
                         ok = wait.together(&p_full[s], nth & 1);
                         if (!ok) break;
                         tmem_fence_after();
                         if (elect()) {
-                            product_columns<kBlocks>(O, S + 32, tile, 1, true);
+                            product_columns<kSteps>(O, S + 32, tile, 1, true);
                             if (j + 1 == end) products_done(&o_full[s]);
                         }
                     }
                     if (n >= 0 && s + 1 == slots && elect()) products_done(&empty[st]);
                     if (nth >= -1 && j + 1 < end && elect()) {
-                        product_rows<kBlocks>(S, s_q + s * kTileBytes, s_kv + 2 * to * kTileBytes);
+                        product_rows<kSteps>(S, s_q + s * kTileBytes, s_kv + 2 * to * kTileBytes);
                         products_done(&s_full[s]);
                     }
                 }
@@ -475,14 +477,13 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
 // sums of dq would be additions in memory by many blocks, in another order each time; here every sum has one owner and one order.
 
 struct AttentionGradArgs {
-    CUtensorMap q, k, v, grad_out;
+    CUtensorMap q, k, v, grad_out, out;
     PlanHeader *hdr;
     const PlanTile *query_tiles, *key_tiles;
-    const bf16 *out, *dout;
     const float *lse;
     float *delta;                // [heads][T]
     bf16 *dq, *dk, *dv;
-    long long ld_out, head_out, ld_dout, head_dout, ld_dq, head_dq, ld_dk, head_dk, ld_dv, head_dv, T;
+    long long ld_dq, head_dq, ld_dk, head_dk, ld_dv, head_dv, T;
     int heads, kv_heads, share, D;
     int causal, window;
     float scale, scale2;
@@ -499,20 +500,48 @@ __device__ __forceinline__ void put_pairs(unsigned at, const float (&v)[32]) {
     tmem_store16(at, u);
 }
 
-template <int kBlocks>
+// v = 2^(v by + off(i)) for pairs i; an eighth of them by polynomial.
+template <typename Off>
+__device__ __forceinline__ void probabilities(float (&v)[32], float2 by, Off off) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float2 e = fma2(make_float2(v[2 * i], v[2 * i + 1]), by, off(i));
+        if (i % 8 == 3) e = exp2_polynomial(e);
+        else { e.x = exp2_fast(e.x); e.y = exp2_fast(e.y); }
+        v[2 * i] = e.x;
+        v[2 * i + 1] = e.y;
+    }
+}
+// v *= d + off(i) for pairs i
+template <typename Off>
+__device__ __forceinline__ void times_difference(float (&v)[32], const float (&d)[32], Off off) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float2 e = mul2(make_float2(v[2 * i], v[2 * i + 1]), add2(make_float2(d[2 * i], d[2 * i + 1]), off(i)));
+        v[2 * i] = e.x;
+        v[2 * i + 1] = e.y;
+    }
+}
+
+template <int kSteps>
 struct QueryGradShape {
+    static constexpr int kBlocks = (kSteps + 3) / 4;
     static constexpr int kKeys = 3, kValues = 2;             // stages: a tile of keys is needed until dq has it, one of values until dP has it
     static constexpr unsigned kSmem = (2 + kKeys + kValues) * kBlocks * kBlockBytes + 1024;
 };
 
-// dq of a tile of queries, and D.  Scores have two places in tensor memory: those of the next tile of keys are there when this one's are done.
-template <int kBlocks>
+// dq of a tile of queries, and D.  The tile's queries and grad_out lie in tensor memory, too: with both operands of a product in shared
+// memory its reads take all of that memory's bandwidth, and the copies' writes come on top.  A thread takes half a row of scores to registers at
+// once, so that the products of the next tile of keys can replace them while it takes the exponentials.
+template <int kSteps>
 __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(const __grid_constant__ AttentionGradArgs a) {
-    using Shape = QueryGradShape<kBlocks>;
+    using Shape = QueryGradShape<kSteps>;
+    constexpr int kBlocks = Shape::kBlocks;
     constexpr int kKeys = Shape::kKeys, kValues = Shape::kValues, kColumns = 512;
     constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ unsigned long long q_full, k_full[kKeys], k_empty[kKeys], v_full[kValues], v_empty[kValues], s_full[2], dp_full, ds_full, o_full, drained;
+    __shared__ unsigned long long q_full, o_read, rows_ready, k_full[kKeys], k_empty[kKeys], v_full[kValues], v_empty[kValues], s_full, s_free, dp_full, ds_full, o_full, k_fixed, drained;
+    __shared__ float s_delta[kTile];
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
@@ -530,12 +559,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     }
     const int lo = a.window ? max(0, t.row - a.window + 1 - t.begin) / kTile : 0;
     const int hi = ((a.causal ? min(t.end, t.row + kTile) : t.end) - t.begin + kTile - 1) / kTile, n = hi - lo;
-    const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_q = smem, s_do = s_q + kTileBytes, s_k = s_do + kTileBytes, s_v = s_k + kKeys * kTileBytes;
+    const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_q = smem, s_do = s_q + kTileBytes, s_k = s_do + kTileBytes, s_v = s_k + kKeys * kTileBytes, s_out = s_k + (kKeys - 1) * kTileBytes;   // the tile's output where the third tile of keys will be
     const Waits wait{&s_dead, a.spin};
 
     if (tid == 0) {
-        for (unsigned long long *bar : {&q_full, &s_full[0], &s_full[1], &dp_full, &o_full, &drained}) mbar_init(bar, 1);
-        mbar_init(&ds_full, 256);
+        for (unsigned long long *bar : {&q_full, &s_full, &dp_full, &o_full, &k_fixed, &drained}) mbar_init(bar, 1);
+        for (unsigned long long *bar : {&rows_ready, &s_free, &ds_full}) mbar_init(bar, 256);
+        mbar_init(&o_read, 128);
         for (int i = 0; i < kKeys; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
         for (int i = 0; i < kValues; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
         s_dead = 0;
@@ -545,16 +575,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const unsigned tmem = uniform(s_tmem), DP = tmem + 256, DQ = tmem + 384;      // scores at 0 and 128
+    const unsigned tmem = uniform(s_tmem), DP = tmem + 128, DQ = tmem + 256, Q = tmem + 384, DO = tmem + 448;      // scores at 0
 
+    const int there = t.end - (t.begin + (hi - 1) * kTile);              // rows of the last tile that are the sequence's
     if (warp == 8) {
-        if (lane == 0) {
-            mbar_expect_tx(&q_full, 2 * kTileBytes);
+        int keys = 0, values = 0;
+        if (elect()) {
+            mbar_expect_tx(&q_full, 3 * kTileBytes);
             tile_load<kBlocks>(s_q, &a.q, head, t.row, &q_full);
             tile_load<kBlocks>(s_do, &a.grad_out, head, t.row, &q_full);
-            int keys = 0, values = 0;
+            tile_load<kBlocks>(s_out, &a.out, head, t.row, &q_full);
             for (int j = 0; j < n; ++j) {
                 const int sk = j % kKeys, sv = j % kValues, row = t.begin + (lo + j) * kTile;
+                if (j == kKeys - 1 && !wait(&o_read, 0)) break;
                 if (j >= kKeys && !wait(&k_empty[sk], (j / kKeys - 1) & 1)) break;
                 mbar_expect_tx(&k_full[sk], kTileBytes);
                 tile_load<kBlocks>(s_k + sk * kTileBytes, &a.k, kv_head, row, &k_full[sk]);
@@ -564,43 +597,50 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
                 tile_load<kBlocks>(s_v + sv * kTileBytes, &a.v, kv_head, row, &v_full[sv]);
                 ++values;
             }
-            mbar_wait_bounded(&q_full, 0, kSpinLimit);                   // the copies in flight land before the block leaves
+        }
+        keys = __reduce_max_sync(0xffffffffu, keys);                     // the elected lane's
+        values = __reduce_max_sync(0xffffffffu, values);
+        if (there < kTile && keys == n) {                                // keys of other sequences must not reach a sum
+            const int st = (n - 1) % kKeys;
+            if (wait.together(&k_full[st], ((n - 1) / kKeys) & 1)) zero_rows<kBlocks>(s_k + st * kTileBytes, there);
+            if (lane == 0) mbar_arrive(&k_fixed);
+        }
+        if (lane == 0) {                                                 // the copies in flight land before the block leaves
+            mbar_wait_bounded(&q_full, 0, kSpinLimit);
             for (int i = max(0, keys - kKeys); i < keys; ++i) mbar_wait_bounded(&k_full[i % kKeys], (i / kKeys) & 1, kSpinLimit);
             for (int i = max(0, values - kValues); i < values; ++i) mbar_wait_bounded(&v_full[i % kValues], (i / kValues) & 1, kSpinLimit);
         }
     } else if (warp == 9) {
         auto scores = [&](int j) {
-            const unsigned tile = s_k + j % kKeys * kTileBytes;
-            if (!wait.together(&k_full[j % kKeys], (j / kKeys) & 1)) return false;
-            const int there = t.end - (t.begin + (lo + j) * kTile);
-            if (there < kTile) zero_rows<kBlocks>(tile, there);
+            if (!wait.together(&k_full[j % kKeys], (j / kKeys) & 1) || (j > 0 && !wait.together(&s_free, (j - 1) & 1))) return false;
+            tmem_fence_after();
             if (elect()) {
-                product_rows<kBlocks>(tmem + (j & 1) * 128, s_q, tile);
-                products_done(&s_full[j & 1]);
+                product_rows_tmem<kSteps>(tmem, Q, s_k + j % kKeys * kTileBytes);
+                products_done(&s_full);
             }
             return true;
         };
         auto dps = [&](int j) {
             if (!wait.together(&v_full[j % kValues], (j / kValues) & 1)) return false;
             if (elect()) {
-                product_rows<kBlocks>(DP, s_do, s_v + j % kValues * kTileBytes);
+                product_rows_tmem<kSteps>(DP, DO, s_v + j % kValues * kTileBytes);
                 products_done(&dp_full);
                 products_done(&v_empty[j % kValues]);
             }
             return true;
         };
-        bool ok = wait.together(&q_full, 0) && scores(0) && dps(0) && (n < 2 || scores(1));
+        bool ok = wait.together(&rows_ready, 0) && scores(0) && dps(0);
         for (int j = 0; ok && j < n; ++j) {
-            ok = wait.together(&ds_full, j & 1);
+            ok = (j + 1 >= n || scores(j + 1)) && wait.together(&ds_full, j & 1) && (j + 1 < n || there >= kTile || wait.together(&k_fixed, 0));
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
-                product_columns<kBlocks>(DQ, DP, s_k + j % kKeys * kTileBytes, 0, j > 0);
-                product_columns<kBlocks>(DQ, DP + 64, s_k + j % kKeys * kTileBytes, 1, true);
+                product_columns<kSteps>(DQ, DP, s_k + j % kKeys * kTileBytes, 0, j > 0);
+                product_columns<kSteps>(DQ, DP + 64, s_k + j % kKeys * kTileBytes, 1, true);
                 products_done(&k_empty[j % kKeys]);
                 if (j + 1 == n) products_done(&o_full);
             }
-            ok = (j + 1 >= n || dps(j + 1)) && (j + 2 >= n || scores(j + 2));
+            ok = j + 1 >= n || dps(j + 1);
         }
         if (elect()) {
             products_done(&drained);
@@ -610,37 +650,52 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
         const int half = warp >> 2, r = tid & 127, row = t.row + r;
         const bool mine = r < t.rows;
         const unsigned lanes = (unsigned)(warp & 3) << 21;
-        float delta = 0.f, lse2 = 0.f;
-        if (mine) {
-            const bf16 *o = a.out + (long long)row * a.ld_out + head * a.head_out, *d = a.dout + (long long)row * a.ld_dout + head * a.head_dout;
-            for (int c = 0; c < a.D; c += 8) {
-                float x[8], y[8];
-                load_vec<bf16, 8, false>(o + c, x);
-                load_vec<bf16, 8, false>(d + c, y);
+        // queries and grad_out go on to tensor memory, a row a thread, one of them a warpgroup; that of grad_out forms D
+        const float lse2 = mine ? a.lse[head * a.T + row] * kLog2e : 0.f;
+        bool ok = wait.together(&q_full, 0);
+        float delta = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) delta = fmaf(x[i], y[i], delta);
+        for (int c = 0; c < 2 * kBlocks; ++c) {
+            unsigned u[16];
+            tile_row(half ? s_do : s_q, r, c, u);
+            tmem_store16((half ? DO : Q) + lanes + 16 * c, u);
+            if (half) {
+                unsigned o[16];
+                tile_row(s_out, r, c, o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    delta = fmaf(bf16_low(o[i]), bf16_low(u[i]), delta);
+                    delta = fmaf(bf16_high(o[i]), bf16_high(u[i]), delta);
+                }
             }
-            lse2 = a.lse[head * a.T + row] * kLog2e;
-            if (half == 0) a.delta[head * a.T + row] = delta;
         }
+        if (half) mbar_arrive(&o_read);
+        tmem_stored();
+        tmem_fence_before();
+        mbar_arrive(&rows_ready);
+        if (half) {
+            s_delta[r] = delta;
+            if (mine) a.delta[head * a.T + row] = delta;
+        }
+        group_sync(1, 256);
+        delta = s_delta[r];
         const int see_lo = a.window ? max(t.begin, row - a.window + 1) : t.begin, see_hi = a.causal ? min(t.end, row + 1) : t.end;
-        bool ok = true;
-        for (int j = 0; j < n; ++j) {
+        for (int j = 0; ok && j < n; ++j) {
             const int key0 = t.begin + (lo + j) * kTile + 64 * half;
             const bool whole = (a.causal ? t.row + 1 : t.end) >= key0 + 64 && (!a.window || t.row + kTile - a.window <= key0) && key0 + 64 <= t.end;
             const int from = see_lo - key0, to = see_hi - key0;
-            ok = wait.together(&s_full[j & 1], (j >> 1) & 1);
+            ok = wait.together(&s_full, j & 1);
             if (!ok) break;
             tmem_fence_after();
             float p[2][32], d[32];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) tmem_load32(tmem + lanes + (j & 1) * 128 + 64 * half + 32 * c, p[c]);
+            for (int c = 0; c < 2; ++c) tmem_load32(tmem + lanes + 64 * half + 32 * c, p[c]);
 #pragma unroll
             for (int c = 0; c < 2; ++c) tmem_loaded(p[c]);
+            tmem_fence_before();
+            mbar_arrive(&s_free);
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int i = 0; i < 32; ++i) p[c][i] = exp2_fast(fmaf(p[c][i], a.scale2, -lse2));
+            for (int c = 0; c < 2; ++c) probabilities(p[c], both(a.scale2), [&](int) { return both(-lse2); });
             ok = wait.together(&dp_full, j & 1);
             if (!ok) break;
             tmem_fence_after();
@@ -648,8 +703,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
             for (int c = 0; c < 2; ++c) {
                 tmem_load32(DP + lanes + 64 * half + 32 * c, d);
                 tmem_loaded(d);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) p[c][i] *= d[i] - delta;
+                times_difference(p[c], d, [&](int) { return both(-delta); });
             }
             if (!whole)                                                  // a select: what is masked may be NaN
 #pragma unroll
@@ -681,22 +735,24 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     if (tid == 0 && s_dead) a.hdr->status = DPPF_ERR_TIMEOUT;
 }
 
-template <int kBlocks>
+template <int kSteps>
 struct KeyGradShape {
-    static constexpr int kStages = 2;                        // of a tile of queries and one of grad_out
-    static constexpr unsigned kSmem = (2 + 2 * kStages) * kBlocks * kBlockBytes + 1024;
+    static constexpr int kBlocks = (kSteps + 3) / 4;
+    static constexpr int kQueries = 3, kOuts = 2;            // stages: a tile of queries is asked for before the one before it is done with
+    static constexpr unsigned kTiles = (2 + kQueries + kOuts) * kBlocks * kBlockBytes;
+    static constexpr unsigned kSmem = kTiles + 2 * 2 * kTile * 4;        // and lse and D of two tiles of queries
 };
 
 // dk and dv of a tile of keys: a row of the transposed scores is a key.  Scores and dP take turns: while the exponentials of one
 // tile are taken, the tensor cores form dk and dP, and dv and the next scores while dS is.
-template <int kBlocks>
+template <int kSteps>
 __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(const __grid_constant__ AttentionGradArgs a) {
-    using Shape = KeyGradShape<kBlocks>;
-    constexpr int kStages = Shape::kStages, kColumns = 512;
+    using Shape = KeyGradShape<kSteps>;
+    constexpr int kBlocks = Shape::kBlocks;
+    constexpr int kQueries = Shape::kQueries, kOuts = Shape::kOuts, kColumns = 512;
     constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
-    extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(16) float s_stat[kStages][2][kTile];            // lse in powers of two, and D, of a tile of queries
-    __shared__ unsigned long long kv_full, q_full[kStages], stat_full[kStages], empty[kStages], s_full, dp_full, p_full, ds_full, o_full, drained;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ unsigned long long kv_full, q_full[kQueries], q_ready[kQueries], q_empty[kQueries], do_full[kOuts], do_ready[kOuts], do_empty[kOuts], stat_full[2], s_full, dp_full, p_full, ds_full, o_full, drained;
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
@@ -713,14 +769,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     const int lo = a.causal ? (t.row - t.begin) / kTile : 0;
     const int hi = ((a.window ? (int)min((long long)t.end, (long long)t.row + t.rows - 1 + a.window) : t.end) - t.begin + kTile - 1) / kTile;
     const int each = hi - lo, n = each * a.share;
-    const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_k = smem, s_v = s_k + kTileBytes, s_q = s_v + kTileBytes;   // a stage: queries, grad_out
+    const unsigned s_k = smem_addr(smem_raw), s_v = s_k + kTileBytes, s_q = s_v + kTileBytes, s_do = s_q + kQueries * kTileBytes;
+    float (*s_stat)[2][kTile] = reinterpret_cast<float (*)[2][kTile]>(smem_raw + Shape::kTiles);      // lse in powers of two, and D, of a tile of queries
     const Waits wait{&s_dead, a.spin};
 
     if (tid == 0) {
         for (unsigned long long *bar : {&kv_full, &s_full, &dp_full, &o_full, &drained}) mbar_init(bar, 1);
         mbar_init(&p_full, 256);
         mbar_init(&ds_full, 256);
-        for (int i = 0; i < kStages; ++i) { mbar_init(&q_full[i], 1); mbar_init(&stat_full[i], 32); mbar_init(&empty[i], 1); }
+        for (int i = 0; i < kQueries; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_ready[i], 1); mbar_init(&q_empty[i], 1); }
+        for (int i = 0; i < kOuts; ++i) { mbar_init(&do_full[i], 1); mbar_init(&do_ready[i], 1); mbar_init(&do_empty[i], 1); mbar_init(&stat_full[i], 32); }
         s_dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -730,90 +788,108 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     tmem_fence_after();
     const unsigned tmem = uniform(s_tmem), DP = tmem + 128, DV = tmem + 256, DK = tmem + 384;     // scores at 0
 
+    auto head_of = [&](int i) { return kv_head * a.share + i / each; };
+    auto row_of = [&](int i) { return t.begin + (lo + i % each) * kTile; };
     if (warp == 8) {
-        int issued = 0;
-        if (lane == 0) {
+        // ---- copies
+        if (elect()) {
+            int queries = 0, outs = 0;
             mbar_expect_tx(&kv_full, 2 * kTileBytes);
             tile_load<kBlocks>(s_k, &a.k, kv_head, t.row, &kv_full);
             tile_load<kBlocks>(s_v, &a.v, kv_head, t.row, &kv_full);
-        }
-        for (int i = 0; i < n; ++i) {
-            const int st = i % kStages, head = kv_head * a.share + i / each, row = t.begin + (lo + i % each) * kTile;
-            if (i >= kStages && !wait.together(&empty[st], (i / kStages - 1) & 1)) break;
-            if (lane == 0) {
-                mbar_expect_tx(&q_full[st], 2 * kTileBytes);
-                tile_load<kBlocks>(s_q + 2 * st * kTileBytes, &a.q, head, row, &q_full[st]);
-                tile_load<kBlocks>(s_q + (2 * st + 1) * kTileBytes, &a.grad_out, head, row, &q_full[st]);
+            for (int i = 0; i < n; ++i) {
+                const int sq = i % kQueries, so = i % kOuts, head = head_of(i), row = row_of(i);
+                if (i >= kQueries && !wait(&q_empty[sq], (i / kQueries - 1) & 1)) break;
+                mbar_expect_tx(&q_full[sq], kTileBytes);
+                tile_load<kBlocks>(s_q + sq * kTileBytes, &a.q, head, row, &q_full[sq]);
+                ++queries;
+                if (i >= kOuts && !wait(&do_empty[so], (i / kOuts - 1) & 1)) break;
+                mbar_expect_tx(&do_full[so], kTileBytes);
+                tile_load<kBlocks>(s_do + so * kTileBytes, &a.grad_out, head, row, &do_full[so]);
+                ++outs;
             }
-            ++issued;
-#pragma unroll
-            for (int k = lane; k < kTile; k += 32) {
-                const bool there = row + k < t.end;
-                const long long at = head * a.T + row + k;
-                s_stat[st][0][k] = there ? a.lse[at] * kLog2e : 0.f;
-                s_stat[st][1][k] = there ? a.delta[at] : 0.f;
-            }
-            mbar_arrive(&stat_full[st]);
-        }
-        if (lane == 0) {                                                 // the copies in flight land before the block leaves
-            mbar_wait_bounded(&kv_full, 0, kSpinLimit);
-            for (int i = max(0, issued - kStages); i < issued; ++i) mbar_wait_bounded(&q_full[i % kStages], (i / kStages) & 1, kSpinLimit);
+            mbar_wait_bounded(&kv_full, 0, kSpinLimit);                  // the copies in flight land before the block leaves
+            for (int i = max(0, queries - kQueries); i < queries; ++i) mbar_wait_bounded(&q_full[i % kQueries], (i / kQueries) & 1, kSpinLimit);
+            for (int i = max(0, outs - kOuts); i < outs; ++i) mbar_wait_bounded(&do_full[i % kOuts], (i / kOuts) & 1, kSpinLimit);
         }
     } else if (warp == 9) {
-        auto tile_q = [&](int i) { return s_q + 2 * (i % kStages) * kTileBytes; };
+        // ---- products
         auto scores = [&](int i) {
-            if (!wait.together(&q_full[i % kStages], (i / kStages) & 1)) return false;
-            const int there = t.end - (t.begin + (lo + i % each) * kTile);
-            if (there < kTile) {
-                zero_rows<kBlocks>(tile_q(i), there);
-                zero_rows<kBlocks>(tile_q(i) + kTileBytes, there);
-            }
+            const int st = i % kQueries;
+            if (!wait.together(&q_ready[st], (i / kQueries) & 1)) return false;
             if (elect()) {
-                product_rows<kBlocks>(tmem, s_k, tile_q(i));
+                product_rows<kSteps>(tmem, s_k, s_q + st * kTileBytes);
                 products_done(&s_full);
             }
             return true;
         };
         auto dps = [&](int i) {
+            const int st = i % kOuts;
+            if (!wait.together(&do_ready[st], (i / kOuts) & 1)) return false;
             if (elect()) {
-                product_rows<kBlocks>(DP, s_v, tile_q(i) + kTileBytes);
+                product_rows<kSteps>(DP, s_v, s_do + st * kTileBytes);
                 products_done(&dp_full);
             }
+            return true;
         };
-        bool ok = wait.together(&kv_full, 0) && scores(0);
-        if (ok) dps(0);
+        bool ok = wait.together(&kv_full, 0) && scores(0) && dps(0);
         for (int i = 0; ok && i < n; ++i) {
+            const unsigned tile_do = s_do + i % kOuts * kTileBytes, tile_q = s_q + i % kQueries * kTileBytes;
             ok = wait.together(&p_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
-                product_columns<kBlocks>(DV, tmem, tile_q(i) + kTileBytes, 0, i > 0);
-                product_columns<kBlocks>(DV, tmem + 64, tile_q(i) + kTileBytes, 1, true);
+                product_columns<kSteps>(DV, tmem, tile_do, 0, i > 0);
+                product_columns<kSteps>(DV, tmem + 64, tile_do, 1, true);
+                products_done(&do_empty[i % kOuts]);
             }
             ok = (i + 1 >= n || scores(i + 1)) && wait.together(&ds_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
-                product_columns<kBlocks>(DK, DP, tile_q(i), 0, i > 0);
-                product_columns<kBlocks>(DK, DP + 64, tile_q(i), 1, true);
-                products_done(&empty[i % kStages]);
+                product_columns<kSteps>(DK, DP, tile_q, 0, i > 0);
+                product_columns<kSteps>(DK, DP + 64, tile_q, 1, true);
+                products_done(&q_empty[i % kQueries]);
                 if (i + 1 == n) products_done(&o_full);
             }
-            if (i + 1 < n) dps(i + 1);
+            ok = i + 1 >= n || dps(i + 1);
         }
         if (elect()) {
             products_done(&drained);
             mbar_wait_bounded(&drained, 0, kSpinLimit);
+        }
+    } else if (warp >= 10) {
+        // ---- tiles as they arrive: rows of other sequences must not reach a sum.  One warp for the queries, with lse and D, one for
+        // grad_out.  Every tile passes here, so that neither warp can be a phase behind.
+        const bool queries = warp == 10;
+        bool ok = true;
+        for (int i = 0; ok && i < n; ++i) {
+            const int st = i % (queries ? kQueries : kOuts), row = row_of(i), there = t.end - row;
+            const unsigned parity = (i / (queries ? kQueries : kOuts)) & 1;
+            if (queries) {
+                // those of two tiles before are done with when its products with dS are
+                if (i >= 2 && !(ok = wait.together(&q_empty[(i - 2) % kQueries], ((i - 2) / kQueries) & 1))) break;
+                const long long at = head_of(i) * a.T + row;
+#pragma unroll
+                for (int k = lane; k < kTile; k += 32) {
+                    s_stat[i & 1][0][k] = k < there ? -kLog2e * a.lse[at + k] : 0.f;
+                    s_stat[i & 1][1][k] = k < there ? -a.delta[at + k] : 0.f;
+                }
+                mbar_arrive(&stat_full[i & 1]);
+            }
+            if (!(ok = wait.together(queries ? &q_full[st] : &do_full[st], parity))) break;
+            if (there < kTile) zero_rows<kBlocks>((queries ? s_q : s_do) + st * kTileBytes, there);
+            if (lane == 0) mbar_arrive(queries ? &q_ready[st] : &do_ready[st]);
         }
     } else if (warp < 8) {
         const int half = warp >> 2, r = tid & 127, key = t.row + r;
         const unsigned lanes = (unsigned)(warp & 3) << 21;
         bool ok = true;
         for (int i = 0; i < n; ++i) {
-            const int st = i % kStages, q0 = t.begin + (lo + i % each) * kTile + 64 * half;
+            const int q0 = row_of(i) + 64 * half;
             const bool whole = q0 + 64 <= t.end && (!a.causal || q0 >= t.row + kTile - 1) && (!a.window || q0 + 63 < t.row + a.window);
             const int from = a.causal ? key - q0 : 0, to = (a.window ? (int)min((long long)t.end, (long long)key + a.window) : t.end) - q0;
-            ok = wait.together(&s_full, i & 1) && wait.together(&stat_full[st], (i / kStages) & 1);
+            ok = wait.together(&s_full, i & 1) && wait.together(&stat_full[i & 1], (i >> 1) & 1);
             if (!ok) break;
             tmem_fence_after();
             float p[2][32], d[32];
@@ -821,17 +897,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             for (int c = 0; c < 2; ++c) tmem_load32(tmem + lanes + 64 * half + 32 * c, p[c]);
 #pragma unroll
             for (int c = 0; c < 2; ++c) tmem_loaded(p[c]);
-            const float4 *lse2 = reinterpret_cast<const float4 *>(&s_stat[st][0][64 * half]), *delta = reinterpret_cast<const float4 *>(&s_stat[st][1][64 * half]);
+            const float2 *lse2 = reinterpret_cast<const float2 *>(&s_stat[i & 1][0][64 * half]), *delta = reinterpret_cast<const float2 *>(&s_stat[i & 1][1][64 * half]);
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    const float4 l = lse2[c * 8 + k / 4];
-                    p[c][k] = exp2_fast(fmaf(p[c][k], a.scale2, -l.x));
-                    p[c][k + 1] = exp2_fast(fmaf(p[c][k + 1], a.scale2, -l.y));
-                    p[c][k + 2] = exp2_fast(fmaf(p[c][k + 2], a.scale2, -l.z));
-                    p[c][k + 3] = exp2_fast(fmaf(p[c][k + 3], a.scale2, -l.w));
-                }
+            for (int c = 0; c < 2; ++c) probabilities(p[c], both(a.scale2), [&](int k) { return lse2[c * 16 + k]; });
             if (!whole)
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
@@ -850,14 +918,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             for (int c = 0; c < 2; ++c) {
                 tmem_load32(DP + lanes + 64 * half + 32 * c, d);
                 tmem_loaded(d);
-#pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    const float4 l = delta[c * 8 + k / 4];
-                    p[c][k] *= d[k] - l.x;
-                    p[c][k + 1] *= d[k + 1] - l.y;
-                    p[c][k + 2] *= d[k + 2] - l.z;
-                    p[c][k + 3] *= d[k + 3] - l.w;
-                }
+                times_difference(p[c], d, [&](int k) { return delta[c * 16 + k]; });
             }
             if (!whole)                                                  // a select: what is masked may be NaN
 #pragma unroll

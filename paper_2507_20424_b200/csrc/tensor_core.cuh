@@ -76,6 +76,17 @@ __device__ __forceinline__ void zero_rows(unsigned tile, int first) {
     __syncwarp();
 }
 
+// Sixteen words of row r of a tile: its columns [32 part, 32 part + 32).
+__device__ __forceinline__ void tile_row(unsigned tile, int r, int part, unsigned (&u)[16]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const int piece = part * 4 + c;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(u[4 * c]), "=r"(u[4 * c + 1]), "=r"(u[4 * c + 2]), "=r"(u[4 * c + 3])
+                     : "r"(tile + (piece >> 3) * kBlockBytes + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) : "memory");
+    }
+}
+
 // ---------------------------------------------------------------- products
 // An instruction's operands lie in uniform registers.  Values that the compiler knows to be the same in all lanes stay there; of
 // others it moves every one over before each instruction, which held the products up (about 100 cycles an instruction, of 64).
@@ -96,7 +107,7 @@ __device__ __forceinline__ unsigned long long operand(unsigned addr, unsigned le
 __device__ __forceinline__ unsigned long long operand_rows(unsigned tile) { return operand(tile, 16); }
 __device__ __forceinline__ unsigned long long operand_columns(unsigned tile) { return operand(tile, kBlockBytes); }
 
-// Instruction descriptor: fp32 sums, bf16 operands, M = 128; kColumns: the second operand's rows are summed over.
+// Instruction descriptor: fp32 sums, bf16 operands, M = 128, N a multiple of 16; kColumns: the second operand's rows are summed over.
 template <int N, bool kColumns>
 __device__ __forceinline__ constexpr unsigned product_kind() {
     return 1u << 4 | 1u << 7 | 1u << 10 | (kColumns ? 1u << 16 : 0u) | (unsigned)(N >> 3) << 17 | (unsigned)(kTile >> 4) << 24;
@@ -111,23 +122,30 @@ __device__ __forceinline__ void product16_tmem(unsigned d, unsigned a, unsigned 
     asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
                  ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"((unsigned)add) : "memory");
 }
-// d[128, 128] = rows of tile a times rows of tile b, summed over 64 * kBlocks columns.
-template <int kBlocks>
+// d[128, 128] = rows of tile a times rows of tile b, summed over the first 16 kSteps columns.
+template <int kSteps>
 __device__ __forceinline__ void product_rows(unsigned d, unsigned a, unsigned b) {
     const unsigned long long da = operand_rows(a), db = operand_rows(b);
 #pragma unroll
-    for (int k = 0; k < 4 * kBlocks; ++k) {
+    for (int k = 0; k < kSteps; ++k) {
         const unsigned at = ((k / 4) * kBlockBytes + (k % 4) * 32) >> 4;
         product16(d, da + at, db + at, product_kind<kTile, false>(), k > 0);
     }
 }
-// d[128, 64 * kBlocks] (+)= p[128, 64] times rows [64 half, 64 half + 64) of tile b, summed over them.  p: bf16 pairs in 32 columns of tensor
+// The same with a's rows in tensor memory, 16 columns in eight there.
+template <int kSteps>
+__device__ __forceinline__ void product_rows_tmem(unsigned d, unsigned a, unsigned b) {
+    const unsigned long long db = operand_rows(b);
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) product16_tmem(d, a + 8 * k, db + (((k / 4) * kBlockBytes + (k % 4) * 32) >> 4), product_kind<kTile, false>(), k > 0);
+}
+// d[128, 16 kSteps] (+)= p[128, 64] times rows [64 half, 64 half + 64) of tile b, summed over them.  p: bf16 pairs in 32 columns of tensor
 // memory.
-template <int kBlocks>
+template <int kSteps>
 __device__ __forceinline__ void product_columns(unsigned d, unsigned p, unsigned b, int half, bool add) {
     const unsigned long long db = operand_columns(b + half * 8192);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) product16_tmem(d, p + k * 8, db + ((k * 2048) >> 4), product_kind<64 * kBlocks, true>(), add || k > 0);
+    for (int k = 0; k < 4; ++k) product16_tmem(d, p + k * 8, db + ((k * 2048) >> 4), product_kind<16 * kSteps, true>(), add || k > 0);
 }
 // Arrives on `bar` when all products that this thread has issued are done.
 __device__ __forceinline__ void products_done(unsigned long long *bar) {
