@@ -500,13 +500,13 @@ __device__ __forceinline__ void put_pairs(unsigned at, const float (&v)[32]) {
     tmem_store16(at, u);
 }
 
-// v = 2^(v by + off(i)) for pairs i; an eighth of them by polynomial.
+// v = 2^(v by + off(i)) for pairs i; a quarter of them by polynomial.
 template <typename Off>
 __device__ __forceinline__ void probabilities(float (&v)[32], float2 by, Off off) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         float2 e = fma2(make_float2(v[2 * i], v[2 * i + 1]), by, off(i));
-        if (i % 8 == 3) e = exp2_polynomial(e);
+        if (i % 4 == 3) e = exp2_polynomial(e);
         else { e.x = exp2_fast(e.x); e.y = exp2_fast(e.y); }
         v[2 * i] = e.x;
         v[2 * i + 1] = e.y;
@@ -611,36 +611,37 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
             for (int i = max(0, values - kValues); i < values; ++i) mbar_wait_bounded(&v_full[i % kValues], (i / kValues) & 1, kSpinLimit);
         }
     } else if (warp == 9) {
+        // A wait behind products that were just issued returns when they have begun, and what it holds up leaves the tensor cores idle
+        // for some 200 cycles: so the waits stand together, in front of the scores, and only that for dS lies between the products.
+        auto arrived = [&](int j) { return wait.together(&k_full[j % kKeys], (j / kKeys) & 1) && wait.together(&v_full[j % kValues], (j / kValues) & 1); };
         auto scores = [&](int j) {
-            if (!wait.together(&k_full[j % kKeys], (j / kKeys) & 1) || (j > 0 && !wait.together(&s_free, (j - 1) & 1))) return false;
-            tmem_fence_after();
-            if (elect()) {
-                product_rows_tmem<kSteps>(tmem, Q, s_k + j % kKeys * kTileBytes);
-                products_done(&s_full);
-            }
-            return true;
+            product_rows_tmem<kSteps>(tmem, Q, s_k + j % kKeys * kTileBytes);
+            products_done(&s_full);
         };
         auto dps = [&](int j) {
-            if (!wait.together(&v_full[j % kValues], (j / kValues) & 1)) return false;
-            if (elect()) {
-                product_rows_tmem<kSteps>(DP, DO, s_v + j % kValues * kTileBytes);
-                products_done(&dp_full);
-                products_done(&v_empty[j % kValues]);
-            }
-            return true;
+            product_rows_tmem<kSteps>(DP, DO, s_v + j % kValues * kTileBytes);
+            products_done(&dp_full);
+            products_done(&v_empty[j % kValues]);
         };
-        bool ok = wait.together(&rows_ready, 0) && scores(0) && dps(0);
+        bool ok = wait.together(&rows_ready, 0) && arrived(0);
+        tmem_fence_after();
+        if (ok && elect()) { scores(0); dps(0); }
         for (int j = 0; ok && j < n; ++j) {
-            ok = (j + 1 >= n || scores(j + 1)) && wait.together(&ds_full, j & 1) && (j + 1 < n || there >= kTile || wait.together(&k_fixed, 0));
+            const bool more = j + 1 < n;
+            ok = more ? arrived(j + 1) && wait.together(&s_free, j & 1) : there >= kTile || wait.together(&k_fixed, 0);
+            if (!ok) break;
+            tmem_fence_after();
+            if (more && elect()) scores(j + 1);
+            ok = wait.together(&ds_full, j & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
                 product_columns<kSteps>(DQ, DP, s_k + j % kKeys * kTileBytes, 0, j > 0);
                 product_columns<kSteps>(DQ, DP + 64, s_k + j % kKeys * kTileBytes, 1, true);
+                if (more) dps(j + 1);
                 products_done(&k_empty[j % kKeys]);
-                if (j + 1 == n) products_done(&o_full);
+                if (!more) products_done(&o_full);
             }
-            ok = j + 1 >= n || dps(j + 1);
         }
         if (elect()) {
             products_done(&drained);
@@ -814,45 +815,39 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
         }
     } else if (warp == 9) {
         // ---- products
+        auto arrived = [&](int i) { return wait.together(&q_ready[i % kQueries], (i / kQueries) & 1) && wait.together(&do_ready[i % kOuts], (i / kOuts) & 1); };
         auto scores = [&](int i) {
-            const int st = i % kQueries;
-            if (!wait.together(&q_ready[st], (i / kQueries) & 1)) return false;
-            if (elect()) {
-                product_rows<kSteps>(tmem, s_k, s_q + st * kTileBytes);
-                products_done(&s_full);
-            }
-            return true;
+            product_rows<kSteps>(tmem, s_k, s_q + i % kQueries * kTileBytes);
+            products_done(&s_full);
         };
         auto dps = [&](int i) {
-            const int st = i % kOuts;
-            if (!wait.together(&do_ready[st], (i / kOuts) & 1)) return false;
-            if (elect()) {
-                product_rows<kSteps>(DP, s_v, s_do + st * kTileBytes);
-                products_done(&dp_full);
-            }
-            return true;
+            product_rows<kSteps>(DP, s_v, s_do + i % kOuts * kTileBytes);
+            products_done(&dp_full);
         };
-        bool ok = wait.together(&kv_full, 0) && scores(0) && dps(0);
+        bool ok = wait.together(&kv_full, 0) && arrived(0);
+        if (ok && elect()) { scores(0); dps(0); }
         for (int i = 0; ok && i < n; ++i) {
             const unsigned tile_do = s_do + i % kOuts * kTileBytes, tile_q = s_q + i % kQueries * kTileBytes;
-            ok = wait.together(&p_full, i & 1);
+            const bool more = i + 1 < n;
+            ok = (!more || arrived(i + 1)) && wait.together(&p_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
                 product_columns<kSteps>(DV, tmem, tile_do, 0, i > 0);
                 product_columns<kSteps>(DV, tmem + 64, tile_do, 1, true);
+                if (more) scores(i + 1);
                 products_done(&do_empty[i % kOuts]);
             }
-            ok = (i + 1 >= n || scores(i + 1)) && wait.together(&ds_full, i & 1);
+            ok = wait.together(&ds_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
                 product_columns<kSteps>(DK, DP, tile_q, 0, i > 0);
                 product_columns<kSteps>(DK, DP + 64, tile_q, 1, true);
+                if (more) dps(i + 1);
                 products_done(&q_empty[i % kQueries]);
-                if (i + 1 == n) products_done(&o_full);
+                if (!more) products_done(&o_full);
             }
-            ok = i + 1 >= n || dps(i + 1);
         }
         if (elect()) {
             products_done(&drained);
