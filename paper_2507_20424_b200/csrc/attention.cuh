@@ -815,7 +815,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
         }
     } else if (warp == 9) {
         // ---- products
-        auto arrived = [&](int i) { return wait.together(&q_ready[i % kQueries], (i / kQueries) & 1) && wait.together(&do_ready[i % kOuts], (i / kOuts) & 1); };
+        auto queries = [&](int i) { return wait.together(&q_ready[i % kQueries], (i / kQueries) & 1); };
+        auto outs = [&](int i) { return wait.together(&do_ready[i % kOuts], (i / kOuts) & 1); };
         auto scores = [&](int i) {
             product_rows<kSteps>(tmem, s_k, s_q + i % kQueries * kTileBytes);
             products_done(&s_full);
@@ -824,21 +825,21 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             product_rows<kSteps>(DP, s_v, s_do + i % kOuts * kTileBytes);
             products_done(&dp_full);
         };
-        bool ok = wait.together(&kv_full, 0) && arrived(0);
+        bool ok = wait.together(&kv_full, 0) && queries(0) && outs(0);
         if (ok && elect()) { scores(0); dps(0); }
         for (int i = 0; ok && i < n; ++i) {
             const unsigned tile_do = s_do + i % kOuts * kTileBytes, tile_q = s_q + i % kQueries * kTileBytes;
             const bool more = i + 1 < n;
-            ok = (!more || arrived(i + 1)) && wait.together(&p_full, i & 1);
+            ok = (!more || queries(i + 1)) && wait.together(&p_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
                 product_columns<kSteps>(DV, tmem, tile_do, 0, i > 0);
                 product_columns<kSteps>(DV, tmem + 64, tile_do, 1, true);
-                if (more) scores(i + 1);
                 products_done(&do_empty[i % kOuts]);
+                if (more) scores(i + 1);
             }
-            ok = wait.together(&ds_full, i & 1);
+            ok = (!more || outs(i + 1)) && wait.together(&ds_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
@@ -854,25 +855,37 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             mbar_wait_bounded(&drained, 0, kSpinLimit);
         }
     } else if (warp >= 10) {
-        // ---- tiles as they arrive: rows of other sequences must not reach a sum.  One warp for the queries, with lse and D, one for
-        // grad_out.  Every tile passes here, so that neither warp can be a phase behind.
+        // ---- tiles as they arrive: rows of other sequences must not reach a sum.  One warp for the queries, one for grad_out and for lse
+        // and D, which it reads a tile ahead.  Every tile passes here, so that neither warp can be a phase behind.
         const bool queries = warp == 10;
+        const int stages = queries ? kQueries : kOuts;
+        float lse[4], delta[4];
+        auto read = [&](int i) {
+            const int row = row_of(i);
+            const long long at = head_of(i) * a.T + row;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool is = row + lane + 32 * k < t.end;
+                lse[k] = is ? __ldcg(a.lse + at + lane + 32 * k) : 0.f;
+                delta[k] = is ? __ldcg(a.delta + at + lane + 32 * k) : 0.f;
+            }
+        };
+        if (!queries) read(0);
         bool ok = true;
         for (int i = 0; ok && i < n; ++i) {
-            const int st = i % (queries ? kQueries : kOuts), row = row_of(i), there = t.end - row;
-            const unsigned parity = (i / (queries ? kQueries : kOuts)) & 1;
-            if (queries) {
+            const int st = i % stages, there = t.end - row_of(i);
+            if (!queries) {
                 // those of two tiles before are done with when its products with dS are
                 if (i >= 2 && !(ok = wait.together(&q_empty[(i - 2) % kQueries], ((i - 2) / kQueries) & 1))) break;
-                const long long at = head_of(i) * a.T + row;
 #pragma unroll
-                for (int k = lane; k < kTile; k += 32) {
-                    s_stat[i & 1][0][k] = k < there ? -kLog2e * a.lse[at + k] : 0.f;
-                    s_stat[i & 1][1][k] = k < there ? -a.delta[at + k] : 0.f;
+                for (int k = 0; k < 4; ++k) {
+                    s_stat[i & 1][0][lane + 32 * k] = -kLog2e * lse[k];
+                    s_stat[i & 1][1][lane + 32 * k] = -delta[k];
                 }
                 mbar_arrive(&stat_full[i & 1]);
+                if (i + 1 < n) read(i + 1);
             }
-            if (!(ok = wait.together(queries ? &q_full[st] : &do_full[st], parity))) break;
+            if (!(ok = wait.together(queries ? &q_full[st] : &do_full[st], (i / stages) & 1))) break;
             if (there < kTile) zero_rows<kBlocks>((queries ? s_q : s_do) + st * kTileBytes, there);
             if (lane == 0) mbar_arrive(queries ? &q_ready[st] : &do_ready[st]);
         }
