@@ -170,18 +170,31 @@ struct ForwardShape {
     static constexpr unsigned kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
 };
 
-// Eight bf16 columns a store, those below D, of 32 columns from `at` on.
-__device__ __forceinline__ void put_columns(bf16 *row, int at, int D, const float (&v)[32], float by) {
+// 32 columns of a row, from column 32 part on, times `by` as bf16 into a tile that no product or copy needs any more.
+__device__ __forceinline__ void put_row(unsigned tile, int r, int part, const float (&v)[32], float by) {
 #pragma unroll
-    for (int i = 0; i < 32; i += 8)
-        if (at + i < D) {
+    for (int c = 0; c < 4; ++c) {
+        const float *f = v + 8 * c;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece_at(tile, r, part * 4 + c)), "r"(bf16_pair(f[0] * by, f[1] * by)), "r"(bf16_pair(f[2] * by, f[3] * by)),
+                     "r"(bf16_pair(f[4] * by, f[5] * by)), "r"(bf16_pair(f[6] * by, f[7] * by)) : "memory");
+    }
+}
+// A warp's 32 rows of a tile, from row r0 on, to memory: kPieces pieces of 16 bytes from `first` on, those of a row by lanes side by side (a
+// row a thread took 4,000 cycles for what takes 1,000 so).  out: row 0 of the tile; rows: how many of the tile are to be written.
+template <int kPieces>
+__device__ __forceinline__ void store_rows(unsigned tile, int r0, int first, bf16 *out, long long ld, int rows, int D) {
+    constexpr int kRows = 32 / kPieces;
+    const int lane = threadIdx.x & 31, piece = first + lane % kPieces;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 32; i += kRows) {
+        const int r = r0 + i + lane / kPieces;
+        if (r < rows && piece * 8 < D) {
             uint4 u;
-            u.x = bf16_pair(v[i] * by, v[i + 1] * by);
-            u.y = bf16_pair(v[i + 2] * by, v[i + 3] * by);
-            u.z = bf16_pair(v[i + 4] * by, v[i + 5] * by);
-            u.w = bf16_pair(v[i + 6] * by, v[i + 7] * by);
-            *reinterpret_cast<uint4 *>(row + at + i) = u;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(piece_at(tile, r, piece)) : "memory");
+            *reinterpret_cast<uint4 *>(out + r * ld + piece * 8) = u;
         }
+    }
 }
 // Rows [0, rows) of a head: value `fill` (0 or NaN) in all columns; threads tid of n.
 __device__ __forceinline__ void fill_rows(bf16 *p, long long ld, int rows, int D, float fill, int tid, int n) {
@@ -231,6 +244,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     __shared__ volatile int s_dead;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const unsigned unit = blockIdx.x % a.units, index = blockIdx.x / a.units;
+    if (tid < 3) prefetch_map(tid == 0 ? &a.q : tid == 1 ? &a.k : &a.v);
     if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T) {                 // not a plan of these rows
         if (blockIdx.x == 0 && tid == 0) a.hdr->status = DPPF_ERR_WORKSPACE;
         return;
@@ -453,13 +467,15 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
             tmem_fence_after();
             const bool mine = r < slot_rows(s);
             const float by = ok ? (sum > 0.f || sum != sum ? 1.0f / sum : 0.f) : __int_as_float(0x7fc00000);
-            bf16 *out = a.out + (long long)row * a.ld_out + slot_head(s) * a.head_out;
+            const unsigned tile = s_q + s * kTileBytes;                  // the queries': their products are done
+#pragma unroll
             for (int c = 0; c < 2 * kBlocks; ++c) {
                 float o[32];
                 tmem_load32(O + c * 32, o);
                 tmem_loaded(o);
-                if (mine) put_columns(out, c * 32, a.D, o, by);
+                put_row(tile, r, c, o, by);
             }
+            store_rows<8 * kBlocks>(tile, r & ~31, 0, a.out + (long long)slot_row(s) * a.ld_out + slot_head(s) * a.head_out, a.ld_out, slot_rows(s), a.D);
             if (mine) a.lse[slot_head(s) * a.T + row] = ok ? (top + log2f(sum)) * kLn2 : __int_as_float(0x7fc00000);
         }
         tmem_fence_before();
@@ -500,13 +516,13 @@ __device__ __forceinline__ void put_pairs(unsigned at, const float (&v)[32]) {
     tmem_store16(at, u);
 }
 
-// v = 2^(v by + off(i)) for pairs i; a quarter of them by polynomial.
+// v = 2^(v by + off(i)) for pairs i; a third of them by polynomial.
 template <typename Off>
 __device__ __forceinline__ void probabilities(float (&v)[32], float2 by, Off off) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         float2 e = fma2(make_float2(v[2 * i], v[2 * i + 1]), by, off(i));
-        if (i % 4 == 3) e = exp2_polynomial(e);
+        if (i % 3 == 2) e = exp2_polynomial(e);
         else { e.x = exp2_fast(e.x); e.y = exp2_fast(e.y); }
         v[2 * i] = e.x;
         v[2 * i + 1] = e.y;
@@ -547,6 +563,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int head = (int)(blockIdx.x % a.heads), kv_head = head / a.share;
     const unsigned index = blockIdx.x / a.heads;
+    if (tid < 5) prefetch_map(tid == 0 ? &a.q : tid == 1 ? &a.grad_out : tid == 2 ? &a.k : tid == 3 ? &a.out : &a.v);
     if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T) {
         if (blockIdx.x == 0 && tid == 0) a.hdr->status = DPPF_ERR_WORKSPACE;
         return;
@@ -721,13 +738,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
         ok = ok && wait.together(&o_full, 0);
         tmem_fence_after();
         const float by = ok ? a.scale : __int_as_float(0x7fc00000);
-        bf16 *dq = a.dq + (long long)row * a.ld_dq + head * a.head_dq;
-        for (int c = half * kBlocks; c < (half + 1) * kBlocks; ++c) {
+#pragma unroll
+        for (int c = 0; c < kBlocks; ++c) {
             float o[32];
-            tmem_load32(DQ + lanes + c * 32, o);
+            tmem_load32(DQ + lanes + (half * kBlocks + c) * 32, o);
             tmem_loaded(o);
-            if (mine) put_columns(dq, c * 32, a.D, o, by);
+            put_row(s_q, r, half * kBlocks + c, o, by);
         }
+        store_rows<4 * kBlocks>(s_q, r & ~31, half * 4 * kBlocks, a.dq + (long long)t.row * a.ld_dq + head * a.head_dq, a.ld_dq, t.rows, a.D);
         tmem_fence_before();
     }
     __syncthreads();
@@ -759,6 +777,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     const int kv_head = (int)(blockIdx.x % a.kv_heads);
     const unsigned index = blockIdx.x / a.kv_heads;
+    if (tid < 4) prefetch_map(tid == 0 ? &a.k : tid == 1 ? &a.q : tid == 2 ? &a.v : &a.grad_out);
     if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T || index >= (unsigned)a.hdr->tiles[kByKey]) return;      // the status is the first kernel's
     const PlanTile t = uniform(a.key_tiles[index]);
     if (t.begin == t.end) {
@@ -905,9 +924,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             for (int c = 0; c < 2; ++c) tmem_load32(tmem + lanes + 64 * half + 32 * c, p[c]);
 #pragma unroll
             for (int c = 0; c < 2; ++c) tmem_loaded(p[c]);
-            const float2 *lse2 = reinterpret_cast<const float2 *>(&s_stat[i & 1][0][64 * half]), *delta = reinterpret_cast<const float2 *>(&s_stat[i & 1][1][64 * half]);
+            const float4 *lse2 = reinterpret_cast<const float4 *>(&s_stat[i & 1][0][64 * half]), *delta = reinterpret_cast<const float4 *>(&s_stat[i & 1][1][64 * half]);
+            auto pair_of = [](const float4 *p, int k) { const float4 f = p[k / 2]; return k % 2 ? make_float2(f.z, f.w) : make_float2(f.x, f.y); };
 #pragma unroll
-            for (int c = 0; c < 2; ++c) probabilities(p[c], both(a.scale2), [&](int k) { return lse2[c * 16 + k]; });
+            for (int c = 0; c < 2; ++c) probabilities(p[c], both(a.scale2), [&](int k) { return pair_of(lse2, c * 16 + k); });
             if (!whole)
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
@@ -926,7 +946,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             for (int c = 0; c < 2; ++c) {
                 tmem_load32(DP + lanes + 64 * half + 32 * c, d);
                 tmem_loaded(d);
-                times_difference(p[c], d, [&](int k) { return delta[c * 16 + k]; });
+                times_difference(p[c], d, [&](int k) { return pair_of(delta, c * 16 + k); });
             }
             if (!whole)                                                  // a select: what is masked may be NaN
 #pragma unroll
@@ -943,13 +963,16 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
         ok = ok && wait.together(&o_full, 0);
         tmem_fence_after();
         const float by = !ok ? __int_as_float(0x7fc00000) : half ? a.scale : 1.0f;
-        bf16 *to = half ? a.dk + (long long)key * a.ld_dk + kv_head * a.head_dk : a.dv + (long long)key * a.ld_dv + kv_head * a.head_dv;
+        const unsigned tile = half ? s_k : s_v;                          // all products are done
+#pragma unroll
         for (int c = 0; c < 2 * kBlocks; ++c) {
             float o[32];
             tmem_load32((half ? DK : DV) + lanes + c * 32, o);
             tmem_loaded(o);
-            if (r < t.rows) put_columns(to, c * 32, a.D, o, by);
+            put_row(tile, r, c, o, by);
         }
+        const long long ld = half ? a.ld_dk : a.ld_dv;
+        store_rows<8 * kBlocks>(tile, r & ~31, 0, (half ? a.dk + kv_head * a.head_dk : a.dv + kv_head * a.head_dv) + t.row * ld, ld, t.rows, a.D);
         tmem_fence_before();
     }
     __syncthreads();

@@ -85,6 +85,11 @@ __device__ __forceinline__ void zero_rows(unsigned tile, int first) {
     __syncwarp();
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
+// Where the 16-byte piece `piece` (eight columns) of row r lies in a tile.
+__device__ __forceinline__ unsigned piece_at(unsigned tile, int r, int piece) { return tile + (piece >> 3) * kBlockBytes + r * 128 + (((piece & 7) ^ (r & 7)) << 4); }
+
 // Sixteen words of row r of a tile: its columns [32 part, 32 part + 32).
 __device__ __forceinline__ void tile_row(unsigned tile, int r, int part, unsigned (&u)[16]) {
 #pragma unroll
@@ -92,7 +97,7 @@ __device__ __forceinline__ void tile_row(unsigned tile, int r, int part, unsigne
         const int piece = part * 4 + c;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                      : "=r"(u[4 * c]), "=r"(u[4 * c + 1]), "=r"(u[4 * c + 2]), "=r"(u[4 * c + 3])
-                     : "r"(tile + (piece >> 3) * kBlockBytes + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) : "memory");
+                     : "r"(piece_at(tile, r, piece)) : "memory");
     }
 }
 
