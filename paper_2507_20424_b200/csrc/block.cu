@@ -21,7 +21,7 @@ int norm_width(int H, std::initializer_list<NormOperand> operands) {
     for (const int n : {8, 2}) {
         bool fits = H % n == 0;
         for (const NormOperand &o : operands) {
-            const size_t boundary = n * type_bytes(o.type) < 16 ? n * type_bytes(o.type) : 16;
+            const size_t boundary = n * type_bytes(o.type);
             fits = fits && (!o.p || (aligned_to(o.p, boundary) && (size_t)o.ld * type_bytes(o.type) % boundary == 0));
         }
         if (fits) return n;
@@ -29,8 +29,9 @@ int norm_width(int H, std::initializer_list<NormOperand> operands) {
     return 1;
 }
 
-// Threads of a block that holds a row.
-int norm_threads(int H) { return ((H + kNormElements - 1) / kNormElements + 31) / 32 * 32; }
+// Threads of a block that holds a row, `each` elements a thread.
+int norm_threads(int H, int each = kNormElements) { return ((H + each - 1) / each + 31) / 32 * 32; }
+int norm_grad_threads(int H) { return norm_threads(H, H <= kNormGradShort ? 8 : kNormElements); }
 
 template <typename TX, typename TO, int N>
 int launch_norm(NormArgs a, cudaStream_t s) {
@@ -49,7 +50,7 @@ int launch_norm_width(const NormArgs &a, int n, cudaStream_t s) {
 int64_t norm_grad_blocks(int64_t T, int H) {
     if (H > kNormGradRow) return T < 32 ? T : 32;                                        // rows of blocks of the columns' kernel
     const int64_t rows = H <= kNormWarpRow ? (T + kNormWarps - 1) / kNormWarps : T;
-    const int64_t most = 148LL * (H <= kNormWarpRow ? 2 : 512 / norm_threads(H));
+    const int64_t most = 148LL * (H <= kNormWarpRow ? 2 : (H <= kNormGradShort ? 1024 : 512) / norm_grad_threads(H));
     return rows < most ? rows : most;
 }
 
@@ -57,9 +58,11 @@ template <typename TX, typename TO, int N>
 int launch_norm_grad(NormGradArgs a, cudaStream_t s) {
     a.groups = a.H / N;
     if (a.H <= kNormWarpRow) {
-        norm_grad_kernel<TX, TO, N, true><<<(unsigned)a.blocks, kNormWarps * 32, 0, s>>>(a);
+        norm_grad_kernel<TX, TO, N, kNormElements, true><<<(unsigned)a.blocks, kNormWarps * 32, 0, s>>>(a);
+    } else if (a.H <= kNormGradShort) {
+        norm_grad_kernel<TX, TO, N, 8, false><<<(unsigned)a.blocks, norm_grad_threads(a.H), 0, s>>>(a);
     } else if (a.H <= kNormGradRow) {
-        norm_grad_kernel<TX, TO, N, false><<<(unsigned)a.blocks, norm_threads(a.H), 0, s>>>(a);
+        norm_grad_kernel<TX, TO, N, kNormElements, false><<<(unsigned)a.blocks, norm_grad_threads(a.H), 0, s>>>(a);
     } else {
         norm_grad_columns_kernel<TX, TO, N><<<dim3((unsigned)((a.groups + kNormWideThreads - 1) / kNormWideThreads), (unsigned)a.blocks), kNormWideThreads, 0, s>>>(a);
         norm_grad_wide_kernel<TX, TO, N><<<(unsigned)a.T, kNormWideThreads, 0, s>>>(a);

@@ -19,9 +19,33 @@ constexpr int kNormElements = 16;                         // of a row in one thr
 constexpr int kNormWarpRow = 32 * kNormElements;          // longest row of a warp
 constexpr int kNormRow = 1024 * kNormElements;            // longest row that a block holds
 constexpr int kNormGradRow = 512 * kNormElements;         // ... with the columns' sums beside it
+constexpr int kNormGradShort = 512 * 8;                   // rows up to this: eight elements a thread
 constexpr int kNormWarps = 8;                             // rows side by side in a block, a warp each
 constexpr int kNormWideThreads = 512;
 constexpr int kNormJoinThreads = 256;
+
+// Eight fp32 in one access of 32 bytes (as two of 16 a warp's accesses touch every 32-byte sector twice); else as everywhere.
+template <typename T, int N, bool kOnce = true>
+__device__ __forceinline__ void load_row(const T *p, float (&f)[N]) {
+    if constexpr (N == 8 && sizeof(T) == 4) {
+        if constexpr (kOnce)
+            asm volatile("ld.global.cs.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(p) : "memory");
+        else
+            asm volatile("ld.global.cg.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(p) : "memory");
+    } else {
+        load_vec<T, N, kOnce>(p, f);
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T *p, const float (&f)[N]) {
+    if constexpr (N == 8 && sizeof(T) == 4)
+        asm volatile("st.global.cs.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                     ::"f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]), "l"(p) : "memory");
+    else
+        store_vec<T, N>(p, f);
+}
 
 struct NormArgs {
     const void *x, *branch, *weight, *bias;
@@ -47,8 +71,8 @@ struct NormGradArgs {
 // N elements of an array whose type is known at run time; weights are read again by every row: kept in the caches.
 template <int N, bool kOnce>
 __device__ __forceinline__ void load_either(const void *p, int is32, long long at, float (&f)[N]) {
-    if (is32) load_vec<float, N, kOnce>(static_cast<const float *>(p) + at, f);
-    else load_vec<bf16, N, kOnce>(static_cast<const bf16 *>(p) + at, f);
+    if (is32) load_row<float, N, kOnce>(static_cast<const float *>(p) + at, f);
+    else load_row<bf16, N, kOnce>(static_cast<const bf16 *>(p) + at, f);
 }
 
 // Sums of K values over the threads of a row: a warp, or the block.  `s` is used by one call in two (the caller alternates), so
@@ -86,7 +110,7 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(co
 #pragma unroll
     for (int g = 0; g < G; ++g) {
         const int at = g * L + t;
-        if (at < a.groups) load_vec<TX, N>(x + (long long)at * N, h[g]);
+        if (at < a.groups) load_row<TX, N>(x + (long long)at * N, h[g]);
         else
 #pragma unroll
             for (int i = 0; i < N; ++i) h[g][i] = 0.f;
@@ -100,7 +124,7 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(co
             load_either<N, true>(a.branch, a.branch32, row * a.ld_branch + (long long)at * N, b);
 #pragma unroll
             for (int i = 0; i < N; ++i) h[g][i] = to_float(from_float<TX>(h[g][i] + b[i]));
-            store_vec<TX, N>(static_cast<TX *>(a.sum) + row * a.ld_sum + (long long)at * N, h[g]);
+            store_row<TX, N>(static_cast<TX *>(a.sum) + row * a.ld_sum + (long long)at * N, h[g]);
         }
     }
 #pragma unroll
@@ -133,7 +157,7 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(co
             const float y = h[g][i] * rstd;
             h[g][i] = a.bias ? fmaf(y, w[i], b[i]) : y * w[i];
         }
-        store_vec<TO, N>(static_cast<TO *>(a.out) + row * a.ld_out + (long long)at * N, h[g]);
+        store_row<TO, N>(static_cast<TO *>(a.out) + row * a.ld_out + (long long)at * N, h[g]);
     }
 }
 
@@ -146,13 +170,13 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_wide_kernel(const __gri
     float sum[1] = {0.f};
     for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
         float h[N];
-        load_vec<TX, N, false>(x + (long long)at * N, h);
+        load_row<TX, N, false>(x + (long long)at * N, h);
         if (a.branch) {
             float b[N];
             load_either<N, true>(a.branch, a.branch32, row * a.ld_branch + (long long)at * N, b);
 #pragma unroll
             for (int i = 0; i < N; ++i) h[i] = to_float(from_float<TX>(h[i] + b[i]));
-            store_vec<TX, N>(static_cast<TX *>(a.sum) + row * a.ld_sum + (long long)at * N, h);
+            store_row<TX, N>(static_cast<TX *>(a.sum) + row * a.ld_sum + (long long)at * N, h);
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) sum[0] += h[i];
@@ -163,7 +187,7 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_wide_kernel(const __gri
     sum[0] = 0.f;
     for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
         float h[N];
-        load_vec<TX, N, false>(from + (long long)at * N, h);
+        load_row<TX, N, false>(from + (long long)at * N, h);
 #pragma unroll
         for (int i = 0; i < N; ++i) sum[0] = fmaf(h[i] - mean, h[i] - mean, sum[0]);
     }
@@ -172,7 +196,7 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_wide_kernel(const __gri
     if (threadIdx.x == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
     for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
         float h[N], w[N], b[N];
-        load_vec<TX, N>(from + (long long)at * N, h);
+        load_row<TX, N>(from + (long long)at * N, h);
         load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
         if (a.bias) load_either<N, false>(a.bias, a.weight32, (long long)at * N, b);
 #pragma unroll
@@ -180,31 +204,25 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_wide_kernel(const __gri
             const float y = (h[i] - mean) * rstd;
             h[i] = a.bias ? fmaf(y, w[i], b[i]) : y * w[i];
         }
-        store_vec<TO, N>(static_cast<TO *>(a.out) + row * a.ld_out + (long long)at * N, h);
+        store_row<TO, N>(static_cast<TO *>(a.out) + row * a.ld_out + (long long)at * N, h);
     }
 }
 
 // ---------------------------------------------------------------- gradient
 
-// dx of N elements, from dy -> u and xh
+// dx of N elements
 template <typename TX, int N>
-__device__ __forceinline__ void norm_dx(const NormGradArgs &a, long long row, int at, const float (&u)[N], const float (&xh)[N], float rstd, float mu, float mx) {
+__device__ __forceinline__ void norm_dx(const NormGradArgs &a, long long row, int at, const float (&u)[N], const float (&xh)[N], const float (&dsum)[N], float rstd, float mu, float mx) {
     float d[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) d[i] = rstd * (u[i] - mu - xh[i] * mx);
-    if (a.dsum) {
-        float b[N];
-        load_vec<TX, N>(static_cast<const TX *>(a.dsum) + row * a.ld_dsum + (long long)at * N, b);
-#pragma unroll
-        for (int i = 0; i < N; ++i) d[i] += b[i];
-    }
-    store_vec<TX, N>(static_cast<TX *>(a.dx) + row * a.ld_dx + (long long)at * N, d);
+    for (int i = 0; i < N; ++i) d[i] = fmaf(rstd, u[i] - mu - xh[i] * mx, dsum[i]);
+    store_row<TX, N>(static_cast<TX *>(a.dx) + row * a.ld_dx + (long long)at * N, d);
 }
 
 // Block `b` writes its columns' sums; threads that share columns (the warps of a block with a warp a row) add theirs in warp order.
-template <int N, bool kWarp>
-__device__ __forceinline__ void put_sums(const NormGradArgs &a, int L, int t, float (&dw)[kNormElements / N][N], float (&db)[kNormElements / N][N]) {
-    constexpr int G = kNormElements / N;
+template <int N, int E, bool kWarp>
+__device__ __forceinline__ void put_sums(const NormGradArgs &a, int L, int t, float (&dw)[E / N][N], float (&db)[E / N][N]) {
+    constexpr int G = E / N;
     float *part = a.part + (long long)blockIdx.x * 2 * a.H;
     if constexpr (kWarp) {
         __shared__ float s_all[2][kNormWarpRow];
@@ -242,9 +260,9 @@ __device__ __forceinline__ void put_sums(const NormGradArgs &a, int L, int t, fl
     }
 }
 
-template <typename TX, typename TO, int N, bool kWarp>
-__global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512) norm_grad_kernel(const __grid_constant__ NormGradArgs a) {
-    constexpr int G = kNormElements / N;
+template <typename TX, typename TO, int N, int E, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512, kWarp ? 2 : E == 8 ? 2 : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs a) {
+    constexpr int G = E / N;
     __shared__ float s_sum[2][2][32];
     const int L = kWarp ? 32 : blockDim.x, t = kWarp ? threadIdx.x & 31 : threadIdx.x;
     float dw[G][N], db[G][N];
@@ -255,14 +273,18 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512) norm_grad_kerne
     const long long step = (long long)gridDim.x * (kWarp ? kNormWarps : 1);
     int odd = 0;
     for (long long row = kWarp ? (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5) : blockIdx.x; row < a.T; row += step) {
-        float u[G][N], xh[G][N], sums[2] = {0.f, 0.f};
+        float u[G][N], xh[G][N], more[G][N], sums[2] = {0.f, 0.f};
         const float mean = a.mean[row], rstd = a.rstd[row];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int at = g * L + t;
             if (at < a.groups) {
-                load_vec<TO, N>(static_cast<const TO *>(a.dy) + row * a.ld_dy + (long long)at * N, u[g]);
-                load_vec<TX, N>(static_cast<const TX *>(a.x) + row * a.ld_x + (long long)at * N, xh[g]);
+                load_row<TO, N>(static_cast<const TO *>(a.dy) + row * a.ld_dy + (long long)at * N, u[g]);
+                load_row<TX, N>(static_cast<const TX *>(a.x) + row * a.ld_x + (long long)at * N, xh[g]);
+                if (a.dsum) load_row<TX, N>(static_cast<const TX *>(a.dsum) + row * a.ld_dsum + (long long)at * N, more[g]);
+                else
+#pragma unroll
+                    for (int i = 0; i < N; ++i) more[g][i] = 0.f;
             }
         }
 #pragma unroll
@@ -286,10 +308,10 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512) norm_grad_kerne
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int at = g * L + t;
-            if (at < a.groups) norm_dx<TX, N>(a, row, at, u[g], xh[g], rstd, sums[0] * a.inv_h, sums[1] * a.inv_h);
+            if (at < a.groups) norm_dx<TX, N>(a, row, at, u[g], xh[g], more[g], rstd, sums[0] * a.inv_h, sums[1] * a.inv_h);
         }
     }
-    put_sums<N, kWarp>(a, L, t, dw, db);
+    put_sums<N, E, kWarp>(a, L, t, dw, db);
     let_next_start();
 }
 
@@ -304,8 +326,8 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_grad_columns_kernel(con
     for (long long row = blockIdx.y; row < a.T; row += gridDim.y) {
         const float mean = a.mean[row], rstd = a.rstd[row];
         float dy[N], x[N];
-        load_vec<TO, N, false>(static_cast<const TO *>(a.dy) + row * a.ld_dy + (long long)at * N, dy);
-        load_vec<TX, N, false>(static_cast<const TX *>(a.x) + row * a.ld_x + (long long)at * N, x);
+        load_row<TO, N, false>(static_cast<const TO *>(a.dy) + row * a.ld_dy + (long long)at * N, dy);
+        load_row<TX, N, false>(static_cast<const TX *>(a.x) + row * a.ld_x + (long long)at * N, x);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             dw[i] = fmaf(dy[i], (x[i] - mean) * rstd, dw[i]);
@@ -326,8 +348,8 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_grad_wide_kernel(const 
     const TX *x = static_cast<const TX *>(a.x) + row * a.ld_x;
     float sums[2] = {0.f, 0.f}, u[N], xh[N], w[N];
     auto load = [&](int at) {
-        load_vec<TO, N, false>(dy + (long long)at * N, u);
-        load_vec<TX, N, false>(x + (long long)at * N, xh);
+        load_row<TO, N, false>(dy + (long long)at * N, u);
+        load_row<TX, N, false>(x + (long long)at * N, xh);
         load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
 #pragma unroll
         for (int i = 0; i < N; ++i) { xh[i] = (xh[i] - mean) * rstd; u[i] *= w[i]; }
@@ -339,8 +361,13 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_grad_wide_kernel(const 
     }
     row_sums<false, 2>(sums, s_sum);
     for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
+        float more[N];
         load(at);
-        norm_dx<TX, N>(a, row, at, u, xh, rstd, sums[0] * a.inv_h, sums[1] * a.inv_h);
+        if (a.dsum) load_row<TX, N>(static_cast<const TX *>(a.dsum) + row * a.ld_dsum + (long long)at * N, more);
+        else
+#pragma unroll
+            for (int i = 0; i < N; ++i) more[i] = 0.f;
+        norm_dx<TX, N>(a, row, at, u, xh, more, rstd, sums[0] * a.inv_h, sums[1] * a.inv_h);
     }
 }
 
