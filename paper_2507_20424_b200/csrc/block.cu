@@ -30,14 +30,23 @@ int norm_width(int H, std::initializer_list<NormOperand> operands) {
 }
 
 // Threads of a block that holds a row, `each` elements a thread.
-int norm_threads(int H, int each = kNormElements) { return ((H + each - 1) / each + 31) / 32 * 32; }
-int norm_grad_threads(int H) { return norm_threads(H, H <= kNormGradShort ? 8 : kNormElements); }
+int norm_threads(int H, int each) { return ((H + each - 1) / each + 31) / 32 * 32; }
+int norm_threads_of(int H) { return norm_threads(H, H <= kNormShort ? 8 : kNormElements); }
+
+// Lanes of a warp for a row: the fewest that hold it, a power of two.
+int norm_lanes(int H) {
+    int lanes = 1;
+    while (lanes * kNormElements < H) lanes *= 2;
+    return lanes;
+}
 
 template <typename TX, typename TO, int N>
 int launch_norm(NormArgs a, cudaStream_t s) {
     a.groups = a.H / N;
-    if (a.H <= kNormWarpRow) norm_kernel<TX, TO, N, true><<<(unsigned)((a.T + kNormWarps - 1) / kNormWarps), kNormWarps * 32, 0, s>>>(a);
-    else if (a.H <= kNormRow) norm_kernel<TX, TO, N, false><<<(unsigned)a.T, norm_threads(a.H), 0, s>>>(a);
+    a.lanes = norm_lanes(a.H);
+    const int64_t side = kNormWarps * 32 / a.lanes;
+    if (a.H <= kNormWarpRow) norm_kernel<TX, TO, N, true><<<(unsigned)((a.T + side - 1) / side), kNormWarps * 32, 0, s>>>(a);
+    else if (a.H <= kNormRow) norm_kernel<TX, TO, N, false><<<(unsigned)a.T, norm_threads(a.H, kNormElements), 0, s>>>(a);
     else norm_wide_kernel<TX, TO, N><<<(unsigned)a.T, kNormWideThreads, 0, s>>>(a);
     return launched();
 }
@@ -49,20 +58,21 @@ int launch_norm_width(const NormArgs &a, int n, cudaStream_t s) {
 // Blocks whose columns' sums the workspace holds.  The SMs are a B200's 148 whatever the device: the size is asked for without one.
 int64_t norm_grad_blocks(int64_t T, int H) {
     if (H > kNormGradRow) return T < 32 ? T : 32;                                        // rows of blocks of the columns' kernel
-    const int64_t rows = H <= kNormWarpRow ? (T + kNormWarps - 1) / kNormWarps : T;
-    const int64_t most = 148LL * (H <= kNormWarpRow ? 2 : (H <= kNormGradShort ? 1024 : 512) / norm_grad_threads(H));
+    const int64_t side = H <= kNormWarpRow ? kNormWarps * 32 / norm_lanes(H) : 1, rows = (T + side - 1) / side;
+    const int64_t most = 148LL * (H <= kNormWarpRow ? 2 : (H <= kNormShort ? 1024 : 512) / norm_threads_of(H));
     return rows < most ? rows : most;
 }
 
 template <typename TX, typename TO, int N>
 int launch_norm_grad(NormGradArgs a, cudaStream_t s) {
     a.groups = a.H / N;
+    a.lanes = norm_lanes(a.H);
     if (a.H <= kNormWarpRow) {
         norm_grad_kernel<TX, TO, N, kNormElements, true><<<(unsigned)a.blocks, kNormWarps * 32, 0, s>>>(a);
-    } else if (a.H <= kNormGradShort) {
-        norm_grad_kernel<TX, TO, N, 8, false><<<(unsigned)a.blocks, norm_grad_threads(a.H), 0, s>>>(a);
+    } else if (a.H <= kNormShort) {
+        norm_grad_kernel<TX, TO, N, 8, false><<<(unsigned)a.blocks, norm_threads_of(a.H), 0, s>>>(a);
     } else if (a.H <= kNormGradRow) {
-        norm_grad_kernel<TX, TO, N, kNormElements, false><<<(unsigned)a.blocks, norm_grad_threads(a.H), 0, s>>>(a);
+        norm_grad_kernel<TX, TO, N, kNormElements, false><<<(unsigned)a.blocks, norm_threads_of(a.H), 0, s>>>(a);
     } else {
         norm_grad_columns_kernel<TX, TO, N><<<dim3((unsigned)((a.groups + kNormWideThreads - 1) / kNormWideThreads), (unsigned)a.blocks), kNormWideThreads, 0, s>>>(a);
         norm_grad_wide_kernel<TX, TO, N><<<(unsigned)a.T, kNormWideThreads, 0, s>>>(a);

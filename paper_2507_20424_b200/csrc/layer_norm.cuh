@@ -4,7 +4,8 @@
 //   u = w dy;  xh = (h - mu) r;  dx = r (u - mean u - xh mean(u xh)) + dsum;  dw = sum_t dy xh;  db = sum_t dy
 //
 // Both are bound by memory: a row is read once, stays in registers (sixteen elements a thread) for the statistics, the second
-// moment taken about the mean, and is written once.  Rows of up to 512 elements take a warp each, longer ones a block; above
+// moment taken about the mean, and is written once.  Rows of up to 512 elements take a warp or, shorter ones, a part of one (a power of two of
+// lanes), longer ones a block; above
 // kNormRow elements (kNormGradRow for the gradient) a block walks the row several times, the later ones from L2.
 //
 // The gradient's blocks stay: each walks rows blockIdx.x, + gridDim.x, ... and keeps its columns' sums of dy xh and dy in registers;
@@ -19,7 +20,7 @@ constexpr int kNormElements = 16;                         // of a row in one thr
 constexpr int kNormWarpRow = 32 * kNormElements;          // longest row of a warp
 constexpr int kNormRow = 1024 * kNormElements;            // longest row that a block holds
 constexpr int kNormGradRow = 512 * kNormElements;         // ... with the columns' sums beside it
-constexpr int kNormGradShort = 512 * 8;                   // rows up to this: eight elements a thread
+constexpr int kNormShort = 512 * 8;                       // rows of blocks up to this: eight elements a thread
 constexpr int kNormWarps = 8;                             // rows side by side in a block, a warp each
 constexpr int kNormWideThreads = 512;
 constexpr int kNormJoinThreads = 256;
@@ -53,6 +54,7 @@ struct NormArgs {
     float *mean, *rstd;
     long long ld_x, ld_branch, ld_sum, ld_out, T;
     int H, groups;               // groups: of N elements
+    int lanes;                   // of a row within a warp
     int branch32, weight32;      // fp32 (else bf16)
     float eps;
 };
@@ -63,26 +65,51 @@ struct NormGradArgs {
     void *dx, *dweight, *dbias;
     float *part;                 // [blocks][2][H]
     long long ld_dy, ld_x, ld_dsum, ld_dx, T;
-    int H, groups, blocks;
+    int H, groups, lanes, blocks;
     int weight32, grad32, add;   // types of the weight and of its gradient; add to the gradients
     float inv_h;
 };
 
-// N elements of an array whose type is known at run time; weights are read again by every row: kept in the caches.
-template <int N, bool kOnce>
+// N elements of an array whose type is known at run time.
+template <int N>
 __device__ __forceinline__ void load_either(const void *p, int is32, long long at, float (&f)[N]) {
-    if (is32) load_row<float, N, kOnce>(static_cast<const float *>(p) + at, f);
-    else load_row<bf16, N, kOnce>(static_cast<const bf16 *>(p) + at, f);
+    if (is32) load_row<float, N>(static_cast<const float *>(p) + at, f);
+    else load_row<bf16, N>(static_cast<const bf16 *>(p) + at, f);
+}
+// The same of a weight or bias, which every row reads again: through the first-level cache (from the second it was several times a
+// bf16 row's own traffic: 40,000 x 768 38 us, 26 so).
+template <int N>
+__device__ __forceinline__ void load_weight(const void *p, int is32, int at, float (&f)[N]) {
+    constexpr int kWords = N < 4 ? N : 4;
+    if (is32) {
+        const float *q = static_cast<const float *>(p) + at;
+        using W = typename Words<kWords>::type;
+#pragma unroll
+        for (int i = 0; i < N / kWords; ++i) {
+            const W w = __ldg(reinterpret_cast<const W *>(q) + i);
+            memcpy(&f[i * kWords], &w, sizeof(W));
+        }
+    } else if constexpr (N == 1) {
+        f[0] = to_float(__ldg(static_cast<const bf16 *>(p) + at));
+    } else {
+        using W = typename Words<N / 2>::type;
+        const W w = __ldg(reinterpret_cast<const W *>(static_cast<const bf16 *>(p) + at));
+        unsigned u[N / 2];
+        memcpy(u, &w, sizeof(W));
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) { f[2 * i] = bf16_low(u[i]); f[2 * i + 1] = bf16_high(u[i]); }
+    }
 }
 
-// Sums of K values over the threads of a row: a warp, or the block.  `s` is used by one call in two (the caller alternates), so
+// Sums of K values over the threads of a row: `lanes` of a warp, or the block.  `s` is used by one call in two (the caller alternates), so
 // that one barrier is enough.
 template <bool kWarp, int K>
-__device__ __forceinline__ void row_sums(float (&v)[K], float (*s)[32]) {
+__device__ __forceinline__ void row_sums(float (&v)[K], float (*s)[32], int lanes = 32) {
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int o = 16; o > 0; o >>= 1)
+        if (!kWarp || o < lanes)
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+            for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
     if constexpr (!kWarp) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
         if (lane == 0)
@@ -102,9 +129,10 @@ template <typename TX, typename TO, int N, bool kWarp>
 __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(const __grid_constant__ NormArgs a) {
     constexpr int G = kNormElements / N;
     __shared__ float s_sum[2][1][32];
-    const int L = kWarp ? 32 : blockDim.x, t = kWarp ? threadIdx.x & 31 : threadIdx.x;
-    const long long row = kWarp ? (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5) : blockIdx.x;
-    if (kWarp && row >= a.T) return;
+    const int L = kWarp ? a.lanes : blockDim.x, t = kWarp ? threadIdx.x & (L - 1) : threadIdx.x;
+    long long row = kWarp ? (long long)blockIdx.x * (kNormWarps * 32 / L) + threadIdx.x / L : blockIdx.x;
+    const bool mine = row < a.T;
+    if (!mine) row = a.T - 1;                                    // a warp's parts go on together: these write nothing
     const TX *x = static_cast<const TX *>(a.x) + row * a.ld_x;
     float h[G][N], sum[1] = {0.f};
 #pragma unroll
@@ -115,13 +143,13 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(co
 #pragma unroll
             for (int i = 0; i < N; ++i) h[g][i] = 0.f;
     }
-    if (a.branch) {
+    if (a.branch && mine) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int at = g * L + t;
             if (at >= a.groups) continue;
             float b[N];
-            load_either<N, true>(a.branch, a.branch32, row * a.ld_branch + (long long)at * N, b);
+            load_either<N>(a.branch, a.branch32, row * a.ld_branch + (long long)at * N, b);
 #pragma unroll
             for (int i = 0; i < N; ++i) h[g][i] = to_float(from_float<TX>(h[g][i] + b[i]));
             store_row<TX, N>(static_cast<TX *>(a.sum) + row * a.ld_sum + (long long)at * N, h[g]);
@@ -131,7 +159,7 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(co
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int i = 0; i < N; ++i) sum[0] += h[g][i];
-    row_sums<kWarp, 1>(sum, s_sum[0]);
+    row_sums<kWarp, 1>(sum, s_sum[0], L);
     const float mean = sum[0] / (float)a.H;
     sum[0] = 0.f;
 #pragma unroll
@@ -142,16 +170,17 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(co
                 h[g][i] -= mean;
                 sum[0] = fmaf(h[g][i], h[g][i], sum[0]);
             }
-    row_sums<kWarp, 1>(sum, s_sum[1]);
+    row_sums<kWarp, 1>(sum, s_sum[1], L);
     const float rstd = 1.0f / sqrtf(sum[0] / (float)a.H + a.eps);
+    if (!mine) return;
     if (t == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
 #pragma unroll
     for (int g = 0; g < G; ++g) {
         const int at = g * L + t;
         if (at >= a.groups) continue;
         float w[N], b[N];
-        load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
-        if (a.bias) load_either<N, false>(a.bias, a.weight32, (long long)at * N, b);
+        load_weight<N>(a.weight, a.weight32, at * N, w);
+        if (a.bias) load_weight<N>(a.bias, a.weight32, at * N, b);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float y = h[g][i] * rstd;
@@ -173,7 +202,7 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_wide_kernel(const __gri
         load_row<TX, N, false>(x + (long long)at * N, h);
         if (a.branch) {
             float b[N];
-            load_either<N, true>(a.branch, a.branch32, row * a.ld_branch + (long long)at * N, b);
+            load_either<N>(a.branch, a.branch32, row * a.ld_branch + (long long)at * N, b);
 #pragma unroll
             for (int i = 0; i < N; ++i) h[i] = to_float(from_float<TX>(h[i] + b[i]));
             store_row<TX, N>(static_cast<TX *>(a.sum) + row * a.ld_sum + (long long)at * N, h);
@@ -197,8 +226,8 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_wide_kernel(const __gri
     for (int at = threadIdx.x; at < a.groups; at += kNormWideThreads) {
         float h[N], w[N], b[N];
         load_row<TX, N>(from + (long long)at * N, h);
-        load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
-        if (a.bias) load_either<N, false>(a.bias, a.weight32, (long long)at * N, b);
+        load_weight<N>(a.weight, a.weight32, at * N, w);
+        if (a.bias) load_weight<N>(a.bias, a.weight32, at * N, b);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float y = (h[i] - mean) * rstd;
@@ -226,9 +255,17 @@ __device__ __forceinline__ void put_sums(const NormGradArgs &a, int L, int t, fl
     float *part = a.part + (long long)blockIdx.x * 2 * a.H;
     if constexpr (kWarp) {
         __shared__ float s_all[2][kNormWarpRow];
+        for (int o = L; o < 32; o *= 2)                          // the rows side by side in a warp
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    dw[g][i] += __shfl_xor_sync(0xffffffffu, dw[g][i], o);
+                    db[g][i] += __shfl_xor_sync(0xffffffffu, db[g][i], o);
+                }
         const int warp = threadIdx.x >> 5;
         for (int w = 0; w < kNormWarps; ++w) {
-            if (warp == w)
+            if (warp == w && (threadIdx.x & 31) < L)
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const int at = g * L + t;
@@ -264,21 +301,24 @@ template <typename TX, typename TO, int N, int E, bool kWarp>
 __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512, kWarp ? 2 : E == 8 ? 2 : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs a) {
     constexpr int G = E / N;
     __shared__ float s_sum[2][2][32];
-    const int L = kWarp ? 32 : blockDim.x, t = kWarp ? threadIdx.x & 31 : threadIdx.x;
+    const int L = kWarp ? a.lanes : blockDim.x, t = kWarp ? threadIdx.x & (L - 1) : threadIdx.x;
     float dw[G][N], db[G][N];
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int i = 0; i < N; ++i) dw[g][i] = db[g][i] = 0.f;
-    const long long step = (long long)gridDim.x * (kWarp ? kNormWarps : 1);
+    const long long step = kWarp ? (long long)gridDim.x * (kNormWarps * 32 / L) : gridDim.x;
+    long long row = kWarp ? (long long)blockIdx.x * (kNormWarps * 32 / L) + threadIdx.x / L : blockIdx.x;
     int odd = 0;
-    for (long long row = kWarp ? (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5) : blockIdx.x; row < a.T; row += step) {
+    // a warp's parts go on together: those past the last row add zeros and write nothing
+    for (long long all = kWarp ? row - threadIdx.x % 32 / L : row; all < a.T; all += step, row += step) {
+        const bool mine = row < a.T;
         float u[G][N], xh[G][N], more[G][N], sums[2] = {0.f, 0.f};
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        const float mean = mine ? a.mean[row] : 0.f, rstd = mine ? a.rstd[row] : 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int at = g * L + t;
-            if (at < a.groups) {
+            if (mine && at < a.groups) {
                 load_row<TO, N>(static_cast<const TO *>(a.dy) + row * a.ld_dy + (long long)at * N, u[g]);
                 load_row<TX, N>(static_cast<const TX *>(a.x) + row * a.ld_x + (long long)at * N, xh[g]);
                 if (a.dsum) load_row<TX, N>(static_cast<const TX *>(a.dsum) + row * a.ld_dsum + (long long)at * N, more[g]);
@@ -290,9 +330,9 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512, kWarp ? 2 : E =
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int at = g * L + t;
-            if (at >= a.groups) continue;
+            if (!mine || at >= a.groups) continue;
             float w[N];
-            load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
+            load_weight<N>(a.weight, a.weight32, at * N, w);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 xh[g][i] = (xh[g][i] - mean) * rstd;
@@ -303,12 +343,12 @@ __global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512, kWarp ? 2 : E =
                 sums[1] = fmaf(u[g][i], xh[g][i], sums[1]);
             }
         }
-        row_sums<kWarp, 2>(sums, s_sum[odd]);
+        row_sums<kWarp, 2>(sums, s_sum[odd], L);
         odd ^= 1;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int at = g * L + t;
-            if (at < a.groups) norm_dx<TX, N>(a, row, at, u[g], xh[g], more[g], rstd, sums[0] * a.inv_h, sums[1] * a.inv_h);
+            if (mine && at < a.groups) norm_dx<TX, N>(a, row, at, u[g], xh[g], more[g], rstd, sums[0] * a.inv_h, sums[1] * a.inv_h);
         }
     }
     put_sums<N, E, kWarp>(a, L, t, dw, db);
@@ -350,7 +390,7 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_grad_wide_kernel(const 
     auto load = [&](int at) {
         load_row<TO, N, false>(dy + (long long)at * N, u);
         load_row<TX, N, false>(x + (long long)at * N, xh);
-        load_either<N, false>(a.weight, a.weight32, (long long)at * N, w);
+        load_weight<N>(a.weight, a.weight32, at * N, w);
 #pragma unroll
         for (int i = 0; i < N; ++i) { xh[i] = (xh[i] - mean) * rstd; u[i] *= w[i]; }
     };
