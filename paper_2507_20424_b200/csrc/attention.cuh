@@ -227,6 +227,12 @@ __device__ __forceinline__ float2 exp2_polynomial(float2 x) {
     return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 
+// A row of NaN, where a wait gave up (copies may still be on their way to the tiles).
+__device__ __forceinline__ void spoil_row(bf16 *row, int D) {
+    const unsigned u = 0x7fc07fc0u;
+    for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4 *>(row + c) = make_uint4(u, u, u, u);
+}
+
 // S = scale q k^T over the keys that a query sees; out = softmax(S) v; lse = log sum exp S.
 // One pass over the keys with a running maximum and sum.  A block has two slots of 128 queries that share their keys and values:
 // while one slot's warpgroup takes the exponentials of its scores (a row a thread), the tensor cores work for the other.
@@ -430,7 +436,8 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
                 for (int i = 0; i < 32; i += 2)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) m[c] = max3(m[c], v[c][i], v[c][i + 1]);
-                const float now = fmaxf(m[0], m[1]) * a.scale2;
+                // a row that does not ask for it keeps its own: no row's bits depend on another's
+                const float now = j == first || grow ? fmaxf(m[0], m[1]) * a.scale2 : -INFINITY;
                 if (j > first) {
                     const float f = now > top ? exp2_fast(top - now) : 1.0f;
                     sum *= f;
@@ -466,16 +473,21 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
             ok = ok && wait.together(&o_full[s], 0);
             tmem_fence_after();
             const bool mine = r < slot_rows(s);
-            const float by = ok ? (sum > 0.f || sum != sum ? 1.0f / sum : 0.f) : __int_as_float(0x7fc00000);
-            const unsigned tile = s_q + s * kTileBytes;                  // the queries': their products are done
+            const float by = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+            bf16 *out = a.out + (long long)slot_row(s) * a.ld_out + slot_head(s) * a.head_out;
+            if (ok) {
+                const unsigned tile = s_q + s * kTileBytes;              // the queries': their products are done
 #pragma unroll
-            for (int c = 0; c < 2 * kBlocks; ++c) {
-                float o[32];
-                tmem_load32(O + c * 32, o);
-                tmem_loaded(o);
-                put_row(tile, r, c, o, by);
+                for (int c = 0; c < 2 * kBlocks; ++c) {
+                    float o[32];
+                    tmem_load32(O + c * 32, o);
+                    tmem_loaded(o);
+                    put_row(tile, r, c, o, by);
+                }
+                store_rows<8 * kBlocks>(tile, r & ~31, 0, out, a.ld_out, slot_rows(s), a.D);
+            } else if (mine) {
+                spoil_row(out + r * a.ld_out, a.D);
             }
-            store_rows<8 * kBlocks>(tile, r & ~31, 0, a.out + (long long)slot_row(s) * a.ld_out + slot_head(s) * a.head_out, a.ld_out, slot_rows(s), a.D);
             if (mine) a.lse[slot_head(s) * a.T + row] = ok ? (top + log2f(sum)) * kLn2 : __int_as_float(0x7fc00000);
         }
         tmem_fence_before();
@@ -737,15 +749,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
         }
         ok = ok && wait.together(&o_full, 0);
         tmem_fence_after();
-        const float by = ok ? a.scale : __int_as_float(0x7fc00000);
+        bf16 *dq = a.dq + (long long)t.row * a.ld_dq + head * a.head_dq;
+        if (ok) {
 #pragma unroll
-        for (int c = 0; c < kBlocks; ++c) {
-            float o[32];
-            tmem_load32(DQ + lanes + (half * kBlocks + c) * 32, o);
-            tmem_loaded(o);
-            put_row(s_q, r, half * kBlocks + c, o, by);
+            for (int c = 0; c < kBlocks; ++c) {
+                float o[32];
+                tmem_load32(DQ + lanes + (half * kBlocks + c) * 32, o);
+                tmem_loaded(o);
+                put_row(s_q, r, half * kBlocks + c, o, a.scale);
+            }
+            store_rows<4 * kBlocks>(s_q, r & ~31, half * 4 * kBlocks, dq, a.ld_dq, t.rows, a.D);
+        } else if (mine) {
+            spoil_row(dq + r * a.ld_dq, a.D);
         }
-        store_rows<4 * kBlocks>(s_q, r & ~31, half * 4 * kBlocks, a.dq + (long long)t.row * a.ld_dq + head * a.head_dq, a.ld_dq, t.rows, a.D);
         tmem_fence_before();
     }
     __syncthreads();
@@ -962,17 +978,21 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
         }
         ok = ok && wait.together(&o_full, 0);
         tmem_fence_after();
-        const float by = !ok ? __int_as_float(0x7fc00000) : half ? a.scale : 1.0f;
-        const unsigned tile = half ? s_k : s_v;                          // all products are done
-#pragma unroll
-        for (int c = 0; c < 2 * kBlocks; ++c) {
-            float o[32];
-            tmem_load32((half ? DK : DV) + lanes + c * 32, o);
-            tmem_loaded(o);
-            put_row(tile, r, c, o, by);
-        }
         const long long ld = half ? a.ld_dk : a.ld_dv;
-        store_rows<8 * kBlocks>(tile, r & ~31, 0, (half ? a.dk + kv_head * a.head_dk : a.dv + kv_head * a.head_dv) + t.row * ld, ld, t.rows, a.D);
+        bf16 *to = (half ? a.dk + kv_head * a.head_dk : a.dv + kv_head * a.head_dv) + t.row * ld;
+        if (ok) {
+            const unsigned tile = half ? s_k : s_v;                      // all products are done
+#pragma unroll
+            for (int c = 0; c < 2 * kBlocks; ++c) {
+                float o[32];
+                tmem_load32((half ? DK : DV) + lanes + c * 32, o);
+                tmem_loaded(o);
+                put_row(tile, r, c, o, half ? a.scale : 1.0f);
+            }
+            store_rows<8 * kBlocks>(tile, r & ~31, 0, to, ld, t.rows, a.D);
+        } else if (r < t.rows) {
+            spoil_row(to + r * ld, a.D);
+        }
         tmem_fence_before();
     }
     __syncthreads();

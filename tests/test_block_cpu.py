@@ -101,3 +101,56 @@ def test_binding_refuses_what_it_cannot_pass_on(b):
         b.dppf_layer_norm_grad(cpu, cpu, torch.zeros(4), torch.zeros(4), w, w)
     with pytest.raises(ValueError):
         b.dppf_rotary(torch.zeros(4, 2, 8), torch.arange(4), torch.ones(4, dtype=torch.float64))
+
+
+def test_attention_plan_refusals(b):
+    size, f = b.load().dppf_attention_plan_bytes, b.load().dppf_attention_plan
+    assert size(-1, 1) == 0 and size(5, 0) == 0 and size(2**24 + 1, 1) == 0 and size(5, 2**20 + 1) == 0
+    assert 0 < size(0, 1) <= size(1000, 4) <= size(10**6, 4) <= size(10**6, 10**5) < 1 << 24
+    ok = dict(s=P[0], sb=32, T=1000, B=4, plan=P[1], n=BIG)
+    call = caller(f, ok, list(ok))
+    for bad in (dict(s=None), dict(plan=None), dict(sb=16), dict(T=-1), dict(B=0), dict(s=P[1] + 256)):
+        assert call(**bad) == b.ERR_INVALID_ARG, bad
+    for bad in (dict(s=P[0] + 2), dict(sb=64, s=P[0] + 4), dict(plan=P[1] + 64)):
+        assert call(**bad) == b.ERR_ALIGNMENT, bad
+    assert call(n=256) == b.ERR_WORKSPACE
+
+
+def test_attention_refusals(b):
+    ok = dict(q=P[0], ldq=512, hq=64, k=P[1], ldk=128, hk=64, v=P[2], ldv=128, hv=64, T=100, B=3, h=8, kv=2, D=64, c=1, w=0, s=0.1, o=P[3], ldo=512, ho=64, lse=P[4], plan=P[5], n=BIG)
+    call = caller(b.load().dppf_attention, ok, list(ok))
+    for bad in ([{k: None} for k in ("q", "k", "v", "o", "lse", "plan")] +
+                [dict(T=-1), dict(T=2**25), dict(B=0), dict(h=0), dict(h=1025, kv=1), dict(kv=0), dict(kv=3), dict(D=0), dict(D=60), dict(D=136, ldq=2000, hq=136), dict(c=2), dict(w=-1), dict(w=5, c=0),
+                 dict(s=0.0), dict(s=-1.0), dict(s=NAN), dict(ldq=504), dict(hq=56), dict(ldk=0), dict(ldo=-8), dict(o=P[0]), dict(o=P[1]), dict(lse=P[3]), dict(lse=P[0]), dict(lse=P[5]), dict(o=P[5]),
+                 dict(ldq=2**39)]):
+        assert call(**bad) == b.ERR_INVALID_ARG, bad
+    for bad in (dict(q=P[0] + 8), dict(k=P[1] + 2), dict(v=P[2] + 8), dict(o=P[3] + 8), dict(ldq=516), dict(hk=68, ldk=200), dict(lse=P[4] + 2), dict(plan=P[5] + 64)):
+        assert call(**bad) == b.ERR_ALIGNMENT, bad
+    assert call(n=512) == b.ERR_WORKSPACE
+    assert call(T=0, q=None, plan=None) == b.OK
+
+
+def test_attention_grad_refusals(b):
+    ok = dict(go=P[0], ldgo=512, hgo=64, q=P[1], ldq=512, hq=64, k=P[2], ldk=128, hk=64, v=P[3], ldv=128, hv=64, o=P[4], ldo=512, ho=64, lse=P[5], T=100, B=3, h=8, kv=2, D=64, c=1, w=0, s=0.1,
+              dq=P[6], lddq=512, hdq=64, dk=P[7], lddk=128, hdk=64, dv=P[8], lddv=128, hdv=64, plan=P[9], n=BIG, ws=P[10], m=BIG)
+    call = caller(b.load().dppf_attention_grad, ok, list(ok))
+    for bad in ([{k: None} for k in ("go", "q", "k", "v", "o", "lse", "dq", "dk", "dv", "plan", "ws")] +
+                [dict(h=7), dict(D=68), dict(s=0.0), dict(w=3, c=0), dict(ldgo=100), dict(lddq=100), dict(dq=P[0]), dict(dq=P[1]), dict(dk=P[2]), dict(dk=P[7] + 128, dv=P[7]), dict(dq=P[5]), dict(dv=P[9]),
+                 dict(dv=P[10]), dict(ws=P[0]), dict(ws=P[5]), dict(ws=P[9]), dict(dk=P[4])]):
+        assert call(**bad) == b.ERR_INVALID_ARG, bad
+    for bad in (dict(go=P[0] + 8), dict(o=P[4] + 2), dict(dq=P[6] + 8), dict(lddk=132), dict(lse=P[5] + 1), dict(ws=P[10] + 64)):
+        assert call(**bad) == b.ERR_ALIGNMENT, bad
+    assert call(n=512) == b.ERR_WORKSPACE and call(m=512) == b.ERR_WORKSPACE
+    assert call(T=0, q=None, plan=None, ws=None) == b.OK
+    assert b.load().dppf_attention_workspace_bytes(0, 4) == 0 and b.load().dppf_attention_workspace_bytes(100, 0) == 0
+    # gradients beside one another in rows of one product do not overlap; shifted by one head they do
+    row = dict(dq=P[6], lddq=768, dk=P[6] + 2 * 512, lddk=768, dv=P[6] + 2 * 640, lddv=768)
+    assert call(**{**row, "m": 512}) == b.ERR_WORKSPACE
+    assert call(**{**row, "dv": P[6] + 2 * 576, "m": 512}) == b.ERR_WORKSPACE and call(**{**row, "dv": P[6] + 2 * 576}) == b.ERR_INVALID_ARG
+
+
+def test_binding_refuses_attention_on_the_host(b):
+    with pytest.raises(ValueError):
+        b.AttentionPlan(torch.zeros(2, dtype=torch.int32), 5)
+    with pytest.raises(ValueError):
+        b.alloc_attention_workspace(0, 4, device="cpu")

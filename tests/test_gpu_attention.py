@@ -7,6 +7,7 @@ sum of their magnitudes times scale.  A sum of exponentials (2 ulp each) adds at
   out      every probability is rounded to bf16: (2^-8 + 2 e) sum p |v|, and 2^-8 |out| for the result
   grads    p is e off (the given lse), dP is off by 2^-20 of its magnitudes' sum and D_t likewise, dS = p (dP - D_t) is rounded to
            bf16: (2^-8 + 2 e) |dS| + p 2^-19 (sum |do v| + sum |do o|) for each, times |k| or |q|, summed;  dv as out; 2^-8 of the result
+  all      exponentials below 2^-126 are 0; times factors of up to 2^16 and summed over up to 2^10 keys that is below 2^-100
 """
 import math
 
@@ -50,7 +51,7 @@ def starts_of(lens, lead=0):
 def within(got, want, tol, what=""):
     assert torch.equal(torch.isfinite(got), torch.isfinite(want)), what
     fine = torch.isfinite(want)
-    off = (got.double() - want)[fine].abs() - tol[fine]
+    off = (got.double() - want)[fine].abs() - tol[fine] - 2.0 ** -100
     assert not off.numel() or float(off.max()) <= 0, (what, float(off.max()), float(tol[fine].max()))
 
 
@@ -173,3 +174,285 @@ def test_backward_lengths(b, lens, heads, kv_heads, D, causal, window):
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 77)])
 def test_backward_heads(b, heads, kv_heads, D, causal, window):
     check_grads(b, [150, 1, 333], heads, kv_heads, D, causal, window, scale=0.11, lead=7, tail=131)
+
+
+def test_gradient_is_the_slope(b):
+    """Against differences of the formula in 64 bits: the loss is sum c out."""
+    starts = starts_of([5, 40, 131])
+    T, heads, kv, D = int(starts[-1]), 4, 2, 32
+    q, k, v = inputs(T, heads, kv, D, seed=5, std=0.5)
+    c = randn((T, heads, D), 6)
+    plan = b.AttentionPlan(starts, T)
+    fwd = b.dppf_attention(q, k, v, plan)
+    grads = b.dppf_attention_grad(c, q, k, v, fwd.out, fwd.lse, plan)
+
+    def loss(q, k, v):
+        out = reference_out(q, k, v, starts)
+        return (c.double() * out).sum()
+
+    at, step = [x.double() for x in (q, k, v)], 1e-5
+    for i in range(3):
+        for seed in range(2):
+            d = torch.randn(at[i].shape, generator=gen(30 + seed), device="cuda", dtype=F64)
+            up, down = ([x + sign * step * d if n == i else x for n, x in enumerate(at)] for sign in (1, -1))
+            slope = float((loss(*up) - loss(*down)) / (2 * step))
+            got = float((grads[i].double() * d).sum())
+            # the gradient's roundings, 2^-8 each of P, dS and the result, add up like random ones: 4 * 2^-8 of the root of the sum of squares
+            assert abs(got - slope) < 4 * HALF * float((grads[i].double() * d).square().sum().sqrt()) + 1e-4, (i, got, slope)
+
+
+def reference_out(q, k, v, starts):
+    out = torch.zeros(q.shape, dtype=F64, device="cuda")
+    at = starts.tolist()
+    share = q.shape[1] // k.shape[1]
+    for a, e in zip(at, at[1:]):
+        for h in range(q.shape[1]):
+            s = q[a:e, h] @ k[a:e, h // share].t() * q.shape[2] ** -0.5
+            s = s.masked_fill(torch.ones_like(s, dtype=torch.bool).triu(1), -math.inf)
+            out[a:e, h] = torch.softmax(s, 1) @ v[a:e, h // share]
+    return out
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(4, 2), (3, 3)])
+@pytest.mark.parametrize("jump", [20.0, 300.0, -300.0])
+@pytest.mark.parametrize("causal", [True, False])
+def test_scores_that_grow_from_tile_to_tile(b, heads, kv_heads, jump, causal):
+    """Keys whose scores rise (or fall) by `jump` from tile to tile: sums have to be taken relative to a new maximum, or most keys vanish."""
+    T, D = 700, 64
+    starts = starts_of([T])
+    q, k, v = (x.clone() for x in inputs(T, heads, kv_heads, D, seed=7, std=0.3))
+    q[..., 0] = 8.0
+    k[..., 0] = (torch.arange(T, device="cuda") // 128 * jump)[:, None].to(BF16)
+    plan = b.AttentionPlan(starts, T)
+    got = b.dppf_attention(q, k, v, plan, causal=causal)
+    want = reference(q, k, v, starts, causal, 0, D ** -0.5)
+    within(got.lse, *want["lse"], "lse")
+    within(got.out, *want["out"], "out")
+    grad_out = randn((T, heads, D), 8)
+    grads = b.dppf_attention_grad(grad_out, q, k, v, got.out, got.lse, plan, causal=causal)
+    want = reference(q, k, v, starts, causal, 0, D ** -0.5, (grad_out, got.out, got.lse))
+    for name in ("q", "k", "v"):
+        within(getattr(grads, name), *want[name], name)
+
+
+@pytest.mark.parametrize("heads,kv_heads,D", [(4, 2, 128), (2, 2, 56)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_other_rows_do_not_matter(b, heads, kv_heads, D, causal):
+    """What stands in rows of other sequences, or of none, NaN and infinities included, changes no bit of a sequence's results."""
+    lens, at = [60, 200, 77], 1
+    starts = starts_of(lens, lead=9)
+    T = int(starts[-1]) + 50
+    a, e = int(starts[at]), int(starts[at + 1])
+    q, k, v = (x.clone() for x in inputs(T, heads, kv_heads, D, seed=9))
+    grad_out = randn((T, heads, D), 10)
+    plan = b.AttentionPlan(starts, T)
+
+    def run():
+        f = b.dppf_attention(q, k, v, plan, causal=causal)
+        return f, b.dppf_attention_grad(grad_out, q, k, v, f.out, f.lse, plan, causal=causal)
+
+    f0, g0 = run()
+    bad = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e38], device="cuda").to(BF16)
+    for t in (q, k, v, grad_out):
+        for rows in (slice(0, a), slice(e, T)):
+            t[rows] = bad[torch.randint(0, 4, t[rows].shape, generator=gen(11), device="cuda")]
+    f1, g1 = run()
+    assert same_bits(f0.out[a:e], f1.out[a:e]) and same_bits(f0.lse[:, a:e], f1.lse[:, a:e])
+    assert all(same_bits(x[a:e], y[a:e]) for x, y in zip(g0, g1))
+    for t in (f1.out, *g1):
+        assert not t[:9].any() and not t[-50:].any()
+
+
+def test_values_that_are_not_finite_spoil_their_queries(b):
+    starts = starts_of([300])
+    q, k, v = (x.clone() for x in inputs(300, 2, 1, 64, seed=12))
+    k[200, 0, 5] = float("nan")
+    out = b.dppf_attention(q, k, v, b.AttentionPlan(starts, 300))
+    assert torch.isnan(out.out[200:].float()).all() and torch.isfinite(out.out[:128].float()).all()
+
+
+def test_layouts(b):
+    """Heads in blocks of their own, padded rows, gradients beside one another; nothing beside them is written."""
+    T, heads, kv, D = 333, 4, 2, 40
+    starts = starts_of([100, 233])
+    base = inputs(T, heads, kv, D, seed=13)
+    grad_out = randn((T, heads, D), 14)
+    plan = b.AttentionPlan(starts, T)
+    f = b.dppf_attention(*base, plan)
+    g = b.dppf_attention_grad(grad_out, *base, f.out, f.lse, plan)
+
+    def by_head(n, pad=8):
+        whole = torch.full((n, T, D + pad), float("nan"), dtype=BF16, device="cuda")
+        return whole, whole[:, :, :D].transpose(0, 1)
+
+    copies = []
+    for t in (*base, grad_out):
+        _, view = by_head(t.shape[1])
+        view.copy_(t)
+        copies.append(view)
+    whole, out = by_head(heads)
+    lse = torch.full((heads, T), float("nan"), device="cuda")
+    b.dppf_attention(*copies[:3], plan, out=out, lse=lse)
+    assert same_bits(out, f.out) and same_bits(lse, f.lse) and torch.isnan(whole[:, :, D:].float()).all()
+    rows = torch.full((T, (heads + 2 * kv) * D + 24), float("nan"), dtype=BF16, device="cuda")
+    cut = lambda n, first: rows[:, first:first + n * D].unflatten(1, (n, D))  # noqa: E731
+    dq, dk, dv = cut(heads, 8), cut(kv, 8 + heads * D), cut(kv, 8 + (heads + kv) * D)
+    got = b.dppf_attention_grad(copies[3], *copies[:3], out, lse, plan, grad_q=dq, grad_k=dk, grad_v=dv)
+    assert got.q is dq and same_bits(dq, g.q) and same_bits(dk, g.k) and same_bits(dv, g.v)
+    assert torch.isnan(rows[:, :8].float()).all() and torch.isnan(rows[:, 8 + (heads + 2 * kv) * D:].float()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_starts_that_are_out_of_order(b, dtype):
+    T = 500
+    q, k, v = inputs(T, 2, 1, 64, seed=15)
+    starts = torch.tensor([-7, 100, 60, 250, 250, 9999, 400], device="cuda").to(dtype)
+    kept = torch.tensor([0, 100, 100, 250, 250, 500, 500], dtype=torch.int32, device="cuda")
+    got = b.dppf_attention(q, k, v, b.AttentionPlan(starts, T))
+    want = b.dppf_attention(q, k, v, b.AttentionPlan(kept, T))
+    assert same_bits(got.out, want.out) and same_bits(got.lse, want.lse)
+    if dtype is torch.int64:
+        far = b.AttentionPlan(torch.tensor([-2 ** 62, 2 ** 40], device="cuda"), T)
+        assert same_bits(b.dppf_attention(q, k, v, far).out, b.dppf_attention(q, k, v, b.AttentionPlan(starts_of([T]), T)).out)
+
+
+def test_many_sequences(b):
+    lens = torch.randint(0, 9, (5000,), generator=torch.Generator().manual_seed(3)).tolist()
+    starts = starts_of(lens)
+    T = int(starts[-1]) + 3
+    q, k, v = inputs(T, 2, 1, 32, seed=16)
+    plan = b.AttentionPlan(starts, T)
+    got = b.dppf_attention(q, k, v, plan, causal=False)
+    # block diagonal scores, some thousands of rows at a time
+    seq = torch.bucketize(torch.arange(T, device="cuda"), starts[1:].long(), right=True)
+    want = torch.zeros(T, 2, 32, dtype=F64, device="cuda")
+    for a in range(0, T - 3, 4000):
+        e = min(T - 3, a + 4000)
+        lo, hi = max(0, a - 16), min(T - 3, e + 16)
+        for h in range(2):
+            s = q[a:e, h].double() @ k[lo:hi, 0].double().t() * 32 ** -0.5
+            want[a:e, h] = torch.softmax(s.masked_fill(seq[a:e, None] != seq[None, lo:hi], -math.inf), 1) @ v[lo:hi, 0].double()
+    within(got.out, want, (HALF + 1e-4) * 6.0 + HALF * want.abs())              # sum p |v| <= max |v| < 6
+    grads = b.dppf_attention_grad(q, q, k, v, got.out, got.lse, plan, causal=False)
+    assert all(torch.isfinite(x.float()).all() for x in grads) and b.dppf_device_status(plan.buffer) == b.OK
+
+
+def test_far_rows(b):
+    T, heads, D = 300_000, 64, 128                                              # 2.5e9 elements
+    n = 300
+    starts = starts_of([n], lead=T - n)
+    q = torch.empty(T, heads, D, dtype=BF16, device="cuda")
+    k, v = torch.empty(T, 2, D, dtype=BF16, device="cuda"), torch.empty(T, 2, D, dtype=BF16, device="cuda")
+    q[-n:], k[-n:], v[-n:] = (x for x in (randn((n, heads, D), 17), randn((n, 2, D), 18), randn((n, 2, D), 19)))
+    far, near = b.AttentionPlan(starts, T), b.AttentionPlan(starts_of([n]), n)
+    f, g = b.dppf_attention(q, k, v, far), b.dppf_attention(q[-n:], k[-n:], v[-n:], near)
+    assert same_bits(f.out[-n:], g.out) and same_bits(f.lse[:, -n:], g.lse) and not f.out[:-n].any()
+    df = b.dppf_attention_grad(q, q, k, v, f.out, f.lse, far)
+    dg = b.dppf_attention_grad(q[-n:], q[-n:], k[-n:], v[-n:], g.out, g.lse, near)
+    assert all(same_bits(x[-n:], y) and not x[:-n].any() for x, y in zip(df, dg))
+
+
+def test_streams_graphs_and_a_shared_plan(b):
+    lens, other = [130, 1, 200], [31, 200, 100]
+    starts = starts_of(lens)
+    T = int(starts[-1])
+    q, k, v = (x.clone() for x in inputs(T, 4, 2, 64, seed=20))
+    grad_out = randn((T, 4, 64), 21)
+    plan, ws = b.AttentionPlan(starts, T), b.alloc_attention_workspace(T, 4)
+
+    def step(ws=ws):
+        f = b.dppf_attention(q, k, v, plan)
+        return (*f, *b.dppf_attention_grad(grad_out, q, k, v, f.out, f.lse, plan, ws=ws))
+
+    want = step()
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for s in sides:                                                             # side by side on one plan, each its own workspace
+        with torch.cuda.stream(s):
+            got.append([step(b.alloc_attention_workspace(T, 4)) for _ in range(4)])
+    torch.cuda.synchronize()
+    assert all(same_bits(x, y) for runs in got for r in runs for x, y in zip(r, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.renew(starts)
+        captured = step()
+    starts.copy_(starts_of(other))
+    q.copy_(randn(q.shape, 22))
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    plan = b.AttentionPlan(starts_of(other), T)
+    assert all(same_bits(x, y) for x, y in zip(captured, step()))
+
+
+def test_waits_that_give_up(b):
+    """With no polls allowed every wait gives up at once: the rows are NaN and the status says so; the next calls are well."""
+    starts = starts_of([300, 20])
+    T = 320
+    q, k, v = inputs(T, 4, 2, 128, seed=23)
+    plan = b.AttentionPlan(starts, T)
+    want = b.dppf_attention(q, k, v, plan)
+    grads = b.dppf_attention_grad(q, q, k, v, want.out, want.lse, plan)
+    try:
+        b.debug_set_poll_limits(0, -1)
+        got = b.dppf_attention(q, k, v, plan)
+        status = b.dppf_device_status(plan.buffer)
+        assert status == b.ERR_TIMEOUT and torch.isnan(got.out.float()).all() and torch.isnan(got.lse).all()
+        plan.renew(starts)
+        assert b.dppf_device_status(plan.buffer) == b.OK
+        bad = b.dppf_attention_grad(q, q, k, v, want.out, want.lse, plan)
+        assert b.dppf_device_status(plan.buffer) == b.ERR_TIMEOUT and all(torch.isnan(x.float()).all() for x in bad)
+    finally:
+        b.debug_set_poll_limits(-1, -1)
+    plan.renew(starts)
+    again = b.dppf_attention(q, k, v, plan)
+    assert same_bits(again.out, want.out) and all(same_bits(x, y) for x, y in zip(grads, b.dppf_attention_grad(q, q, k, v, again.out, again.lse, plan)))
+    assert b.dppf_device_status(plan.buffer) == b.OK
+
+
+def test_a_plan_of_other_rows_writes_nothing(b):
+    plan = b.AttentionPlan(starts_of([64]), 64)
+    q, k, v = inputs(64, 1, 1, 64, seed=24)
+    plan.buffer[:4096].zero_()
+    out, lse = torch.full_like(q, 7.0), torch.full((1, 64), 7.0, device="cuda")
+    b.dppf_attention(q, k, v, plan, out=out, lse=lse)
+    assert b.dppf_device_status(plan.buffer) == b.ERR_WORKSPACE and (out == 7).all() and (lse == 7).all()
+    got = b.dppf_attention_grad(q, q, k, v, out, lse, plan, grad_q=torch.full_like(q, 7.0), grad_k=torch.full_like(k, 7.0), grad_v=torch.full_like(v, 7.0))
+    assert all((x == 7).all() for x in got)
+
+
+def test_no_tokens_and_refusals(b):
+    plan = b.AttentionPlan(torch.zeros(3, dtype=torch.int32, device="cuda"), 0)
+    empty = torch.empty(0, 4, 64, dtype=BF16, device="cuda")
+    f = b.dppf_attention(empty, empty[:, :2], empty[:, :2], plan)
+    assert f.out.shape == (0, 4, 64) and f.lse.shape == (4, 0)
+    assert b.dppf_attention_grad(empty, empty, empty[:, :2], empty[:, :2], f.out, f.lse, plan).k.shape == (0, 2, 64)
+    T = 20
+    q, k, v = inputs(T, 4, 2, 64, seed=25)
+    plan = b.AttentionPlan(starts_of([T]), T)
+    for bad in (dict(q=q.float()), dict(k=k[:, :1]), dict(v=v[:10]), dict(q=q[..., :32]), dict(out=q[:, :2]), dict(q=q[0]), dict(lse=torch.empty(3, T, device="cuda")), dict(q=q.half())):
+        a = {"q": q, "k": k, "v": v, "out": None, "lse": None, **bad}
+        with pytest.raises(ValueError):
+            b.dppf_attention(a["q"], a["k"], a["v"], plan, out=a["out"], lse=a["lse"])
+    q3 = torch.cat([q, q], 1)[:, :7]
+    odd = torch.zeros(T, 4, 72, dtype=BF16, device="cuda")
+    for args, kw, status in (((q3, k, v), {}, b.ERR_INVALID_ARG), ((q, k, v), dict(window=5, causal=False), b.ERR_INVALID_ARG), ((q, k, v), dict(window=-1), b.ERR_INVALID_ARG),
+                             ((q, k, v), dict(scale=0.0), b.ERR_INVALID_ARG), ((q, k, v), dict(scale=float("nan")), b.ERR_INVALID_ARG), ((q, k, v), dict(out=q), b.ERR_INVALID_ARG),
+                             ((odd[..., 1:65], k, v), {}, b.ERR_ALIGNMENT), ((odd[..., :60], odd[:, :2, :60], odd[:, :2, :60]), {}, b.ERR_INVALID_ARG)):
+        with pytest.raises(b.DppfError) as err:
+            b.dppf_attention(*args, plan, **kw)
+        assert err.value.status == status
+    f = b.dppf_attention(q, k, v, plan)
+    with pytest.raises(b.DppfError):
+        b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan, grad_q=f.out)
+    with pytest.raises(ValueError):
+        b.dppf_attention_grad(q, q, k, v, f.out, f.lse[:2], plan)
+    with pytest.raises(ValueError):
+        b.dppf_attention_grad(q[:, :2], q, k, v, f.out, f.lse, plan)
+    with pytest.raises(ValueError):
+        b.AttentionPlan(torch.zeros(1, dtype=torch.int32, device="cuda"), 5)
+    with pytest.raises(ValueError):
+        b.AttentionPlan(torch.zeros(2, device="cuda"), 5)
+    with pytest.raises(ValueError):
+        plan.renew(torch.zeros(5, dtype=torch.int32, device="cuda"))
