@@ -514,8 +514,10 @@ class LayerNorm(NamedTuple):
 
 def _rows(t: torch.Tensor, shape, what: str, device, dtype=None):
     """(pointer, row stride) of the rows of t, which has this shape (the last dimension its columns), this device and, if given, this type."""
-    if t.shape != shape or t.device != device or (dtype is not None and t.dtype != dtype):
+    if t.shape != shape or t.device != device or (dtype is not None and t.dtype is not dtype):
         raise ValueError(f"{what} must be a tensor of shape {tuple(shape)}{'' if dtype is None else f' and type {dtype}'} on {device}")
+    if t.is_contiguous() and len(shape) > 1:
+        return t.data_ptr(), shape[-1]
     _, _, ld = _matrix(t if t.dim() == 2 else t.view(-1, shape[-1]), what)
     return t.data_ptr(), ld
 
@@ -523,12 +525,19 @@ def _rows(t: torch.Tensor, shape, what: str, device, dtype=None):
 def dppf_layer_norm(x, weight, bias=None, eps=1e-5, branch=None, sum_out=None, out=None, out_dtype=None) -> LayerNorm:
     """Layer norm of the rows of ``x[..., H]`` or, with ``branch``, of ``x + branch``, which is written to ``sum_out`` (may be ``x``;
     new if not given).  ``out_dtype`` (default: x's) is used when ``out`` is not given."""
-    shape, dev, H = x.shape, x.device, x.shape[-1] if x.dim() else 0
+    shape, dev, kind = x.shape, x.device, weight.dtype
+    if not x.is_cuda or not shape:
+        raise ValueError("x must be a CUDA tensor of rows")
+    H = shape[-1]
     px, ld_x = _rows(x, shape, "x", dev)
     T = x.numel() // H if H else 0
-    for t in (weight, bias):
-        if t is not None and (t.dtype != weight.dtype or t.numel() != H or t.device != dev or not t.is_contiguous()):
-            _vector(t, H, "weight and bias", dev, (weight.dtype,))
+    if weight.numel() != H or weight.device != dev or not weight.is_contiguous():
+        _vector(weight, H, "weight", dev, (kind,))
+    pw, p_bias = weight.data_ptr(), None
+    if bias is not None:
+        if bias.dtype is not kind or bias.numel() != H or bias.device != dev or not bias.is_contiguous():
+            _vector(bias, H, "bias", dev, (kind,))
+        p_bias = bias.data_ptr()
     pb, tb, ld_b, ps, ld_s = None, FLOAT32, 0, None, 0
     if branch is not None:
         pb, ld_b = _rows(branch, shape, "branch", dev)
@@ -540,10 +549,12 @@ def dppf_layer_norm(x, weight, bias=None, eps=1e-5, branch=None, sum_out=None, o
         raise ValueError("sum_out is for the sum with a branch")
     if out is None:
         out = x.new_empty(shape, dtype=out_dtype)
-    po, ld_o = _rows(out, shape, "out", dev)
+        po, ld_o = out.data_ptr(), H
+    else:
+        po, ld_o = _rows(out, shape, "out", dev)
     stats = x.new_empty((2, *shape[:-1]), dtype=torch.float32)
     at = stats.data_ptr()
-    _call(dev, load().dppf_layer_norm, "dppf_layer_norm", px, _type(x, "x"), ld_x, pb, tb, ld_b, weight.data_ptr(), _ptr(bias), _type(weight, "weight"), T, H, eps, ps, ld_s,
+    _call(dev, load().dppf_layer_norm, "dppf_layer_norm", px, _type(x, "x"), ld_x, pb, tb, ld_b, pw, p_bias, _type(weight, "weight"), T, H, eps, ps, ld_s,
           po, _type(out, "out"), ld_o, at, at + 4 * T)
     mean, rstd = stats.unbind()
     return LayerNorm(out, x if sum_out is None else sum_out, mean, rstd)
@@ -560,21 +571,22 @@ def dppf_layer_norm_grad(grad_out, x, mean, rstd, weight, grad_weight, grad_bias
     """Gradient of :func:`dppf_layer_norm` from its ``sum`` (here ``x``), ``mean`` and ``rstd``: written to (or, with ``accumulate``, added
     to) ``grad_weight`` and ``grad_bias``; returns that of x and of the branch, in ``grad_x`` (may be ``grad_sum`` or ``grad_out``; new if
     not given), with ``grad_sum``, the gradient that reaches the sum past the norm, added."""
-    shape, dev, H = x.shape, x.device, x.shape[-1] if x.dim() else 0
+    shape, dev = x.shape, x.device
+    if not x.is_cuda or not shape:
+        raise ValueError("x must be a CUDA tensor of rows")
+    H = shape[-1]
     px, ld_x = _rows(x, shape, "x", dev)
     T = x.numel() // H if H else 0
     pg, ld_g = _rows(grad_out, shape, "grad_out", dev)
-    for t in (mean, rstd):
-        if t.dtype is not torch.float32 or t.numel() != T or t.device != dev or not t.is_contiguous():
-            _vector(t, T, "mean and rstd", dev)
-    _vector(weight, H, "weight", dev, tuple(_TYPES))
-    for t in (grad_weight, grad_bias):
-        if t is not None and (t.dtype != grad_weight.dtype or t.numel() != H or t.device != dev or not t.is_contiguous()):
-            _vector(t, H, "grad_weight and grad_bias", dev, (grad_weight.dtype,))
+    for t, n, kind in ((mean, T, torch.float32), (rstd, T, torch.float32), (weight, H, weight.dtype), (grad_weight, H, grad_weight.dtype), (grad_bias, H, grad_weight.dtype)):
+        if t is not None and (t.dtype is not kind or t.numel() != n or t.device != dev or not t.is_contiguous()):    # quickly; _vector says what is wrong
+            _vector(t, n, "mean and rstd, weight, grad_weight and grad_bias", dev, (kind,))
     ps, ld_s = (None, 0) if grad_sum is None else _rows(grad_sum, shape, "grad_sum", dev, x.dtype)
     if grad_x is None:
         grad_x = x.new_empty(shape)
-    pd, ld_d = _rows(grad_x, shape, "grad_x", dev, x.dtype)
+        pd, ld_d = grad_x.data_ptr(), H
+    else:
+        pd, ld_d = _rows(grad_x, shape, "grad_x", dev, x.dtype)
     if ws is not None:
         _workspace(ws, dev)
     elif T:
