@@ -554,21 +554,24 @@ __device__ __forceinline__ void times_difference(float (&v)[32], const float (&d
 template <int kSteps>
 struct QueryGradShape {
     static constexpr int kBlocks = (kSteps + 3) / 4;
+    static constexpr bool kApart = kSteps <= 6;              // dS has a place of its own in tensor memory
     static constexpr int kKeys = 3, kValues = 2;             // stages: a tile of keys is needed until dq has it, one of values until dP has it
     static constexpr unsigned kSmem = (2 + kKeys + kValues) * kBlocks * kBlockBytes + 1024;
 };
 
 // dq of a tile of queries, and D.  The tile's queries and grad_out lie in tensor memory, too: with both operands of a product in shared
 // memory its reads take all of that memory's bandwidth, and the copies' writes come on top.  A thread takes half a row of scores to registers at
-// once, so that the products of the next tile of keys can replace them while it takes the exponentials.
+// once, so that the products of the next tile of keys can replace them while it takes the exponentials.  With heads of up to 96 there is room
+// for dS beside dP, and the next dP comes as early; else it waits for the products with dS, whose place it takes.
 template <int kSteps>
 __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(const __grid_constant__ AttentionGradArgs a) {
     using Shape = QueryGradShape<kSteps>;
     constexpr int kBlocks = Shape::kBlocks;
     constexpr int kKeys = Shape::kKeys, kValues = Shape::kValues, kColumns = 512;
+    constexpr bool kApart = Shape::kApart;
     constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ unsigned long long q_full, o_read, rows_ready, k_full[kKeys], k_empty[kKeys], v_full[kValues], v_empty[kValues], s_full, s_free, dp_full, ds_full, o_full, k_fixed, drained;
+    __shared__ unsigned long long q_full, o_read, rows_ready, k_full[kKeys], k_empty[kKeys], v_full[kValues], v_empty[kValues], s_full, s_free, dp_full, dp_free, ds_full, o_full, k_fixed, drained;
     __shared__ float s_delta[kTile];
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
@@ -593,7 +596,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
 
     if (tid == 0) {
         for (unsigned long long *bar : {&q_full, &s_full, &dp_full, &o_full, &k_fixed, &drained}) mbar_init(bar, 1);
-        for (unsigned long long *bar : {&rows_ready, &s_free, &ds_full}) mbar_init(bar, 256);
+        for (unsigned long long *bar : {&rows_ready, &s_free, &dp_free, &ds_full}) mbar_init(bar, 256);
         mbar_init(&o_read, 128);
         for (int i = 0; i < kKeys; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
         for (int i = 0; i < kValues; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
@@ -604,7 +607,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const unsigned tmem = uniform(s_tmem), DP = tmem + 128, DQ = tmem + 256, Q = tmem + 384, DO = tmem + 448;      // scores at 0
+    const unsigned tmem = uniform(s_tmem), DP = tmem + 128, DQ = tmem + 256, Q = DQ + 16 * kSteps, DO = Q + 8 * kSteps;      // scores at 0
+    const unsigned DS = kApart ? tmem + 448 : DP;                        // a half of 64 columns as pairs in 32: side by side, or in front of what it comes from
+    constexpr int kHalf = kApart ? 32 : 64;
 
     const int there = t.end - (t.begin + (hi - 1) * kTile);              // rows of the last tile that are the sequence's
     if (warp == 8) {
@@ -661,13 +666,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
             if (!ok) break;
             tmem_fence_after();
             if (more && elect()) scores(j + 1);
+            if (kApart && more) {
+                ok = wait.together(&dp_free, j & 1);
+                if (!ok) break;
+                tmem_fence_after();
+                if (elect()) dps(j + 1);
+            }
             ok = wait.together(&ds_full, j & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
-                product_columns<kSteps>(DQ, DP, s_k + j % kKeys * kTileBytes, 0, j > 0);
-                product_columns<kSteps>(DQ, DP + 64, s_k + j % kKeys * kTileBytes, 1, true);
-                if (more) dps(j + 1);
+                product_columns<kSteps>(DQ, DS, s_k + j % kKeys * kTileBytes, 0, j > 0);
+                product_columns<kSteps>(DQ, DS + kHalf, s_k + j % kKeys * kTileBytes, 1, true);
+                if (!kApart && more) dps(j + 1);
                 products_done(&k_empty[j % kKeys]);
                 if (!more) products_done(&o_full);
             }
@@ -685,7 +696,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
         bool ok = wait.together(&q_full, 0);
         float delta = 0.f;
 #pragma unroll
-        for (int c = 0; c < 2 * kBlocks; ++c) {
+        for (int c = 0; c < kSteps / 2; ++c) {
             unsigned u[16];
             tile_row(half ? s_do : s_q, r, c, u);
             tmem_store16((half ? DO : Q) + lanes + 16 * c, u);
@@ -733,6 +744,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
             for (int c = 0; c < 2; ++c) {
                 tmem_load32(DP + lanes + 64 * half + 32 * c, d);
                 tmem_loaded(d);
+                if (kApart && c) {
+                    tmem_fence_before();
+                    mbar_arrive(&dp_free);
+                }
                 times_difference(p[c], d, [&](int) { return both(-delta); });
             }
             if (!whole)                                                  // a select: what is masked may be NaN
@@ -741,8 +756,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                         if (c * 32 + i < from || c * 32 + i >= to) p[c][i] = 0.f;
+            if (kApart && j > 0) {                                       // the products with the dS before are done
+                ok = wait.together(&k_empty[(j - 1) % kKeys], ((j - 1) / kKeys) & 1);
+                if (!ok) break;
+                tmem_fence_after();
+            }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) put_pairs(DP + lanes + 64 * half + 16 * c, p[c]);
+            for (int c = 0; c < 2; ++c) put_pairs(DS + lanes + kHalf * half + 16 * c, p[c]);
             tmem_stored();
             tmem_fence_before();
             mbar_arrive(&ds_full);
@@ -773,21 +793,24 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
 template <int kSteps>
 struct KeyGradShape {
     static constexpr int kBlocks = (kSteps + 3) / 4;
+    static constexpr bool kApart = kSteps <= 6;              // the probabilities have a place of their own in tensor memory
     static constexpr int kQueries = 3, kOuts = 2;            // stages: a tile of queries is asked for before the one before it is done with
     static constexpr unsigned kTiles = (2 + kQueries + kOuts) * kBlocks * kBlockBytes;
     static constexpr unsigned kSmem = kTiles + 2 * 2 * kTile * 4;        // and lse and D of two tiles of queries
 };
 
 // dk and dv of a tile of keys: a row of the transposed scores is a key.  Scores and dP take turns: while the exponentials of one
-// tile are taken, the tensor cores form dk and dP, and dv and the next scores while dS is.
+// tile are taken, the tensor cores form dk and dP, and dv and the next scores while dS is.  With heads of up to 96 there is room for
+// the probabilities beside the scores, and the next scores come as soon as a thread has its half row in registers.
 template <int kSteps>
 __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(const __grid_constant__ AttentionGradArgs a) {
     using Shape = KeyGradShape<kSteps>;
     constexpr int kBlocks = Shape::kBlocks;
     constexpr int kQueries = Shape::kQueries, kOuts = Shape::kOuts, kColumns = 512;
+    constexpr bool kApart = Shape::kApart;
     constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ unsigned long long kv_full, q_full[kQueries], q_ready[kQueries], q_empty[kQueries], do_full[kOuts], do_ready[kOuts], do_empty[kOuts], stat_full[2], s_full, dp_full, p_full, ds_full, o_full, drained;
+    __shared__ unsigned long long kv_full, q_full[kQueries], q_ready[kQueries], q_empty[kQueries], do_full[kOuts], do_ready[kOuts], do_empty[kOuts], stat_full[2], s_full, s_free, dp_full, p_full, ds_full, o_full, drained;
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
@@ -812,6 +835,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     if (tid == 0) {
         for (unsigned long long *bar : {&kv_full, &s_full, &dp_full, &o_full, &drained}) mbar_init(bar, 1);
         mbar_init(&p_full, 256);
+        mbar_init(&s_free, 256);
         mbar_init(&ds_full, 256);
         for (int i = 0; i < kQueries; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_ready[i], 1); mbar_init(&q_empty[i], 1); }
         for (int i = 0; i < kOuts; ++i) { mbar_init(&do_full[i], 1); mbar_init(&do_ready[i], 1); mbar_init(&do_empty[i], 1); mbar_init(&stat_full[i], 32); }
@@ -822,7 +846,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const unsigned tmem = uniform(s_tmem), DP = tmem + 128, DV = tmem + 256, DK = tmem + 384;     // scores at 0
+    const unsigned tmem = uniform(s_tmem), DP = tmem + 128, DV = tmem + 256, DK = DV + 16 * kSteps;     // scores at 0
+    const unsigned P = kApart ? tmem + 448 : tmem;                       // a half of 64 columns as pairs in 32
+    constexpr int kHalf = kApart ? 32 : 64;
 
     auto head_of = [&](int i) { return kv_head * a.share + i / each; };
     auto row_of = [&](int i) { return t.begin + (lo + i % each) * kTile; };
@@ -865,14 +891,20 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
         for (int i = 0; ok && i < n; ++i) {
             const unsigned tile_do = s_do + i % kOuts * kTileBytes, tile_q = s_q + i % kQueries * kTileBytes;
             const bool more = i + 1 < n;
-            ok = (!more || queries(i + 1)) && wait.together(&p_full, i & 1);
+            ok = !more || queries(i + 1);
+            if (kApart && more) {
+                ok = ok && wait.together(&s_free, i & 1);
+                tmem_fence_after();
+                if (ok && elect()) scores(i + 1);
+            }
+            ok = ok && wait.together(&p_full, i & 1);
             if (!ok) break;
             tmem_fence_after();
             if (elect()) {
-                product_columns<kSteps>(DV, tmem, tile_do, 0, i > 0);
-                product_columns<kSteps>(DV, tmem + 64, tile_do, 1, true);
+                product_columns<kSteps>(DV, P, tile_do, 0, i > 0);
+                product_columns<kSteps>(DV, P + kHalf, tile_do, 1, true);
                 products_done(&do_empty[i % kOuts]);
-                if (more) scores(i + 1);
+                if (!kApart && more) scores(i + 1);
             }
             ok = (!more || outs(i + 1)) && wait.together(&ds_full, i & 1);
             if (!ok) break;
@@ -940,6 +972,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
             for (int c = 0; c < 2; ++c) tmem_load32(tmem + lanes + 64 * half + 32 * c, p[c]);
 #pragma unroll
             for (int c = 0; c < 2; ++c) tmem_loaded(p[c]);
+            if (kApart) {
+                tmem_fence_before();
+                mbar_arrive(&s_free);
+            }
             const float4 *lse2 = reinterpret_cast<const float4 *>(&s_stat[i & 1][0][64 * half]), *delta = reinterpret_cast<const float4 *>(&s_stat[i & 1][1][64 * half]);
             auto pair_of = [](const float4 *p, int k) { const float4 f = p[k / 2]; return k % 2 ? make_float2(f.z, f.w) : make_float2(f.x, f.y); };
 #pragma unroll
@@ -950,8 +986,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
 #pragma unroll
                     for (int k = 0; k < 32; ++k)
                         if (c * 32 + k < from || c * 32 + k >= to) p[c][k] = 0.f;
+            if (kApart && i > 0) {                                       // the products with the probabilities before are done
+                ok = wait.together(&do_empty[(i - 1) % kOuts], ((i - 1) / kOuts) & 1);
+                if (!ok) break;
+                tmem_fence_after();
+            }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) put_pairs(tmem + lanes + 64 * half + 16 * c, p[c]);
+            for (int c = 0; c < 2; ++c) put_pairs(P + lanes + kHalf * half + 16 * c, p[c]);
             tmem_stored();
             tmem_fence_before();
             mbar_arrive(&p_full);
