@@ -446,8 +446,8 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
  * dS_ij = P_ij (grad_out_i . v_j - D_i):
  *   grad_q_i = scale sum_j dS_ij k_j;   grad_k_j = scale sum_i dS_ij q_i;   grad_v_j = sum_i P_ij grad_out_i
  * the last two over the query heads that share the key head as well.  All three are written whole (zeros for rows of no
- * sequence).  P and dS are rounded to bf16 for their products, sums run in fp32 in an order that the batch fixes, results
- * are rounded at the end.  Arguments as above; grad_out and out as q, grad_q as q, grad_k and grad_v as k; gradients may be heads
+ * sequence).  P and dS are rounded to bf16 for their products, sums run in fp32 in an order that the batch fixes (few key heads of
+ * few tokens: the heads that share one in parts, joined in order), results are rounded at the end.  Arguments as above; grad_out and out as q, grad_q as q, grad_k and grad_v as k; gradients may be heads
  * of the same rows (as those of one product are) but must not overlap each other or an input.
  * ws: dppf_attention_workspace_bytes(T, heads) bytes, 128-byte aligned, no initialisation.
  */

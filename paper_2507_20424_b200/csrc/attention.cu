@@ -80,6 +80,15 @@ int launch_attention(const AttentionArgs &a, long long blocks, int dev, cudaStre
     return launched();
 }
 
+// Parts that the heads of a key head are dealt out to: where tiles of keys are fewer than the SMs (148, whatever the device: the workspace
+// is laid out by this, and its size is asked for without one), as many as give each SM one, and no more than there are heads.
+int grad_splits(int64_t T, int kv_heads, int share) {
+    const int64_t tiles = (T + kTile - 1) / kTile * kv_heads, want = (148 + tiles - 1) / tiles;
+    return (int)(tiles >= 148 ? 1 : want < share ? want : share);
+}
+// Rows of parts at most: of splits kv_heads T, with splits kv_heads <= heads, and splits tiles < 148 + tiles where there are parts at all.
+int64_t grad_part_rows(int64_t T, int heads) { return T * heads < 2 * 148 * kTile ? T * heads : 2 * 148 * kTile; }
+
 std::atomic<int> g_query_ready[3][kMaxDevices], g_key_ready[3][kMaxDevices];
 
 template <int kSteps>
@@ -89,6 +98,10 @@ int launch_attention_grad(const AttentionGradArgs &a, long long query_blocks, lo
         return DPPF_ERR_CUDA;
     attention_grad_query_kernel<kSteps><<<(unsigned)query_blocks, kGradThreads, kQuerySmem, s>>>(a);
     if (cudaPeekAtLastError() == cudaSuccess) attention_grad_key_kernel<kSteps><<<(unsigned)key_blocks, kGradThreads, kKeySmem, s>>>(a);
+    if (a.splits > 1 && cudaPeekAtLastError() == cudaSuccess) {
+        const long long pieces = a.kv_heads * a.T * (a.D / 8);
+        attention_grad_join_kernel<<<dim3((unsigned)((pieces + kJoinThreads - 1) / kJoinThreads), 2), kJoinThreads, 0, s>>>(a);
+    }
     return launched();
 }
 
@@ -162,7 +175,8 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
 }
 
 size_t dppf_attention_workspace_bytes(int64_t T, int heads) {
-    return T >= 1 && T <= DPPF_MAX_ATTENTION_TOKENS && heads >= 1 && heads <= DPPF_MAX_HEADS ? round256((size_t)T * (size_t)heads * sizeof(float)) : 0;
+    return T >= 1 && T <= DPPF_MAX_ATTENTION_TOKENS && heads >= 1 && heads <= DPPF_MAX_HEADS 
+               ? round256((size_t)T * (size_t)heads * sizeof(float)) + (size_t)grad_part_rows(T, heads) * 2 * DPPF_MAX_ATTENTION_WIDTH * sizeof(float) : 0;
 }
 
 int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_grad_out, const void *q, int64_t ld_q, int64_t head_q, const void *k, int64_t ld_k,
@@ -211,6 +225,8 @@ int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_
     a.query_tiles = reinterpret_cast<const PlanTile *>(base + l.list[kByQuery]);
     a.key_tiles = reinterpret_cast<const PlanTile *>(base + l.list[kByKey]);
     a.lse = lse; a.delta = static_cast<float *>(ws);
+    a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(ws) + round256((size_t)T * (size_t)heads * sizeof(float)));
+    a.splits = grad_splits(T, kv_heads, heads / kv_heads);
     a.dq = static_cast<bf16 *>(grad_q); a.dk = static_cast<bf16 *>(grad_k); a.dv = static_cast<bf16 *>(grad_v);
     a.ld_dq = ld_grad_q; a.head_dq = head_grad_q; a.ld_dk = ld_grad_k; a.head_dk = head_grad_k; a.ld_dv = ld_grad_v; a.head_dv = head_grad_v;
     a.T = T; a.heads = heads; a.kv_heads = kv_heads; a.share = heads / kv_heads; a.D = D;
@@ -218,7 +234,7 @@ int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_
     a.scale = scale;
     a.scale2 = (float)((double)scale * 1.4426950408889634);
     a.spin = dppf_internal::first_pass_polls();
-    const long long query_blocks = (long long)heads * l.most[kByQuery], key_blocks = (long long)kv_heads * l.most[kByKey];
+    const long long query_blocks = (long long)heads * l.most[kByQuery], key_blocks = (long long)kv_heads * a.splits * l.most[kByKey];
     if (query_blocks > INT_MAX) return DPPF_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     if (D <= 64) return launch_attention_grad<4>(a, query_blocks, key_blocks, dev, s);

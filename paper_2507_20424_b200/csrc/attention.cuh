@@ -512,7 +512,8 @@ struct AttentionGradArgs {
     float *delta;                // [heads][T]
     bf16 *dq, *dk, *dv;
     long long ld_dq, head_dq, ld_dk, head_dk, ld_dv, head_dv, T;
-    int heads, kv_heads, share, D;
+    float *part;                 // [splits][2][kv_heads][T][D]: dv and dk (without scale) of a part of the heads that share a key head
+    int heads, kv_heads, share, splits, D;
     int causal, window;
     float scale, scale2;
     int spin;
@@ -814,12 +815,18 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
-    const int kv_head = (int)(blockIdx.x % a.kv_heads);
-    const unsigned index = blockIdx.x / a.kv_heads;
+    const int unit = (int)(blockIdx.x % (a.kv_heads * a.splits)), kv_head = unit / a.splits, split = unit % a.splits;
+    const unsigned index = blockIdx.x / (a.kv_heads * a.splits);
     if (tid < 4) prefetch_map(tid == 0 ? &a.k : tid == 1 ? &a.q : tid == 2 ? &a.v : &a.grad_out);
     if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T || index >= (unsigned)a.hdr->tiles[kByKey]) return;      // the status is the first kernel's
     const PlanTile t = uniform(a.key_tiles[index]);
+    auto part_row = [&](int which, int row) { return a.part + (((long long)(split * 2 + which) * a.kv_heads + kv_head) * a.T + row) * a.D; };
     if (t.begin == t.end) {
+        if (a.splits > 1) {
+            for (int which = 0; which < 2; ++which)
+                for (int i = tid; i < t.rows * a.D; i += kGradThreads) part_row(which, t.row)[i] = 0.f;
+            return;
+        }
         fill_rows(a.dk + (long long)t.row * a.ld_dk + kv_head * a.head_dk, a.ld_dk, t.rows, a.D, 0.f, tid, kGradThreads);
         fill_rows(a.dv + (long long)t.row * a.ld_dv + kv_head * a.head_dv, a.ld_dv, t.rows, a.D, 0.f, tid, kGradThreads);
         return;
@@ -827,7 +834,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     // blocks of queries [lo, hi) that see any of these keys, of each head in turn
     const int lo = a.causal ? (t.row - t.begin) / kTile : 0;
     const int hi = ((a.window ? (int)min((long long)t.end, (long long)t.row + t.rows - 1 + a.window) : t.end) - t.begin + kTile - 1) / kTile;
-    const int each = hi - lo, n = each * a.share;
+    const int head0 = kv_head * a.share + split * a.share / a.splits, heads = kv_head * a.share + (split + 1) * a.share / a.splits - head0;
+    const int each = hi - lo, n = each * heads;
     const unsigned s_k = smem_addr(smem_raw), s_v = s_k + kTileBytes, s_q = s_v + kTileBytes, s_do = s_q + kQueries * kTileBytes;
     float (*s_stat)[2][kTile] = reinterpret_cast<float (*)[2][kTile]>(smem_raw + Shape::kTiles);      // lse in powers of two, and D, of a tile of queries
     const Waits wait{&s_dead, a.spin};
@@ -850,7 +858,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     const unsigned P = kApart ? tmem + 448 : tmem;                       // a half of 64 columns as pairs in 32
     constexpr int kHalf = kApart ? 32 : 64;
 
-    auto head_of = [&](int i) { return kv_head * a.share + i / each; };
+    auto head_of = [&](int i) { return head0 + i / each; };
     auto row_of = [&](int i) { return t.begin + (lo + i % each) * kTile; };
     if (warp == 8) {
         // ---- copies
@@ -1021,7 +1029,20 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
         tmem_fence_after();
         const long long ld = half ? a.ld_dk : a.ld_dv;
         bf16 *to = (half ? a.dk + kv_head * a.head_dk : a.dv + kv_head * a.head_dv) + t.row * ld;
-        if (ok) {
+        if (a.splits > 1) {
+            float *part = part_row(half, key);
+            for (int c = 0; c < 2 * kBlocks; ++c) {
+                float o[32];
+                if (ok) {
+                    tmem_load32((half ? DK : DV) + lanes + c * 32, o);
+                    tmem_loaded(o);
+                }
+                if (r < t.rows)
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        if (c * 32 + i < a.D) *reinterpret_cast<float4 *>(part + c * 32 + i) = ok ? make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]) : make_float4(NAN, NAN, NAN, NAN);
+            }
+        } else if (ok) {
             const unsigned tile = half ? s_k : s_v;                      // all products are done
 #pragma unroll
             for (int c = 0; c < 2 * kBlocks; ++c) {
@@ -1040,6 +1061,30 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     tmem_fence_after();
     if (warp == 9) tmem_free(tmem, kColumns);
     if (tid == 0 && s_dead) a.hdr->status = DPPF_ERR_TIMEOUT;
+}
+
+// The parts of dk and dv, added in order, eight columns of a row a thread.  blockIdx.y: 0 dv, 1 dk.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads) attention_grad_join_kernel(const __grid_constant__ AttentionGradArgs a) {
+    const int pieces = a.D / 8, which = blockIdx.y;
+    const long long rows = a.kv_heads * a.T, i = (long long)blockIdx.x * kJoinThreads + threadIdx.x;
+    if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T || i >= rows * pieces) return;
+    const long long at = i / pieces, kv_head = at / a.T, row = at - kv_head * a.T;
+    const int piece = (int)(i - at * pieces);
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float4 *p = reinterpret_cast<const float4 *>(a.part + ((s * 2 + which) * rows + at) * a.D + piece * 8);
+        const float4 x = __ldcs(p), y = __ldcs(p + 1);
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+        v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+    }
+    const float by = which ? a.scale : 1.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= by;
+    bf16 *to = which ? a.dk + row * a.ld_dk + kv_head * a.head_dk : a.dv + row * a.ld_dv + kv_head * a.head_dv;
+    store_vec<bf16, 8>(to + piece * 8, v);
 }
 
 }  // namespace

@@ -348,8 +348,11 @@ def test_far_rows(b):
     f, g = b.dppf_attention(q, k, v, far), b.dppf_attention(q[-n:], k[-n:], v[-n:], near)
     assert same_bits(f.out[-n:], g.out) and same_bits(f.lse[:, -n:], g.lse) and not f.out[:-n].any()
     df = b.dppf_attention_grad(q, q, k, v, f.out, f.lse, far)
-    dg = b.dppf_attention_grad(q[-n:], q[-n:], k[-n:], v[-n:], g.out, g.lse, near)
-    assert all(same_bits(x[-n:], y) and not x[:-n].any() for x, y in zip(df, dg))
+    # the heads that share a key head may be summed in other parts where there are few rows: against the formulas
+    want = reference(q[-n:], k[-n:], v[-n:], starts_of([n]), True, 0, D ** -0.5, (q[-n:], g.out, g.lse))
+    for name, x in zip("qkv", df):
+        within(x[-n:], *want[name], name)
+        assert not x[:-n].any()
 
 
 def test_streams_graphs_and_a_shared_plan(b):
