@@ -76,7 +76,9 @@ template <int kSteps>
 int launch_attention(const AttentionArgs &a, long long blocks, int dev, cudaStream_t s) {
     constexpr int kSmem = (int)ForwardShape<kSteps>::kSmem;
     if (!allow_smem(attention_kernel<kSteps>, dev, g_forward_ready[kSteps / 2 - 2], kSmem)) return DPPF_ERR_CUDA;
-    attention_kernel<kSteps><<<(unsigned)blocks, kForwardThreads, kSmem, s>>>(a);
+    const int sms = multiprocessors(dev);
+    if (sms < 0) return DPPF_ERR_CUDA;
+    attention_kernel<kSteps><<<(unsigned)(blocks < sms ? blocks : sms), kForwardThreads, kSmem, s>>>(a);
     return launched();
 }
 

@@ -167,7 +167,7 @@ struct ForwardShape {
     static constexpr unsigned kTileBytes = kBlocks * kBlockBytes;
     static constexpr int kStages = kBlocks == 2 ? 2 : 4;                 // of a tile of keys and one of values
     static constexpr int kPolynomial = kBlocks == 2 ? 8 : 4;             // one in so many exponentials is a polynomial
-    static constexpr unsigned kSmem = (2 + 2 * kStages) * kTileBytes + 1024;
+    static constexpr unsigned kSmem = (2 + 2 * kStages) * kTileBytes + 2 * kBlockBytes + 1024;      // and half a tile of results a slot
 };
 
 // 32 columns of a row, from column 32 part on, times `by` as bf16 into a tile that no product or copy needs any more.
@@ -237,6 +237,51 @@ __device__ __forceinline__ void spoil_row(bf16 *row, int D) {
 // One pass over the keys with a running maximum and sum.  A block has two slots of 128 queries that share their keys and values:
 // while one slot's warpgroup takes the exponentials of its scores (a row a thread), the tensor cores work for the other.
 // Scores and output sums stay in tensor memory; the probabilities replace the scores there as bf16, the first operand of the second product.
+// A block stays for several tiles: the next one's copies and first products run while this one's results are written.  Tiles come
+// sorted by work; a round of them is dealt out forwards, the next backwards, so that every block gets about the same.
+
+struct ForwardItem {             // a tile of queries, two slots: rows [row, row + rows) of a head, key blocks [lo, hi) counted from the sequence's begin
+    PlanTile t;
+    int head0, kv_head, lo[2], hi[2], first, last, slots;
+    bool by_head;
+    __device__ __forceinline__ ForwardItem(const AttentionArgs &a, const PlanTile &tile, int unit) : t(tile), by_head(a.by_head) {
+        head0 = by_head ? 2 * unit : unit;
+        kv_head = head0 / a.share;
+        slots = by_head || t.rows > kTile ? 2 : 1;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            lo[s] = a.window ? max(0, row(s) - a.window + 1 - t.begin) / kTile : 0;
+            hi[s] = ((a.causal ? min(t.end, row(s) + kTile) : t.end) - t.begin + kTile - 1) / kTile;
+        }
+        first = slots == 2 ? min(lo[0], lo[1]) : lo[0];
+        last = slots == 2 ? max(hi[0], hi[1]) : hi[0];
+    }
+    __device__ __forceinline__ bool idle() const { return t.begin == t.end; }                                  // rows of no sequence
+    __device__ __forceinline__ int row(int s) const { return by_head ? t.row : t.row + s * kTile; }
+    __device__ __forceinline__ int rows(int s) const { return by_head ? t.rows : min(kTile, t.rows - s * kTile); }
+    __device__ __forceinline__ int head(int s) const { return by_head ? head0 + s : head0; }
+    __device__ __forceinline__ int key0(int j) const { return t.begin + j * kTile; }
+};
+
+// The items of this block, in order; the plan is read an item ahead.
+struct ForwardItems {
+    const PlanTile *tiles;
+    unsigned total, units, round, at;
+    PlanTile ahead;
+    __device__ __forceinline__ unsigned index(unsigned r) const { return r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+    __device__ __forceinline__ explicit ForwardItems(const AttentionArgs &a) : tiles(a.tiles), total(uniform((unsigned)a.hdr->tiles[a.list]) * (unsigned)a.units), units(a.units), round(0), at(index(0)) {
+        if (at < total) ahead = tiles[at / units];
+    }
+    __device__ __forceinline__ bool there() const { return at < total; }
+    __device__ __forceinline__ ForwardItem take(const AttentionArgs &a) {
+        const PlanTile t = uniform(ahead);
+        const int unit = (int)(at % units);
+        at = index(++round);
+        if (at < total) ahead = tiles[at / units];
+        return ForwardItem(a, t, unit);
+    }
+};
+
 template <int kSteps>
 __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __grid_constant__ AttentionArgs a) {
     using Shape = ForwardShape<kSteps>;
@@ -245,47 +290,24 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     constexpr unsigned kTileBytes = Shape::kTileBytes;
     constexpr int kColumns = 512;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ unsigned long long q_full[2], k_full[kStages], v_full[kStages], empty[kStages], v_fixed, s_full[2], p_half[2], p_full[2], o_full[2], drained;
+    __shared__ unsigned long long q_full[2], q_free[2], k_full[kStages], v_full[kStages], v_ready[kStages], empty[kStages], s_full[2], p_half[2], p_full[2], o_full[2], o_free[2], drained;
     __shared__ unsigned s_tmem;
     __shared__ volatile int s_dead;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
-    const unsigned unit = blockIdx.x % a.units, index = blockIdx.x / a.units;
     if (tid < 3) prefetch_map(tid == 0 ? &a.q : tid == 1 ? &a.k : &a.v);
     if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T) {                 // not a plan of these rows
         if (blockIdx.x == 0 && tid == 0) a.hdr->status = DPPF_ERR_WORKSPACE;
         return;
     }
-    if (index >= (unsigned)a.hdr->tiles[a.list]) return;
-    const PlanTile t = uniform(a.tiles[index]);
-    // slots: query rows [row, row + rows) of a head
-    const int head0 = a.by_head ? 2 * unit : unit, kv_head = head0 / a.share;
-    auto slot_row = [&](int s) { return a.by_head ? t.row : t.row + s * kTile; };
-    auto slot_rows = [&](int s) { return a.by_head ? t.rows : min(kTile, t.rows - s * kTile); };
-    auto slot_head = [&](int s) { return a.by_head ? head0 + s : head0; };
-    if (t.begin == t.end) {                                              // rows of no sequence
-        for (int s = 0; s < (a.by_head ? 2 : 1); ++s) {
-            fill_rows(a.out + (long long)t.row * a.ld_out + (head0 + s) * a.head_out, a.ld_out, t.rows, a.D, 0.f, tid, kForwardThreads);
-            for (int i = tid; i < t.rows; i += kForwardThreads) a.lse[(head0 + s) * a.T + t.row + i] = -INFINITY;
-        }
-        return;
-    }
-    // key blocks [lo, hi) of a slot, counted from the sequence's begin; the blocks that both need come in once
-    auto block_lo = [&](int s) { return a.window ? max(0, slot_row(s) - a.window + 1 - t.begin) / kTile : 0; };
-    auto block_hi = [&](int s) { return slot_rows(s) <= 0 ? 0 : ((a.causal ? min(t.end, slot_row(s) + kTile) : t.end) - t.begin + kTile - 1) / kTile; };
-    const int lo0 = block_lo(0), hi0 = block_hi(0), hi1 = block_hi(1), lo1 = hi1 ? block_lo(1) : 0;
-    const int lo = hi1 ? min(lo0, lo1) : lo0, hi = max(hi0, hi1);
-    const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_q = smem, s_kv = smem + 2 * kTileBytes;
+    const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_q = smem, s_kv = smem + 2 * kTileBytes, s_out = s_kv + 2 * kStages * kTileBytes;
     const Waits wait{&s_dead, a.spin};
-
-    const int slots = hi1 ? 2 : 1;
     if (tid == 0) {
         for (int s = 0; s < 2; ++s) {
-            for (unsigned long long *bar : {&q_full[s], &s_full[s], &o_full[s]}) mbar_init(bar, 1);
-            mbar_init(&p_half[s], 128);
-            mbar_init(&p_full[s], 128);
+            for (unsigned long long *bar : {&q_full[s], &q_free[s], &s_full[s], &o_full[s]}) mbar_init(bar, 1);
+            for (unsigned long long *bar : {&p_half[s], &p_full[s], &o_free[s]}) mbar_init(bar, 128);
         }
-        for (int i = 0; i < kStages; ++i) { mbar_init(&k_full[i], 1); mbar_init(&v_full[i], 1); mbar_init(&empty[i], 1); }
-        mbar_init(&v_fixed, 1);
+        for (int i = 0; i < kStages; ++i)
+            for (unsigned long long *bar : {&k_full[i], &v_full[i], &v_ready[i], &empty[i]}) mbar_init(bar, 1);
         mbar_init(&drained, 1);
         s_dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -294,201 +316,251 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const unsigned tmem = uniform(s_tmem);                                        // scores of slot s at 128 s, its output at 256 + 128 s
+    const unsigned tmem = uniform(s_tmem);                               // scores of slot s at 128 s, its output at 256 + 128 s
 
+    // Phases are counted on from item to item: q_full, q_free, o_full, o_free by the slot's items, s_full, p_half, p_full by its tiles of keys,
+    // the stages by all tiles of keys.
     if (warp >= 8) {
         give_registers<kControlRegisters>();
-        const int last = hi - 1, there = t.end - (t.begin + last * kTile);       // rows of the last tile that are the sequence's
         if (warp == 8) {
             // ---- copies
-            int issued = 0;                                              // key tiles; the same or one less of values
+            unsigned pairs = 0, items[2] = {0, 0};
             bool ok = true;
-            if (elect()) {
-                for (int s = 0; s < slots; ++s) {
-                    mbar_expect_tx(&q_full[s], kTileBytes);
-                    tile_load<kBlocks>(s_q + s * kTileBytes, &a.q, slot_head(s), slot_row(s), &q_full[s]);
-                    if (s == 0) {
-                        mbar_expect_tx(&k_full[0], kTileBytes);
-                        tile_load<kBlocks>(s_kv, &a.k, kv_head, t.begin + lo * kTile, &k_full[0]);
-                    }
-                }
-                for (int j = lo; j < hi; ++j, ++issued) {
-                    const int st = issued % kStages, row = t.begin + j * kTile;
-                    if (issued >= kStages && !(ok = wait(&empty[st], (issued / kStages - 1) & 1))) break;
-                    if (issued) {
+            for (ForwardItems all(a); ok && all.there();) {
+                const ForwardItem it = all.take(a);
+                if (it.idle()) continue;
+                if (elect()) {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+                        if (ok && s < it.slots) ok = items[s] == 0 || wait(&q_free[s], (items[s] - 1) & 1);
+                    for (int j = it.first; ok && j < it.last; ++j) {
+                        const unsigned st = pairs % kStages;
+                        ok = pairs < kStages || wait(&empty[st], (pairs / kStages - 1) & 1);
+                        if (!ok) break;
+                        auto query = [&](int s) {
+                            mbar_expect_tx(&q_full[s], kTileBytes);
+                            tile_load<kBlocks>(s_q + s * kTileBytes, &a.q, it.head(s), it.row(s), &q_full[s]);
+                            ++items[s];
+                        };
+                        if (j == it.first) query(0);
                         mbar_expect_tx(&k_full[st], kTileBytes);
-                        tile_load<kBlocks>(s_kv + 2 * st * kTileBytes, &a.k, kv_head, row, &k_full[st]);
+                        tile_load<kBlocks>(s_kv + 2 * st * kTileBytes, &a.k, it.kv_head, it.key0(j), &k_full[st]);
+                        if (j == it.first && it.slots == 2) query(1);
+                        mbar_expect_tx(&v_full[st], kTileBytes);
+                        tile_load<kBlocks>(s_kv + (2 * st + 1) * kTileBytes, &a.v, it.kv_head, it.key0(j), &v_full[st]);
+                        ++pairs;
                     }
-                    mbar_expect_tx(&v_full[st], kTileBytes);
-                    tile_load<kBlocks>(s_kv + (2 * st + 1) * kTileBytes, &a.v, kv_head, row, &v_full[st]);
                 }
+                ok = __all_sync(0xffffffffu, ok);
             }
-            issued = __reduce_max_sync(0xffffffffu, issued);             // the elected lane's
-            if (there < kTile && issued == hi - lo) {                    // values of other sequences must not reach a sum
-                const int st = (issued - 1) % kStages;
-                if (wait.together(&v_full[st], ((issued - 1) / kStages) & 1)) zero_rows<kBlocks>(s_kv + (2 * st + 1) * kTileBytes, there);
-                if (lane == 0) mbar_arrive(&v_fixed);
-            }
-            if (lane == 0) {                                             // the copies in flight land before the block leaves
-                for (int s = 0; s < slots; ++s) mbar_wait_bounded(&q_full[s], 0, kSpinLimit);
-                if (issued == 0) mbar_wait_bounded(&k_full[0], 0, kSpinLimit);
-                for (int i = max(0, issued - kStages); i < issued; ++i) {
+            if (elect()) {                                               // the copies in flight land before the block leaves
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+                    if (items[s]) mbar_wait_bounded(&q_full[s], (items[s] - 1) & 1, kSpinLimit);
+                for (unsigned i = pairs > kStages ? pairs - kStages : 0; i < pairs; ++i) {
                     mbar_wait_bounded(&k_full[i % kStages], (i / kStages) & 1, kSpinLimit);
                     mbar_wait_bounded(&v_full[i % kStages], (i / kStages) & 1, kSpinLimit);
                 }
             }
         } else if (warp == 9) {
             // ---- products: of one slot the probabilities times the values of tile j, then the scores of tile j + 1; then of the other
-            bool ok = wait.together(&q_full[0], 0) && (slots == 1 || wait.together(&q_full[1], 0));
-            for (int j = lo - 1; ok && j < hi; ++j) {
-                const int n = j - lo, st = n % kStages, to = (n + 1) % kStages;
-                const unsigned tile = s_kv + (2 * st + 1) * kTileBytes;
-                ok = (n < 0 || (wait.together(&v_full[st], (n / kStages) & 1) && (j < last || there >= kTile || wait.together(&v_fixed, 0)))) &&
-                     (j + 1 >= hi || wait.together(&k_full[to], ((n + 1) / kStages) & 1));
-                for (int s = 0; ok && s < slots; ++s) {
-                    const int first = s ? lo1 : lo0, end = s ? hi1 : hi0, nth = j - first;
-                    const unsigned S = tmem + s * 128, O = tmem + 256 + s * 128;
-                    if (nth >= 0 && j < end) {
-                        ok = wait.together(&p_half[s], nth & 1);
-                        if (!ok) break;
-                        tmem_fence_after();
-                        if (elect()) product_columns<kSteps>(O, S, tile, 0, nth > 0);
-                        ok = wait.together(&p_full[s], nth & 1);
-                        if (!ok) break;
-                        tmem_fence_after();
-                        if (elect()) {
-                            product_columns<kSteps>(O, S + 32, tile, 1, true);
-                            if (j + 1 == end) products_done(&o_full[s]);
+            const bool leader = elect();
+            unsigned pairs = 0, item_phase = 0, tile_phase = 0, later = 0;          // bit s: of slot s; later: the slot had an item before
+            bool ok = true;
+            for (ForwardItems all(a); ok && all.there();) {
+                const ForwardItem it = all.take(a);
+                if (it.idle()) continue;
+                const int slots = it.slots, lo0 = it.lo[0], hi0 = it.hi[0], lo1 = it.lo[1], hi1 = it.hi[1], lo = it.first, hi = it.last;
+                ok = wait.together(&q_full[0], item_phase & 1) && (slots == 1 || wait.together(&q_full[1], item_phase >> 1 & 1));
+                for (int j = lo - 1; ok && j < hi; ++j) {
+                    const unsigned n = pairs + (unsigned)(j - lo), st = n % kStages, to = (n + 1) % kStages;     // n is used from j = lo on
+                    const unsigned tile = s_kv + (2 * st + 1) * kTileBytes;
+                    ok = (j < lo || wait.together(&v_ready[st], (n / kStages) & 1)) && (j + 1 >= hi || wait.together(&k_full[to], ((n + 1) / kStages) & 1));
+#pragma unroll 1
+                    for (int s = 0; ok && s < slots; ++s) {
+                        const int first = s ? lo1 : lo0, end = s ? hi1 : hi0;
+                        const unsigned S = tmem + s * 128, O = tmem + 256 + s * 128;
+                        if (j >= first && j < end) {
+                            ok = wait.together(&p_half[s], tile_phase >> s & 1) && (j > first || !(later >> s & 1) || wait.together(&o_free[s], (item_phase >> s & 1) ^ 1));
+                            if (!ok) break;
+                            tmem_fence_after();
+                            if (leader) product_columns<kSteps>(O, S, tile, 0, j > first);
+                            ok = wait.together(&p_full[s], tile_phase >> s & 1);
+                            if (!ok) break;
+                            tmem_fence_after();
+                            if (leader) {
+                                product_columns<kSteps>(O, S + 32, tile, 1, true);
+                                if (j + 1 == end) products_done(&o_full[s]);
+                            }
+                            tile_phase ^= 1u << s;
+                        }
+                        if (j >= lo && s + 1 == slots && leader) products_done(&empty[st]);
+                        if (j + 1 >= first && j + 1 < end && leader) {
+                            product_rows<kSteps>(S, s_q + s * kTileBytes, s_kv + 2 * to * kTileBytes);
+                            products_done(&s_full[s]);
+                            if (j + 2 == end) products_done(&q_free[s]);
                         }
                     }
-                    if (n >= 0 && s + 1 == slots && elect()) products_done(&empty[st]);
-                    if (nth >= -1 && j + 1 < end && elect()) {
-                        product_rows<kSteps>(S, s_q + s * kTileBytes, s_kv + 2 * to * kTileBytes);
-                        products_done(&s_full[s]);
-                    }
                 }
+                pairs += (unsigned)(hi - lo);
+                item_phase ^= slots == 2 ? 3u : 1u;
+                later |= slots == 2 ? 3u : 1u;
             }
-            if (elect()) {                                               // nothing is in flight when the block leaves
+            if (leader) {                                               // nothing is in flight when the block leaves
                 products_done(&drained);
                 mbar_wait_bounded(&drained, 0, kSpinLimit);
+            }
+        } else if (warp == 10) {
+            // ---- values as they arrive: rows of other sequences must not reach a sum.  Every tile passes here, so that the warp cannot be
+            // a phase behind.
+            unsigned pairs = 0;
+            bool ok = true;
+            for (ForwardItems all(a); ok && all.there();) {
+                const ForwardItem it = all.take(a);
+                if (it.idle()) continue;
+                for (int j = it.first; j < it.last; ++j, ++pairs) {
+                    const unsigned st = pairs % kStages;
+                    if (!(ok = wait.together(&v_full[st], (pairs / kStages) & 1))) break;
+                    const int there = it.t.end - it.key0(j);
+                    if (there < kTile) zero_rows<kBlocks>(s_kv + (2 * st + 1) * kTileBytes, there);
+                    if (lane == 0) mbar_arrive(&v_ready[st]);
+                }
             }
         }
     } else {
         // ---- softmax: a row a thread
         take_registers<kSoftmaxRegisters>();
-        const int s = warp >> 2, r = tid & 127, row = slot_row(s) + r;
-        const int first = s ? lo1 : lo0, last = s ? hi1 : hi0;
+        const int s = warp >> 2, r = tid & 127;
         const unsigned lanes = (unsigned)(warp & 3) << 21, S = tmem + lanes + s * 128, O = tmem + lanes + 256 + s * 128;
-        // keys [see_lo, see_hi) of this row
-        const int see_lo = a.window ? max(t.begin, row - a.window + 1) : t.begin, see_hi = a.causal ? min(t.end, row + 1) : t.end;
-        float top = -INFINITY, sum = 0.f;                                // of the scaled scores, in powers of two
+        unsigned items = 0, tiles = 0;
         bool ok = true;
-        for (int j = first; j < last; ++j) {
-            ok = wait.together(&s_full[s], (j - first) & 1);
-            if (!ok) break;
-            tmem_fence_after();
-            float v[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_load32(S + c * 32, v[c]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_loaded(v[c]);
-            const int key0 = t.begin + j * kTile;
-            // blocks that every row of the tile sees whole need no masks
-            const bool whole = (a.causal ? slot_row(s) + 1 : t.end) >= key0 + kTile && (!a.window || slot_row(s) + kTile - a.window <= key0) && key0 + kTile <= t.end;
-            if (!whole) {
-                const int from = see_lo - key0, to = see_hi - key0;
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c * 32 + i < from || c * 32 + i >= to) v[c][i] = -INFINITY;
-            }
-            unsigned p[2][16];
-            auto exponentials = [&](int c, float2 &sums, unsigned (&to)[16], float &high) {      // of 32 columns
-                const float2 by = both(a.scale2), off = both(top == -INFINITY ? 0.f : -top);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float2 e = fma2(make_float2(v[c][2 * i], v[c][2 * i + 1]), by, off);
-                    if (i % kPolynomial == 3) { high = max3(high, e.x, e.y); e = exp2_polynomial(e); }
-                    else { e.x = exp2_fast(e.x); e.y = exp2_fast(e.y); }
-                    sums = add2(sums, e);
-                    to[i] = bf16_pair(e.x, e.y);
+        for (ForwardItems all(a); all.there();) {
+            const ForwardItem it = all.take(a);
+            const PlanTile &t = it.t;
+            if (it.idle()) {
+                for (int h = 0; h < (it.by_head ? 2 : 1); ++h) {
+                    fill_rows(a.out + (long long)t.row * a.ld_out + (it.head0 + h) * a.head_out, a.ld_out, t.rows, a.D, 0.f, tid, 256);
+                    for (int i = tid; i < t.rows; i += 256) a.lse[(it.head0 + h) * a.T + t.row + i] = -INFINITY;
                 }
-            };
-            // The sums stay relative to the maximum of the first tile until an exponential would be above 2^60, which is rare: fp32 and
-            // bf16 keep their relative precision up to 2^127.  So no maximum is taken of what the first half's sum tells: it is at least
-            // the largest of them.  (A polynomial's argument above 128 would come out as any number: those are looked at.)
-            float2 sums = make_float2(0.f, 0.f);
-            float high = -INFINITY;                                      // of the second half, and of the first's polynomials
-            if (j > first) {
-                exponentials(0, sums, p[0], high);
-                exponentials(1, sums, p[1], high);
+                continue;
             }
-            float m[2] = {-INFINITY, -INFINITY};
+            if (s >= it.slots) continue;
+            const int slot_row = it.row(s), row = slot_row + r, first = s ? it.lo[1] : it.lo[0], last = s ? it.hi[1] : it.hi[0];
+            const bool mine = r < it.rows(s);
+            // keys [see_lo, see_hi) of this row
+            const int see_lo = a.window ? max(t.begin, row - a.window + 1) : t.begin, see_hi = a.causal ? min(t.end, row + 1) : t.end;
+            float top = -INFINITY, sum = 0.f;                            // of the scaled scores, in powers of two
+            for (int j = first; ok && j < last; ++j, ++tiles) {
+                ok = wait.together(&s_full[s], tiles & 1);
+                if (!ok) break;
+                tmem_fence_after();
+                float v[4][32];
 #pragma unroll
-            for (int i = 0; i < 32; i += 2)
+                for (int c = 0; c < 4; ++c) tmem_load32(S + c * 32, v[c]);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) m[c] = max3(m[c], v[c + 2][i], v[c + 2][i + 1]);
-            const float most = fmaxf(m[0], m[1]) * a.scale2;
-            const bool grow = top == -INFINITY || sums.x + sums.y > 0x1p60f || fmaxf(high, most - top) > 60.0f;
-            if (j == first || __any_sync(0xffffffffu, grow)) {
+                for (int c = 0; c < 4; ++c) tmem_loaded(v[c]);
+                const int key0 = it.key0(j);
+                // blocks that every row of the tile sees whole need no masks
+                const bool whole = (a.causal ? slot_row + 1 : t.end) >= key0 + kTile && (!a.window || slot_row + kTile - a.window <= key0) && key0 + kTile <= t.end;
+                if (!whole) {
+                    const int from = see_lo - key0, to = see_hi - key0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (c * 32 + i < from || c * 32 + i >= to) v[c][i] = -INFINITY;
+                }
+                unsigned p[2][16];
+                auto exponentials = [&](int c, float2 &sums, unsigned (&to)[16], float &high) {      // of 32 columns
+                    const float2 by = both(a.scale2), off = both(top == -INFINITY ? 0.f : -top);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float2 e = fma2(make_float2(v[c][2 * i], v[c][2 * i + 1]), by, off);
+                        if (i % kPolynomial == 3) { high = max3(high, e.x, e.y); e = exp2_polynomial(e); }
+                        else { e.x = exp2_fast(e.x); e.y = exp2_fast(e.y); }
+                        sums = add2(sums, e);
+                        to[i] = bf16_pair(e.x, e.y);
+                    }
+                };
+                // The sums stay relative to the maximum of the first tile until an exponential would be above 2^60, which is rare: fp32 and
+                // bf16 keep their relative precision up to 2^127.  So no maximum is taken of what the first half's sum tells: it is at least
+                // the largest of them.  (A polynomial's argument above 128 would come out as any number: those are looked at.)
+                float2 sums = make_float2(0.f, 0.f);
+                float high = -INFINITY;                                      // of the second half, and of the first's polynomials
+                if (j > first) {
+                    exponentials(0, sums, p[0], high);
+                    exponentials(1, sums, p[1], high);
+                }
+                float m[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                 for (int i = 0; i < 32; i += 2)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) m[c] = max3(m[c], v[c][i], v[c][i + 1]);
-                // a row that does not ask for it keeps its own: no row's bits depend on another's
-                const float now = j == first || grow ? fmaxf(m[0], m[1]) * a.scale2 : -INFINITY;
-                if (j > first) {
-                    const float f = now > top ? exp2_fast(top - now) : 1.0f;
-                    sum *= f;
-                    for (int c = 0; c < 4 * kBlocks; ++c) {
-                        float o[16];
-                        unsigned u[16];
-                        tmem_load16(O + c * 16, o);
+                    for (int c = 0; c < 2; ++c) m[c] = max3(m[c], v[c + 2][i], v[c + 2][i + 1]);
+                const float most = fmaxf(m[0], m[1]) * a.scale2;
+                const bool grow = top == -INFINITY || sums.x + sums.y > 0x1p60f || fmaxf(high, most - top) > 60.0f;
+                if (j == first || __any_sync(0xffffffffu, grow)) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(o[i] * f);
-                        tmem_store16(O + c * 16, u);
+                    for (int i = 0; i < 32; i += 2)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) m[c] = max3(m[c], v[c][i], v[c][i + 1]);
+                    // a row that does not ask for it keeps its own: no row's bits depend on another's
+                    const float now = j == first || grow ? fmaxf(m[0], m[1]) * a.scale2 : -INFINITY;
+                    if (j > first) {
+                        const float f = now > top ? exp2_fast(top - now) : 1.0f;
+                        sum *= f;
+                        for (int c = 0; c < 4 * kBlocks; ++c) {
+                            float o[16];
+                            unsigned u[16];
+                            tmem_load16(O + c * 16, o);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(o[i] * f);
+                            tmem_store16(O + c * 16, u);
+                        }
                     }
+                    top = fmaxf(top, now);
+                    sums = make_float2(0.f, 0.f);
+                    exponentials(0, sums, p[0], high);
+                    exponentials(1, sums, p[1], high);
                 }
-                top = fmaxf(top, now);
-                sums = make_float2(0.f, 0.f);
-                exponentials(0, sums, p[0], high);
-                exponentials(1, sums, p[1], high);
+                tmem_store16(S, p[0]);
+                tmem_store16(S + 16, p[1]);
+                tmem_stored();
+                tmem_fence_before();
+                mbar_arrive(&p_half[s]);
+                exponentials(2, sums, p[0], high);
+                tmem_store16(S + 32, p[0]);
+                exponentials(3, sums, p[1], high);
+                tmem_store16(S + 48, p[1]);
+                sum += sums.x + sums.y;
+                tmem_stored();
+                tmem_fence_before();
+                mbar_arrive(&p_full[s]);
             }
-            tmem_store16(S, p[0]);
-            tmem_store16(S + 16, p[1]);
-            tmem_stored();
-            tmem_fence_before();
-            mbar_arrive(&p_half[s]);
-            exponentials(2, sums, p[0], high);
-            tmem_store16(S + 32, p[0]);
-            exponentials(3, sums, p[1], high);
-            tmem_store16(S + 48, p[1]);
-            sum += sums.x + sums.y;
-            tmem_stored();
-            tmem_fence_before();
-            mbar_arrive(&p_full[s]);
-        }
-        if (last > first) {
-            ok = ok && wait.together(&o_full[s], 0);
+            ok = ok && wait.together(&o_full[s], items & 1);
+            ++items;
             tmem_fence_after();
-            const bool mine = r < slot_rows(s);
-            const float by = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
-            bf16 *out = a.out + (long long)slot_row(s) * a.ld_out + slot_head(s) * a.head_out;
-            if (ok) {
-                const unsigned tile = s_q + s * kTileBytes;              // the queries': their products are done
-#pragma unroll
-                for (int c = 0; c < 2 * kBlocks; ++c) {
-                    float o[32];
-                    tmem_load32(O + c * 32, o);
-                    tmem_loaded(o);
-                    put_row(tile, r, c, o, by);
-                }
-                store_rows<8 * kBlocks>(tile, r & ~31, 0, out, a.ld_out, slot_rows(s), a.D);
-            } else if (mine) {
-                spoil_row(out + r * a.ld_out, a.D);
+            bf16 *out = a.out + (long long)slot_row * a.ld_out + it.head(s) * a.head_out;
+            if (mine) a.lse[it.head(s) * a.T + row] = ok ? (top + log2f(sum)) * kLn2 : __int_as_float(0x7fc00000);
+            if (!ok) {                                                   // this item's rows and those of all that follow
+                if (mine) spoil_row(out + r * a.ld_out, a.D);
+                continue;
             }
-            if (mine) a.lse[slot_head(s) * a.T + row] = ok ? (top + log2f(sum)) * kLn2 : __int_as_float(0x7fc00000);
+            const float by = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+            float o[2 * kBlocks][32];
+#pragma unroll
+            for (int c = 0; c < 2 * kBlocks; ++c) tmem_load32(O + c * 32, o[c]);
+#pragma unroll
+            for (int c = 0; c < 2 * kBlocks; ++c) tmem_loaded(o[c]);
+            tmem_fence_before();
+            mbar_arrive(&o_free[s]);
+            const unsigned tile = s_out + s * kBlockBytes;               // 64 columns at a time
+#pragma unroll
+            for (int c = 0; c < kBlocks; ++c) {
+                put_row(tile, r, 0, o[2 * c], by);
+                put_row(tile, r, 1, o[2 * c + 1], by);
+                store_rows<8>(tile, r & ~31, 0, out + 64 * c, a.ld_out, it.rows(s), a.D - 64 * c);
+                __syncwarp();
+            }
         }
         tmem_fence_before();
     }
