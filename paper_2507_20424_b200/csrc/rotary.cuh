@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kRotaryThreads = 256;
 constexpr int kRotaryMaxTokens = 16;          // of a block
-constexpr int kRotaryTable = 4096;            // cosines (and as many sines) that a block holds
+constexpr int kRotaryTable = 1024;            // cosines (and as many sines) that a block holds
 
 struct RotaryArgs {
     const void *x;
@@ -26,6 +26,22 @@ struct RotaryArgs {
     int positions64, inverse;
     float scale;
 };
+
+template <int N>
+__device__ __forceinline__ void table_load(const float *p, float (&f)[N]) {      // starts are multiples of N
+    if constexpr (N >= 4)
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(p + i);
+            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+        }
+    else if constexpr (N == 2) {
+        const float2 v = *reinterpret_cast<const float2 *>(p);
+        f[0] = v.x; f[1] = v.y;
+    } else {
+        f[0] = p[0];
+    }
+}
 
 template <typename T, int N, bool kInterleaved>
 __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_constant__ RotaryArgs a) {
@@ -55,7 +71,9 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
             store_vec<T, N>(out + at, v);
             continue;
         }
-        const float *cs = s_cos + t * a.half + g * N, *sn = s_sin + t * a.half + g * N;
+        float cs[N], sn[N];
+        table_load(s_cos + t * a.half + g * N, cs);
+        table_load(s_sin + t * a.half + g * N, sn);
         if constexpr (kInterleaved) {
             float v[2 * N];
             if constexpr (N == 1) { v[0] = to_float(x[2 * g]); v[1] = to_float(x[2 * g + 1]); }   // a pair may lie across its boundary
