@@ -66,7 +66,7 @@ struct AttentionShape {
     float scale;
     bool fine() const {
         return plan_shape(T, B) && heads >= 1 && heads <= DPPF_MAX_HEADS && kv_heads >= 1 && heads % kv_heads == 0 && D >= 8 && D <= DPPF_MAX_ATTENTION_WIDTH && D % 8 == 0 &&
-               (causal == 0 || causal == 1) && window >= 0 && (window == 0 || causal) && std::isfinite(scale) && scale > 0.f;
+               (causal == 0 || causal == 1) && window >= 0 && (window == 0 || causal) && std::isfinite((float)((double)scale * 1.4426950408889634)) && scale > 0.f;
     }
 };
 
@@ -164,8 +164,8 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
     a.out = static_cast<bf16 *>(out);
     a.lse = lse_out;
     a.ld_out = ld_out; a.head_out = head_out; a.T = T;
-    a.heads = heads; a.D = D;
-    a.causal = causal; a.window = window;
+    a.heads = heads; a.D = D; a.B = (int)B;
+    a.causal = causal; a.window = window < T ? window : 0;
     a.scale = scale;
     a.scale2 = (float)((double)scale * 1.4426950408889634);
     a.spin = dppf_internal::first_pass_polls();
@@ -231,8 +231,8 @@ int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_
     a.splits = grad_splits(T, kv_heads, heads / kv_heads);
     a.dq = static_cast<bf16 *>(grad_q); a.dk = static_cast<bf16 *>(grad_k); a.dv = static_cast<bf16 *>(grad_v);
     a.ld_dq = ld_grad_q; a.head_dq = head_grad_q; a.ld_dk = ld_grad_k; a.head_dk = head_grad_k; a.ld_dv = ld_grad_v; a.head_dv = head_grad_v;
-    a.T = T; a.heads = heads; a.kv_heads = kv_heads; a.share = heads / kv_heads; a.D = D;
-    a.causal = causal; a.window = window;
+    a.T = T; a.heads = heads; a.kv_heads = kv_heads; a.share = heads / kv_heads; a.D = D; a.B = (int)B;
+    a.causal = causal; a.window = window < T ? window : 0;
     a.scale = scale;
     a.scale2 = (float)((double)scale * 1.4426950408889634);
     a.spin = dppf_internal::first_pass_polls();

@@ -21,8 +21,9 @@ struct PlanHeader {          // first bytes of the plan
     int status;              // dppf_status seen by the kernels
     unsigned magic;
     int tiles[kPlanLists];
-    int T;
+    int T, B;                // what the lists' places go by
 };
+__device__ __forceinline__ bool is_plan(const PlanHeader *h, long long T, int B) { return h->magic == kPlanMagic && h->T == T && h->B == B; }
 struct PlanTile { int row, rows, begin, end; };       // first row, rows of this tile; its sequence's rows (begin == end: no sequence)
 
 __device__ __forceinline__ PlanTile uniform(const PlanTile &t) { return {uniform(t.row), uniform(t.rows), uniform(t.begin), uniform(t.end)}; }
@@ -136,6 +137,7 @@ __global__ void __launch_bounds__(kPlanThreads) attention_plan_kernel(const __gr
     if (tid == 0) {
         a.hdr->status = DPPF_OK;
         a.hdr->T = T;
+        a.hdr->B = a.B;
         a.hdr->magic = kPlanMagic;
     }
 }
@@ -150,7 +152,7 @@ struct AttentionArgs {
     bf16 *out;
     float *lse;                  // [heads][T]
     long long ld_out, head_out, T;
-    int list, heads, share, D;   // share: query heads of a key head
+    int list, heads, share, D, B;   // share: query heads of a key head
     int by_head, units;          // the two slots of a block: two heads of a tile of 128 rows, or the halves of one of 256; blocks of a tile
     int causal, window;          // window 0: none
     float scale, scale2;         // scale * log2 e
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
     __shared__ volatile int s_dead;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     if (tid < 3) prefetch_map(tid == 0 ? &a.q : tid == 1 ? &a.k : &a.v);
-    if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T) {                 // not a plan of these rows
+    if (!is_plan(a.hdr, a.T, a.B)) {                 // not a plan of these rows and sequences
         if (blockIdx.x == 0 && tid == 0) a.hdr->status = DPPF_ERR_WORKSPACE;
         return;
     }
@@ -593,7 +595,7 @@ struct AttentionGradArgs {
     bf16 *dq, *dk, *dv;
     long long ld_dq, head_dq, ld_dk, head_dk, ld_dv, head_dv, T;
     float *part;                 // [splits][2][kv_heads][T][D]: dv and dk (without scale) of a part of the heads that share a key head
-    int heads, kv_heads, share, splits, D;
+    int heads, kv_heads, share, splits, D, B;
     int causal, window;
     float scale, scale2;
     int spin;
@@ -660,7 +662,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     const int head = (int)(blockIdx.x % a.heads), kv_head = head / a.share;
     const unsigned index = blockIdx.x / a.heads;
     if (tid < 5) prefetch_map(tid == 0 ? &a.q : tid == 1 ? &a.grad_out : tid == 2 ? &a.k : tid == 3 ? &a.out : &a.v);
-    if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T) {
+    if (!is_plan(a.hdr, a.T, a.B)) {
         if (blockIdx.x == 0 && tid == 0) a.hdr->status = DPPF_ERR_WORKSPACE;
         return;
     }
@@ -898,7 +900,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_key_kernel(con
     const int unit = (int)(blockIdx.x % (a.kv_heads * a.splits)), kv_head = unit / a.splits, split = unit % a.splits;
     const unsigned index = blockIdx.x / (a.kv_heads * a.splits);
     if (tid < 4) prefetch_map(tid == 0 ? &a.k : tid == 1 ? &a.q : tid == 2 ? &a.v : &a.grad_out);
-    if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T || index >= (unsigned)a.hdr->tiles[kByKey]) return;      // the status is the first kernel's
+    if (!is_plan(a.hdr, a.T, a.B) || index >= (unsigned)a.hdr->tiles[kByKey]) return;      // the status is the first kernel's
     const PlanTile t = uniform(a.key_tiles[index]);
     auto part_row = [&](int which, int row) { return a.part + (((long long)(split * 2 + which) * a.kv_heads + kv_head) * a.T + row) * a.D; };
     if (t.begin == t.end) {
@@ -1148,7 +1150,7 @@ constexpr int kJoinThreads = 256;
 __global__ void __launch_bounds__(kJoinThreads) attention_grad_join_kernel(const __grid_constant__ AttentionGradArgs a) {
     const int pieces = a.D / 8, which = blockIdx.y;
     const long long rows = a.kv_heads * a.T, i = (long long)blockIdx.x * kJoinThreads + threadIdx.x;
-    if (a.hdr->magic != kPlanMagic || a.hdr->T != a.T || i >= rows * pieces) return;
+    if (!is_plan(a.hdr, a.T, a.B) || i >= rows * pieces) return;
     const long long at = i / pieces, kv_head = at / a.T, row = at - kv_head * a.T;
     const int piece = (int)(i - at * pieces);
     float v[8];

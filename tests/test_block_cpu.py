@@ -121,7 +121,7 @@ def test_attention_refusals(b):
     call = caller(b.load().dppf_attention, ok, list(ok))
     for bad in ([{k: None} for k in ("q", "k", "v", "o", "lse", "plan")] +
                 [dict(T=-1), dict(T=2**25), dict(B=0), dict(h=0), dict(h=1025, kv=1), dict(kv=0), dict(kv=3), dict(D=0), dict(D=60), dict(D=136, ldq=2000, hq=136), dict(c=2), dict(w=-1), dict(w=5, c=0),
-                 dict(s=0.0), dict(s=-1.0), dict(s=NAN), dict(ldq=504), dict(hq=56), dict(ldk=0), dict(ldo=-8), dict(o=P[0]), dict(o=P[1]), dict(lse=P[3]), dict(lse=P[0]), dict(lse=P[5]), dict(o=P[5]),
+                 dict(s=0.0), dict(s=-1.0), dict(s=NAN), dict(s=3e38), dict(ldq=504), dict(hq=56), dict(ldk=0), dict(ldo=-8), dict(o=P[0]), dict(o=P[1]), dict(lse=P[3]), dict(lse=P[0]), dict(lse=P[5]), dict(o=P[5]),
                  dict(ldq=2**39)]):
         assert call(**bad) == b.ERR_INVALID_ARG, bad
     for bad in (dict(q=P[0] + 8), dict(k=P[1] + 2), dict(v=P[2] + 8), dict(o=P[3] + 8), dict(ldq=516), dict(hk=68, ldk=200), dict(lse=P[4] + 2), dict(plan=P[5] + 64)):

@@ -414,6 +414,30 @@ def test_waits_that_give_up(b):
     assert b.dppf_device_status(plan.buffer) == b.OK
 
 
+def test_a_plan_of_other_sequences_writes_nothing(b):
+    """The lists of a plan lie where its numbers of rows and sequences put them: another number is told from the plan itself."""
+    T = 900
+    q, k, v = inputs(T, 2, 1, 64, seed=26)
+    plan = b.AttentionPlan(starts_of([300, 300, 300]), T)
+    plan.sequences = 600                                                        # as a C caller may get it wrong
+    plan.buffer = torch.cat([plan.buffer, torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")])
+    out, lse = torch.full_like(q, 7.0), torch.full((2, T), 7.0, device="cuda")
+    b.dppf_attention(q, k, v, plan, out=out, lse=lse)
+    assert b.dppf_device_status(plan.buffer) == b.ERR_WORKSPACE and (out == 7).all() and (lse == 7).all()
+    got = b.dppf_attention_grad(q, q, k, v, out, lse, plan, grad_q=torch.full_like(q, 7.0), grad_k=torch.full_like(k, 7.0), grad_v=torch.full_like(v, 7.0))
+    assert all((x == 7).all() for x in got)
+
+
+@pytest.mark.parametrize("window", [500, 501, 2 ** 31 - 1])
+def test_windows_as_long_as_the_batch(b, window):
+    T = 500
+    q, k, v = inputs(T, 3, 3, 64, seed=27)
+    plan = b.AttentionPlan(starts_of([T]), T)
+    f, g = b.dppf_attention(q, k, v, plan), b.dppf_attention(q, k, v, plan, window=window)
+    assert same_bits(f.out, g.out) and same_bits(f.lse, g.lse)
+    assert all(same_bits(x, y) for x, y in zip(b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan), b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan, window=window)))
+
+
 def test_a_plan_of_other_rows_writes_nothing(b):
     plan = b.AttentionPlan(starts_of([64]), 64)
     q, k, v = inputs(64, 1, 1, 64, seed=24)
@@ -459,3 +483,29 @@ def test_no_tokens_and_refusals(b):
         b.AttentionPlan(torch.zeros(2, device="cuda"), 5)
     with pytest.raises(ValueError):
         plan.renew(torch.zeros(5, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_random_batches(b, seed):
+    """Batches of more tiles than SMs, so that blocks stay for several: heads, widths, masks and lengths at random, rows of no sequence in between."""
+    import random
+    rng = random.Random(1000 + seed)
+    kv_heads = rng.choice([1, 2, 3, 5, 8])
+    heads = kv_heads * rng.choice([1, 2, 3, 4] if kv_heads > 3 else [4, 6, 7, 8, 12])
+    D = 8 * rng.randrange(1, 17)
+    lens = [rng.choice([0, 1, rng.randrange(2, 130), rng.randrange(100, 700), rng.randrange(600, 1500)]) for _ in range(rng.randrange(4, 12))]
+    lead, tail = rng.choice([0, rng.randrange(1, 300)]), rng.choice([0, rng.randrange(1, 300)])
+    causal = rng.random() < 0.7
+    window = rng.choice([0, rng.randrange(1, 900)]) if causal else 0
+    starts = starts_of(lens, lead)
+    T = int(starts[-1]) + tail
+    q, k, v = inputs(T, heads, kv_heads, D, seed=seed)
+    scale = rng.uniform(0.02, 0.3)
+    plan = b.AttentionPlan(starts, T)
+    got = b.dppf_attention(q, k, v, plan, causal=causal, window=window, scale=scale)
+    want = reference(q, k, v, starts, causal, window, scale)
+    within(got.lse, *want["lse"], "lse")
+    within(got.out, *want["out"], "out")
+    again = b.dppf_attention(q, k, v, plan, causal=causal, window=window, scale=scale)
+    assert same_bits(again.out, got.out) and same_bits(again.lse, got.lse)
+    check_grads(b, lens, heads, kv_heads, D, causal, window, scale=scale, lead=lead, tail=tail, seed=seed)
