@@ -548,7 +548,7 @@ def dppf_layer_norm(x, weight, bias=None, eps=1e-5, branch=None, sum_out=None, o
     elif sum_out is not None:
         raise ValueError("sum_out is for the sum with a branch")
     if out is None:
-        out = x.new_empty(shape, dtype=out_dtype)
+        out = torch.empty_like(x, dtype=out_dtype) if x.is_contiguous() else x.new_empty(shape, dtype=out_dtype)     # the first a microsecond less
         po, ld_o = out.data_ptr(), H
     else:
         po, ld_o = _rows(out, shape, "out", dev)
@@ -583,7 +583,7 @@ def dppf_layer_norm_grad(grad_out, x, mean, rstd, weight, grad_weight, grad_bias
             _vector(t, n, "mean and rstd, weight, grad_weight and grad_bias", dev, (kind,))
     ps, ld_s = (None, 0) if grad_sum is None else _rows(grad_sum, shape, "grad_sum", dev, x.dtype)
     if grad_x is None:
-        grad_x = x.new_empty(shape)
+        grad_x = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
         pd, ld_d = grad_x.data_ptr(), H
     else:
         pd, ld_d = _rows(grad_x, shape, "grad_x", dev, x.dtype)
@@ -612,13 +612,17 @@ def rotary_frequencies(turned, base=10000.0, scaling="plain", factor=1.0, origin
 
 def _heads(t: torch.Tensor, what: str):
     """(tokens, heads, width, token stride, head stride) of a 3-D CUDA tensor with unit stride within a head."""
-    if t.dim() != 3 or not t.is_cuda or (t.shape[2] > 1 and t.stride(2) != 1):
+    if t.dim() != 3 or not t.is_cuda:
         raise ValueError(f"{what} must be a 3-D CUDA tensor [tokens, heads, width] with unit stride within a head")
     T, heads, D = t.shape
-    ld, head, _ = t.stride()
+    ld, head, one = t.stride()
+    if one != 1 and D > 1:
+        raise ValueError(f"{what} must be a 3-D CUDA tensor [tokens, heads, width] with unit stride within a head")
     if heads <= 1:
         head = D                                              # the stride of a single head, or token, says nothing
-    return T, heads, D, ld if T > 1 else (heads - 1) * head + D, head
+    if T <= 1:
+        ld = (heads - 1) * head + D
+    return T, heads, D, ld, head
 
 
 def dppf_rotary(x, positions, frequencies, scale=1.0, interleaved=False, inverse=False, out=None):
@@ -632,10 +636,13 @@ def dppf_rotary(x, positions, frequencies, scale=1.0, interleaved=False, inverse
     if frequencies.dtype is not torch.float64 or frequencies.device != dev or not frequencies.is_contiguous():
         _vector(frequencies, half, "frequencies", dev, (torch.float64,))
     if out is None:
-        out = x.new_empty(x.shape)
-    elif out.shape != x.shape or out.dtype != x.dtype or out.device != dev:
-        raise ValueError("out must have the shape, type and device of x")
-    _, _, _, ld_o, head_o = _heads(out, "out")
+        out, ld_o, head_o = x.new_empty(x.shape), heads * D, D
+    elif out is x:
+        ld_o, head_o = ld, head
+    else:
+        if out.shape != x.shape or out.dtype != x.dtype or out.device != dev:
+            raise ValueError("out must have the shape, type and device of x")
+        _, _, _, ld_o, head_o = _heads(out, "out")
     _call(dev, load().dppf_rotary, "dppf_rotary", x.data_ptr(), _type(x, "x"), ld, head, T, heads, D, 2 * half, int(bool(interleaved)), positions.data_ptr(),
           _ID_BITS[positions.dtype], frequencies.data_ptr(), scale, int(bool(inverse)), out.data_ptr(), ld_o, head_o)
     return out
@@ -667,38 +674,44 @@ class Attention(NamedTuple):
     lse: torch.Tensor           # fp32 [heads, T]
 
 
-def _attention_heads(t, what, device, tokens):
+def _attention_heads(t, what, device, tokens, shape=None):
+    """(shape, pointer, token stride, head stride) of bf16 heads of this many tokens (of this shape)."""
     if t.dtype is not torch.bfloat16 or t.device != device:
         raise ValueError(f"{what} must be bf16 on {device}")
-    T, heads, D, ld, head = _heads(t, what)
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{what} must have the shape {tuple(shape)}")
+    T, _, _, ld, head = _heads(t, what)
     if T != tokens:
         raise ValueError(f"{what} must have the plan's {tokens} tokens")
-    return heads, D, (t.data_ptr(), ld, head)
+    return t.shape, t.data_ptr(), ld, head
 
 
 def _attention_inputs(q, k, v, plan, scale):
-    heads, D, at_q = _attention_heads(q, "q", plan.device, plan.tokens)
-    kv_heads, Dk, at_k = _attention_heads(k, "k", plan.device, plan.tokens)
-    kv2, Dv, at_v = _attention_heads(v, "v", plan.device, plan.tokens)
-    if Dk != D or Dv != D or kv2 != kv_heads:
-        raise ValueError("q, k and v must have heads of one width, k and v as many heads")
-    return heads, kv_heads, D, at_q, at_k, at_v, (D ** -0.5 if scale is None else scale)
+    device, tokens = plan.device, plan.tokens
+    shape, *at_q = _attention_heads(q, "q", device, tokens)
+    kv, *at_k = _attention_heads(k, "k", device, tokens)
+    _, *at_v = _attention_heads(v, "v", device, tokens, kv)
+    D = shape[2]
+    if kv[2] != D:
+        raise ValueError("q, k and v must have heads of one width")
+    return shape, kv, (*at_q, *at_k, *at_v), (D ** -0.5 if scale is None else scale)
 
 
 def dppf_attention(q, k, v, plan: AttentionPlan, causal=True, window=0, scale=None, out=None, lse=None) -> Attention:
     """Attention of ``q[T, heads, D]`` over the keys ``k`` and values ``v[T, kv_heads, D]`` of the same sequence (``causal``: up to the
     token itself; ``window``: the last so many).  ``scale``: default 1 / sqrt(D).  bf16; ``out``, ``lse``: new if not given."""
-    heads, kv_heads, D, at_q, at_k, at_v, scale = _attention_inputs(q, k, v, plan, scale)
+    shape, kv, at_qkv, scale = _attention_inputs(q, k, v, plan, scale)
+    _, heads, D = shape
     if out is None:
-        out = q.new_empty(q.shape)
-    elif out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    _, _, at_o = _attention_heads(out, "out", plan.device, plan.tokens)
+        out = q.new_empty(shape)
+        at_o = (out.data_ptr(), heads * D, D)
+    else:
+        at_o = _attention_heads(out, "out", plan.device, plan.tokens, shape)[1:]
     if lse is None:
         lse = q.new_empty((heads, plan.tokens), dtype=torch.float32)
     else:
         _vector(lse, heads * plan.tokens, "lse", plan.device)
-    _call(plan.device, load().dppf_attention, "dppf_attention", *at_q, *at_k, *at_v, plan.tokens, plan.sequences, heads, kv_heads, D, int(bool(causal)), int(window), scale,
+    _call(plan.device, load().dppf_attention, "dppf_attention", *at_qkv, plan.tokens, plan.sequences, heads, kv[1], D, int(bool(causal)), int(window), scale,
           *at_o, lse.data_ptr(), plan.buffer.data_ptr(), plan.buffer.nbytes)
     return Attention(out, lse)
 
@@ -720,21 +733,22 @@ def dppf_attention_grad(grad_out, q, k, v, out, lse, plan: AttentionPlan, causal
                         ws=None) -> AttentionGrads:
     """Gradients of :func:`dppf_attention` with respect to ``q``, ``k`` and ``v``, from its ``out`` and ``lse``, written whole to ``grad_q``,
     ``grad_k`` and ``grad_v`` (new if not given)."""
-    heads, kv_heads, D, at_q, at_k, at_v, scale = _attention_inputs(q, k, v, plan, scale)
-    given = []
-    for t, like, what in ((grad_out, q, "grad_out"), (out, q, "out"), (grad_q, q, "grad_q"), (grad_k, k, "grad_k"), (grad_v, v, "grad_v")):
-        if t is None and what.startswith("grad_") and what != "grad_out":
-            t = like.new_empty(like.shape)
-        elif t.shape != like.shape:
-            raise ValueError(f"{what} has not the shape that goes with q, k and v")
-        given.append((t, _attention_heads(t, what, plan.device, plan.tokens)[2]))
-    (_, at_go), (_, at_o), (grad_q, at_dq), (grad_k, at_dk), (grad_v, at_dv) = given
-    _vector(lse, heads * plan.tokens, "lse", plan.device)
+    shape, kv, at_qkv, scale = _attention_inputs(q, k, v, plan, scale)
+    device, tokens, (_, heads, D) = plan.device, plan.tokens, shape
+    at_go = _attention_heads(grad_out, "grad_out", device, tokens, shape)[1:]
+    at_o = _attention_heads(out, "out", device, tokens, shape)[1:]
+    grad_q = q.new_empty(shape) if grad_q is None else grad_q
+    grad_k = k.new_empty(kv) if grad_k is None else grad_k
+    grad_v = v.new_empty(kv) if grad_v is None else grad_v
+    at_dq = _attention_heads(grad_q, "grad_q", device, tokens, shape)[1:]
+    at_dk = _attention_heads(grad_k, "grad_k", device, tokens, kv)[1:]
+    at_dv = _attention_heads(grad_v, "grad_v", device, tokens, kv)[1:]
+    _vector(lse, heads * tokens, "lse", device)
     if ws is not None:
-        _workspace(ws, plan.device)
-    elif plan.tokens:
-        ws = alloc_attention_workspace(plan.tokens, heads, plan.device)
-    _call(plan.device, load().dppf_attention_grad, "dppf_attention_grad", *at_go, *at_q, *at_k, *at_v, *at_o, lse.data_ptr(), plan.tokens, plan.sequences, heads, kv_heads, D,
+        _workspace(ws, device)
+    elif tokens:
+        ws = alloc_attention_workspace(tokens, heads, device)
+    _call(device, load().dppf_attention_grad, "dppf_attention_grad", *at_go, *at_qkv, *at_o, lse.data_ptr(), tokens, plan.sequences, heads, kv[1], D,
           int(bool(causal)), int(window), scale, *at_dq, *at_dk, *at_dv, plan.buffer.data_ptr(), plan.buffer.nbytes, _ptr(ws), 0 if ws is None else ws.nbytes)
     return AttentionGrads(grad_q, grad_k, grad_v)
 
