@@ -31,7 +31,6 @@ int norm_width(int H, std::initializer_list<NormOperand> operands) {
 
 // Threads of a block that holds a row, `each` elements a thread.
 int norm_threads(int H, int each) { return ((H + each - 1) / each + 31) / 32 * 32; }
-int norm_threads_of(int H) { return norm_threads(H, H <= kNormShort ? 8 : kNormElements); }
 
 // Lanes of a warp for a row: the fewest that hold it, a power of two.
 int norm_lanes(int H) {
@@ -59,7 +58,7 @@ int launch_norm_width(const NormArgs &a, int n, cudaStream_t s) {
 int64_t norm_grad_blocks(int64_t T, int H) {
     if (H > kNormGradRow) return T < 32 ? T : 32;                                        // rows of blocks of the columns' kernel
     const int64_t side = H <= kNormWarpRow ? kNormWarps * 32 / norm_lanes(H) : 1, rows = (T + side - 1) / side;
-    const int64_t most = 148LL * (H <= kNormWarpRow ? 2 : (H <= kNormShort ? 1024 : 512) / norm_threads_of(H));
+    const int64_t most = 148LL * (H <= kNormWarpRow ? 2 : 1024 / norm_threads(H, kNormGradElements));
     return rows < most ? rows : most;
 }
 
@@ -69,10 +68,8 @@ int launch_norm_grad(NormGradArgs a, cudaStream_t s) {
     a.lanes = norm_lanes(a.H);
     if (a.H <= kNormWarpRow) {
         norm_grad_kernel<TX, TO, N, kNormElements, true><<<(unsigned)a.blocks, kNormWarps * 32, 0, s>>>(a);
-    } else if (a.H <= kNormShort) {
-        norm_grad_kernel<TX, TO, N, 8, false><<<(unsigned)a.blocks, norm_threads_of(a.H), 0, s>>>(a);
     } else if (a.H <= kNormGradRow) {
-        norm_grad_kernel<TX, TO, N, kNormElements, false><<<(unsigned)a.blocks, norm_threads_of(a.H), 0, s>>>(a);
+        norm_grad_kernel<TX, TO, N, kNormGradElements, false><<<(unsigned)a.blocks, norm_threads(a.H, kNormGradElements), 0, s>>>(a);
     } else {
         norm_grad_columns_kernel<TX, TO, N><<<dim3((unsigned)((a.groups + kNormWideThreads - 1) / kNormWideThreads), (unsigned)a.blocks), kNormWideThreads, 0, s>>>(a);
         norm_grad_wide_kernel<TX, TO, N><<<(unsigned)a.T, kNormWideThreads, 0, s>>>(a);

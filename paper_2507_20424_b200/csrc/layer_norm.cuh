@@ -24,11 +24,11 @@ namespace {
 constexpr int kNormElements = 16;                         // of a row in one thread
 constexpr int kNormWarpRow = 32 * kNormElements;          // longest row of a warp
 constexpr int kNormRow = 1024 * kNormElements;            // longest row that a block holds
-constexpr int kNormGradRow = 512 * kNormElements;         // ... with the columns' sums beside it
-constexpr int kNormShort = 512 * 8;                       // rows of blocks up to this: eight elements a thread
+constexpr int kNormGradElements = 8;                     // the gradient's, of rows of blocks: the columns' sums lie beside them
+constexpr int kNormGradRow = 1024 * kNormGradElements;    // longest row that a block holds so
 constexpr int kNormWarps = 8;                             // rows side by side in a block, a warp each
 constexpr int kNormWideThreads = 512;
-constexpr int kNormJoinThreads = 256;
+constexpr int kNormJoinThreads = 1024;
 
 // Eight fp32 in one access of 32 bytes (as two of 16 a warp's accesses touch every 32-byte sector twice); else as everywhere.
 template <typename T, int N, bool kOnce = true>
@@ -303,7 +303,7 @@ __device__ __forceinline__ void put_sums(const NormGradArgs &a, int L, int t, fl
 }
 
 template <typename TX, typename TO, int N, int E, bool kWarp>
-__global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 512, kWarp ? 2 : E == 8 ? 2 : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs a) {
+__global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024, kWarp ? 2 : 1) norm_grad_kernel(const __grid_constant__ NormGradArgs a) {
     constexpr int G = E / N;
     __shared__ float s_sum[2][2][32];
     const int L = kWarp ? a.lanes : blockDim.x, t = kWarp ? threadIdx.x & (L - 1) : threadIdx.x;
@@ -416,7 +416,8 @@ __global__ void __launch_bounds__(kNormWideThreads) norm_grad_wide_kernel(const 
     }
 }
 
-// The blocks' sums, added in block order by eight threads a column (every eighth block each) and then those eight.
+// The blocks' sums, added in block order by 32 threads a column (every 32nd block each; with eight it took 10 us for 296 blocks of 4,096 columns) and
+// then those 32.
 // blockIdx.y: 0 the weight's gradient, 1 the bias's.
 __global__ void __launch_bounds__(kNormJoinThreads) norm_join_kernel(const __grid_constant__ NormGradArgs a) {
     constexpr int kParts = kNormJoinThreads / 32;
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(kNormJoinThreads) norm_join_kernel(const __gri
     float sum = 0.f;
     if (c < a.H) {
         const float *p = a.part + (long long)blockIdx.y * a.H + c;
-#pragma unroll 4
+#pragma unroll 8
         for (int b = part; b < a.blocks; b += kParts) sum += __ldcg(p + (long long)b * 2 * a.H);
     }
     s_part[part][lane] = sum;
