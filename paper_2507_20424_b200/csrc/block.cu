@@ -44,8 +44,9 @@ int launch_norm(NormArgs a, cudaStream_t s) {
     a.groups = a.H / N;
     a.lanes = norm_lanes(a.H);
     const int64_t side = kNormWarps * 32 / a.lanes;
-    if (a.H <= kNormWarpRow) norm_kernel<TX, TO, N, true><<<(unsigned)((a.T + side - 1) / side), kNormWarps * 32, 0, s>>>(a);
-    else if (a.H <= kNormRow) norm_kernel<TX, TO, N, false><<<(unsigned)a.T, norm_threads(a.H, kNormElements), 0, s>>>(a);
+    if (a.H <= kNormWarpRow) norm_kernel<TX, TO, N, kNormElements, true><<<(unsigned)((a.T + side - 1) / side), kNormWarps * 32, 0, s>>>(a);
+    else if (a.H <= kNormRow && sizeof(TX) == 2 && !a.branch) norm_kernel<TX, TO, N, sizeof(TX) == 2 ? 2 * kNormElements : kNormElements, false><<<(unsigned)a.T, norm_threads(a.H, 2 * kNormElements), 0, s>>>(a);
+    else if (a.H <= kNormRow) norm_kernel<TX, TO, N, kNormElements, false><<<(unsigned)a.T, norm_threads(a.H, kNormElements), 0, s>>>(a);
     else norm_wide_kernel<TX, TO, N><<<(unsigned)a.T, kNormWideThreads, 0, s>>>(a);
     return launched();
 }

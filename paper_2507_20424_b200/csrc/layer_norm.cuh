@@ -4,7 +4,8 @@
 //   u = w dy;  xh = (h - mu) r;  dx = r (u - mean u - xh mean(u xh)) + dsum;  dw = sum_t dy xh;  db = sum_t dy
 //
 // Both are bound by memory: a row is read once, stays in registers (sixteen elements a thread) for the statistics, the second
-// moment taken about the mean, and is written once.  Rows of up to 512 elements take a warp or, shorter ones, a part of one (a power of two of
+// moment taken about the mean, and is written once.  (Of a bf16 row alone 32 elements a thread, 64 bytes, as of an fp32 one: 8,192 x 8,192 86 -> 72 us,
+// 40,000 x 768 37 -> 32; an fp32 row with 32, or a branch beside it, 123 -> 126.)  Rows of up to 512 elements take a warp or, shorter ones, a part of one (a power of two of
 // lanes), longer ones a block; above
 // kNormRow elements (kNormGradRow for the gradient) a block walks the row several times, the later ones from L2.
 //
@@ -13,9 +14,9 @@
 // depends on T and H alone.
 //
 // Measured on a B200 (copy rate 6.54 TB/s): 16,384 x 4,096, fp32 stream plus a bf16 branch to bf16, 123 us (6.55 TB/s); its gradient with the
-// stream's, 167 us (5.6 TB/s), of which the joining launch is 10: reads and writes mixed, 49 % of the warps resident (64 registers).
-// bf16 rows without a stream are bound by latency: 8,192 x 8,192 86 us (3.1 TB/s).  Tried and lost: blocks that stay for several rows and read
-// ahead (123 -> 130 us; 8,192 x 8,192 bf16 86 -> 70), weights held in registers (gradient 167 -> 217).
+// stream's, 164 us (5.7 TB/s): reads and writes mixed, half of the warps resident (64 registers).  bf16 rows without a stream are bound by
+// latency: 8,192 x 8,192 72 us (3.7 TB/s), the gradient with the stream's 148.  Tried and lost: blocks that stay for several rows and read
+// ahead (123 -> 130 us; 8,192 x 8,192 bf16 70), weights held in registers (gradient 167 -> 217), eight elements a thread forward (123 -> 131).
 #pragma once
 #include "local_common.cuh"
 
@@ -130,9 +131,9 @@ __device__ __forceinline__ void row_sums(float (&v)[K], float (*s)[32], int lane
     }
 }
 
-template <typename TX, typename TO, int N, bool kWarp>
-__global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : 1024) norm_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int G = kNormElements / N;
+template <typename TX, typename TO, int N, int E, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kNormWarps * 32 : E > kNormElements ? 512 : 1024) norm_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int G = E / N;
     __shared__ float s_sum[2][1][32];
     const int L = kWarp ? a.lanes : blockDim.x, t = kWarp ? threadIdx.x & (L - 1) : threadIdx.x;
     long long row = kWarp ? (long long)blockIdx.x * (kNormWarps * 32 / L) + threadIdx.x / L : blockIdx.x;
