@@ -164,9 +164,8 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
     a.out = static_cast<bf16 *>(out);
     a.lse = lse_out;
     a.ld_out = ld_out; a.head_out = head_out; a.T = T;
-    a.heads = heads; a.D = D; a.B = (int)B;
+    a.D = D; a.B = (int)B;
     a.causal = causal; a.window = window < T ? window : 0;
-    a.scale = scale;
     a.scale2 = (float)((double)scale * 1.4426950408889634);
     a.spin = dppf_internal::first_pass_polls();
     const long long blocks = (long long)a.units * l.most[a.list];

@@ -51,13 +51,7 @@ __device__ __forceinline__ void mbar_arrive(unsigned long long *bar) {
 template <int kRegisters> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
 template <int kRegisters> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
 
-// Barrier `id` (1 .. 15) of `threads` threads; true in all if `any` is in one.
-__device__ __forceinline__ bool group_any(int id, int threads, bool any) {
-    unsigned r;
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %3, 0;\n bar.red.or.pred p, %1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(r) : "r"(id), "r"(threads), "r"((unsigned)any) : "memory");
-    return r != 0;
-}
+// Barrier `id` (1 .. 15) of `threads` threads.
 __device__ __forceinline__ void group_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // ---------------------------------------------------------------- copies
