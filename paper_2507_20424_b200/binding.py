@@ -694,7 +694,7 @@ def _attention_inputs(q, k, v, plan, scale):
     D = shape[2]
     if kv[2] != D:
         raise ValueError("q, k and v must have heads of one width")
-    return shape, kv, (*at_q, *at_k, *at_v), (D ** -0.5 if scale is None else scale)
+    return shape, kv, (*at_q, *at_k, *at_v), (max(D, 1) ** -0.5 if scale is None else scale)
 
 
 def dppf_attention(q, k, v, plan: AttentionPlan, causal=True, window=0, scale=None, out=None, lse=None) -> Attention:

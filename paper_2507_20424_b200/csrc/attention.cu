@@ -50,7 +50,7 @@ bool heads_map(CUtensorMap *map, const HeadRows &h) {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)h.D, (cuuint64_t)h.heads, (cuuint64_t)h.T};
-    const cuuint64_t strides[2] = {(cuuint64_t)h.head * 2, (cuuint64_t)h.ld * 2};
+    const cuuint64_t strides[2] = {(cuuint64_t)(h.heads > 1 ? h.head : h.D) * 2, (cuuint64_t)h.ld * 2};     // a single head's may be 0
     const cuuint32_t box[3] = {64, 1, kTile}, one[3] = {1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(h.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -509,3 +509,28 @@ def test_random_batches(b, seed):
     again = b.dppf_attention(q, k, v, plan, causal=causal, window=window, scale=scale)
     assert same_bits(again.out, got.out) and same_bits(again.lse, got.lse)
     check_grads(b, lens, heads, kv_heads, D, causal, window, scale=scale, lead=lead, tail=tail, seed=seed)
+
+
+def test_the_stride_of_a_single_head_says_nothing(b):
+    """0 or any other multiple of 8 at the C entries, where the binding gives the width."""
+    T, D = 150, 64
+    q, k, v = (t.contiguous() for t in inputs(T, 1, 1, D, seed=31))
+    plan = b.AttentionPlan(starts_of([100, 50]), T)
+    want = b.dppf_attention(q, k, v, plan)
+    grads = b.dppf_attention_grad(q, q, k, v, want.out, want.lse, plan)
+    ws, lib, stream = b.alloc_attention_workspace(T, 1), b.load(), torch.cuda.current_stream().cuda_stream
+    at = (plan.buffer.data_ptr(), plan.buffer.nbytes)
+    for head in (0, 8, 4096):
+        out, lse, got = torch.empty_like(q), torch.empty_like(want.lse), [torch.empty_like(q) for _ in range(3)]
+        rows = lambda t: (t.data_ptr(), D, head)  # noqa: E731
+        assert lib.dppf_attention(*rows(q), *rows(k), *rows(v), T, 2, 1, 1, D, 1, 0, D ** -0.5, *rows(out), lse.data_ptr(), *at, stream) == 0
+        assert lib.dppf_attention_grad(*rows(q), *rows(q), *rows(k), *rows(v), *rows(want.out), want.lse.data_ptr(), T, 2, 1, 1, D, 1, 0, D ** -0.5,
+                                       *[x for t in got for x in rows(t)], *at, ws.data_ptr(), ws.nbytes, stream) == 0
+        assert same_bits(out, want.out) and same_bits(lse, want.lse) and all(same_bits(x, y) for x, y in zip(got, grads))
+
+
+def test_heads_of_no_width_are_refused(b):
+    none = torch.empty(5, 2, 0, dtype=BF16, device="cuda")
+    with pytest.raises(b.DppfError) as err:
+        b.dppf_attention(none, none, none, b.AttentionPlan(starts_of([5]), 5))
+    assert err.value.status == b.ERR_INVALID_ARG
