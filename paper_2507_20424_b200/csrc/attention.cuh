@@ -214,19 +214,21 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // 2^x of two numbers on the multiply-add pipes, for a part of the exponentials: the special function unit gives 16 a cycle and SM,
-// as many as the products of a tile ask for in their time.  x = n + f with n whole and |f| <= 1/2: the fp32 sum x + 1.5 2^23 ends in n,
-// a polynomial of degree 4 (least relative error with p(0) = 1 on the interval: 2.9e-6, far below the 2^-8 of the bf16 result) gives 2^f,
-// and n is added to its exponent.  x <= -127 gives 0.
+// as many as the products of a tile ask for in their time.  x = n + f with n whole and |f| <= 1/2: the fp32 sum x + 1.5 2^23 + 127 ends in
+// n + 127, the exponent field of 2^n, and a polynomial of degree 4 (least relative error with p(0) = 1 on the interval: 2.9e-6, far below the 2^-8 of
+// the bf16 result) gives 2^f, its last step with f and 1 times 2^n.  x <= -127 gives 0 and NaN stays NaN (an addition to the polynomial's exponent
+// field made it a finite number; that was 2 % faster in the gradient of heads of 64, up to 1 % elsewhere).  x above 127.5 gives any
+// number: the forward kernel looks for those, the gradient's are masked.
 __device__ __forceinline__ float2 exp2_polynomial(float2 x) {
-    const float kRound = 12582912.0f;
+    const float kRound = 12582912.0f + 127.0f;
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.0f));
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-127.0f));
     const float2 t = add2(x, both(kRound)), n = add2(t, both(-kRound)), f = fma2(n, both(-1.0f), x);
+    const float2 s = make_float2(__int_as_float(__float_as_int(t.x) << 23), __int_as_float(__float_as_int(t.y) << 23)), fs = mul2(f, s);
     float2 p = fma2(f, both(0.009582852944731712f), both(0.055906426161527634f));
     p = fma2(p, f, both(0.24024099111557007f));
     p = fma2(p, f, both(0.6931241750717163f));
-    p = fma2(p, f, both(1.0f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+    return fma2(p, fs, s);
 }
 
 // A row of NaN, where a wait gave up (copies may still be on their way to the tiles).
