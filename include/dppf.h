@@ -574,7 +574,9 @@ int dppf_device_status(const void *ws, void *cuda_stream);
  * default.  A budget of 0 makes every such wait give up at once while the copies themselves
  * still complete (the block waits for them with the full budget before it leaves), which is
  * how the tests drive the give-up path on a healthy GPU.  Applies to dppf_consensus_rounds,
- * dppf_consensus and dppf_consensus_static (staged schedule) and dppf_consensus_general.
+ * dppf_consensus and dppf_consensus_static (staged schedule) and dppf_consensus_general; to the
+ * waits of dppf_policy_loss, dppf_attention and dppf_attention_grad with first_pass_polls, those
+ * of the last one's first kernel (D and grad_q) with the smaller of the two.
  * Always returns DPPF_OK.
  */
 int dppf_debug_set_poll_limits(int first_pass_polls, int later_pass_polls);

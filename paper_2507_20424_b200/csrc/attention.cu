@@ -6,6 +6,7 @@
 
 #include "attention.cuh"
 #include "local_host.cuh"
+#include <algorithm>
 
 namespace {
 
@@ -235,6 +236,7 @@ int dppf_attention_grad(const void *grad_out, int64_t ld_grad_out, int64_t head_
     a.scale = scale;
     a.scale2 = (float)((double)scale * 1.4426950408889634);
     a.spin = dppf_internal::first_pass_polls();
+    a.spin_query = std::min(a.spin, dppf_internal::later_pass_polls());
     const long long query_blocks = (long long)heads * l.most[kByQuery], key_blocks = (long long)kv_heads * a.splits * l.most[kByKey];
     if (query_blocks > INT_MAX) return DPPF_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);

@@ -600,7 +600,7 @@ struct AttentionGradArgs {
     int heads, kv_heads, share, splits, D, B;
     int causal, window;
     float scale, scale2;
-    int spin;
+    int spin_query, spin;        // polls of a wait in the kernel over the keys, for a tile of queries, and in the other
 };
 
 constexpr int kGradThreads = 384;          // two warpgroups that halve a tile's columns, one of copies and products
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
     const int lo = a.window ? max(0, t.row - a.window + 1 - t.begin) / kTile : 0;
     const int hi = ((a.causal ? min(t.end, t.row + kTile) : t.end) - t.begin + kTile - 1) / kTile, n = hi - lo;
     const unsigned smem = (smem_addr(smem_raw) + 1023) & ~1023u, s_q = smem, s_do = s_q + kTileBytes, s_k = s_do + kTileBytes, s_v = s_k + kKeys * kTileBytes, s_out = s_k + (kKeys - 1) * kTileBytes;   // the tile's output where the third tile of keys will be
-    const Waits wait{&s_dead, a.spin};
+    const Waits wait{&s_dead, a.spin_query};
 
     if (tid == 0) {
         for (unsigned long long *bar : {&q_full, &s_full, &dp_full, &o_full, &k_fixed, &drained}) mbar_init(bar, 1);
@@ -800,6 +800,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) attention_grad_query_kernel(c
         tmem_fence_before();
         mbar_arrive(&rows_ready);
         if (half) {
+            if (!ok) delta = __int_as_float(0x7fc00000);                 // of tiles that did not come: the other kernel must not take it for D
             s_delta[r] = delta;
             if (mine) a.delta[head * a.T + row] = delta;
         }

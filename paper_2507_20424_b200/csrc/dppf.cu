@@ -79,6 +79,7 @@ std::atomic<int> g_spin_first{kSpinLimit}, g_spin_later{kSpinLimit};
 }  // namespace
 namespace dppf_internal {
 int first_pass_polls() { return g_spin_first.load(std::memory_order_relaxed); }
+int later_pass_polls() { return g_spin_later.load(std::memory_order_relaxed); }
 }
 namespace {
 

@@ -9,7 +9,8 @@
 #include <initializer_list>
 
 namespace dppf_internal {
-int first_pass_polls();          // poll budget set by dppf_debug_set_poll_limits
+int first_pass_polls();          // poll budgets set by dppf_debug_set_poll_limits
+int later_pass_polls();
 }
 
 namespace {

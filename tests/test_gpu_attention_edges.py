@@ -90,3 +90,27 @@ def test_a_nan_query_in_each_place_of_a_tile(b, D, share, first):
     seen = rows_below(T, first + torch.arange(heads, device="cuda").view(-1, share).amax(1) + 1)      # by the last of the heads' queries
     check_rows(grads.v, want.v, seen, "grad_v")
     assert torch.isnan(grads.k[seen].float()).all()
+
+
+# ---------------------------------------------------------------- waits that give up in one kernel
+
+@pytest.mark.parametrize("heads,kv_heads,D", [(4, 2, 128), (2, 2, 64), (8, 1, 72)])
+def test_only_the_first_kernel_of_the_gradient_gives_up(b, heads, kv_heads, D):
+    """It forms D_i as well as grad_q: what is made of the D that it did not form must not look like a gradient."""
+    starts = starts_of([300, 20])
+    T = 330                                                                     # the last ten of no sequence
+    q, k, v = inputs(T, heads, kv_heads, D, seed=5)
+    plan = b.AttentionPlan(starts, T)
+    f = b.dppf_attention(q, k, v, plan)
+    want = b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan)
+    try:
+        b.debug_set_poll_limits(-1, 0)
+        got = b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan)
+        assert b.dppf_device_status(plan.buffer) == b.ERR_TIMEOUT
+    finally:
+        b.debug_set_poll_limits(-1, -1)
+    assert torch.isnan(got.q[:320].float()).all() and torch.isnan(got.k[:320].float()).all()
+    assert same_bits(got.v, want.v) and not got.q[320:].any() and not got.k[320:].any()
+    plan.renew(starts)
+    again = b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan)
+    assert all(same_bits(x, y) for x, y in zip(again, want)) and b.dppf_device_status(plan.buffer) == b.OK
