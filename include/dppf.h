@@ -431,8 +431,8 @@ int dppf_attention_plan(const void *starts, int start_bits, int64_t T, int64_t B
  *   S_ij = scale q_i . k_j;   lse_out[h T + i] = log sum_j exp S_ij;   out_i = sum_j exp(S_ij - lse_i) v_j
  * q, out: heads heads, k, v: kv_heads heads (a divisor) of D elements (a multiple of 8, up to DPPF_MAX_ATTENTION_WIDTH), bf16, laid
  * out as for dppf_rotary, starts and strides multiples of 16 bytes.  Products of bf16, sums and softmax in fp32; the
- * probabilities (relative to about the largest) are rounded to bf16 for the product with v, out at the end.  scale > 0, and times
- * log2 e an fp32 number.  A key or value row that is not finite
+ * probabilities (relative to the largest or to one up to 2^20 smaller) are rounded to bf16 for the product with v, out at the end.  Values above 2^107 / (keys of the
+ * sequence) in magnitude may overflow the sums where the result would not.  scale > 0, and times log2 e an fp32 number.  A key or value row that is not finite
  * spoils the queries that see it and those after it in its tile of 128, never another sequence's.  T == 0 does nothing.
  * dppf_device_status(plan, stream): DPPF_ERR_TIMEOUT if a bounded wait gave up (the rows concerned are NaN), DPPF_ERR_WORKSPACE
  * if the plan was not one of T rows and B sequences (nothing is written).

@@ -159,6 +159,7 @@ struct AttentionArgs {
     int spin;
 };
 
+constexpr float kRise = 0x1p20f, kRiseLog2 = 20.0f;      // exponentials relative to a maximum taken earlier
 constexpr int kForwardThreads = 384;       // two warpgroups of a slot each, one of copies and products
 // Of the 168 registers a thread that a block of 384 starts with: a row of scores stays in a softmax thread's.
 constexpr int kSoftmaxRegisters = 208, kControlRegisters = 88;
@@ -494,9 +495,11 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
                         to[i] = bf16_pair(e.x, e.y);
                     }
                 };
-                // The sums stay relative to the maximum of the first tile until an exponential would be above 2^60, which is rare: fp32 and
-                // bf16 keep their relative precision up to 2^127.  So no maximum is taken of what the first half's sum tells: it is at least
-                // the largest of them.  (A polynomial's argument above 128 would come out as any number: those are looked at.)
+                // The sums stay relative to the maximum of the first tile until an exponential would be above kRise, which is rare: fp32 and
+                // bf16 keep their relative precision up to 2^127, and the sum of the values, up to kRise times the keys times the largest
+                // of them, stays below that for values of up to 2^107 / keys.  (At 2^60 in place of 2^20 that was 2^67 / keys; the times are
+                // the same.)  So no maximum is taken of what the first half's sum tells: it is at least the largest of them.  (A polynomial's
+                // argument above 127.5 would come out as any number: those are looked at.)
                 float2 sums = make_float2(0.f, 0.f);
                 float high = -INFINITY;                                      // of the second half, and of the first's polynomials
                 if (j > first) {
@@ -509,7 +512,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_kernel(const __g
 #pragma unroll
                     for (int c = 0; c < 2; ++c) m[c] = max3(m[c], v[c + 2][i], v[c + 2][i + 1]);
                 const float most = fmaxf(m[0], m[1]) * a.scale2;
-                const bool grow = top == -INFINITY || sums.x + sums.y > 0x1p60f || fmaxf(high, most - top) > 60.0f;
+                const bool grow = top == -INFINITY || sums.x + sums.y > kRise || fmaxf(high, most - top) > kRiseLog2;
                 if (j == first || __any_sync(0xffffffffu, grow)) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 2)

@@ -114,3 +114,23 @@ def test_only_the_first_kernel_of_the_gradient_gives_up(b, heads, kv_heads, D):
     plan.renew(starts)
     again = b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan)
     assert all(same_bits(x, y) for x, y in zip(again, want)) and b.dppf_device_status(plan.buffer) == b.OK
+
+
+# ---------------------------------------------------------------- large values under scores that rise
+
+@pytest.mark.parametrize("heads,kv_heads,D", [(4, 2, 64), (3, 3, 128)])
+@pytest.mark.parametrize("jump", [9.0, 16.0, 20.0, 41.0])                       # 13 to 59 powers of two
+@pytest.mark.parametrize("offset", [0, 64])                                     # from tile to tile, or from half to half
+@pytest.mark.parametrize("causal", [True, False])
+def test_large_values_under_growing_scores(b, heads, kv_heads, D, jump, offset, causal):
+    """Sums are kept relative to an older maximum for a while; what that multiplies the values by has to leave them finite.  700 keys: up to 2^98."""
+    T = 700
+    starts = starts_of([T])
+    q, k, v = (x.clone() for x in inputs(T, heads, kv_heads, D, seed=7, std=0.3))
+    q[..., 0] = 8.0
+    k[..., 0] = ((torch.arange(T, device="cuda") + offset) // 128 * jump)[:, None].to(BF16)
+    v = (v.float() * 2.0 ** 95).to(BF16)                                        # 0.3 * 2^95, and 1.6 * 2^95 = 2^95.7 the largest
+    got = b.dppf_attention(q, k, v, b.AttentionPlan(starts, T), causal=causal, scale=0.125)
+    want = reference(q, k, v, starts, causal, 0, 0.125)
+    within(got.lse, *want["lse"], "lse")
+    within(got.out, *want["out"], "out")
