@@ -432,8 +432,11 @@ int dppf_attention_plan(const void *starts, int start_bits, int64_t T, int64_t B
  * q, out: heads heads, k, v: kv_heads heads (a divisor) of D elements (a multiple of 8, up to DPPF_MAX_ATTENTION_WIDTH), bf16, laid
  * out as for dppf_rotary, starts and strides multiples of 16 bytes.  Products of bf16, sums and softmax in fp32; the
  * probabilities (relative to the largest or to one up to 2^20 smaller) are rounded to bf16 for the product with v, out at the end.  Values above 2^107 / (keys of the
- * sequence) in magnitude may overflow the sums where the result would not.  scale > 0, and times log2 e an fp32 number.  A key or value row that is not finite
- * spoils the queries that see it and those after it in its tile of 128, never another sequence's.  T == 0 does nothing.
+ * sequence) in magnitude may overflow the sums where the result would not.  scale > 0, and times log2 e an fp32 number.  T == 0 does nothing.
+ * Rows that are not finite: a query row spoils its own results, a key row those of the queries that see it.  A value row reaches further:
+ * products are formed of tiles of 128 rows, counted from the sequence's start, and a masked probability of 0 times NaN or an infinity
+ * is NaN.  So it spoils all queries of each tile in which one sees any key of its own tile: those before it in its tile and, with a window, some
+ * behind the window's end.  In the columns where it is finite it spoils none, and never another sequence's rows.
  * dppf_device_status(plan, stream): DPPF_ERR_TIMEOUT if a bounded wait gave up (the rows concerned are NaN), DPPF_ERR_WORKSPACE
  * if the plan was not one of T rows and B sequences (nothing is written).
  */
@@ -449,7 +452,9 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
  * the last two over the query heads that share the key head as well.  All three are written whole (zeros for rows of no
  * sequence).  P and dS are rounded to bf16 for their products, sums run in fp32 in an order that the batch fixes (few key heads of
  * few tokens: the heads that share one in parts, joined in order), results are rounded at the end.  Arguments as above; grad_out and out as q, grad_q as q, grad_k and grad_v as k; gradients may be heads
- * of the same rows (as those of one product are) but must not overlap each other or an input.
+ * of the same rows (as those of one product are) but must not overlap each other or an input.  Rows that are not finite spoil the
+ * gradients that they enter for the pairs that see each other and, through masked zeros, for all pairs of two tiles (as above) in which one
+ * does: a key row grad_q, a query row grad_k, a grad_out row grad_v.
  * ws: dppf_attention_workspace_bytes(T, heads) bytes, 128-byte aligned, no initialisation.
  */
 size_t dppf_attention_workspace_bytes(int64_t T, int heads);

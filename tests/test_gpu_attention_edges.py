@@ -134,3 +134,93 @@ def test_large_values_under_growing_scores(b, heads, kv_heads, D, jump, offset, 
     want = reference(q, k, v, starts, causal, 0, 0.125)
     within(got.lse, *want["lse"], "lse")
     within(got.out, *want["out"], "out")
+
+
+# ---------------------------------------------------------------- how far a row that is not finite reaches
+
+MASKS = [(True, 0), (False, 0), (True, 1), (True, 100), (True, 300)]
+
+
+def reach(T, at, causal, window):
+    """Two masks over a sequence's rows: those that see key `at`, and those whose tile of 128 holds one that sees a key of `at`'s tile."""
+    i = torch.arange(T, device="cuda")
+    gap = i[:, None] - i
+    seen = torch.ones(T, T, dtype=torch.bool, device="cuda")
+    if causal:
+        seen &= gap >= 0
+    if window:
+        seen &= gap < window
+    tiles = torch.zeros(T, T, dtype=torch.bool, device="cuda")
+    for r in range(0, T, 128):
+        for c in range(0, T, 128):
+            tiles[r:r + 128, c:c + 128] = seen[r:r + 128, c:c + 128].any()
+    return seen, tiles
+
+
+def placed(mask, lead, T):
+    """mask as one over the T rows of a batch, its first row being row `lead`."""
+    out = torch.zeros(T, dtype=torch.bool, device="cuda")
+    out[lead:lead + len(mask)] = mask
+    return out
+
+
+def check_reach(got, clean, sure, may, what):
+    """[T, heads, D]: NaN in `sure` rows (of column 5 alone where only that can be), clean's bits outside of `may`."""
+    assert torch.isnan(got[sure][..., 5].float()).all(), what
+    assert same_bits(got[~may], clean[~may]), what
+
+
+@pytest.mark.parametrize("causal,window", MASKS)
+@pytest.mark.parametrize("heads,kv_heads,D", [(4, 2, 64), (2, 1, 128), (3, 3, 72)])
+@pytest.mark.parametrize("at", [0, 130, 200, 255, 256, 599])
+@pytest.mark.parametrize("value", [NAN, float("inf")])
+def test_how_far_rows_that_are_not_finite_reach(b, causal, window, heads, kv_heads, D, at, value):
+    lead, n, T = 77, 600, 750
+    starts = starts_of([70, n, 0, 3], lead=7)
+    q, k, v = inputs(T, heads, kv_heads, D, seed=9)
+    grad_out = randn((T, heads, D), 10)
+    plan = b.AttentionPlan(starts, T)
+    kw = dict(causal=causal, window=window)
+    f = b.dppf_attention(q, k, v, plan, **kw)
+    g = b.dppf_attention_grad(grad_out, q, k, v, f.out, f.lse, plan, **kw)
+    seen, tiles = reach(n, at, causal, window)
+    queries, near_queries = placed(seen[:, at], lead, T), placed(tiles[:, at], lead, T)      # that see it as a key
+    keys, near_keys = placed(seen[at], lead, T), placed(tiles[at], lead, T)                  # that it sees as a query
+    none, own = torch.zeros_like(queries), placed(torch.arange(n, device="cuda") == at, lead, T)
+
+    def spoiled(t):
+        t = t.clone()
+        t[lead + at, :, 5] = value
+        return t
+
+    # forward: a value reaches the tiles, a key those that see it, a query itself (an infinite score may be of no weight)
+    bad = b.dppf_attention(q, k, spoiled(v), plan, **kw)
+    assert same_bits(bad.lse, f.lse)
+    others = torch.arange(D, device="cuda") != 5
+    assert same_bits(bad.out[..., others], f.out[..., others])
+    assert not torch.isfinite(bad.out[queries][..., 5].float()).any()
+    assert same_bits(bad.out[~near_queries], f.out[~near_queries])
+    bad = b.dppf_attention(q, spoiled(k), v, plan, **kw)
+    check_reach(bad.out, f.out, queries if value != value else none, queries, "key, out")
+    assert same_bits(bad.lse[:, ~queries], f.lse[:, ~queries])
+    bad = b.dppf_attention(spoiled(q), k, v, plan, **kw)
+    check_reach(bad.out, f.out, own if value != value else none, own, "query, out")
+
+    # the gradient, from the statistics of finite rows
+    bad = b.dppf_attention_grad(spoiled(grad_out), q, k, v, f.out, f.lse, plan, **kw)
+    check_reach(bad.q, g.q, own if value != value else none, own, "grad_out, grad_q")
+    check_reach(bad.k, g.k, keys if value != value else none, keys, "grad_out, grad_k")
+    check_reach(bad.v, g.v, none, near_keys, "grad_out, grad_v")
+    assert not torch.isfinite(bad.v[keys][..., 5].float()).any() and same_bits(bad.v[..., others], g.v[..., others])
+    bad = b.dppf_attention_grad(grad_out, q, spoiled(k), v, f.out, f.lse, plan, **kw)
+    check_reach(bad.q, g.q, queries if value != value else none, near_queries, "key, grad_q")
+    check_reach(bad.k, g.k, own if value != value else none, own, "key, grad_k")
+    check_reach(bad.v, g.v, own if value != value else none, own, "key, grad_v")
+    bad = b.dppf_attention_grad(grad_out, q, k, spoiled(v), f.out, f.lse, plan, **kw)
+    check_reach(bad.q, g.q, queries if value != value else none, queries, "value, grad_q")
+    check_reach(bad.k, g.k, own if value != value else none, own, "value, grad_k")
+    assert same_bits(bad.v, g.v)
+    bad = b.dppf_attention_grad(grad_out, spoiled(q), k, v, f.out, f.lse, plan, **kw)
+    check_reach(bad.q, g.q, own if value != value else none, own, "query, grad_q")
+    check_reach(bad.k, g.k, keys if value != value else none, near_keys, "query, grad_k")
+    check_reach(bad.v, g.v, keys if value != value else none, keys, "query, grad_v")
