@@ -421,11 +421,24 @@ def _type(t: torch.Tensor, what: str) -> int:
     return _TYPES[t.dtype]
 
 
+_MAX_INT, _MAX_INT64 = 2 ** 31 - 1, 2 ** 63 - 1       # ctypes passes the low 32 bits of a larger number without a word
+
+
+def _size(n, what: str, most=_MAX_INT) -> int:
+    """n as an integer that the C entry's type holds."""
+    n = int(n)
+    if not -most <= n <= most:
+        raise ValueError(f"{what} must be at most {most}")
+    return n
+
+
 def _matrix(t: torch.Tensor, what: str):
     """(rows, columns, row stride) of a 2-D CUDA tensor with unit column stride."""
     if t.dim() != 2 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError(f"{what} must be a 2-D CUDA tensor with unit column stride")
     rows, cols = t.shape
+    if cols > _MAX_INT:
+        _size(cols, f"{what}'s columns")
     return rows, cols, (t.stride(0) if rows > 1 else cols)     # the stride of a single row says nothing
 
 
@@ -529,6 +542,8 @@ def dppf_layer_norm(x, weight, bias=None, eps=1e-5, branch=None, sum_out=None, o
     if not x.is_cuda or not shape:
         raise ValueError("x must be a CUDA tensor of rows")
     H = shape[-1]
+    if H > _MAX_INT:
+        _size(H, "x's columns")
     px, ld_x = _rows(x, shape, "x", dev)
     T = x.numel() // H if H else 0
     if weight.numel() != H or weight.device != dev or not weight.is_contiguous():
@@ -561,7 +576,7 @@ def dppf_layer_norm(x, weight, bias=None, eps=1e-5, branch=None, sum_out=None, o
 
 
 def alloc_layer_norm_workspace(T: int, H: int, device="cuda") -> torch.Tensor:
-    n = int(load().dppf_layer_norm_workspace_bytes(int(T), int(H)))
+    n = int(load().dppf_layer_norm_workspace_bytes(_size(T, "T", _MAX_INT64), _size(H, "H")))
     if n == 0:
         raise ValueError("invalid T or H")
     return torch.empty(n, dtype=torch.uint8, device=device)
@@ -575,6 +590,8 @@ def dppf_layer_norm_grad(grad_out, x, mean, rstd, weight, grad_weight, grad_bias
     if not x.is_cuda or not shape:
         raise ValueError("x must be a CUDA tensor of rows")
     H = shape[-1]
+    if H > _MAX_INT:
+        _size(H, "x's columns")
     px, ld_x = _rows(x, shape, "x", dev)
     T = x.numel() // H if H else 0
     pg, ld_g = _rows(grad_out, shape, "grad_out", dev)
@@ -605,8 +622,9 @@ def rotary_frequencies(turned, base=10000.0, scaling="plain", factor=1.0, origin
     adapted to contexts ``factor`` times as long as the model's (``original_length`` tokens; for "by parts")."""
     if scaling not in POSITIONS:
         raise ValueError(f"scaling must be one of {', '.join(POSITIONS)}")
-    values, scale = (ctypes.c_double * max(1, int(turned) // 2))(), ctypes.c_float()
-    _check(load().dppf_rotary_frequencies(int(turned), base, POSITIONS[scaling], factor, int(original_length), values, ctypes.byref(scale)), "dppf_rotary_frequencies")
+    turned, original_length = _size(turned, "turned"), _size(original_length, "original_length", _MAX_INT64)
+    values, scale = (ctypes.c_double * max(1, turned // 2))(), ctypes.c_float()
+    _check(load().dppf_rotary_frequencies(turned, base, POSITIONS[scaling], factor, original_length, values, ctypes.byref(scale)), "dppf_rotary_frequencies")
     return torch.tensor(list(values), dtype=torch.float64, device=device), scale.value
 
 
@@ -615,6 +633,8 @@ def _heads(t: torch.Tensor, what: str):
     if t.dim() != 3 or not t.is_cuda:
         raise ValueError(f"{what} must be a 3-D CUDA tensor [tokens, heads, width] with unit stride within a head")
     T, heads, D = t.shape
+    if heads > _MAX_INT or D > _MAX_INT:
+        _size(max(heads, D), f"{what}'s heads and their width")
     ld, head, one = t.stride()
     if one != 1 and D > 1:
         raise ValueError(f"{what} must be a 3-D CUDA tensor [tokens, heads, width] with unit stride within a head")
@@ -653,7 +673,7 @@ class AttentionPlan:
     ``starts[b + 1] - 1`` of ``tokens``.  Made once a batch, on the current stream, and used by every layer."""
 
     def __init__(self, starts, tokens):
-        self.tokens, self.sequences, self.device = int(tokens), starts.numel() - 1, starts.device
+        self.tokens, self.sequences, self.device = _size(tokens, "tokens", _MAX_INT64), starts.numel() - 1, starts.device
         if not starts.is_cuda:
             raise ValueError("starts must be a CUDA tensor")
         n = int(load().dppf_attention_plan_bytes(self.tokens, self.sequences))
@@ -686,6 +706,11 @@ def _attention_heads(t, what, device, tokens, shape=None):
     return t.shape, t.data_ptr(), ld, head
 
 
+def _window(n) -> int:
+    """A window beyond 32 bits is longer than any batch, so that the longest that the C entries take does the same."""
+    return max(-1, min(int(n), _MAX_INT))
+
+
 def _attention_inputs(q, k, v, plan, scale):
     device, tokens = plan.device, plan.tokens
     shape, *at_q = _attention_heads(q, "q", device, tokens)
@@ -711,7 +736,7 @@ def dppf_attention(q, k, v, plan: AttentionPlan, causal=True, window=0, scale=No
         lse = q.new_empty((heads, plan.tokens), dtype=torch.float32)
     else:
         _vector(lse, heads * plan.tokens, "lse", plan.device)
-    _call(plan.device, load().dppf_attention, "dppf_attention", *at_qkv, plan.tokens, plan.sequences, heads, kv[1], D, int(bool(causal)), int(window), scale,
+    _call(plan.device, load().dppf_attention, "dppf_attention", *at_qkv, plan.tokens, plan.sequences, heads, kv[1], D, int(bool(causal)), _window(window), scale,
           *at_o, lse.data_ptr(), plan.buffer.data_ptr(), plan.buffer.nbytes)
     return Attention(out, lse)
 
@@ -723,7 +748,7 @@ class AttentionGrads(NamedTuple):
 
 
 def alloc_attention_workspace(T: int, heads: int, device="cuda") -> torch.Tensor:
-    n = int(load().dppf_attention_workspace_bytes(int(T), int(heads)))
+    n = int(load().dppf_attention_workspace_bytes(_size(T, "T", _MAX_INT64), _size(heads, "heads")))
     if n == 0:
         raise ValueError("invalid T or number of heads")
     return torch.empty(n, dtype=torch.uint8, device=device)
@@ -749,7 +774,7 @@ def dppf_attention_grad(grad_out, q, k, v, out, lse, plan: AttentionPlan, causal
     elif tokens:
         ws = alloc_attention_workspace(tokens, heads, device)
     _call(device, load().dppf_attention_grad, "dppf_attention_grad", *at_go, *at_qkv, *at_o, lse.data_ptr(), tokens, plan.sequences, heads, kv[1], D,
-          int(bool(causal)), int(window), scale, *at_dq, *at_dk, *at_dv, plan.buffer.data_ptr(), plan.buffer.nbytes, _ptr(ws), 0 if ws is None else ws.nbytes)
+          int(bool(causal)), _window(window), scale, *at_dq, *at_dk, *at_dv, plan.buffer.data_ptr(), plan.buffer.nbytes, _ptr(ws), 0 if ws is None else ws.nbytes)
     return AttentionGrads(grad_q, grad_k, grad_v)
 
 

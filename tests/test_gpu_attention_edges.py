@@ -224,3 +224,38 @@ def test_how_far_rows_that_are_not_finite_reach(b, causal, window, heads, kv_hea
     check_reach(bad.q, g.q, own if value != value else none, own, "query, grad_q")
     check_reach(bad.k, g.k, keys if value != value else none, near_keys, "query, grad_k")
     check_reach(bad.v, g.v, keys if value != value else none, keys, "query, grad_v")
+
+
+# ---------------------------------------------------------------- numbers beyond 32 bits
+
+@pytest.mark.parametrize("more", [2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 70 + 1])
+def test_windows_beyond_32_bits_are_none(b, more):
+    T = 300
+    q, k, v = inputs(T, 2, 2, 64, seed=11)
+    plan = b.AttentionPlan(starts_of([T]), T)
+    f = b.dppf_attention(q, k, v, plan)
+    got = b.dppf_attention(q, k, v, plan, window=more)
+    assert same_bits(got.out, f.out) and same_bits(got.lse, f.lse)
+    want = b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan)
+    assert all(same_bits(x, y) for x, y in zip(want, b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan, window=more)))
+    for call in (lambda w: b.dppf_attention(q, k, v, plan, window=w), lambda w: b.dppf_attention_grad(q, q, k, v, f.out, f.lse, plan, window=w)):
+        with pytest.raises(b.DppfError) as err:
+            call(-more)
+        assert err.value.status == b.ERR_INVALID_ARG
+
+
+def test_sizes_beyond_32_bits_are_refused(b):
+    H = 2 ** 32 + 8                                                             # 8 to a 32-bit integer
+    x = torch.empty(1, H, dtype=BF16, device="cuda")
+    for rows in (x, x[0]):
+        with pytest.raises(ValueError):
+            b.dppf_layer_norm(rows, x[0])
+    stat = torch.ones(1, device="cuda")
+    with pytest.raises(ValueError):
+        b.dppf_layer_norm_grad(x, x, stat, stat, x[0], x[0], grad_x=x)
+    with pytest.raises(ValueError):
+        b.dppf_embedding(x, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        b.dppf_rotary(x.view(1, 1, H), torch.zeros(1, dtype=torch.int64, device="cuda"), torch.ones(1, dtype=torch.float64, device="cuda"), out=x.view(1, 1, H))
+    with pytest.raises(ValueError):
+        b.AttentionPlan(torch.zeros(2, dtype=torch.int32, device="cuda"), 2 ** 64 + 5)
