@@ -259,3 +259,31 @@ def test_sizes_beyond_32_bits_are_refused(b):
         b.dppf_rotary(x.view(1, 1, H), torch.zeros(1, dtype=torch.int64, device="cuda"), torch.ones(1, dtype=torch.float64, device="cuda"), out=x.view(1, 1, H))
     with pytest.raises(ValueError):
         b.AttentionPlan(torch.zeros(2, dtype=torch.int32, device="cuda"), 2 ** 64 + 5)
+
+
+# ---------------------------------------------------------------- many sequences
+
+@pytest.mark.parametrize("causal,window", [(False, 0), (True, 0), (True, 3)])
+def test_gradients_of_many_sequences(b, causal, window):
+    """More sequences than the plan's kernel has threads, against the formulas; sequences of no rows among them."""
+    lens = torch.randint(0, 9, (3000,), generator=torch.Generator().manual_seed(5)).tolist()
+    lens[1030], lens[2040] = 300, 129                                           # and some that do not fit a tile, past the first thousand
+    lead, tail = 5, 140
+    starts = starts_of(lens, lead)
+    T = int(starts[-1]) + tail
+    q, k, v = inputs(T, 2, 1, 32, seed=12)
+    grad_out = randn((T, 2, 32), 13)
+    plan = b.AttentionPlan(starts, T)
+    kw = dict(causal=causal, window=window)
+    f = b.dppf_attention(q, k, v, plan, **kw)
+    want = reference(q, k, v, starts, causal, window, 32 ** -0.5)
+    within(f.lse, *want["lse"], "lse")
+    within(f.out, *want["out"], "out")
+    got = b.dppf_attention_grad(grad_out, q, k, v, f.out, f.lse, plan, **kw)
+    want = reference(q, k, v, starts, causal, window, 32 ** -0.5, (grad_out, f.out, f.lse))
+    for name in "qkv":
+        within(getattr(got, name), *want[name], name)
+    for t in (f.out, *got):
+        assert not t[:lead].any() and not t[T - tail:].any()
+    for rows in (slice(0, lead), slice(T - tail, T)):
+        assert (f.lse[:, rows] == -math.inf).all()                              # minus infinity, not plus
