@@ -430,9 +430,11 @@ int dppf_attention_plan(const void *starts, int start_bits, int64_t T, int64_t B
  * and key head h / (heads / kv_heads):
  *   S_ij = scale q_i . k_j;   lse_out[h T + i] = log sum_j exp S_ij;   out_i = sum_j exp(S_ij - lse_i) v_j
  * q, out: heads heads, k, v: kv_heads heads (a divisor) of D elements (a multiple of 8, up to DPPF_MAX_ATTENTION_WIDTH), bf16, laid
- * out as for dppf_rotary, starts and strides multiples of 16 bytes.  Products of bf16, sums and softmax in fp32; the
- * probabilities (relative to the largest or to one up to 2^20 smaller) are rounded to bf16 for the product with v, out at the end.  Values above 2^107 / (keys of the
- * sequence) in magnitude may overflow the sums where the result would not.  scale > 0, and times log2 e an fp32 number.  T == 0 does nothing.
+ * out as for dppf_rotary, starts and strides multiples of 16 bytes.  Products of bf16, sums and softmax in fp32;
+ * exponentials are off by up to 3.3e-6 of themselves (some come from a polynomial), which lse and the gradient's P take over.  The
+ * probabilities (relative to the largest or to one up to 2^20 smaller) are rounded to bf16 for the product with v, out at the end.  Values above
+ * 2^107 / (keys of the sequence) in magnitude may overflow the sums where the result would not.  scale > 0, and times log2 e an fp32
+ * number.  T == 0 does nothing.
  * Rows that are not finite: a query row spoils its own results, a key row those of the queries that see it.  A value row reaches further:
  * products are formed of tiles of 128 rows, counted from the sequence's start, and a masked probability of 0 times NaN or an infinity
  * is NaN.  So it spoils all queries of each tile in which one sees any key of its own tile: those before it in its tile and, with a window, some
@@ -451,10 +453,11 @@ int dppf_attention(const void *q, int64_t ld_q, int64_t head_q, const void *k, i
  *   grad_q_i = scale sum_j dS_ij k_j;   grad_k_j = scale sum_i dS_ij q_i;   grad_v_j = sum_i P_ij grad_out_i
  * the last two over the query heads that share the key head as well.  All three are written whole (zeros for rows of no
  * sequence).  P and dS are rounded to bf16 for their products, sums run in fp32 in an order that the batch fixes (few key heads of
- * few tokens: the heads that share one in parts, joined in order), results are rounded at the end.  Arguments as above; grad_out and out as q, grad_q as q, grad_k and grad_v as k; gradients may be heads
- * of the same rows (as those of one product are) but must not overlap each other or an input.  Rows that are not finite spoil the
- * gradients that they enter for the pairs that see each other and, through masked zeros, for all pairs of two tiles (as above) in which one
- * does: a key row grad_q, a query row grad_k, a grad_out row grad_v.
+ * few tokens: the heads that share one in parts, joined in order), results are rounded at the end.  Arguments as above; grad_out and
+ * out as q, grad_q as q, grad_k and grad_v as k; gradients may be heads of the same rows (as those of one product are) but must not
+ * overlap each other or an input.  Rows that are not finite spoil the gradients that they enter for the pairs that see each other and,
+ * through masked zeros, for all pairs of two tiles (as above) in which one does: a key row grad_q, a query row grad_k, a grad_out
+ * row grad_v.  ws holds D and, wherever T and heads allow it, parts of grad_k and grad_v, used for few key heads of few tokens alone.
  * ws: dppf_attention_workspace_bytes(T, heads) bytes, 128-byte aligned, no initialisation.
  */
 size_t dppf_attention_workspace_bytes(int64_t T, int heads);

@@ -248,8 +248,9 @@ __device__ __forceinline__ void spoil_row(bf16 *row, int D) {
 // Rounded to fewer bits: the probabilities, to bf16 for the second product (relative to about the largest; the sum that they are divided by is of
 // the fp32 values), and the result.  What bounds it: a slot's chain of scores (512 cycles of the tensor cores), copy to registers (110), exponentials
 // (1,700: 128 a thread, a part on the multiply-add pipes) and the second product (512), two of which run by turns: about 3,200 cycles for two
-// tiles of 128 x 128 x 128, 2,048 of them products.  Measured on a B200: 16,384 tokens in four sequences, 16 heads of 128, all keys 450 us
-// (1,220 TFLOP/s); 8,192 tokens in six documents, 32 heads, causal 269 us (1,094 TFLOP/s); in runs of seconds the 1,000 W limit makes that 310.
+// tiles of 128 x 128 x 128, 2,048 of them products.  Measured on a B200: 16,384 tokens in four sequences, 16 heads of 128 on four
+// key heads, all keys 456 us (1,205 TFLOP/s; with a key head each 531); 8,192 tokens in six documents, 32 heads on eight, causal 273 us (1,079 TFLOP/s); in
+// runs of seconds the 1,000 W limit makes that 311.
 // Tried and lost: one maximum a tile before the exponentials (3 to 5 %), two threads a row (10 %), a warp for each slot's products (10 %),
 // products from registers that the compiler does not know to be uniform (25 %).
 
